@@ -411,6 +411,114 @@ int heatkv_selftest_wait_expiry(heatkv_ctx* ctx, void* stream);
 int heatkv_device_status(heatkv_ctx* ctx, void* stream);
 const char* heatkv_strerror(int status);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Paged cache for requests of any length.  No counterpart in the paper: the cache above is planned for images, whose lengths are known
+ * before they start; prompts, text that is answered token by token and drafted tokens are not.  Here a request's tokens lie in pages of
+ * HEATKV_PAGE_TOKENS that its row of a block table lists, every head keeps every token, and G = n_heads / n_kv_heads query heads share a
+ * kv head.  These calls need no context and keep nothing between them: all buffers are the caller's, lengths and tables stay on the
+ * device, and no call waits for the device unless it says so.
+ *
+ * One step of a batch: heatkv_paged_tables (pages and slots of the new tokens), then per layer heatkv_paged_store (their K and V into the
+ * layer's pool) and heatkv_paged_attention, or heatkv_paged_select and heatkv_paged_sparse_attention.  Requests' new tokens lie one
+ * request after another in all token tensors: request i has the tokens q_begin[i] .. q_begin[i + 1] - 1, and the last of them is its token
+ * number kv_len[i] - 1.
+ *
+ * Keys and values below kv_len must be finite; what the pool holds past them, and in pages that no table lists, may be anything, NaN
+ * included.  Entries of tables and slot maps outside of the pool are not followed: nothing is stored there, and what is read is zero. */
+typedef enum { HEATKV_DTYPE_BF16 = 0, HEATKV_DTYPE_FP16 = 1 } heatkv_dtype;
+
+#define HEATKV_PAGED_MAX_SEQ 4096          /* requests of a call                                        */
+#define HEATKV_PAGED_MAX_SELECT 32768      /* pages of a request from which heatkv_paged_select chooses */
+
+typedef struct {                 /* one layer's pool                                                                   */
+  void* k;                       /* DEVICE [n_pages][n_kv_heads][64][d], d contiguous, 16-byte aligned; strides below  */
+  void* v;                       /* DEVICE, the same shape and strides                                                 */
+  int8_t* k_code;                /* DEVICE [n_pages][n_kv_heads][d] page summaries, 16-byte aligned, or NULL: none kept */
+  float* k_scale;                /* DEVICE [n_pages][n_kv_heads], or NULL with k_code                                  */
+  int64_t page_stride, head_stride, row_stride;   /* elements, multiples of 8                                          */
+  int32_t n_pages, n_kv_heads;
+  int32_t d;                     /* 64 or 128                                                                          */
+  int32_t dtype;                 /* heatkv_dtype of k, v and of the activations that go with them                      */
+} heatkv_paged_pool;
+
+typedef struct {                 /* the requests of a step                                                             */
+  const int32_t* q_begin;        /* DEVICE [n_seq + 1] first new token of every request, and their number              */
+  const int32_t* kv_len;         /* DEVICE [n_seq] tokens of the request, the new ones included; 0: none               */
+  const int32_t* block_table;    /* DEVICE [n_seq][table_pages] page numbers, rows table_stride elements apart         */
+  int64_t table_stride;
+  int32_t n_seq, table_pages;
+  int32_t n_tokens;              /* rows of the token tensors, at least q_begin[n_seq]                                 */
+  int32_t max_new;               /* new tokens of the longest request: picks the kernel; any value gives right results */
+} heatkv_paged_batch;
+
+typedef struct {                 /* element strides of [n_tokens][n_heads][d] activations: at least d, multiples of 8 (o_*: of 4) */
+  int64_t q_tok, q_head, o_tok, o_head;
+} heatkv_token_strides;
+
+/* Block tables and slot maps of a step, from its requests' lengths.  Request i takes need_i = ceil((past_i + new_i) / 64) -
+ * ceil(past_i / 64) fresh pages for its new tokens; in request order they come from a ring of free pages.  A request is refused when
+ * need_i > 0 and the pages wanted up to and including it exceed the free ones, or when it needs more than table_pages: it takes no
+ * pages, its slots are -1 and its kv_len is 0 in this step (so its rows of the attention are zero).
+ *   new_tokens, past_tokens DEVICE [n_seq] (negative counts as 0)
+ *   free_pages DEVICE [n_pages] the ring; state DEVICE int32[4]: {place of its oldest entry, entries, 0, 0}
+ *   state_out DEVICE int32[4]: {place and entries after the call, requests refused, new tokens of all requests}; another buffer than
+ *             state, so that a step can be repeated
+ *   block_table DEVICE, in and out: entries ceil(past_i / 64) .. are written for the fresh pages
+ *   q_begin DEVICE [n_seq + 1], kv_len DEVICE [n_seq], slot_map DEVICE [n_tokens] (page * 64 + row, -1: none; also past the last token),
+ *   positions DEVICE [n_tokens] (past_i + place among the new tokens) or NULL                                                  */
+int heatkv_paged_tables(const int32_t* new_tokens, const int32_t* past_tokens, int n_seq, const int32_t* free_pages, int n_pages,
+                        const int32_t* state, int32_t* state_out, int32_t* block_table, int64_t table_stride, int table_pages,
+                        int32_t* q_begin, int32_t* kv_len, int32_t* slot_map, int32_t* positions, int n_tokens, void* stream);
+
+/* Gives back the pages that hold only tokens from keep_len[i] on (0: the request is over; less than kv_len[i]: drafted tokens were
+ * turned down), request by request, to the end of the ring.  DEVICE pointers as above; state_out: {.., .., 0, pages given back}.  The
+ * tables are left as they are: the caller's lengths say what of them counts. */
+int heatkv_paged_release(const int32_t* kv_len, const int32_t* keep_len, int n_seq, const int32_t* block_table, int64_t table_stride,
+                         int table_pages, int32_t* free_pages, int n_pages, const int32_t* state, int32_t* state_out, void* stream);
+
+/* K and V rows of new tokens to their slots: k_new, v_new DEVICE [n_tokens][n_kv_heads][d], strides in elements (multiples of 8).
+ * Tokens with a slot outside of the pool are left out; no slot may occur twice.  With page summaries kept, every page whose last row is
+ * among the slots gets its own: the mean of its 64 keys in 32 bits (a tree sum: rows i and i + 32, then i and i + 16, and so on),
+ * scale = max|mean| * (1 / 127), code = round-to-nearest-even(mean / scale).  A page's rows that come with this call must lie one after
+ * another in k_new, as heatkv_paged_tables puts them. */
+int heatkv_paged_store(const heatkv_paged_pool* pool /*HOST*/, const void* k_new, const void* v_new, int64_t tok_stride,
+                       int64_t head_stride, const int32_t* slot_map, int n_tokens, void* stream);
+
+/* Workspace of the two attention calls below on the current device, in bytes (DEVICE, 256-byte aligned).  It must be zero before its
+ * first use and may then serve any number of calls that do not overlap on the GPU, of this batch or a smaller one (fewer requests and
+ * tokens) with as many heads. */
+int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, uint64_t* bytes);
+
+/* Attention of every request's new tokens over its pages: out = softmax(sm_scale q K^T) V, with causal != 0 over the keys up to the
+ * token's own position, else over all kv_len of the request (an image's scale, whose tokens see one another).  Sums and softmax
+ * statistics in 32 bits, probabilities rounded to 16 before the product with V.
+ *   q DEVICE [n_tokens][n_heads][d], out the same shape; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
+ *   lse DEVICE fp32 [n_tokens][n_heads], the natural logarithm of the sum of exponentials, or NULL
+ * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows past q_begin[n_seq] are left
+ * as they are.  n_heads / n_kv_heads at most 32. */
+int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
+                           const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
+                           uint64_t workspace_bytes, void* stream);
+
+/* The pages that every query token attends to, per kv head: the first `sink` pages, the last `local` ones (local >= 1: the token's own
+ * page is among them) and, up to n_select in all, those between whose summary scores highest against the query's: the sum of the
+ * group's query heads in 32 bits, in head order, as 8-bit codes like a page's; score = (whole-number dot product of the codes) * the
+ * page's scale, ties to the lower page.  sel DEVICE int32 [n_tokens][n_kv_heads][n_select]: page places in the request's table row,
+ * ascending, -1 after the last.  n_select >= sink + local.  Pages between must have summaries (they are whole by then). */
+int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
+                        const heatkv_token_strides* st, int sink, int local, int n_select, int32_t* sel, void* stream);
+
+/* Causal attention of every new token over the pages that sel lists for it (distinct places in the request's table row; entries below 0,
+ * past the token's own page or past the table count for nothing).  Other arguments and results as heatkv_paged_attention; rows past
+ * q_begin[n_seq] become zero.  n_heads / n_kv_heads at most 16. */
+int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
+                                  const heatkv_token_strides* st, const int32_t* sel, int n_select, float sm_scale, void* out,
+                                  float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Reads the workspace's status word (synchronises `stream`): HEATKV_OK, or HEATKV_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel
+ * ran out; the workspace must then be zeroed again. */
+int heatkv_paged_status(const void* workspace /*DEVICE*/, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

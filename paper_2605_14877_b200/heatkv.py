@@ -26,6 +26,9 @@ __all__ = [
     "CACHE_BF16", "CACHE_FP8_E4M3", "heatkv_launch_count", "heatkv_kernel_launches", "heatkv_pair_launches", "heatkv_lone_launches", "heatkv_last_attention", "heatkv_rank_dispersion", "heatkv_seq_reservation",
     "KernelStats", "AttentionForm", "ATTENTION_NONE", "ATTENTION_GENERIC", "ATTENTION_TCGEN05", "ATTENTION_CTA_PAIRS",
     "heatkv_selftest_wait_expiry", "heatkv_device_status", "heatkv_strerror", "heatkv_attention_split", "arena_bytes_for",
+    "PagedPool", "PagedBatch", "TokenStrides", "DTYPE_BF16", "DTYPE_FP16", "PAGED_MAX_SEQ", "PAGED_MAX_SELECT", "heatkv_paged_tables",
+    "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention", "heatkv_paged_select",
+    "heatkv_paged_sparse_attention", "heatkv_paged_status",
 ]
 
 MAX_K, MAX_BATCH, PAGE_TOKENS = 16, 128, 64
@@ -100,6 +103,81 @@ class AttentionForm(C.Structure):
     _fields_ = [("kernel", C.c_int32), ("items", C.c_int32), ("longest_piece", C.c_int32), ("lone", C.c_int32)]
 
 
+# ---- paged cache of requests of any length
+PAGED_MAX_SEQ, PAGED_MAX_SELECT = 4096, 32768
+DTYPE_BF16, DTYPE_FP16 = 0, 1
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16}
+
+
+def _expect(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tensor:
+    """x, if it has the type and shape (None: any extent); the library sees pointers only."""
+    if x.dtype != dtype or x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"{what}: expected {dtype} {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
+    return x
+
+
+def _packed(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tensor:
+    if not _expect(x, dtype, shape, what).is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor")
+    return x
+
+
+class PagedPool(C.Structure):
+    """One layer's pages: k, v [n_pages, n_kv_heads, 64, d] views (d contiguous, any other strides) and, for page selection,
+    their summaries.  Keeps the tensors alive."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_code", C.c_void_p), ("k_scale", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32)]
+
+    @classmethod
+    def make(cls, k: torch.Tensor, v: torch.Tensor, k_code: Optional[torch.Tensor] = None,
+             k_scale: Optional[torch.Tensor] = None) -> "PagedPool":
+        if k.dtype not in _DTYPES:
+            raise ValueError(f"k: expected bfloat16 or float16, got {k.dtype}")
+        _expect(k, k.dtype, (None, None, PAGE_TOKENS, None), "k")
+        _expect(v, k.dtype, k.shape, "v")
+        if k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k, v: expected equal strides, the last dimension contiguous")
+        p = cls()
+        p.tensors = (k, v, k_code, k_scale)
+        p.k, p.v = k.data_ptr(), v.data_ptr()
+        if k_code is not None:
+            p.k_code = _packed(k_code, torch.int8, (k.shape[0], k.shape[1], k.shape[3]), "k_code").data_ptr()
+        if k_scale is not None:
+            p.k_scale = _packed(k_scale, torch.float32, (k.shape[0], k.shape[1]), "k_scale").data_ptr()
+        p.page_stride, p.head_stride, p.row_stride = k.stride()[:3]
+        p.n_pages, p.n_kv_heads, p.d, p.dtype = k.shape[0], k.shape[1], k.shape[3], _DTYPES[k.dtype]
+        p.torch_dtype, p.addr = k.dtype, C.addressof(p)
+        return p
+
+
+class PagedBatch(C.Structure):
+    """The requests of a step: int32 tensors q_begin [n_seq + 1], kv_len [n_seq], block_table [n_seq, pages]; n_tokens rows in the token
+    tensors, max_new new tokens in the longest request.  Keeps the tensors alive."""
+    _fields_ = [("q_begin", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("n_seq", C.c_int32), ("table_pages", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32)]
+
+    @classmethod
+    def make(cls, q_begin: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, n_tokens: int, max_new: int) -> "PagedBatch":
+        n = kv_len.shape[0]
+        _packed(q_begin, torch.int32, (n + 1,), "q_begin")
+        _packed(kv_len, torch.int32, (n,), "kv_len")
+        _expect(block_table, torch.int32, (n, None), "block_table")
+        if block_table.stride(1) != 1:
+            raise ValueError("block_table: expected contiguous rows")
+        b = cls()
+        b.tensors = (q_begin, kv_len, block_table)
+        b.q_begin, b.kv_len, b.block_table = q_begin.data_ptr(), kv_len.data_ptr(), block_table.data_ptr()
+        b.table_stride = block_table.stride(0) if n > 1 else block_table.shape[1]
+        b.n_seq, b.table_pages, b.n_tokens, b.max_new = n, block_table.shape[1], int(n_tokens), int(max_new)
+        b.addr = C.addressof(b)
+        return b
+
+
+class TokenStrides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("q_tok", "q_head", "o_tok", "o_head")]
+
+
 def lib_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), "libheatkv.so")
 
@@ -114,7 +192,9 @@ def exported_symbols():
             "heatkv_retained_indices", "heatkv_export_head", "heatkv_export_head_fp8",
             "heatkv_attention_split", "heatkv_split_plan", "heatkv_lone_plan", "heatkv_allocator_stats", "heatkv_launch_count",
             "heatkv_kernel_launches", "heatkv_pair_launches", "heatkv_lone_launches", "heatkv_last_attention", "heatkv_rank_dispersion", "heatkv_selftest_wait_expiry", "heatkv_device_status",
-            "heatkv_strerror"]
+            "heatkv_strerror",
+            "heatkv_paged_tables", "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention",
+            "heatkv_paged_select", "heatkv_paged_sparse_attention", "heatkv_paged_status"]
 
 
 def _load() -> C.CDLL:
@@ -168,6 +248,15 @@ _lib.heatkv_selftest_wait_expiry.argtypes = [_P, _P]
 _lib.heatkv_kernel_launches.argtypes = [_P, C.POINTER(KernelStats)]
 _lib.heatkv_rank_dispersion.argtypes = [_P, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, _P]
 _lib.heatkv_seq_reservation.argtypes = [_P, C.c_int, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
+_I, _L = C.c_int, C.c_int64
+_lib.heatkv_paged_tables.argtypes = [_P, _P, _I, _P, _I, _P, _P, _P, _L, _I, _P, _P, _P, _P, _I, _P]
+_lib.heatkv_paged_release.argtypes = [_P, _P, _I, _P, _L, _I, _P, _I, _P, _P, _P]
+_lib.heatkv_paged_store.argtypes = [_P, _P, _P, _L, _L, _P, _I, _P]
+_lib.heatkv_paged_workspace_bytes.argtypes = [_P, _P, _I, C.POINTER(C.c_uint64)]
+_lib.heatkv_paged_attention.argtypes = [_P, _P, _I, _P, _P, _I, C.c_float, _P, _P, _P, C.c_uint64, _P]
+_lib.heatkv_paged_select.argtypes = [_P, _P, _I, _P, _P, _I, _I, _I, _P, _P]
+_lib.heatkv_paged_sparse_attention.argtypes = [_P, _P, _I, _P, _P, _P, _I, C.c_float, _P, _P, _P, C.c_uint64, _P]
+_lib.heatkv_paged_status.argtypes = [_P, _P]
 for _n in exported_symbols():
     if _n != "heatkv_strerror":
         getattr(_lib, _n).restype = C.c_int
@@ -456,3 +545,117 @@ def heatkv_selftest_wait_expiry(ctx: int, stream=None) -> int:
 
 def heatkv_device_status(ctx: int, stream=None) -> int:
     return _lib.heatkv_device_status(ctx, _stream(stream))
+
+
+# ---------------------------------------------------------------------------------------------- paged cache
+def heatkv_paged_tables(new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map,
+                        positions=None, stream=None) -> None:
+    """Pages, slots and positions of a step's new tokens, from the requests' lengths (int32 tensors on the device)."""
+    n = new_tokens.shape[0]
+    i32 = torch.int32
+    _packed(new_tokens, i32, (n,), "new_tokens")
+    _packed(past_tokens, i32, (n,), "past_tokens")
+    _packed(free_pages, i32, (None,), "free_pages")
+    _packed(state, i32, (4,), "state")
+    _packed(state_out, i32, (4,), "state_out")
+    _packed(q_begin, i32, (n + 1,), "q_begin")
+    _packed(kv_len, i32, (n,), "kv_len")
+    _packed(slot_map, i32, (None,), "slot_map")
+    if _expect(block_table, i32, (n, None), "block_table").stride(1) != 1:
+        raise ValueError("block_table: expected contiguous rows")
+    if positions is not None:
+        _packed(positions, i32, slot_map.shape, "positions")
+    pages = block_table.shape[1]
+    _check(_lib.heatkv_paged_tables(new_tokens.data_ptr(), past_tokens.data_ptr(), n, free_pages.data_ptr(), free_pages.shape[0],
+                                    state.data_ptr(), state_out.data_ptr(), block_table.data_ptr(), block_table.stride(0) if n > 1 else pages,
+                                    pages, q_begin.data_ptr(), kv_len.data_ptr(), slot_map.data_ptr(), _ptr(positions), slot_map.shape[0],
+                                    _stream(stream)), "heatkv_paged_tables")
+
+
+def heatkv_paged_release(kv_len, keep_len, block_table, free_pages, state, state_out, stream=None) -> None:
+    """Gives back the pages that hold only tokens from keep_len on."""
+    n, i32 = kv_len.shape[0], torch.int32
+    _packed(kv_len, i32, (n,), "kv_len")
+    _packed(keep_len, i32, (n,), "keep_len")
+    _packed(free_pages, i32, (None,), "free_pages")
+    _packed(state, i32, (4,), "state")
+    _packed(state_out, i32, (4,), "state_out")
+    if _expect(block_table, i32, (n, None), "block_table").stride(1) != 1:
+        raise ValueError("block_table: expected contiguous rows")
+    pages = block_table.shape[1]
+    _check(_lib.heatkv_paged_release(kv_len.data_ptr(), keep_len.data_ptr(), n, block_table.data_ptr(),
+                                     block_table.stride(0) if n > 1 else pages, pages, free_pages.data_ptr(), free_pages.shape[0],
+                                     state.data_ptr(), state_out.data_ptr(), _stream(stream)), "heatkv_paged_release")
+
+
+def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> None:
+    """K and V rows [n_tokens, n_kv_heads, d] (equal strides, d contiguous) to their slots, and the summaries of pages that fill up."""
+    shape = (slot_map.shape[0], pool.n_kv_heads, pool.d)
+    _packed(slot_map, torch.int32, (None,), "slot_map")
+    _expect(k_new, pool.torch_dtype, shape, "k_new")
+    _expect(v_new, pool.torch_dtype, shape, "v_new")
+    tok, head, one = k_new.stride()
+    if v_new.stride() != (tok, head, one) or one != 1:
+        raise ValueError("k_new, v_new: expected equal strides, the last dimension contiguous")
+    _check(_lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), tok, head, slot_map.data_ptr(), shape[0],
+                                   _stream(stream)), "heatkv_paged_store")
+
+
+def heatkv_paged_workspace_bytes(pool: PagedPool, batch: PagedBatch, n_heads: int) -> int:
+    """Bytes of workspace that attention over this batch needs (a zeroed uint8 tensor; it may be used again and again)."""
+    out = C.c_uint64()
+    _check(_lib.heatkv_paged_workspace_bytes(pool.addr, batch.addr, n_heads, C.byref(out)), "heatkv_paged_workspace_bytes")
+    return out.value
+
+
+def _token_strides(pool, batch, q, out):
+    """Strides of q and out, None where both are packed."""
+    shape = (batch.n_tokens, None, pool.d)
+    _expect(q, pool.torch_dtype, shape, "q")
+    sq = q.stride()
+    if sq[2] != 1:
+        raise ValueError("q: expected the last dimension contiguous")
+    if out is None:
+        return None if q.is_contiguous() else C.byref(TokenStrides(sq[0], sq[1], sq[0], sq[1]))
+    _expect(out, pool.torch_dtype, q.shape, "out")
+    so = out.stride()
+    if so[2] != 1:
+        raise ValueError("out: expected the last dimension contiguous")
+    return None if q.is_contiguous() and out.is_contiguous() else C.byref(TokenStrides(sq[0], sq[1], so[0], so[1]))
+
+
+def heatkv_paged_attention(pool: PagedPool, batch: PagedBatch, q, out, lse, workspace, causal: bool = True, sm_scale: float = 0.0,
+                           stream=None) -> None:
+    """out [n_tokens, n_heads, d] and (unless None) lse [n_tokens, n_heads] of the new tokens' attention over their requests' pages."""
+    st = _token_strides(pool, batch, q, out)
+    if lse is not None:
+        _packed(lse, torch.float32, q.shape[:2], "lse")
+    _check(_lib.heatkv_paged_attention(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _ptr(lse),
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "heatkv_paged_attention")
+
+
+def heatkv_paged_select(pool: PagedPool, batch: PagedBatch, q, sel, sink: int, local: int, stream=None) -> None:
+    """sel [n_tokens, n_kv_heads, n_select]: the pages each new token attends to (places in its request's table row, ascending, -1
+    after the last)."""
+    st = _token_strides(pool, batch, q, None)
+    _packed(sel, torch.int32, (batch.n_tokens, pool.n_kv_heads, None), "sel")
+    _check(_lib.heatkv_paged_select(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, sink, local, sel.shape[2], sel.data_ptr(),
+                                    _stream(stream)), "heatkv_paged_select")
+
+
+def heatkv_paged_sparse_attention(pool: PagedPool, batch: PagedBatch, q, sel, out, lse, workspace, sm_scale: float = 0.0,
+                                  stream=None) -> None:
+    """heatkv_paged_attention (causal) over the pages that sel lists for each token."""
+    st = _token_strides(pool, batch, q, out)
+    _packed(sel, torch.int32, (batch.n_tokens, pool.n_kv_heads, None), "sel")
+    if lse is not None:
+        _packed(lse, torch.float32, q.shape[:2], "lse")
+    _check(_lib.heatkv_paged_sparse_attention(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, sel.data_ptr(), sel.shape[2], sm_scale,
+                                              out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                              _stream(stream)), "heatkv_paged_sparse_attention")
+
+
+def heatkv_paged_status(workspace, stream=None) -> int:
+    """0, or -7 if a bounded wait of a kernel that used this workspace ran out (synchronises the stream)."""
+    return _lib.heatkv_paged_status(workspace.data_ptr(), _stream(stream))

@@ -1,0 +1,453 @@
+"""The paged cache for requests of any length against plain numpy (whole numbers and summaries bit for bit, attention in 64 bits).
+
+Tolerances.  With u = 2^-8 (bf16, 8 significant bits) or 2^-11 (fp16, 11), the relative rounding of a 16-bit result: the output is rounded once (u |out|), the
+probabilities once (u sum p |v|); a logit is a 32-bit sum of d products and one scaling, off by at most (d + 8) 2^-24 of sum |q k| scale,
+which moves a probability by twice that and the logarithm of the sum by once that; exponentials and sums of 32 bits add 2^-18.  In fp16
+a probability may be subnormal: at most 2^-25 of the largest each."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as P
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def hk():
+    import paper_2605_14877_b200 as hk
+    return hk
+
+
+def _i32(x):
+    return torch.tensor(np.asarray(x, dtype=np.int32), device="cuda")
+
+
+def _np(x):
+    return x.detach().float().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ tables and slots
+
+TABLES = {
+    "one": dict(new=[1], past=[0]),
+    "one_page_ends": dict(new=[1, 1, 1], past=[63, 64, 65]),
+    "nothing_new": dict(new=[0, 5, 0], past=[100, 0, 0]),
+    "prompts": dict(new=[1, 64, 65, 200, 1000, 63], past=[0, 0, 63, 7, 128, 1]),
+    "negative": dict(new=[-3, 4], past=[5, -7]),
+    "pool_too_small": dict(new=[100, 300, 10, 1, 200, 0], past=[0, 0, 54, 64, 0, 64], free=4),
+    "row_too_short": dict(new=[100, 700, 64], past=[0, 0, 0], width=6),
+    "no_free_page": dict(new=[1, 1, 1], past=[3, 64, 70], free=0),
+    "places_to_spare": dict(new=[70, 3], past=[10, 10], spare=37),
+    "many": dict(new=[1 + i % 3 for i in range(4096)], past=[(i * 37) % 300 for i in range(4096)]),
+    "long": dict(new=[40000, 3], past=[25000, 64 * 900 - 1]),
+}
+
+
+def _tables_case(new, past, free=None, width=None, spare=0, seed=0):
+    rng = np.random.default_rng(seed)
+    had = [-(-max(p, 0) // PAGE) for p in past]
+    width = width or max(-(-(max(n, 0) + max(p, 0)) // PAGE) for n, p in zip(new, past)) + 2
+    wanted = sum(max(-(-(max(n, 0) + max(p, 0)) // PAGE) - h, 0) for n, p, h in zip(new, past, had))
+    free = wanted + 3 if free is None else free
+    n_pages = sum(had) + free + 2
+    order = rng.permutation(n_pages)
+    table = np.full((len(new), width), -1)
+    at = 0
+    for i, h in enumerate(had):
+        table[i, :h] = order[at: at + h]
+        at += h
+    fifo = list(order[at: at + free])
+    head = n_pages - 2                                     # the ring goes round its end
+    ring = np.full(n_pages, -1)
+    for j, page in enumerate(fifo):
+        ring[(head + j) % n_pages] = page
+    total = sum(max(n, 0) for n in new)
+    return table, fifo, ring, head, n_pages, max(total + spare, 1)
+
+
+@pytest.mark.parametrize("name", TABLES)
+def test_tables(hk, name):
+    c = TABLES[name]
+    table, fifo, ring, head, n_pages, n_tokens = _tables_case(**c)
+    want = P.tables(c["new"], c["past"], fifo, table, n_tokens)
+    wide = torch.full((len(c["new"]), table.shape[1] + 5), -7, dtype=torch.int32, device="cuda")
+    dev = wide[:, : table.shape[1]]
+    dev.copy_(_i32(table))
+    state, state_out = _i32([head, len(fifo), 0, 0]), _i32([9] * 4)
+    n = len(c["new"])
+    q_begin, kv, slots, pos = _i32([-5] * (n + 1)), _i32([-5] * n), _i32([-5] * n_tokens), _i32([-5] * n_tokens)
+    free = _i32(ring)
+    for positions in (pos, None):                          # twice: the call may be repeated
+        hk.heatkv_paged_tables(_i32(c["new"]), _i32(c["past"]), free, state, state_out, dev, q_begin, kv, slots, positions)
+    got = [x.cpu().numpy() for x in (dev, q_begin, kv, slots, pos)]
+    for g, w, what in zip(got, want, ("table", "q_begin", "kv_len", "slots", "positions")):
+        assert np.array_equal(g, w), what
+    taken, refused = want[5:]
+    assert state_out.tolist() == [(head + taken) % n_pages, len(fifo) - taken, refused, want[1][-1]]
+    assert np.array_equal(free.cpu().numpy(), ring) and (wide[:, table.shape[1]:] == -7).all()
+
+
+def test_release_gives_pages_back_in_order(hk):
+    new, past = [1, 64, 65, 200, 40], [0, 0, 63, 7, 0]
+    table, fifo, ring, head, n_pages, n_tokens = _tables_case(new, past)
+    dev, state, mid, end = _i32(table), _i32([head, len(fifo), 0, 0]), _i32([0] * 4), _i32([0] * 4)
+    n = len(new)
+    q_begin, kv, slots, free = _i32([0] * (n + 1)), _i32([0] * n), _i32([0] * n_tokens), _i32(ring)
+    hk.heatkv_paged_tables(_i32(new), _i32(past), free, state, mid, dev, q_begin, kv, slots)
+    keep = [1, 0, 65, 64, 400]                             # all, none, some, exactly one page, more than there are
+    hk.heatkv_paged_release(kv, _i32(keep), dev, free, mid, end)
+    lens, rows = kv.tolist(), dev.cpu().numpy()
+    back = [rows[i, j] for i in range(n) for j in range(-(-min(keep[i], lens[i]) // PAGE), -(-lens[i] // PAGE))]
+    h, count = mid.tolist()[:2]
+    got = free.cpu().numpy()
+    assert [got[(h + count + j) % n_pages] for j in range(len(back))] == back
+    assert end.tolist() == [h, count + len(back), 0, len(back)] and len(back) == 4
+    # what was given back is handed out again, the oldest first
+    again = P.tables([64 * (count + len(back))], [0], [got[(h + j) % n_pages] for j in range(count + len(back))], np.full((1, 99), -1), 6400)
+    row, out = _i32(np.full((1, 99), -1)), _i32([0] * 4)
+    hk.heatkv_paged_tables(_i32([64 * (count + len(back))]), _i32([0]), free, end, out, row, _i32([0, 0]), _i32([0]), _i32([0] * 6400))
+    assert np.array_equal(row.cpu().numpy(), again[0]) and out.tolist()[1] == 0
+
+
+# ------------------------------------------------------------------------------------------------ pools
+
+def _pool(hk, g, n_pages, Hkv, d, dtype, layout="head", summaries=True, fill=math.nan):
+    """A pool whose every value is `fill`; layout "head": [page][head][row][d], "token": [page][row][head][d]."""
+    if layout == "head":
+        k, v = (torch.full((n_pages, Hkv, PAGE, d), fill, dtype=dtype, device="cuda") for _ in "kv")
+    else:
+        k, v = (torch.full((n_pages, PAGE, Hkv, d + 8), fill, dtype=dtype, device="cuda")[..., :d].transpose(1, 2) for _ in "kv")
+    code = torch.full((n_pages, Hkv, d), 99, dtype=torch.int8, device="cuda") if summaries else None
+    scale = torch.full((n_pages, Hkv), -1.0, device="cuda") if summaries else None
+    return hk.PagedPool.make(k, v, code, scale), k, v, code, scale
+
+
+def _batch(hk, rng, lens, n_pages, spare=0):
+    """lens: (new, kv) per request; pages in random order.  Returns (batch, table, q_begin)."""
+    width = max(max(-(-kv // PAGE) for _, kv in lens), 1) + 1
+    order = rng.permutation(n_pages)
+    table = np.full((len(lens), width), -1)
+    at = 0
+    for i, (_, kv) in enumerate(lens):
+        h = -(-kv // PAGE)
+        table[i, :h] = order[at: at + h]
+        at += h
+    assert at <= n_pages
+    q_begin = np.concatenate([[0], np.cumsum([n for n, _ in lens])])
+    b = hk.PagedBatch.make(_i32(q_begin), _i32([kv for _, kv in lens]), _i32(table), int(q_begin[-1]) + spare, max(max(n for n, _ in lens), 1))
+    return b, table, q_begin
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,Hkv,layout", [(128, 8, "head"), (128, 1, "token"), (64, 5, "token"), (64, 16, "head")])
+def test_store(hk, dtype, d, Hkv, layout):
+    rng = np.random.default_rng(d + Hkv)
+    g = torch.Generator("cuda").manual_seed(d + Hkv)
+    dt = DTYPES[dtype]
+    n_pages = 24
+    pool, k, v, code, scale = _pool(hk, g, n_pages, Hkv, d, dt, layout, fill=0.0)
+    k.normal_(generator=g), v.normal_(generator=g)
+    # (past, new): a page that fills up with what was there, whole pages, a page's last row alone, nothing that fills up
+    parts = [(10, 200), (0, 128), (63, 1), (64, 3), (5, 59)]
+    order = list(rng.permutation(n_pages))
+    slots, full = [], []
+    for past, new in parts:
+        pages = [order.pop() for _ in range(-(-(past + new) // PAGE))]
+        slots += [pages[p // PAGE] * PAGE + p % PAGE for p in range(past, past + new)]
+        full += [pages[p // PAGE] for p in range(past, past + new) if p % PAGE == PAGE - 1]
+    at = 200                                               # behind the first request
+    slots[at:at] = [-1, n_pages * PAGE, 2**31 - 1]         # tokens without a place
+    T = len(slots)
+    qkv = torch.empty(T, 3, Hkv, d, dtype=dt, device="cuda").normal_(generator=g)
+    before = [_np(x) for x in (k, v)]
+    hk.heatkv_paged_store(pool, qkv[:, 1], qkv[:, 2], _i32(slots))
+    new = [_np(qkv[:, 1]), _np(qkv[:, 2])]
+    for x, b, n in zip((k, v), before, new):
+        for t, s in enumerate(slots):
+            if 0 <= s < n_pages * PAGE:
+                b[s // PAGE, :, s % PAGE] = n[t]
+        assert np.array_equal(_np(x), b)
+    assert len(full) == 7
+    for page in range(n_pages):
+        for h in range(Hkv):
+            if page in full:
+                c, s = P.summary(before[0][page, h])
+                assert np.array_equal(code[page, h].cpu().numpy(), c) and scale[page, h].item() == s
+            else:
+                assert (code[page, h] == 99).all() and scale[page, h].item() == -1.0
+
+
+def test_store_of_one_head_shared_and_of_zero_keys(hk):
+    """K and V broadcast over the heads (stride 0), a page of zeros (scale 0, codes 0), and no summaries kept."""
+    pool, k, v, code, scale = _pool(hk, None, 3, 4, 64, torch.bfloat16)
+    x = torch.zeros(64, 1, 64, dtype=torch.bfloat16, device="cuda").expand(64, 4, 64)
+    hk.heatkv_paged_store(pool, x, x, _i32(range(64, 128)))
+    assert (k[1] == 0).all() and (code[1] == 0).all() and (scale[1] == 0).all() and k[0].isnan().all() and k[2].isnan().all()
+    pool, k, v, _, _ = _pool(hk, None, 3, 4, 64, torch.bfloat16, summaries=False)
+    hk.heatkv_paged_store(pool, x, x, _i32(range(64)))
+    assert (v[0] == 0).all() and v[1].isnan().all()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+
+def _filled(hk, g, rng, lens, Hkv, d, dt, layout="head", spare_pages=2, **more):
+    """A pool whose requests' rows are random and everything else NaN."""
+    n_pages = sum(-(-kv // PAGE) for _, kv in lens) + spare_pages
+    pool, k, v, code, scale = _pool(hk, g, n_pages, Hkv, d, dt, layout)
+    b, table, q_begin = _batch(hk, rng, lens, n_pages, **more)
+    for i, (_, kv) in enumerate(lens):
+        for pg in range(-(-kv // PAGE)):
+            rows = min(PAGE, kv - pg * PAGE)
+            for x in (k, v):
+                x[table[i, pg], :, :rows] = torch.empty(Hkv, rows, d, dtype=dt, device="cuda").normal_(generator=g)
+    return pool, b, table, q_begin, k, v, code, scale
+
+
+def _check(out, lse, q, k, v, lens, table, q_begin, Hkv, causal, scale, dtype, chosen=None):
+    G, d = q.shape[1] // Hkv, q.shape[2]
+    u = 2.0**-8 if dtype == "bf16" else 2.0**-11
+    out, q, k, v = (_np(x).astype(np.float64) for x in (out, q, k, v))
+    lse = None if lse is None else lse.cpu().numpy().astype(np.float64)
+    for i, (n, kv) in enumerate(lens):
+        pages = table[i, : -(-kv // PAGE)]
+        for h in range(Hkv):
+            keys, values = k[pages, h].reshape(-1, d), v[pages, h].reshape(-1, d)
+            rows = slice(q_begin[i], q_begin[i] + n)
+            at = np.arange(kv - n, kv)
+            j = np.arange(len(keys))
+            seen = np.broadcast_to(j < kv, (n, len(keys)))
+            if causal:
+                seen = seen & (j <= at[:, None])
+            if chosen is not None:
+                seen = seen & np.repeat(chosen[i][h], PAGE, axis=1)
+            for g in range(G):
+                o, l, pv, reach = P.attention(q[rows, h * G + g], keys, values, seen, scale)
+                off = (d + 8) * 2.0**-24 * reach + 2.0**-18
+                big = np.abs(np.where(np.isfinite(values), values, 0.0)).max(initial=0.0)
+                tol = u * np.abs(o) + (u + 2 * off)[:, None] * pv + (len(keys) * 2.0**-25 * big if dtype == "fp16" else 0.0) + 1e-30
+                got = out[rows, h * G + g]
+                assert np.isfinite(got).all()
+                assert (np.abs(got - o) <= tol).all(), (i, h, g, float((np.abs(got - o) / tol).max()))
+                if lse is not None:
+                    gl = lse[rows, h * G + g]
+                    assert np.array_equal(np.isinf(gl), np.isinf(l))
+                    fin = np.isfinite(l)
+                    assert (np.abs(gl - l)[fin] <= (off + 2.0**-22 * np.abs(l))[fin]).all(), (i, h, g)
+
+
+LENS = {                                                   # (new tokens, tokens in all) per request
+    "one_key": [(1, 1)],
+    "one_of_each": [(1, 2), (1, 63), (1, 64), (1, 65), (1, 128), (1, 129)],
+    "no_keys": [(1, 0), (1, 70), (0, 0), (2, 0), (0, 100)],
+    "decode": [(1, 1000), (1, 17), (1, 3), (1, 517), (1, 64)],
+    "long_one": [(1, 20011)],
+    "drafts": [(5, 130), (1, 40), (3, 64), (5, 5), (4, 66)],
+    "more_new_than_tokens": [(4, 2), (3, 0), (2, 65)],
+    "short_prompts": [(1, 1), (33, 33), (64, 64), (65, 65), (127, 127)],
+    "prompt": [(300, 300)],
+    "chunk_behind": [(130, 700), (257, 260), (128, 128 * 3)],
+    "mixed": [(1, 900), (200, 450), (1, 5), (70, 1000)],
+}
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(16, 16, 128, "bf16"), (32, 8, 128, "fp16"), (28, 4, 64, "bf16"), (5, 5, 64, "fp16"), (8, 1, 128, "bf16")])
+@pytest.mark.parametrize("name", LENS)
+def test_attention(hk, name, H, Hkv, d, dtype, causal):
+    lens = LENS[name]
+    rng = np.random.default_rng(len(name) + H)
+    g = torch.Generator("cuda").manual_seed(len(name) + H)
+    dt = DTYPES[dtype]
+    layout = "token" if (H + len(name)) % 2 else "head"
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, Hkv, d, dt, layout, spare=3)
+    T = b.n_tokens
+    q = torch.empty(T, H, d, dtype=dt, device="cuda").normal_(generator=g)
+    out, lse = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws, causal=causal)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, causal, 1 / math.sqrt(d), dtype)
+    assert (out[q_begin[-1]:] == 7.0).all() and (lse[q_begin[-1]:] == 7.0).all()
+    again = torch.zeros_like(out)
+    hk.heatkv_paged_attention(pool, b, q, again, None, ws, causal=causal)
+    assert torch.equal(again[: q_begin[-1]], out[: q_begin[-1]])      # and the same bits again, without the logarithms
+
+
+@pytest.mark.parametrize("G", [1, 3, 16, 17, 32])
+def test_attention_any_group(hk, G):
+    """Query heads per kv head, from one to as many as a row tile holds."""
+    lens = [(1, 200), (2, 64), (1, 1)]
+    rng, g = np.random.default_rng(G), torch.Generator("cuda").manual_seed(G)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 128, torch.bfloat16)
+    q = torch.empty(b.n_tokens, 2 * G, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_tokens, 2 * G, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 2 * G), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws, sm_scale=0.05)
+    _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 0.05, "bf16")
+
+
+@pytest.mark.parametrize("max_new", [1, 4, 1000])
+@pytest.mark.parametrize("name", ["decode", "drafts", "mixed"])
+def test_attention_with_a_wrong_longest_request(hk, name, max_new):
+    """max_new picks the kernel and nothing else."""
+    lens = LENS[name]
+    rng, g = np.random.default_rng(3), torch.Generator("cuda").manual_seed(3)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 4, 128, torch.bfloat16)
+    b.max_new = max_new
+    q = torch.empty(b.n_tokens, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_tokens, 16, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 16), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, 4, True, 1 / math.sqrt(128), "bf16")
+
+
+@pytest.mark.parametrize("name", ["decode", "chunk_behind"])
+def test_attention_strides_streams_and_shifted_maxima(hk, name):
+    """q inside a QKV tensor, out with a gap between heads, another stream than the tensors', and logits whose maximum rises by
+    hundreds along the keys (every reference moves) or sits on the first key."""
+    lens = LENS[name]
+    rng, g = np.random.default_rng(5), torch.Generator("cuda").manual_seed(5)
+    for rise in (40.0, -40.0):
+        pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 64, torch.bfloat16)
+        for i, (_, kv) in enumerate(lens):
+            for pg in range(-(-kv // PAGE)):
+                k[table[i, pg], :, :, 0] = rise * pg / max(kv // PAGE, 1)
+        qkv = torch.empty(b.n_tokens, 8, 64, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        qkv[:, :, 0] = 16.0
+        q = qkv[:, 2:6]
+        wide = torch.full((b.n_tokens, 4, 80), 7.0, dtype=torch.bfloat16, device="cuda")
+        out, lse = wide[..., :64], torch.zeros(b.n_tokens, 4, device="cuda")
+        ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 4), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        hk.heatkv_paged_attention(pool, b, q, out, lse, ws, stream=side)
+        side.synchronize()
+        _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 0.125, "bf16")
+        assert (wide[..., 64:] == 7.0).all()
+
+
+def test_attention_of_a_pool_past_32_bits(hk):
+    """Pages whose first element lies past 2^31 and, in bytes, past 2^32."""
+    Hkv, d, n_pages = 8, 128, 33500
+    k, v = (torch.empty(n_pages, Hkv, PAGE, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    g = torch.Generator("cuda").manual_seed(0)
+    table = np.array([[n_pages - 1, 3, n_pages - 2], [n_pages - 7, 32768, -1]])
+    lens = [(1, 180), (70, 100)]
+    code = torch.zeros(n_pages, Hkv, d, dtype=torch.int8, device="cuda")
+    pool = hk.PagedPool.make(k, v, code, torch.zeros(n_pages, Hkv, device="cuda"))
+    b = hk.PagedBatch.make(_i32([0, 1, 71]), _i32([180, 100]), _i32(table), 71, 70)
+    slots = [table[i, p // PAGE] * PAGE + p % PAGE for i, (_, kv) in enumerate(lens) for p in range(kv)]
+    kv_new = torch.empty(2, len(slots), Hkv, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    hk.heatkv_paged_store(pool, kv_new[0], kv_new[1], _i32(slots))
+    q = torch.empty(71, 16, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.zeros_like(q), torch.zeros(71, 16, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 16), dtype=torch.uint8, device="cuda")
+    used = sorted(set(table[table >= 0].tolist()))
+    small = {p: i for i, p in enumerate(used)}
+    mapped = np.vectorize(lambda p: small.get(p, -1))(table)
+    ks, vs = k[used], v[used]
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    _check(out, lse, q, ks, vs, lens, mapped, [0, 1, 71], Hkv, True, 1 / math.sqrt(d), "bf16")
+    b.max_new = 1
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    _check(out, lse, q, ks, vs, lens, mapped, [0, 1, 71], Hkv, True, 1 / math.sqrt(d), "bf16")
+    c, s = P.summary(_np(k[n_pages - 1, 2]))
+    assert np.array_equal(code[n_pages - 1, 2].cpu().numpy(), c)
+
+
+# ------------------------------------------------------------------------------------------------ page selection
+
+def _summaries(k, code, scale, pages):
+    for page in pages:
+        for h in range(k.shape[1]):
+            c, s = P.summary(_np(k[page, h]))
+            code[page, h], scale[page, h] = torch.from_numpy(c).to(torch.int8), float(s)
+
+
+@pytest.mark.parametrize("sink,local,n_select", [(0, 1, 1), (1, 2, 8), (2, 3, 5), (0, 1, 40)])
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(16, 16, 128, "bf16"), (14, 2, 64, "fp16"), (16, 1, 128, "fp16"), (8, 2, 128, "bf16")])
+@pytest.mark.parametrize("name", ["decode", "drafts", "no_keys", "more_new_than_tokens", "chunk_behind"])
+def test_select_and_sparse_attention(hk, name, H, Hkv, d, dtype, sink, local, n_select):
+    lens = LENS[name]
+    rng, g = np.random.default_rng(H + d), torch.Generator("cuda").manual_seed(H + d)
+    dt = DTYPES[dtype]
+    pool, b, table, q_begin, k, v, code, scale = _filled(hk, g, rng, lens, Hkv, d, dt, spare=2)
+    for i, (_, kv) in enumerate(lens):
+        _summaries(k, code, scale, table[i, : kv // PAGE])
+    # ties: two pages of the longest request have the same summary, and one head's codes are all zero
+    longest = max(range(len(lens)), key=lambda i: lens[i][1])
+    if lens[longest][1] >= 4 * PAGE:
+        a, c = table[longest, 1], table[longest, 3]
+        code[a], scale[a] = code[c], scale[c]
+    code[:, Hkv - 1] = 0
+    T, G = b.n_tokens, H // Hkv
+    q = torch.empty(T, H, d, dtype=dt, device="cuda").normal_(generator=g)
+    sel = torch.full((T, Hkv, n_select), -9, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, sink, local)
+    got, qf, cn, sn = sel.cpu().numpy(), _np(q), code.cpu().numpy(), scale.cpu().numpy()
+    chosen = []
+    for i, (n, kv) in enumerate(lens):
+        pages = table[i, : -(-kv // PAGE)]
+        mask = np.zeros((Hkv, n, len(pages)), dtype=bool)
+        for t in range(n):
+            pos = kv - n + t
+            for h in range(Hkv):
+                want = P.select(qf[q_begin[i] + t, h * G:(h + 1) * G], cn[pages, h], sn[pages, h], pos, sink, local, n_select) if pos >= 0 else []
+                assert got[q_begin[i] + t, h].tolist() == want + [-1] * (n_select - len(want)), (i, t, h)
+                mask[h, t, want] = True
+        chosen.append(mask)
+    assert (got[q_begin[-1]:] == -1).all()
+    out, lse = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype, chosen)
+    assert (out[q_begin[-1]:] == 0).all() and torch.isneginf(lse[q_begin[-1]:]).all()
+
+
+def test_select_of_a_long_context(hk):
+    """1500 pages, scores that are nearly all equal (three codes), and the score's sign."""
+    n_pages, Hkv, d = 1500, 2, 64
+    rng, g = np.random.default_rng(1), torch.Generator("cuda").manual_seed(1)
+    pool, k, v, code, scale = _pool(hk, g, n_pages, Hkv, d, torch.bfloat16, fill=0.0)
+    code.copy_(torch.randint(-1, 2, code.shape, generator=g, device="cuda"))
+    scale.copy_(2.0 ** torch.randint(-2, 1, scale.shape, generator=g, device="cuda"))
+    kv = n_pages * PAGE - 5
+    b, table, _ = _batch(hk, rng, [(3, kv)], n_pages)
+    q = torch.randint(-1, 2, (3, 4, d), generator=g, device="cuda").to(torch.bfloat16)
+    q[2] = 0
+    sel = torch.zeros(3, Hkv, 200, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, 3, 4)
+    pages, cn, sn = table[0, :n_pages], code.cpu().numpy(), scale.cpu().numpy()
+    for t in range(3):
+        for h in range(Hkv):
+            assert sel[t, h].tolist() == P.select(_np(q)[t, 2 * h: 2 * h + 2], cn[pages, h], sn[pages, h], kv - 3 + t, 3, 4, 200)
+
+
+def test_sparse_attention_over_lists_of_any_kind(hk):
+    """Gaps in a list, entries past the token's page and past the table, an empty list, pages out of order."""
+    lens = [(2, 500), (1, 64 * 6)]
+    rng, g = np.random.default_rng(2), torch.Generator("cuda").manual_seed(2)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 128, torch.bfloat16)
+    sel = np.full((3, 2, 5), -1)
+    sel[0, 0] = [3, -1, 7, 0, 2**30]
+    sel[0, 1] = [1, 2, -5, 8, 9]                           # page 8: past the token's own; 9: past the table
+    sel[1, 0] = [7, 6, 5, 4, 3]
+    sel[2] = [[5, -1, -1, -1, -1], [0, 1, 2, 3, 4]]
+    chosen = [np.zeros((2, n, -(-kv // PAGE)), dtype=bool) for n, kv in lens]
+    for t, (i, at) in enumerate([(0, 0), (0, 1), (1, 0)]):
+        for h in range(2):
+            for p in sel[t, h]:
+                if 0 <= p < chosen[i].shape[2]:
+                    chosen[i][h, at, p] = True
+    q = torch.empty(3, 8, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.full_like(q, 7.0), torch.full((3, 8), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 8), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_sparse_attention(pool, b, q, _i32(sel), out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(128), "bf16", chosen)
+    assert (out[1, 4:] == 0).all()

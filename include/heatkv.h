@@ -451,7 +451,7 @@ typedef struct {                 /* the requests of a step                      
   int32_t max_new;               /* new tokens of the longest request: picks the kernel; any value gives right results */
 } heatkv_paged_batch;
 
-typedef struct {                 /* element strides of [n_tokens][n_heads][d] activations: at least d, multiples of 8 (o_*: of 4) */
+typedef struct {                 /* element strides of [n_tokens][n_heads][d] activations: at least d, multiples of 8 */
   int64_t q_tok, q_head, o_tok, o_head;
 } heatkv_token_strides;
 
@@ -495,7 +495,7 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
  *   q DEVICE [n_tokens][n_heads][d], out the same shape; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
  *   lse DEVICE fp32 [n_tokens][n_heads], the natural logarithm of the sum of exponentials, or NULL
  * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows past q_begin[n_seq] are left
- * as they are.  n_heads / n_kv_heads at most 32. */
+ * as they are.  n_heads / n_kv_heads at most 128. */
 int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
                            uint64_t workspace_bytes, void* stream);

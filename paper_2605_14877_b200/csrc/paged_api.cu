@@ -61,7 +61,7 @@ int attention_params(const heatkv_paged_pool* pool, const heatkv_paged_batch* b,
   if (rc != HEATKV_OK) return rc;
   const int64_t row = (int64_t)n_heads * pool->d;
   const heatkv_token_strides s = st ? *st : heatkv_token_strides{row, pool->d, row, pool->d};
-  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || ((s.q_tok | s.q_head) & 7) || ((s.o_tok | s.o_head) & 3)) return HEATKV_ERR_INVALID_ARG;
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || ((s.q_tok | s.q_head | s.o_tok | s.o_head) & 7)) return HEATKV_ERR_INVALID_ARG;
   if (s.q_tok < pool->d || s.q_head < pool->d || s.o_tok < pool->d || s.o_head < pool->d) return HEATKV_ERR_INVALID_ARG;
   if (!(sm_scale == sm_scale) || sm_scale > 1e30f) return HEATKV_ERR_INVALID_ARG;
   *p = PagedParams{};
@@ -90,10 +90,8 @@ int attention_params(const heatkv_paged_pool* pool, const heatkv_paged_batch* b,
 }
 
 uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int n_tokens, int n_seq) {
-  (void)G;
-  (void)n_tokens;
-  (void)n_seq;
-  return PAGED_WS_PARTIALS + paged_small_partial_bytes(d, dev.n_sm);
+  const uint64_t a = paged_small_partial_bytes(d, dev.n_sm), b = paged_tc_partial_bytes(d, dev.n_sm, G, n_tokens, n_seq);
+  return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 
 int place_workspace(const PagedDevice& dev, const heatkv_paged_pool* pool, void* ws, uint64_t bytes, PagedParams* p) {
@@ -174,8 +172,9 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
   rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);
   if (rc != HEATKV_OK) return rc;
   p.causal = causal != 0;
-  if (p.G > 32) return HEATKV_ERR_SHAPE_MISMATCH;
-  return done(launch_paged_small(p, *pool, dev, static_cast<cudaStream_t>(stream)));
+  // up to 32 rows of the longest request: the warp-level kernel
+  const bool few = (int64_t)p.max_new * p.G <= 32;
+  return done((few ? launch_paged_small : launch_paged_tc)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 
 int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,

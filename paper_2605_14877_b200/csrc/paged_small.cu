@@ -13,8 +13,7 @@
 
 #include <cuda_fp16.h>
 
-#include "paged.h"
-#include "tc_common.cuh"
+#include "paged_wait.cuh"
 
 namespace heatkv {
 namespace {
@@ -250,7 +249,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) paged_small_kernel(const __grid
         }
         const int page = __shfl_sync(0xffffffffu, pages, in);
         const uint32_t st = g % stages, use = g / stages;
-        if (use > 0) ok = warp_wait(empty(st), (use - 1) & 1, abort_flag, p.status);
+        if (use > 0) ok = wait_all(empty(st), (use - 1) & 1, abort_flag, p.status, 1);
         if (!ok) break;
         if (leader) {
           mbar_expect_tx(full(st), 2 * L::TILE);
@@ -269,7 +268,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) paged_small_kernel(const __grid
       for (uint32_t s = 0; s < (uint32_t)stages; ++s) {
         if (g <= s) break;
         const uint32_t uses = (g - s + stages - 1) / stages;       // copies into this stage so far
-        for (uint32_t t = 0; t < WAIT_LIMIT && !mbar_try(full(s), (uses - 1) & 1); ++t) {}
+        settle(full(s), (uses - 1) & 1);
       }
     }
     return;
@@ -328,7 +327,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) paged_small_kernel(const __grid
         if (lp < 0 || lp >= p.table_pages) lp = 1 << 24;           // past every limit
       }
       const uint32_t st = g % stages, use = g / stages;
-      ok = __all_sync(0xffffffffu, mbar_wait(full(st), use & 1, abort_flag, p.status));
+      ok = wait_all(full(st), use & 1, abort_flag, p.status, 2);
       if (!ok) break;
       const uint32_t kt = sbase + st * 2 * L::TILE, vt = kt + L::TILE;
       const int first = lp * PAGE + key0;                          // key number of this warp's first key

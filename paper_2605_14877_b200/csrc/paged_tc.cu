@@ -1,0 +1,805 @@
+// Attention of many query rows over a paged cache (chunks of prompts, an image's scale) on the tensor cores' own memory.
+//
+// A row tile is floor(128 / G) consecutive tokens of a request times the G query heads of one kv head; an item is two of them (A and B),
+// which share the stream of key tiles (128 keys: two pages).  The key tiles of all items, request by request, head by head, in token
+// order, are dealt out in equal runs, one per SM, so that every SM ends at the same time whatever the lengths; an item that a run's border
+// cuts leaves unnormalised rows in the workspace, where the warp that arrives last for its 32 rows adds the parts up in key order.
+// Warp roles as in attn_tc.cu:
+//   warp 0       walks the CTA's run, tells the others the items (a two-entry ring) and sends for Q, K and V (TMA);
+//   warp 1       issues the products: S = Q K^T and O += P V, accumulators in tensor memory;
+//   warps 4-7    softmax of tile A, warps 8-11 of tile B, one thread a row; they write the item's rows, too.
+// Tensor memory: S_A/P_A 0..127, S_B/P_B 128..255, O_A 256..383, O_B 384..511.  Rows past a request's last key in its last page are
+// whatever the pool holds: their logits are masked, their values overwritten by zeros before the product (warp 1).
+// Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and leaves.
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "paged_wait.cuh"
+
+namespace heatkv {
+namespace {
+
+using namespace tc;
+
+constexpr int BM = 128, BN = 128;
+constexpr int THREADS = 384;
+constexpr int KV_STAGES = 2;
+// Register hand-over between warpgroups, inside what the launch allocates (checked against the compiled kernel before it runs).
+constexpr int REGS_LAUNCH = 168, REGS_SMALL = 72, REGS_SOFTMAX = 216;
+static_assert(128 * REGS_SMALL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register hand-over exceeds the CTA's allocation");
+constexpr uint32_t HALF_COLS_BYTES = 128 * 128;        // one 64-column half of a 128-row tile
+constexpr uint32_t SLOT_BYTES = PAGE * 128;            // a page inside one column half
+constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 rows x 32 columns on their way out
+
+template <int D>
+struct Layout {
+  static constexpr int NCH = D / 64;
+  static constexpr uint32_t TILE_BYTES = NCH * HALF_COLS_BYTES;
+  static constexpr uint32_t SM_Q = 0;
+  static constexpr uint32_t SM_K = SM_Q + 2 * TILE_BYTES;
+  static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;
+  static constexpr uint32_t SM_OUT = SM_V + KV_STAGES * TILE_BYTES;
+  static constexpr uint32_t SM_BAR = SM_OUT + 8 * STAGE_BYTES;
+  static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;
+  static_assert(SM_ALLOC <= 227 * 1024, "shared memory of one CTA");
+  // one part of a cut item: O of both tiles (groups of four columns outermost), then references and sums
+  static constexpr int SLOT_FLOATS = 2 * BM * D + 2 * 2 * BM;
+};
+enum Bar : uint32_t {
+  Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 6, V_FULL = 8, V_EMPTY = 10, S_FULL = 12, P_FULL = 14, PV_DONE = 18, ITEM_FULL = 20, ITEM_EMPTY = 22,
+  N_BARS = 24
+};
+constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256;
+enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1 };
+
+struct TcParams {
+  PagedParams a;
+  // the plan of the call: key tiles (of all heads) before every request; its first item; key tiles of one head before every item
+  int64_t* seq_prefix;        // [n_seq + 1]
+  int32_t* item_begin;        // [n_seq + 1]
+  int32_t* item_prefix;       // [items]
+  int32_t* runs;              // [n_sm][RUN_WORDS] where every CTA's run starts
+  int32_t items;              // room for the items
+  int32_t n_cta;
+};
+enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_TILES, R_C0_FIRST, R_C1_FIRST, R_C1_LAST, RUN_WORDS };
+struct TcMaps {
+  CUtensorMap q, k, v;
+};
+
+__device__ __forceinline__ int request_tokens(const PagedParams& p, int i, int& b) {
+  b = max(p.q_begin[i], 0);
+  return max(min(p.q_begin[i + 1], p.n_tokens) - b, 0);
+}
+__device__ __forceinline__ int request_keys(const PagedParams& p, int i) { return min(max(p.kv_len[i], 0), p.table_pages * PAGE); }
+// Key tiles of the item that starts at token `tok` of a request: up to the last key that its last token sees, at least one (which then
+// is masked whole, so that rows without keys are written like all others).
+__device__ __forceinline__ int item_tiles(const PagedParams& p, int tok, int n, int kv) {
+  const int upto = p.causal ? min(kv, kv - n + min(n, tok + 2 * p.tile_tokens)) : kv;
+  return max(1, (upto + BN - 1) / BN);
+}
+
+constexpr int PT = 1024;
+// One CTA: what every request's items weigh, and the sums that the attention kernel's CTAs look their run up in.
+__global__ void __launch_bounds__(PT) plan_kernel(const TcParams tp) {
+  const PagedParams& p = tp.a;
+  __shared__ int64_t sums[PT / 32][2];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pair = 2 * p.tile_tokens;
+  auto scan = [&](int64_t v, int which, int64_t& all) {
+    int64_t inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp][which] = inc;
+    __syncthreads();
+    int64_t before = 0;
+    all = 0;
+    for (int w = 0; w < PT / 32; ++w) {
+      if (w < warp) before += sums[w][which];
+      all += sums[w][which];
+    }
+    return before + inc - v;
+  };
+  // items of every request
+  const int per = (p.n_seq + PT - 1) / PT, i0 = min(tid * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
+  int64_t items = 0, all;
+  int b;
+  for (int i = i0; i < i1; ++i) items += (request_tokens(p, i, b) + pair - 1) / pair;
+  int64_t at = scan(items, 0, all);
+  for (int i = i0; i < i1; ++i) {
+    tp.item_begin[i] = (int)min(at, (int64_t)tp.items);
+    at += (request_tokens(p, i, b) + pair - 1) / pair;
+  }
+  if (tid == 0) tp.item_begin[p.n_seq] = (int)min(all, (int64_t)tp.items);
+  __syncthreads();
+  // a warp per request: key tiles before every item
+  for (int i = warp; i < p.n_seq; i += PT / 32) {
+    const int n = request_tokens(p, i, b), kv = request_keys(p, i), first = tp.item_begin[i], count = tp.item_begin[i + 1] - first;
+    int before = 0;
+    for (int base = 0; base < count; base += 32) {
+      const int w = base + lane < count ? item_tiles(p, (base + lane) * pair, n, kv) : 0;
+      int inc = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+      }
+      if (base + lane < count) tp.item_prefix[first + base + lane] = before + inc - w;
+      before += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) tp.seq_prefix[i] = (int64_t)before * p.Hkv;
+  }
+  __syncthreads();
+  int64_t w = 0;
+  for (int i = i0; i < i1; ++i) w += tp.seq_prefix[i];
+  int64_t x = scan(w, 1, all);
+  for (int i = i0; i < i1; ++i) {
+    const int64_t v = tp.seq_prefix[i];
+    tp.seq_prefix[i] = x;
+    x += v;
+  }
+  if (tid == 0) tp.seq_prefix[p.n_seq] = all;
+  __syncthreads();
+  // the runs: where each starts, and which CTAs hold the first and the last part of the items at its two ends
+  const int grid = (int)min((int64_t)tp.n_cta, all);               // every run holds a tile, so all CTAs between have a part
+  auto bound = [&](int c) { return all * c / grid; };
+  auto owner = [&](int64_t y) {
+    int c = (int)(y * grid / all);
+    while (c + 1 < grid && bound(c + 1) <= y) ++c;
+    while (c > 0 && bound(c) > y) --c;
+    return c;
+  };
+  struct Place {
+    int seq, head, item, j0, tiles;
+    int64_t begin;
+  };
+  auto place = [&](int64_t y) {
+    Place r;
+    int lo = 0, hi = p.n_seq - 1;                                  // last request that starts at or before y
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tp.seq_prefix[mid] <= y) lo = mid; else hi = mid - 1;
+    }
+    r.seq = lo;
+    const int64_t s0 = tp.seq_prefix[lo], per_head = (tp.seq_prefix[lo + 1] - s0) / p.Hkv;
+    r.head = (int)((y - s0) / per_head);
+    const int local = (int)(y - s0 - r.head * per_head);
+    const int first = tp.item_begin[r.seq];
+    lo = 0;
+    hi = tp.item_begin[r.seq + 1] - first - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tp.item_prefix[first + mid] <= local) lo = mid; else hi = mid - 1;
+    }
+    r.item = lo;
+    r.j0 = local - tp.item_prefix[first + lo];
+    r.begin = y - r.j0;
+    int b0;
+    const int n = request_tokens(p, r.seq, b0);
+    r.tiles = item_tiles(p, lo * pair, n, request_keys(p, r.seq));
+    return r;
+  };
+  for (int c = tid; c < tp.n_cta; c += PT) {
+    int32_t* run = tp.runs + c * RUN_WORDS;
+    if (c >= grid) {
+      run[R_TILES] = 0;
+      continue;
+    }
+    const int64_t y0 = bound(c), y1 = bound(c + 1);
+    const Place a = place(y0), z = place(y1 - 1);
+    run[R_SEQ] = a.seq;
+    run[R_HEAD] = a.head;
+    run[R_ITEM] = a.item;
+    run[R_J0] = a.j0;
+    run[R_TILES] = (int)min(y1 - y0, (int64_t)INT32_MAX);
+    run[R_C0_FIRST] = owner(a.begin);
+    run[R_C1_FIRST] = owner(a.begin + a.tiles - 1);
+    run[R_C1_LAST] = owner(z.begin + z.tiles - 1);
+  }
+}
+
+__device__ __forceinline__ int ring_word(const volatile int32_t* ring, int word) { return __shfl_sync(0xffffffffu, ring[word], 0); }
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (F16) {
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+  }
+  return pack_bf16(lo, hi);
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
+  using L = Layout<D>;
+  constexpr int NCH = L::NCH;
+  constexpr uint32_t TILE_BYTES = L::TILE_BYTES, SM_Q = L::SM_Q, SM_K = L::SM_K, SM_V = L::SM_V, SM_OUT = L::SM_OUT, SM_BAR = L::SM_BAR;
+  // How far (log2) a maximum may rise above the reference of its row's exponentials: bf16 and the 32-bit sums have room for 2^32,
+  // fp16 probabilities for 2^15.
+  constexpr float THRESHOLD = F16 ? 8.f : RESCALE_THRESHOLD;
+  const PagedParams& p = tp.a;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t sbase = (raw + 1023u) & ~1023u;
+  unsigned char* sgen = smem_raw + (sbase - raw);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(sgen + SM_BAR + BAR_ABORT);
+  volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(sgen + SM_BAR + BAR_TMEM_PTR);
+  volatile int32_t* ring_base = reinterpret_cast<volatile int32_t*>(sgen + SM_BAR + BAR_RING);
+  auto bar = [&](uint32_t which) { return sbase + SM_BAR + which * 8; };
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+
+  pdl_trigger();
+  if (threadIdx.x == 0) {
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(bar(Q_FULL + x), 1);
+      mbar_init(bar(Q_EMPTY + x), 1);
+      mbar_init(bar(S_FULL + x), 1);
+      mbar_init(bar(P_FULL + 2 * x), BM);
+      mbar_init(bar(P_FULL + 2 * x + 1), BM);
+      mbar_init(bar(PV_DONE + x), 1);
+      mbar_init(bar(ITEM_FULL + x), 1);
+      mbar_init(bar(ITEM_EMPTY + x), 9);
+    }
+    for (int s = 0; s < KV_STAGES; ++s) {
+      mbar_init(bar(K_FULL + s), 1);
+      mbar_init(bar(K_EMPTY + s), 1);
+      mbar_init(bar(V_FULL + s), 1);
+      mbar_init(bar(V_EMPTY + s), 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 0) {
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + SM_BAR + BAR_TMEM_PTR), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (threadIdx.x == 0) *abort_flag = *reinterpret_cast<volatile uint32_t*>(p.status) != 0;      // an earlier CTA gave up: do not wait again
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_smem, 0);
+
+  if (warp < 4) {
+    reg_dealloc<REGS_SMALL>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- the CTA's run, and the copies
+      const bool leader = elect_one();
+      const int32_t* run = tp.runs + blockIdx.x * RUN_WORDS;
+      int left = run[R_TILES], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
+      if (left > 0) {
+        seq = run[R_SEQ];
+        head = run[R_HEAD];
+        item = run[R_ITEM];
+        j0 = run[R_J0];
+      }
+      uint32_t g = 0, iq[2] = {0, 0};                              // key tiles sent for; items that loaded query tile x
+      uint32_t armed_k = 0, armed_v = 0, armed_q = 0, par_k = 0, par_v = 0, par_q = 0;
+      const uint32_t q_bytes = (uint32_t)(p.tile_tokens * p.G) * 128;
+      bool ok = true;
+      for (uint32_t it = 0; ok; ++it) {
+        const uint32_t slot = it & 1;
+        volatile int32_t* ring = ring_base + slot * 16;
+        if (it >= 2) ok = wait_all(bar(ITEM_EMPTY + slot), ((it >> 1) - 1) & 1, abort_flag, p.status, 1 + ITEM_EMPTY);
+        if (!ok) break;
+        if (left <= 0) {
+          if (lane == 0) ring[W_KIND] = 0;
+          __syncwarp();
+          if (leader) mbar_arrive(bar(ITEM_FULL + slot));
+          break;
+        }
+        int q_first;
+        const int n_items = tp.item_begin[seq + 1] - tp.item_begin[seq];
+        const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
+        const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
+        const int tiles = item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
+        const int nq = tokens > p.tile_tokens ? 2 : 1;
+        if (lane == 0) {
+          ring[W_KIND] = 1;
+          ring[W_SEQ] = seq;
+          ring[W_HEAD] = head;
+          ring[W_TOK0] = q_first + tok;
+          ring[W_TOKENS] = tokens;
+          ring[W_POS0] = kv - n + tok;
+          ring[W_KV] = kv;
+          ring[W_J0] = j0;
+          ring[W_NT] = n_tiles;
+          ring[W_TILES] = tiles;
+          ring[W_C0] = it == 0 ? run[R_C0_FIRST] : (int)blockIdx.x;
+          ring[W_C1] = it == 0 ? run[R_C1_FIRST] : run[R_C1_LAST];
+        }
+        __syncwarp();
+        if (leader) mbar_arrive(bar(ITEM_FULL + slot));
+        left -= n_tiles;
+        const int32_t* table = p.block_table + seq * p.table_stride;
+        const int n_pages = (kv + PAGE - 1) / PAGE;
+        int pages = -1;
+        for (int j = 0; j < n_tiles && ok; ++j, ++g) {
+          if ((j & 15) == 0) {                                     // page numbers of 16 tiles at a time, one per lane
+            const int pg = 2 * (j0 + j) + lane;
+            pages = pg < n_pages ? table[pg] : -1;
+            if (pages >= p.n_pages || pages < 0) pages = -1;       // (a box outside of the map arrives as zeros)
+          }
+          const int pg0 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15)), pg1 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15) + 1);
+          const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
+          auto load = [&](uint32_t smem, const CUtensorMap* map, uint32_t full) {
+            if (!leader) return;
+            mbar_expect_tx(full, TILE_BYTES);
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch) {
+              tma_load_4d(smem + ch * HALF_COLS_BYTES, map, ch * 64, 0, head, pg0, full);
+              tma_load_4d(smem + ch * HALF_COLS_BYTES + SLOT_BYTES, map, ch * 64, 0, head, pg1, full);
+            }
+          };
+          if (use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
+          if (!ok) break;
+          armed_k |= 1u << st;
+          par_k = (par_k & ~(1u << st)) | ((use & 1) << st);
+          load(sbase + SM_K + st * TILE_BYTES, &maps.k, bar(K_FULL + st));
+          if (j == 0) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              if (y >= nq || !ok) continue;
+              if (iq[y] > 0) ok = wait_all(bar(Q_EMPTY + y), (iq[y] - 1) & 1, abort_flag, p.status, 1 + Q_EMPTY);
+              if (!ok) continue;
+              armed_q |= 1u << y;
+              par_q = (par_q & ~(1u << y)) | ((iq[y] & 1) << y);
+              ++iq[y];
+              if (leader) {
+                mbar_expect_tx(bar(Q_FULL + y), NCH * q_bytes);
+                for (int ch = 0; ch < NCH; ++ch)
+                  tma_load_4d(sbase + SM_Q + y * TILE_BYTES + ch * HALF_COLS_BYTES, &maps.q, ch * 64, head * p.G, q_first + tok + y * p.tile_tokens, 0,
+                              bar(Q_FULL + y));
+              }
+            }
+            if (!ok) break;
+          }
+          if (use > 0) ok = wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
+          if (!ok) break;
+          armed_v |= 1u << st;
+          par_v = (par_v & ~(1u << st)) | ((use & 1) << st);
+          load(sbase + SM_V + st * TILE_BYTES, &maps.v, bar(V_FULL + st));
+          __syncwarp();
+        }
+        __syncwarp();
+        // the next item of the run: the request's next tokens, its next head, the next request with tokens
+        j0 = 0;
+        if (++item == n_items) {
+          item = 0;
+          if (++head == p.Hkv) {
+            head = 0;
+            do ++seq; while (left > 0 && seq + 1 < p.n_seq && tp.item_begin[seq + 1] == tp.item_begin[seq]);
+          }
+        }
+      }
+      if (!ok || *abort_flag) {
+        // leaving early: every copy under way lands before the CTA exits
+        for (int s = 0; s < KV_STAGES; ++s) {
+          if (armed_k & (1u << s))
+            settle(bar(K_FULL + s), (par_k >> s) & 1);
+          if (armed_v & (1u << s))
+            settle(bar(V_FULL + s), (par_v >> s) & 1);
+        }
+        for (int y = 0; y < 2; ++y)
+          if (armed_q & (1u << y))
+            settle(bar(Q_FULL + y), (par_q >> y) & 1);
+      }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- products
+      constexpr uint32_t TYPE = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;           // operand types: the descriptor's default is bf16
+      constexpr uint32_t IDESC_S = instr_desc(BM, BN, 0, 0) & TYPE, IDESC_PV = instr_desc(BM, D, 0, 1) & TYPE;
+      bool ok = true;
+      auto mma_wait = [&](uint32_t which, uint32_t parity) { return wait_all(bar(which), parity, abort_flag, p.status, 1 + which); };
+      const uint32_t q_lo = desc_lo(sbase + SM_Q, 16), k_lo = desc_lo(sbase + SM_K, 16), v_lo = desc_lo(sbase + SM_V, HALF_COLS_BYTES);
+      auto issue_s = [&](uint32_t lead, int x, int st) {
+        const uint32_t qa = q_lo + x * (TILE_BYTES >> 4), ka = k_lo + st * (TILE_BYTES >> 4);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t off = ((ks >> 2) * HALF_COLS_BYTES + (ks & 3) * 32) >> 4;
+          mma_ss(lead, tmem + x * 128, qa + off, ka + off, IDESC_S, ks > 0);
+        }
+      };
+      auto issue_pv = [&](uint32_t lead, int x, int st, int h, bool first) {
+        const uint32_t va = v_lo + st * (TILE_BYTES >> 4);
+#pragma unroll
+        for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
+          mma_ts(lead, tmem + 256 + x * 128, tmem + x * 128 + ks * 8, va + ks * (2048 >> 4), IDESC_PV, !(first && ks == 0));
+      };
+      uint32_t g = 0, cx[2] = {0, 0}, iq[2] = {0, 0};
+      for (uint32_t it = 0; ok; ++it) {
+        const uint32_t slot = it & 1;
+        volatile int32_t* ring = ring_base + slot * 16;
+        ok = mma_wait(ITEM_FULL + slot, (it >> 1) & 1);
+        if (!ok) break;
+        if (ring_word(ring, W_KIND) == 0) break;
+        const int nq = ring_word(ring, W_TOKENS) > p.tile_tokens ? 2 : 1, n_tiles = ring_word(ring, W_NT);
+        const int kv_left = ring_word(ring, W_KV) - ring_word(ring, W_J0) * BN;      // keys of the request from the item's first on
+        // values of the tile: waited for, and rows without a key in the request's last page made zero
+        auto values = [&](uint32_t st, uint32_t parity, int j) {
+          if (!mma_wait(V_FULL + st, parity)) return false;
+          const int left = kv_left - j * BN;
+          if (left < BN && left > 0 && (left & (PAGE - 1))) {
+            const int r0 = left, r1 = (left + PAGE - 1) & ~(PAGE - 1);
+            for (int i = lane; i < (r1 - r0) * 8 * NCH; i += 32) {
+              const int ch = i / ((r1 - r0) * 8), rest = i - ch * (r1 - r0) * 8;
+              const uint32_t at = SM_V + st * TILE_BYTES + ch * HALF_COLS_BYTES + (r0 + (rest >> 3)) * 128 + (rest & 7) * 16;
+              *reinterpret_cast<int4*>(sgen + at) = make_int4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+          return true;
+        };
+        const uint32_t st0 = g % KV_STAGES, par0 = (g / KV_STAGES) & 1;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (x < nq && ok) ok = mma_wait(Q_FULL + x, iq[x] & 1);
+        if (ok) ok = mma_wait(K_FULL + st0, par0);
+        if (ok) {
+          const uint32_t lead = elect_one();
+          tc_fence_after();
+          for (int x = 0; x < nq; ++x) {
+            issue_s(lead, x, st0);
+            tc_commit(lead, bar(S_FULL + x));
+            if (n_tiles == 1) tc_commit(lead, bar(Q_EMPTY + x));
+          }
+          tc_commit(lead, bar(K_EMPTY + st0));
+        }
+        if (ok) ok = values(st0, par0, 0);
+        for (int j = 0; j < n_tiles && ok; ++j) {
+          const uint32_t st = (g + j) % KV_STAGES, stn = (g + j + 1) % KV_STAGES;
+          const uint32_t parn = ((g + j + 1) / KV_STAGES) & 1;
+          const bool more = j + 1 < n_tiles;
+          const uint32_t lead = elect_one();
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= nq || !ok) continue;
+            const uint32_t ph = (cx[x] + j) & 1;
+            ok = mma_wait(P_FULL + 2 * x, ph);
+            if (!ok) continue;
+            tc_fence_after();
+            issue_pv(lead, x, st, 0, j == 0);
+            if (more && x == 0) ok = mma_wait(K_FULL + stn, parn);
+            if (!ok) continue;
+            ok = mma_wait(P_FULL + 2 * x + 1, ph);
+            if (!ok) continue;
+            tc_fence_after();
+            issue_pv(lead, x, st, 1, false);
+            if (more) {
+              issue_s(lead, x, stn);
+              tc_commit(lead, bar(S_FULL + x));
+              if (j + 2 == n_tiles) tc_commit(lead, bar(Q_EMPTY + x));
+            } else {
+              tc_commit(lead, bar(PV_DONE + x));
+            }
+          }
+          if (ok) {
+            tc_commit(lead, bar(V_EMPTY + st));
+            if (more) tc_commit(lead, bar(K_EMPTY + stn));
+          }
+          if (ok && more) ok = values(stn, parn, j + 1);
+        }
+        g += n_tiles;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (x < nq) {
+            cx[x] += n_tiles;
+            ++iq[x];
+          }
+        __syncwarp();
+        if (ok && elect_one()) mbar_arrive(bar(ITEM_EMPTY + slot));
+      }
+    }
+  } else {
+    reg_alloc<REGS_SOFTMAX>();
+    // ------------------------------------------------------------------ softmax and results
+    const int x = (warp - 4) >> 2;
+    const int row = (warp & 3) * 32 + lane;                        // row of the tile == TMEM lane
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lane_base + x * 128, t_o = tmem + lane_base + 256 + x * 128;
+    unsigned char* stage = sgen + SM_OUT + (warp - 4) * STAGE_BYTES;
+    const int row_tok = row / p.G, row_head = row - row_tok * p.G;
+    uint32_t cx = 0, items_x = 0;
+    bool ok = true;
+    for (uint32_t it = 0; ok; ++it) {
+      const uint32_t slot = it & 1;
+      volatile int32_t* ring = ring_base + slot * 16;
+      ok = wait_all(bar(ITEM_FULL + slot), (it >> 1) & 1, abort_flag, p.status, 1 + ITEM_FULL);
+      if (!ok) break;
+      if (ring_word(ring, W_KIND) == 0) break;
+      const int n_tiles = ring_word(ring, W_NT), tokens = ring_word(ring, W_TOKENS);
+      if (x == 0 || tokens > p.tile_tokens) {
+        const int kv = ring_word(ring, W_KV), pos0 = ring_word(ring, W_POS0), skipped = ring_word(ring, W_J0) * BN;
+        const bool valid = row_tok < p.tile_tokens && x * p.tile_tokens + row_tok < tokens;
+        // keys that the row sees, counted from the run's first
+        const int sees = p.causal && valid ? min(pos0 + x * p.tile_tokens + row_tok + 1, kv) : kv;
+        const int lim = sees - skipped;
+        const int least = __reduce_min_sync(0xffffffffu, lim);
+        float m_ref = NO_MAX, l_sum = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < n_tiles && ok; ++j) {
+          const uint32_t ph = (cx + j) & 1;
+          ok = wait_all(bar(S_FULL + x), ph, abort_flag, p.status, 1 + S_FULL);
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t r0[32], r1[32], r2[32], r3[32];
+          tmem_ld32(t_s, r0);
+          tmem_ld32(t_s + 32, r1);
+          tmem_ld32(t_s + 64, r2);
+          tmem_ld32(t_s + 96, r3);
+          tmem_wait_ld();
+          if ((j + 1) * BN > least) {                              // some row of the warp does not see the whole tile
+            const int left = lim - j * BN;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              if (i >= left) r0[i] = 0xff800000u;
+              if (i + 32 >= left) r1[i] = 0xff800000u;
+              if (i + 64 >= left) r2[i] = 0xff800000u;
+              if (i + 96 >= left) r3[i] = 0xff800000u;
+            }
+          }
+          float mq[8];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            mq[c] = fmaxf(__uint_as_float(r0[c]), __uint_as_float(r1[c]));
+            mq[4 + c] = fmaxf(__uint_as_float(r2[c]), __uint_as_float(r3[c]));
+          }
+#pragma unroll
+          for (int i = 4; i < 32; i += 4) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              mq[c] = fmax3(mq[c], __uint_as_float(r0[i + c]), __uint_as_float(r1[i + c]));
+              mq[4 + c] = fmax3(mq[4 + c], __uint_as_float(r2[i + c]), __uint_as_float(r3[i + c]));
+            }
+          }
+          const float mx = fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7]))) * p.scale_log2;
+          const float m_new = fmaxf(m_ref, mx);
+          const bool grow = m_new > m_ref + THRESHOLD;             // also on the first tile with a key the row sees
+          if (j > 0 && __any_sync(0xffffffffu, grow)) {
+            // O is complete up to tile j - 1: the commit behind S_FULL covers every product issued before it
+            const float f = grow ? exp2f(m_ref - m_new) : 1.f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t r[32];
+              tmem_ld32(t_o + c * 32, r);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+              tmem_st32(t_o + c * 32, r);
+            }
+            tmem_wait_st();
+            l_sum *= f;
+          }
+          if (grow) m_ref = m_new;
+          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), shift2 = pack2(-m_ref, -m_ref);
+          uint64_t sum2 = pack2(0.f, 0.f);
+          auto exp_chunk = [&](const uint32_t (&rc)[32], int c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift2);
+              float x0, x1;
+              unpack2(xx, x0, x1);
+              const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+              sum2 = add2(sum2, pack2(e0, e1));
+              pk[i >> 1] = pack16<F16>(e0, e1);
+            }
+            tmem_st16(t_s + c * 16, pk);
+          };
+          exp_chunk(r0, 0);
+          exp_chunk(r1, 1);
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(bar(P_FULL + 2 * x));                        // the product with values 0..63 may start
+          exp_chunk(r2, 2);
+          exp_chunk(r3, 3);
+          float sa, sb;
+          unpack2(sum2, sa, sb);
+          l_sum += sa + sb;
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(bar(P_FULL + 2 * x + 1));
+        }
+        if (ok) ok = wait_all(bar(PV_DONE + x), items_x & 1, abort_flag, p.status, 1 + PV_DONE);
+        ++items_x;
+        cx += n_tiles;
+        if (ok) {
+          tc_fence_after();
+          const int tok = ring_word(ring, W_TOK0) + x * p.tile_tokens + row_tok, hd = ring_word(ring, W_HEAD) * p.G + row_head;
+          const int64_t o_at = (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head;
+          // 32 columns of the warp's rows, through shared memory so that four lanes write 64 bytes of a row
+          auto store_rows = [&](const float (&acc)[32], float inv, int c) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              int4 v;
+              v.x = (int)pack16<F16>(acc[i] * inv, acc[i + 1] * inv);
+              v.y = (int)pack16<F16>(acc[i + 2] * inv, acc[i + 3] * inv);
+              v.z = (int)pack16<F16>(acc[i + 4] * inv, acc[i + 5] * inv);
+              v.w = (int)pack16<F16>(acc[i + 6] * inv, acc[i + 7] * inv);
+              *reinterpret_cast<int4*>(stage + lane * 64 + (((i >> 3) ^ ((lane >> 1) & 3)) << 4)) = v;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int r = k * 8 + (lane >> 2), ch = lane & 3;
+              const int4 v = *reinterpret_cast<const int4*>(stage + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
+              const int64_t at = __shfl_sync(0xffffffffu, o_at, r);
+              if (__shfl_sync(0xffffffffu, (int)valid, r))
+                *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.out) + at + c * 32 + ch * 8) = v;
+            }
+            __syncwarp();
+          };
+          auto finish = [&](float m, float l) {                    // 1 / sum, and the row's logarithm
+            const bool any = sees > 0;
+            if (p.lse && valid) p.lse[(int64_t)tok * p.H + hd] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            const float inv = any ? 1.f / l : 0.f;
+            __syncwarp();                                          // the loads of tensor memory that follow are the whole warp's
+            return inv;
+          };
+          const int tiles = ring_word(ring, W_TILES);
+          if (n_tiles == tiles) {
+            const float inv = finish(m_ref, l_sum);
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t r[32];
+              tmem_ld32(t_o + c * 32, r);
+              tmem_wait_ld();
+              float acc[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) acc[i] = __uint_as_float(r[i]);
+              store_rows(acc, inv, c);
+            }
+          } else {
+            const int c0 = ring_word(ring, W_C0), c1 = ring_word(ring, W_C1), me = blockIdx.x;
+            auto part = [&](int c) { return p.partials + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * L::SLOT_FLOATS; };
+            uint32_t* ctr = p.counters + c0 * 8 + (warp - 4);
+            // all other parts of these 32 rows there already?  Then this one stays in tensor memory
+            uint32_t last = 0;
+            if (lane == 0) {
+              uint32_t seen;
+              asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(ctr) : "memory");
+              last = seen == (uint32_t)(c1 - c0);
+              if (last) *reinterpret_cast<volatile uint32_t*>(ctr) = 0;
+            }
+            last = __shfl_sync(0xffffffffu, last, 0);
+            if (!last) {
+              float* own = part(me);
+              int4* oc = reinterpret_cast<int4*>(own) + x * BM + row;
+#pragma unroll 1
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t r[32];
+                tmem_ld32(t_o + c * 32, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 8; ++q) oc[(c * 8 + q) * (2 * BM)] = make_int4((int)r[4 * q], (int)r[4 * q + 1], (int)r[4 * q + 2], (int)r[4 * q + 3]);
+              }
+              own[2 * BM * D + x * BM + row] = m_ref;
+              own[2 * BM * D + 2 * BM + x * BM + row] = l_sum;
+              __threadfence();
+              __syncwarp();
+              if (lane == 0) {
+                const uint32_t old = atomicAdd(ctr, 1u);
+                last = old == (uint32_t)(c1 - c0);
+                if (last) *reinterpret_cast<volatile uint32_t*>(ctr) = 0;
+              }
+              last = __shfl_sync(0xffffffffu, last, 0);
+            }
+            if (last) {
+              __threadfence();
+              // in key order, this warp's own part from tensor memory at its place
+              auto m_of = [&](int c) { return c == me ? m_ref : __ldcg(part(c) + 2 * BM * D + x * BM + row); };
+              float m_all = NO_MAX;
+              for (int c = c0; c <= c1; ++c) m_all = fmaxf(m_all, m_of(c));
+              float l_all = 0.f;
+              for (int c = c0; c <= c1; ++c)
+                l_all = fmaf(c == me ? l_sum : __ldcg(part(c) + 2 * BM * D + 2 * BM + x * BM + row), exp2f(m_of(c) - m_all), l_all);
+              const float inv = finish(m_all, l_all);
+#pragma unroll 1
+              for (int cc = 0; cc < D / 32; ++cc) {
+                uint32_t r[32];
+                tmem_ld32(t_o + cc * 32, r);
+                tmem_wait_ld();
+                float acc[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+#pragma unroll 1
+                for (int c = c0; c <= c1; ++c) {
+                  const float w = exp2f(m_of(c) - m_all);
+                  if (c == me) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[i] = fmaf(__uint_as_float(r[i]), w, acc[i]);
+                    continue;
+                  }
+                  const float4* oc = reinterpret_cast<const float4*>(part(c)) + (cc * 8) * (2 * BM) + x * BM + row;
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    const float4 v = __ldcg(oc + i * (2 * BM));
+                    acc[4 * i] = fmaf(v.x, w, acc[4 * i]);
+                    acc[4 * i + 1] = fmaf(v.y, w, acc[4 * i + 1]);
+                    acc[4 * i + 2] = fmaf(v.z, w, acc[4 * i + 2]);
+                    acc[4 * i + 3] = fmaf(v.w, w, acc[4 * i + 3]);
+                  }
+                }
+                store_rows(acc, inv, cc);
+              }
+            }
+          }
+          tc_fence_before();                                       // orders this item's reads of O before the next one's products
+        }
+      }
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(bar(ITEM_EMPTY + slot));
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// room for the plan of a call, in bytes
+uint64_t plan_items(int tile_tokens, int n_tokens, int n_seq) { return (uint64_t)n_tokens / (2 * (uint64_t)tile_tokens) + (uint64_t)n_seq; }
+uint64_t run_bytes(int n_sm) { return ((uint64_t)n_sm * RUN_WORDS * 4 + 255) / 256 * 256; }
+uint64_t plan_bytes(int tile_tokens, int n_tokens, int n_seq) {
+  return (12 * ((uint64_t)n_seq + 1) + 4 * plan_items(tile_tokens, n_tokens, n_seq) + 255) / 256 * 256;
+}
+
+template <int D, bool F16>
+cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
+  auto kernel = paged_tc_kernel<D, F16>;
+  constexpr int smem = (int)Layout<D>::SM_ALLOC;
+  cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (rc != cudaSuccess) return rc;
+  // the register hand-over must fit in what the launch allocates, or it would wait for ever
+  cudaFuncAttributes attr;
+  rc = cudaFuncGetAttributes(&attr, kernel);
+  if (rc != cudaSuccess) return rc;
+  if (attr.numRegs * THREADS < 128 * REGS_SMALL + 256 * REGS_SOFTMAX) return cudaErrorLaunchOutOfResources;
+  rc = launch_pdl(plan_kernel, dim3(1), dim3(PT), 0, stream, tp);
+  if (rc != cudaSuccess) return rc;
+  return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, stream, tp, maps);
+}
+
+}  // namespace
+
+uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int n_tokens, int n_seq) {
+  const uint64_t floats = d == 128 ? Layout<128>::SLOT_FLOATS : Layout<64>::SLOT_FLOATS;
+  return run_bytes(n_sm) + plan_bytes(BM / G, n_tokens, n_seq) + 2 * (uint64_t)n_sm * floats * 4;
+}
+
+cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {
+  TcParams tp;
+  tp.a = p;
+  tp.a.tile_tokens = BM / p.G;
+  tp.seq_prefix = reinterpret_cast<int64_t*>(p.partials + run_bytes(dev.n_sm) / 4);
+  tp.item_begin = reinterpret_cast<int32_t*>(tp.seq_prefix + p.n_seq + 1);
+  tp.item_prefix = tp.item_begin + p.n_seq + 1;
+  tp.runs = reinterpret_cast<int32_t*>(p.partials);
+  tp.n_cta = dev.n_sm;
+  tp.items = (int32_t)std::min<uint64_t>(plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq), INT32_MAX);
+  tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(tp.a.tile_tokens, p.n_tokens, p.n_seq)) / 4;
+  TcMaps maps;
+  if (!paged_encode_pool(dev, &maps.k, pool.k, pool) || !paged_encode_pool(dev, &maps.v, pool.v, pool)) return cudaErrorInvalidValue;
+  // query rows: (column, head, token); a tile is the group's heads of tile_tokens tokens
+  const cuuint64_t dims[4] = {(cuuint64_t)pool.d, (cuuint64_t)p.H, (cuuint64_t)p.n_tokens, 1};
+  const cuuint64_t strides[3] = {(cuuint64_t)p.q_head * 2, (cuuint64_t)p.q_tok * 2, 16};
+  const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)tp.a.tile_tokens, 1}, unit[4] = {1, 1, 1, 1};
+  const bool fp16 = pool.dtype == HEATKV_DTYPE_FP16;
+  if (dev.encode(&maps.q, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(p.q), dims, strides, box, unit,
+                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  if (pool.d == 128) return fp16 ? launch<128, true>(tp, maps, dev.n_sm, stream) : launch<128, false>(tp, maps, dev.n_sm, stream);
+  return fp16 ? launch<64, true>(tp, maps, dev.n_sm, stream) : launch<64, false>(tp, maps, dev.n_sm, stream);
+}
+
+}  // namespace heatkv

@@ -278,9 +278,9 @@ def test_attention(hk, name, H, Hkv, d, dtype, causal):
     assert torch.equal(again[: q_begin[-1]], out[: q_begin[-1]])      # and the same bits again, without the logarithms
 
 
-@pytest.mark.parametrize("G", [1, 3, 16, 17, 32])
+@pytest.mark.parametrize("G", [1, 3, 16, 17, 32, 33, 64, 128])
 def test_attention_any_group(hk, G):
-    """Query heads per kv head, from one to as many as a row tile holds."""
+    """Query heads per kv head, from one to 128."""
     lens = [(1, 200), (2, 64), (1, 1)]
     rng, g = np.random.default_rng(G), torch.Generator("cuda").manual_seed(G)
     pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 128, torch.bfloat16)

@@ -82,7 +82,7 @@ cudaError_t launch_paged_tables(const TablesParams& p, cudaStream_t stream);
 cudaError_t launch_paged_release(const ReleaseParams& p, cudaStream_t stream);
 cudaError_t launch_paged_store(StoreParams p, cudaStream_t stream);
 cudaError_t launch_paged_select(const SelectParams& p, int n_sm, cudaStream_t stream);
-// warp-level kernel: row tiles of up to 32 rows
+// warp-level kernel: row tiles of up to 64 rows
 uint64_t paged_small_partial_bytes(int d, int n_sm);
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 // tensor-memory kernel: row tiles of up to 128 rows
@@ -96,6 +96,16 @@ inline bool paged_encode_pool(const PagedDevice& dev, CUtensorMap* m, void* base
   const cuuint32_t box[4] = {64, PAGE, 1, 1}, unit[4] = {1, 1, 1, 1};
   return dev.encode(m, pool.dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base,
                     dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// query rows: boxes of 64 columns x the G heads of a kv head x tile_tokens tokens: (column, head, token)
+inline bool paged_encode_q(const PagedDevice& dev, CUtensorMap* m, const PagedParams& p, const heatkv_paged_pool& pool) {
+  const cuuint64_t dims[4] = {(cuuint64_t)pool.d, (cuuint64_t)p.H, (cuuint64_t)p.n_tokens, 1};
+  const cuuint64_t strides[3] = {(cuuint64_t)p.q_head * 2, (cuuint64_t)p.q_tok * 2, 16};
+  const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens, 1}, unit[4] = {1, 1, 1, 1};
+  return dev.encode(m, pool.dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                    const_cast<void*>(p.q), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

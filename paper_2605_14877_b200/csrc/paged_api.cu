@@ -50,6 +50,7 @@ int check_batch(const heatkv_paged_pool* pool, const heatkv_paged_batch* b, int 
     return HEATKV_ERR_INVALID_ARG;
   if (b->table_stride < b->table_pages) return HEATKV_ERR_INVALID_ARG;
   if (b->n_seq > PAGED_MAX_SEQ || b->table_pages > PAGED_MAX_TABLE) return HEATKV_ERR_TOO_LARGE;
+  if (((int64_t)b->n_tokens + b->n_seq) * pool->n_kv_heads > (1 << 30)) return HEATKV_ERR_TOO_LARGE;        // units have 31-bit numbers
   if (n_heads < 1 || n_heads % pool->n_kv_heads != 0 || n_heads / pool->n_kv_heads > 128) return HEATKV_ERR_SHAPE_MISMATCH;
   return HEATKV_OK;
 }
@@ -172,8 +173,8 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
   rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);
   if (rc != HEATKV_OK) return rc;
   p.causal = causal != 0;
-  // up to 32 rows of the longest request: the warp-level kernel
-  const bool few = (int64_t)p.max_new * p.G <= 32;
+  // up to 64 rows of the longest request: the warp-level kernel
+  const bool few = (int64_t)p.max_new * p.G <= 64;
   return done((few ? launch_paged_small : launch_paged_tc)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 
@@ -201,7 +202,8 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
   int rc = attention_params(pool, batch, n_heads, q, st, sm_scale, out, lse, &p);
   if (rc != HEATKV_OK) return rc;
   if (!sel || n_select < 1) return HEATKV_ERR_INVALID_ARG;
-  if (p.G > 16) return HEATKV_ERR_SHAPE_MISMATCH;
+  if (p.G > 64) return HEATKV_ERR_SHAPE_MISMATCH;
+  if ((int64_t)p.n_tokens * p.Hkv * ((n_select + 3) / 4) > (1 << 30)) return HEATKV_ERR_TOO_LARGE;
   PagedDevice dev;
   if (!paged_device(&dev)) return done(cudaErrorInitializationError);
   rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);

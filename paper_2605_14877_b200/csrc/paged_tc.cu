@@ -788,16 +788,9 @@ cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool,
   tp.items = (int32_t)std::min<uint64_t>(plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq), INT32_MAX);
   tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(tp.a.tile_tokens, p.n_tokens, p.n_seq)) / 4;
   TcMaps maps;
-  if (!paged_encode_pool(dev, &maps.k, pool.k, pool) || !paged_encode_pool(dev, &maps.v, pool.v, pool)) return cudaErrorInvalidValue;
-  // query rows: (column, head, token); a tile is the group's heads of tile_tokens tokens
-  const cuuint64_t dims[4] = {(cuuint64_t)pool.d, (cuuint64_t)p.H, (cuuint64_t)p.n_tokens, 1};
-  const cuuint64_t strides[3] = {(cuuint64_t)p.q_head * 2, (cuuint64_t)p.q_tok * 2, 16};
-  const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)tp.a.tile_tokens, 1}, unit[4] = {1, 1, 1, 1};
-  const bool fp16 = pool.dtype == HEATKV_DTYPE_FP16;
-  if (dev.encode(&maps.q, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(p.q), dims, strides, box, unit,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  if (!paged_encode_pool(dev, &maps.k, pool.k, pool) || !paged_encode_pool(dev, &maps.v, pool.v, pool) || !paged_encode_q(dev, &maps.q, tp.a, pool))
     return cudaErrorInvalidValue;
+  const bool fp16 = pool.dtype == HEATKV_DTYPE_FP16;
   if (pool.d == 128) return fp16 ? launch<128, true>(tp, maps, dev.n_sm, stream) : launch<128, false>(tp, maps, dev.n_sm, stream);
   return fp16 ? launch<64, true>(tp, maps, dev.n_sm, stream) : launch<64, false>(tp, maps, dev.n_sm, stream);
 }

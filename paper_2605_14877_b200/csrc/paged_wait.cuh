@@ -5,21 +5,16 @@
 
 namespace heatkv {
 
-constexpr uint64_t PAGED_WAIT_NS = 2000000000ull;      // far above any launch's longest legitimate wait for one tile
+constexpr long long PAGED_WAIT_CYCLES = 4000000000ll;   // about two seconds: far above any launch's longest legitimate wait for one tile
 
-__device__ __forceinline__ uint64_t global_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
 // Returns false when the CTA is leaving (this wait or another one ran out); the first to run out leaves its `code` in the status word.
 __device__ __forceinline__ bool timed_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status, uint32_t code) {
   if (tc::mbar_try(bar, parity)) return true;
-  const uint64_t begun = global_ns();
+  const long long begun = clock64();
 #pragma unroll 1
   while (!tc::mbar_try(bar, parity)) {
     if (*abort_flag) return false;
-    if (global_ns() - begun > PAGED_WAIT_NS) {
+    if (clock64() - begun > PAGED_WAIT_CYCLES) {
       *abort_flag = 1;
       atomicCAS(status, 0u, code);
       return false;
@@ -33,9 +28,9 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
 }
 // Before leaving early: a copy under way lands (or a second passes).
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
-  const uint64_t begun = global_ns();
+  const long long begun = clock64();
 #pragma unroll 1
-  while (!tc::mbar_try(bar, parity) && global_ns() - begun < PAGED_WAIT_NS / 2) {}
+  while (!tc::mbar_try(bar, parity) && clock64() - begun < PAGED_WAIT_CYCLES / 2) {}
 }
 
 }  // namespace heatkv

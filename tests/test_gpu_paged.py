@@ -410,6 +410,21 @@ def test_select_and_sparse_attention(hk, name, H, Hkv, d, dtype, sink, local, n_
     assert (out[q_begin[-1]:] == 0).all() and torch.isneginf(lse[q_begin[-1]:]).all()
 
 
+@pytest.mark.parametrize("G", [1, 17, 33, 64])
+def test_sparse_attention_any_group(hk, G):
+    """Query heads per kv head from one to 64; every second page."""
+    lens = [(1, 500), (3, 64), (1, 130)]
+    rng, g = np.random.default_rng(G), torch.Generator("cuda").manual_seed(G)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 128, torch.bfloat16)
+    q = torch.empty(b.n_tokens, 2 * G, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    sel = np.tile(np.arange(0, 8, 2), (b.n_tokens, 2, 1))
+    chosen = [np.broadcast_to(np.arange(-(-kv // PAGE)) % 2 == 0, (2, n, -(-kv // PAGE))) for n, kv in lens]
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_tokens, 2 * G, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 2 * G), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_sparse_attention(pool, b, q, _i32(sel), out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(128), "bf16", chosen)
+
+
 def test_select_of_a_long_context(hk):
     """1500 pages, scores that are nearly all equal (three codes), and the score's sign."""
     n_pages, Hkv, d = 1500, 2, 64

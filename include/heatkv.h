@@ -509,8 +509,8 @@ int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch*
                         const heatkv_token_strides* st, int sink, int local, int n_select, int32_t* sel, void* stream);
 
 /* Causal attention of every new token over the pages that sel lists for it (distinct places in the request's table row; entries below 0,
- * past the token's own page or past the table count for nothing).  Other arguments and results as heatkv_paged_attention; rows past
- * q_begin[n_seq] become zero.  n_heads / n_kv_heads at most 64. */
+ * past the token's own page or past the table count for nothing).  Other arguments and results as heatkv_paged_attention.
+ * n_heads / n_kv_heads at most 64. */
 int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                                   const heatkv_token_strides* st, const int32_t* sel, int n_select, float sm_scale, void* out,
                                   float* lse, void* workspace, uint64_t workspace_bytes, void* stream);

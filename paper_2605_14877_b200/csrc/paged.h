@@ -16,6 +16,8 @@ constexpr int PAGED_MAX_TABLE = 1 << 19;       // pages of a block table row
 constexpr int PAGED_MAX_PAGES = 1 << 25;       // pages of a pool: slot numbers have 31 bits
 constexpr int PAGED_MAX_SELECT_PAGES = 32768;  // pages of a context whose scores one CTA keeps in shared memory
 
+constexpr int PAGED_SPARSE_CHUNK = 16;         // new tokens from which selected pages are attended to for many tokens at once
+
 // Workspace: 64 words (word 0: status of bounded waits), then arrival counters, then partial results.
 constexpr int PAGED_WS_HEAD_WORDS = 64;
 constexpr int PAGED_WS_CTRS = 1024;            // one per CTA of a launch and group of 32 rows at most
@@ -86,7 +88,8 @@ cudaError_t launch_paged_select(const SelectParams& p, int n_sm, cudaStream_t st
 uint64_t paged_small_partial_bytes(int d, int n_sm);
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 // tensor-memory kernel: row tiles of up to 128 rows
-uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int n_tokens, int n_seq);
+uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, int n_seq);
+bool paged_tc_takes_lists(int G, int n_sel, int table_pages);
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 
 // boxes of 64 columns x 64 rows of one page and head: (column, row, head, page)

@@ -90,14 +90,14 @@ int attention_params(const heatkv_paged_pool* pool, const heatkv_paged_batch* b,
   return HEATKV_OK;
 }
 
-uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int n_tokens, int n_seq) {
-  const uint64_t a = paged_small_partial_bytes(d, dev.n_sm), b = paged_tc_partial_bytes(d, dev.n_sm, G, n_tokens, n_seq);
+uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_tokens, int n_seq) {
+  const uint64_t a = paged_small_partial_bytes(d, dev.n_sm), b = paged_tc_partial_bytes(d, dev.n_sm, G, Hkv, n_tokens, n_seq);
   return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 
 int place_workspace(const PagedDevice& dev, const heatkv_paged_pool* pool, void* ws, uint64_t bytes, PagedParams* p) {
   if (!ws || !aligned(ws, 256)) return HEATKV_ERR_INVALID_ARG;
-  if (bytes < workspace_bytes(dev, pool->d, p->G, p->n_tokens, p->n_seq)) return HEATKV_ERR_TOO_LARGE;
+  if (bytes < workspace_bytes(dev, pool->d, p->G, p->Hkv, p->n_tokens, p->n_seq)) return HEATKV_ERR_TOO_LARGE;
   p->status = static_cast<uint32_t*>(ws);
   p->counters = p->status + PAGED_WS_HEAD_WORDS;
   p->partials = reinterpret_cast<float*>(static_cast<char*>(ws) + PAGED_WS_PARTIALS);
@@ -158,7 +158,7 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
   PagedDevice dev;
   if (!bytes) return HEATKV_ERR_INVALID_ARG;
   if (!paged_device(&dev)) return done(cudaErrorInitializationError);
-  *bytes = workspace_bytes(dev, pool->d, n_heads / pool->n_kv_heads, batch->n_tokens, batch->n_seq);
+  *bytes = workspace_bytes(dev, pool->d, n_heads / pool->n_kv_heads, pool->n_kv_heads, batch->n_tokens, batch->n_seq);
   return HEATKV_OK;
 }
 
@@ -211,7 +211,9 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
   p.causal = 1;
   p.sel = sel;
   p.n_sel = n_select;
-  return done(launch_paged_small(p, *pool, dev, static_cast<cudaStream_t>(stream)));
+  // tokens of a chunk share the pages that they select: they are taken together
+  const bool chunk = p.max_new >= PAGED_SPARSE_CHUNK && paged_tc_takes_lists(p.G, n_select, p.table_pages);
+  return done((chunk ? launch_paged_tc : launch_paged_small)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 
 int heatkv_paged_status(const void* workspace, void* stream) {

@@ -279,11 +279,11 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
         out_slot = pieces > 1 ? idx : -1;
         tok0 = unit / p.Hkv;
         head = unit - tok0 * p.Hkv;
-        tokens = 1;
         seq = find_last(p.q_begin, p.n_seq, tok0);
         const int e = p.q_begin[seq + 1];
         kv = p.kv_len[seq];
-        pos0 = tok0 < e ? kv - e + tok0 : -1;
+        tokens = tok0 >= p.q_begin[seq] && tok0 < e ? 1 : 0;       // rows past the last request's are nobody's
+        pos0 = tokens ? kv - e + tok0 : -1;
         tiles = p.n_sel;
       } else {
         seq = find_last(chunk_begin, p.n_seq, idx);

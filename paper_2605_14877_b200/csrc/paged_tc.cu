@@ -10,6 +10,11 @@
 //   warps 4-7    softmax of tile A, warps 8-11 of tile B, one thread a row; they write the item's rows, too.
 // Tensor memory: S_A/P_A 0..127, S_B/P_B 128..255, O_A 256..383, O_B 384..511.  Rows past a request's last key in its last page are
 // whatever the pool holds: their logits are masked, their values overwritten by zeros before the product (warp 1).
+//
+// Over selected pages (SPARSE) the keys of an item are the pages that any of its tokens selected, in ascending order, and a row sees a page
+// if its token is among those that did: neighbouring tokens select much the same pages, so a page is read and multiplied once for all of
+// them instead of once for each.  The copy warp merges the tokens' lists (in shared memory, a token per lane and tile) as it goes and
+// hands the tokens' bits to the softmax warps beside each tile.
 // Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and leaves.
 #include <algorithm>
 
@@ -32,6 +37,8 @@ constexpr uint32_t HALF_COLS_BYTES = 128 * 128;        // one 64-column half of 
 constexpr uint32_t SLOT_BYTES = PAGE * 128;            // a page inside one column half
 constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 rows x 32 columns on their way out
 
+constexpr int LIST_ENTRIES = 8192;                     // 16-bit places of an item's lists
+
 template <int D>
 struct Layout {
   static constexpr int NCH = D / 64;
@@ -41,8 +48,9 @@ struct Layout {
   static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;
   static constexpr uint32_t SM_OUT = SM_V + KV_STAGES * TILE_BYTES;
   static constexpr uint32_t SM_BAR = SM_OUT + 8 * STAGE_BYTES;
-  static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;
-  static_assert(SM_ALLOC <= 227 * 1024, "shared memory of one CTA");
+  static constexpr uint32_t SM_LIST = SM_BAR + 512;
+  static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;             // (and the lists where pages are selected)
+  static_assert(SM_ALLOC + LIST_ENTRIES * 2 <= 227 * 1024, "shared memory of one CTA");
   // one part of a cut item: O of both tiles (groups of four columns outermost), then references and sums
   static constexpr int SLOT_FLOATS = 2 * BM * D + 2 * 2 * BM;
 };
@@ -50,7 +58,9 @@ enum Bar : uint32_t {
   Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 6, V_FULL = 8, V_EMPTY = 10, S_FULL = 12, P_FULL = 14, PV_DONE = 18, ITEM_FULL = 20, ITEM_EMPTY = 22,
   N_BARS = 24
 };
-constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256;
+constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256, BAR_INFO = 384;
+constexpr int INFO_RING = 4;                           // key tiles whose pages and bits are kept: the copy warp is at most two ahead of the softmax
+enum InfoWord : int { I_PLACE = 0, I_BITS = 2, INFO_WORDS = 8 };   // two places; bits of tile A for both, of tile B for both
 enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1 };
 
 struct TcParams {
@@ -58,7 +68,7 @@ struct TcParams {
   // the plan of the call: key tiles (of all heads) before every request; its first item; key tiles of one head before every item
   int64_t* seq_prefix;        // [n_seq + 1]
   int32_t* item_begin;        // [n_seq + 1]
-  int32_t* item_prefix;       // [items]
+  int32_t* item_prefix;       // [items]; SPARSE: [items * Hkv + 1] key tiles before every item and kv head
   int32_t* runs;              // [n_sm][RUN_WORDS] where every CTA's run starts
   int32_t items;              // room for the items
   int32_t n_cta;
@@ -80,8 +90,62 @@ __device__ __forceinline__ int item_tiles(const PagedParams& p, int tok, int n, 
   return max(1, (upto + BN - 1) / BN);
 }
 
+// The lists of selected pages of an item's tokens, merged by a warp: lane l has token l of tile A and token l of tile B.  Whatever the
+// order of a list, its entries come one after another, so every entry is met exactly once.
+constexpr int NO_PAGE = 1 << 24;
+struct Merge {
+  const uint16_t* list;
+  int n_sel, a, b, a_end, b_end, va, vb;
+  __device__ int entry(int& i, int end) const {
+    int v = 0xffff;
+    while (i < end && (v = list[i]) == 0xffff) ++i;
+    return i < end ? v : NO_PAGE;
+  }
+  __device__ void start(const uint16_t* l, int n, int tokens, int tile_tokens, int lane) {
+    list = l;
+    n_sel = n;
+    const bool in_a = lane < min(tile_tokens, tokens), in_b = lane < tile_tokens && tile_tokens + lane < tokens;
+    a = lane * n;
+    a_end = in_a ? a + n : a;
+    b = (tile_tokens + lane) * n;
+    b_end = in_b ? b + n : b;
+    va = entry(a, a_end);
+    vb = entry(b, b_end);
+  }
+  // the next page (NO_PAGE: none is left) and the tokens of each tile that selected it
+  __device__ int next(uint32_t& bits_a, uint32_t& bits_b) {
+    const int page = __reduce_min_sync(0xffffffffu, min(va, vb));
+    const bool ha = va == page && page < NO_PAGE, hb = vb == page && page < NO_PAGE;
+    bits_a = __ballot_sync(0xffffffffu, ha);
+    bits_b = __ballot_sync(0xffffffffu, hb);
+    if (ha) {
+      ++a;
+      va = entry(a, a_end);
+    }
+    if (hb) {
+      ++b;
+      vb = entry(b, b_end);
+    }
+    __syncwarp();
+    return page;
+  }
+};
+// An item's lists into shared memory; entries that count for nothing become 0xffff.
+__device__ __forceinline__ void load_lists(const PagedParams& p, uint16_t* list, int tok0, int tokens, int pos0, int head, int lane) {
+  const int total = tokens * p.n_sel;
+#pragma unroll 4
+  for (int i = lane; i < total; i += 32) {
+    const int t = i / p.n_sel;
+    const int place = __ldg(p.sel + ((int64_t)(tok0 + t) * p.Hkv + head) * p.n_sel + (i - t * p.n_sel)), pos = pos0 + t;
+    list[i] = place >= 0 && pos >= 0 && place <= pos / PAGE && place < p.table_pages ? (uint16_t)place : (uint16_t)0xffff;
+  }
+  __syncwarp();
+}
+
 constexpr int PT = 1024;
-// One CTA: what every request's items weigh, and the sums that the attention kernel's CTAs look their run up in.
+// One CTA: what every request's items weigh, and the sums that the attention kernel's CTAs look their run up in.  FIRST: only the items
+// of every request (selected pages: union_kernel then weighs them, and plan_runs_kernel sums that up).
+template <bool FIRST>
 __global__ void __launch_bounds__(PT) plan_kernel(const TcParams tp) {
   const PagedParams& p = tp.a;
   __shared__ int64_t sums[PT / 32][2];
@@ -117,6 +181,7 @@ __global__ void __launch_bounds__(PT) plan_kernel(const TcParams tp) {
     at += (request_tokens(p, i, b) + pair - 1) / pair;
   }
   if (tid == 0) tp.item_begin[p.n_seq] = (int)min(all, (int64_t)tp.items);
+  if (FIRST) return;
   __syncthreads();
   // a warp per request: key tiles before every item
   for (int i = warp; i < p.n_seq; i += PT / 32) {
@@ -204,6 +269,104 @@ __global__ void __launch_bounds__(PT) plan_kernel(const TcParams tp) {
   }
 }
 
+// Key tiles of every item and kv head over selected pages: half of the pages that its tokens' lists give when merged.  A warp each.
+constexpr int UNION_WARPS = 4;
+__global__ void __launch_bounds__(UNION_WARPS * 32) union_kernel(const TcParams tp) {
+  extern __shared__ uint16_t lists[];
+  const PagedParams& p = tp.a;
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = 2 * p.tile_tokens;
+  const int64_t x = (int64_t)blockIdx.x * UNION_WARPS + warp;
+  const int item = (int)(x / p.Hkv), head = (int)(x - (int64_t)item * p.Hkv);
+  if (item >= tp.item_begin[p.n_seq]) return;
+  int lo = 0, hi = p.n_seq - 1, b;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (tp.item_begin[mid] <= item) lo = mid; else hi = mid - 1;
+  }
+  const int n = request_tokens(p, lo, b), kv = request_keys(p, lo), tok = (item - tp.item_begin[lo]) * pair, tokens = min(n - tok, pair);
+  uint16_t* list = lists + warp * pair * p.n_sel;
+  load_lists(p, list, b + tok, tokens, kv - n + tok, head, lane);
+  Merge merge;
+  merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
+  int pages = 0;
+  uint32_t bits_a, bits_b;
+  while (merge.next(bits_a, bits_b) < NO_PAGE) ++pages;
+  if (lane == 0) tp.item_prefix[x] = max(1, (pages + 1) / 2);
+}
+
+// One CTA: the sums over items and kv heads, and the runs.
+__global__ void __launch_bounds__(PT) plan_runs_kernel(const TcParams tp) {
+  const PagedParams& p = tp.a;
+  __shared__ int64_t sums[PT / 32];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int count = tp.item_begin[p.n_seq] * p.Hkv, per = (count + PT - 1) / PT, i0 = min(tid * per, count), i1 = min(i0 + per, count);
+  int64_t mine = 0;
+  for (int i = i0; i < i1; ++i) mine += tp.item_prefix[i];
+  int64_t inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  int64_t at = inc - mine, all = 0;
+  for (int w = 0; w < PT / 32; ++w) {
+    if (w < warp) at += sums[w];
+    all += sums[w];
+  }
+  for (int i = i0; i < i1; ++i) {
+    const int v = tp.item_prefix[i];
+    tp.item_prefix[i] = (int)min(at, (int64_t)INT32_MAX);
+    at += v;
+  }
+  if (tid == 0) tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
+  __syncthreads();
+  all = min(all, (int64_t)INT32_MAX);
+  const int grid = (int)min((int64_t)tp.n_cta, all);
+  auto bound = [&](int c) { return all * c / grid; };
+  auto owner = [&](int64_t y) {
+    int c = (int)(y * grid / all);
+    while (c + 1 < grid && bound(c + 1) <= y) ++c;
+    while (c > 0 && bound(c) > y) --c;
+    return c;
+  };
+  auto item_of = [&](int64_t y) {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tp.item_prefix[mid] <= y) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  };
+  for (int c = tid; c < tp.n_cta; c += PT) {
+    int32_t* run = tp.runs + c * RUN_WORDS;
+    if (c >= grid) {
+      run[R_TILES] = 0;
+      continue;
+    }
+    const int64_t y0 = bound(c), y1 = bound(c + 1);
+    const int a = item_of(y0), z = item_of(y1 - 1);
+    int lo = 0, hi = p.n_seq - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tp.item_begin[mid] <= a / p.Hkv) lo = mid; else hi = mid - 1;
+    }
+    run[R_SEQ] = lo;
+    run[R_HEAD] = a % p.Hkv;
+    run[R_ITEM] = a / p.Hkv - tp.item_begin[lo];
+    run[R_J0] = (int)(y0 - tp.item_prefix[a]);
+    run[R_TILES] = (int)(y1 - y0);
+    run[R_C0_FIRST] = owner(tp.item_prefix[a]);
+    run[R_C1_FIRST] = owner(tp.item_prefix[a + 1] - 1);
+    run[R_C1_LAST] = owner(tp.item_prefix[z + 1] - 1);
+  }
+}
+
 __device__ __forceinline__ int ring_word(const volatile int32_t* ring, int word) { return __shfl_sync(0xffffffffu, ring[word], 0); }
 
 template <bool F16>
@@ -215,7 +378,7 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return pack_bf16(lo, hi);
 }
 
-template <int D, bool F16>
+template <int D, bool F16, bool SPARSE>
 __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
   using L = Layout<D>;
   constexpr int NCH = L::NCH;
@@ -231,6 +394,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(sgen + SM_BAR + BAR_ABORT);
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(sgen + SM_BAR + BAR_TMEM_PTR);
   volatile int32_t* ring_base = reinterpret_cast<volatile int32_t*>(sgen + SM_BAR + BAR_RING);
+  volatile int32_t* info_base = reinterpret_cast<volatile int32_t*>(sgen + SM_BAR + BAR_INFO);
   auto bar = [&](uint32_t which) { return sbase + SM_BAR + which * 8; };
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
@@ -299,7 +463,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         const int n_items = tp.item_begin[seq + 1] - tp.item_begin[seq];
         const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
         const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
-        const int tiles = item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
+        const int flat = SPARSE ? (tp.item_begin[seq] + item) * p.Hkv + head : 0;
+        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
         const int nq = tokens > p.tile_tokens ? 2 : 1;
         if (lane == 0) {
           ring[W_KIND] = 1;
@@ -321,13 +486,33 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         const int32_t* table = p.block_table + seq * p.table_stride;
         const int n_pages = (kv + PAGE - 1) / PAGE;
         int pages = -1;
+        Merge merge;
+        uint32_t bits[4];
+        if (SPARSE) {
+          uint16_t* list = reinterpret_cast<uint16_t*>(sgen + L::SM_LIST);
+          load_lists(p, list, q_first + tok, tokens, kv - n + tok, head, lane);
+          merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
+          for (int i = 0; i < 2 * j0; ++i) merge.next(bits[0], bits[1]);      // pages of the parts before this one
+        }
         for (int j = 0; j < n_tiles && ok; ++j, ++g) {
-          if ((j & 15) == 0) {                                     // page numbers of 16 tiles at a time, one per lane
+          if (!SPARSE && (j & 15) == 0) {                          // page numbers of 16 tiles at a time, one per lane
             const int pg = 2 * (j0 + j) + lane;
             pages = pg < n_pages ? table[pg] : -1;
             if (pages >= p.n_pages || pages < 0) pages = -1;       // (a box outside of the map arrives as zeros)
           }
-          const int pg0 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15)), pg1 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15) + 1);
+          int pg0, pg1, place0 = 0, place1 = 0;
+          if (SPARSE) {
+            place0 = merge.next(bits[0], bits[2]);
+            place1 = merge.next(bits[1], bits[3]);
+            const int place = (lane & 1) ? place1 : place0;
+            pages = place < NO_PAGE ? table[place] : -1;
+            if (pages >= p.n_pages || pages < 0) pages = -1;
+            pg0 = __shfl_sync(0xffffffffu, pages, 0);
+            pg1 = __shfl_sync(0xffffffffu, pages, 1);
+          } else {
+            pg0 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15));
+            pg1 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15) + 1);
+          }
           const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
           auto load = [&](uint32_t smem, const CUtensorMap* map, uint32_t full) {
             if (!leader) return;
@@ -340,6 +525,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           };
           if (use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
           if (!ok) break;
+          if (SPARSE && lane == 0) {
+            volatile int32_t* info = info_base + (g % INFO_RING) * INFO_WORDS;
+            info[I_PLACE] = place0;
+            info[I_PLACE + 1] = place1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) info[I_BITS + i] = (int32_t)bits[i];
+          }
+          __syncwarp();
           armed_k |= 1u << st;
           par_k = (par_k & ~(1u << st)) | ((use & 1) << st);
           load(sbase + SM_K + st * TILE_BYTES, &maps.k, bar(K_FULL + st));
@@ -370,13 +563,25 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         }
         __syncwarp();
         // the next item of the run: the request's next tokens, its next head, the next request with tokens
+        // (over selected pages the heads come first: the order of the sums)
         j0 = 0;
-        if (++item == n_items) {
-          item = 0;
+        bool request_done;
+        if (SPARSE) {
           if (++head == p.Hkv) {
             head = 0;
-            do ++seq; while (left > 0 && seq + 1 < p.n_seq && tp.item_begin[seq + 1] == tp.item_begin[seq]);
+            ++item;
           }
+          request_done = item == n_items;
+        } else {
+          if (++item == n_items) {
+            item = 0;
+            ++head;
+          }
+          request_done = head == p.Hkv;
+        }
+        if (request_done) {
+          item = head = 0;
+          do ++seq; while (left > 0 && seq + 1 < p.n_seq && tp.item_begin[seq + 1] == tp.item_begin[seq]);
         }
       }
       if (!ok || *abort_flag) {
@@ -420,13 +625,29 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         if (!ok) break;
         if (ring_word(ring, W_KIND) == 0) break;
         const int nq = ring_word(ring, W_TOKENS) > p.tile_tokens ? 2 : 1, n_tiles = ring_word(ring, W_NT);
-        const int kv_left = ring_word(ring, W_KV) - ring_word(ring, W_J0) * BN;      // keys of the request from the item's first on
+        const int kv_len = ring_word(ring, W_KV), kv_left = kv_len - ring_word(ring, W_J0) * BN;      // keys of the request from the item's first on
         // values of the tile: waited for, and rows without a key in the request's last page made zero
         auto values = [&](uint32_t st, uint32_t parity, int j) {
           if (!mma_wait(V_FULL + st, parity)) return false;
-          const int left = kv_left - j * BN;
-          if (left < BN && left > 0 && (left & (PAGE - 1))) {
-            const int r0 = left, r1 = (left + PAGE - 1) & ~(PAGE - 1);
+          int r0 = 0, r1 = 0;
+          if (SPARSE) {
+            const volatile int32_t* info = info_base + ((g + j) % INFO_RING) * INFO_WORDS;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const int place = ring_word(info, I_PLACE + hf), rows = place < NO_PAGE ? kv_len - place * PAGE : PAGE;
+              if (rows > 0 && rows < PAGE) {
+                r0 = hf * PAGE + rows;
+                r1 = hf * PAGE + PAGE;
+              }
+            }
+          } else {
+            const int left = kv_left - j * BN;
+            if (left < BN && left > 0) {
+              r0 = left;
+              r1 = (left + PAGE - 1) & ~(PAGE - 1);
+            }
+          }
+          if (r0 < r1) {
             for (int i = lane; i < (r1 - r0) * 8 * NCH; i += 32) {
               const int ch = i / ((r1 - r0) * 8), rest = i - ch * (r1 - r0) * 8;
               const uint32_t at = SM_V + st * TILE_BYTES + ch * HALF_COLS_BYTES + (r0 + (rest >> 3)) * 128 + (rest & 7) * 16;
@@ -506,7 +727,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
     const uint32_t t_s = tmem + lane_base + x * 128, t_o = tmem + lane_base + 256 + x * 128;
     unsigned char* stage = sgen + SM_OUT + (warp - 4) * STAGE_BYTES;
     const int row_tok = row / p.G, row_head = row - row_tok * p.G;
-    uint32_t cx = 0, items_x = 0;
+    uint32_t cx = 0, items_x = 0, g = 0;                            // key tiles of this tile's rows; its items; key tiles in all
     bool ok = true;
     for (uint32_t it = 0; ok; ++it) {
       const uint32_t slot = it & 1;
@@ -520,7 +741,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         const bool valid = row_tok < p.tile_tokens && x * p.tile_tokens + row_tok < tokens;
         // keys that the row sees, counted from the run's first
         const int sees = p.causal && valid ? min(pos0 + x * p.tile_tokens + row_tok + 1, kv) : kv;
-        const int lim = sees - skipped;
+        const int lim = SPARSE ? sees : sees - skipped;
         const int least = __reduce_min_sync(0xffffffffu, lim);
         float m_ref = NO_MAX, l_sum = 0.f;
 #pragma unroll 1
@@ -535,7 +756,30 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           tmem_ld32(t_s + 64, r2);
           tmem_ld32(t_s + 96, r3);
           tmem_wait_ld();
-          if ((j + 1) * BN > least) {                              // some row of the warp does not see the whole tile
+          bool sel0 = true, sel1 = true;                           // does the row see the tile's two pages at all
+          if (SPARSE) {
+            const volatile int32_t* info = info_base + ((g + j) % INFO_RING) * INFO_WORDS;
+            const int place0 = info[I_PLACE], place1 = info[I_PLACE + 1];
+            sel0 = valid && ((uint32_t)info[I_BITS + 2 * x] >> row_tok & 1u);
+            sel1 = valid && ((uint32_t)info[I_BITS + 2 * x + 1] >> row_tok & 1u);
+            // (in pages that no row selected, and in the last one past the row's own position)
+            if (place0 * PAGE + PAGE > least) {
+              const int left = sees - place0 * PAGE;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                if (i >= left) r0[i] = 0xff800000u;
+                if (i + 32 >= left) r1[i] = 0xff800000u;
+              }
+            }
+            if (place1 * PAGE + PAGE > least) {
+              const int left = sees - place1 * PAGE;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                if (i >= left) r2[i] = 0xff800000u;
+                if (i + 32 >= left) r3[i] = 0xff800000u;
+              }
+            }
+          } else if ((j + 1) * BN > least) {                       // some row of the warp does not see the whole tile
             const int left = lim - j * BN;
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
@@ -559,7 +803,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
               mq[4 + c] = fmax3(mq[4 + c], __uint_as_float(r2[i + c]), __uint_as_float(r3[i + c]));
             }
           }
-          const float mx = fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7]))) * p.scale_log2;
+          const float mx0 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), mx1 = fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7]));
+          const float mx = (SPARSE ? fmaxf(sel0 ? mx0 : -INFINITY, sel1 ? mx1 : -INFINITY) : fmaxf(mx0, mx1)) * p.scale_log2;
           const float m_new = fmaxf(m_ref, mx);
           const bool grow = m_new > m_ref + THRESHOLD;             // also on the first tile with a key the row sees
           if (j > 0 && __any_sync(0xffffffffu, grow)) {
@@ -579,12 +824,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           }
           if (grow) m_ref = m_new;
           const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), shift2 = pack2(-m_ref, -m_ref);
+          // (a page that the row did not select: every exponent minus infinity)
+          const uint64_t none2 = pack2(-INFINITY, -INFINITY);
           uint64_t sum2 = pack2(0.f, 0.f);
-          auto exp_chunk = [&](const uint32_t (&rc)[32], int c) {
+          auto exp_chunk = [&](const uint32_t (&rc)[32], uint64_t shift, int c) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift2);
+              const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift);
               float x0, x1;
               unpack2(xx, x0, x1);
               const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
@@ -593,13 +840,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             }
             tmem_st16(t_s + c * 16, pk);
           };
-          exp_chunk(r0, 0);
-          exp_chunk(r1, 1);
+          exp_chunk(r0, sel0 ? shift2 : none2, 0);
+          exp_chunk(r1, sel0 ? shift2 : none2, 1);
           tmem_wait_st();
           tc_fence_before();
           mbar_arrive(bar(P_FULL + 2 * x));                        // the product with values 0..63 may start
-          exp_chunk(r2, 2);
-          exp_chunk(r3, 3);
+          exp_chunk(r2, sel1 ? shift2 : none2, 2);
+          exp_chunk(r3, sel1 ? shift2 : none2, 3);
           float sa, sb;
           unpack2(sum2, sa, sb);
           l_sum += sa + sb;
@@ -637,7 +884,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             __syncwarp();
           };
           auto finish = [&](float m, float l) {                    // 1 / sum, and the row's logarithm
-            const bool any = sees > 0;
+            const bool any = SPARSE ? l > 0.f : sees > 0;
             if (p.lse && valid) p.lse[(int64_t)tok * p.H + hd] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             const float inv = any ? 1.f / l : 0.f;
             __syncwarp();                                          // the loads of tensor memory that follow are the whole warp's
@@ -734,6 +981,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           tc_fence_before();                                       // orders this item's reads of O before the next one's products
         }
       }
+      g += n_tiles;
       __syncwarp();
       if (ok && lane == 0) mbar_arrive(bar(ITEM_EMPTY + slot));
     }
@@ -748,15 +996,19 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
 
 // room for the plan of a call, in bytes
 uint64_t plan_items(int tile_tokens, int n_tokens, int n_seq) { return (uint64_t)n_tokens / (2 * (uint64_t)tile_tokens) + (uint64_t)n_seq; }
+// tokens of a row tile over selected pages: a bit each in a word
+int sparse_tile_tokens(int G) { return std::min(32, BM / G); }
 uint64_t run_bytes(int n_sm) { return ((uint64_t)n_sm * RUN_WORDS * 4 + 255) / 256 * 256; }
-uint64_t plan_bytes(int tile_tokens, int n_tokens, int n_seq) {
-  return (12 * ((uint64_t)n_seq + 1) + 4 * plan_items(tile_tokens, n_tokens, n_seq) + 255) / 256 * 256;
+// (room for either kind of call: over selected pages every kv head's items count for themselves, and have at most 32 tokens a tile)
+uint64_t plan_bytes(int G, int Hkv, int n_tokens, int n_seq) {
+  const uint64_t dense = plan_items(BM / G, n_tokens, n_seq), sparse = plan_items(sparse_tile_tokens(G), n_tokens, n_seq) * Hkv + 1;
+  return (12 * ((uint64_t)n_seq + 1) + 4 * std::max(dense, sparse) + 255) / 256 * 256;
 }
 
-template <int D, bool F16>
+template <int D, bool F16, bool SPARSE>
 cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
-  auto kernel = paged_tc_kernel<D, F16>;
-  constexpr int smem = (int)Layout<D>::SM_ALLOC;
+  auto kernel = paged_tc_kernel<D, F16, SPARSE>;
+  constexpr int smem = (int)Layout<D>::SM_ALLOC + (SPARSE ? LIST_ENTRIES * 2 : 0);
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (rc != cudaSuccess) return rc;
   // the register hand-over must fit in what the launch allocates, or it would wait for ever
@@ -764,35 +1016,50 @@ cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_
   rc = cudaFuncGetAttributes(&attr, kernel);
   if (rc != cudaSuccess) return rc;
   if (attr.numRegs * THREADS < 128 * REGS_SMALL + 256 * REGS_SOFTMAX) return cudaErrorLaunchOutOfResources;
-  rc = launch_pdl(plan_kernel, dim3(1), dim3(PT), 0, stream, tp);
+  rc = launch_pdl(plan_kernel<SPARSE>, dim3(1), dim3(PT), 0, stream, tp);
   if (rc != cudaSuccess) return rc;
+  if (SPARSE) {
+    const int lists = UNION_WARPS * 2 * tp.a.tile_tokens * tp.a.n_sel * 2;
+    rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, UNION_WARPS * LIST_ENTRIES * 2);
+    if (rc != cudaSuccess) return rc;
+    rc = launch_pdl(union_kernel, dim3((unsigned)(((int64_t)tp.items * tp.a.Hkv + UNION_WARPS - 1) / UNION_WARPS)), dim3(UNION_WARPS * 32), lists, stream, tp);
+    if (rc != cudaSuccess) return rc;
+    rc = launch_pdl(plan_runs_kernel, dim3(1), dim3(PT), 0, stream, tp);
+    if (rc != cudaSuccess) return rc;
+  }
   return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, stream, tp, maps);
+}
+template <int D, bool F16>
+cudaError_t launch_either(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
+  return tp.a.sel ? launch<D, F16, true>(tp, maps, grid, stream) : launch<D, F16, false>(tp, maps, grid, stream);
 }
 
 }  // namespace
 
-uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int n_tokens, int n_seq) {
+uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, int n_seq) {
   const uint64_t floats = d == 128 ? Layout<128>::SLOT_FLOATS : Layout<64>::SLOT_FLOATS;
-  return run_bytes(n_sm) + plan_bytes(BM / G, n_tokens, n_seq) + 2 * (uint64_t)n_sm * floats * 4;
+  return run_bytes(n_sm) + plan_bytes(G, Hkv, n_tokens, n_seq) + 2 * (uint64_t)n_sm * floats * 4;
 }
+
+bool paged_tc_takes_lists(int G, int n_sel, int table_pages) { return 2 * sparse_tile_tokens(G) * n_sel <= LIST_ENTRIES && table_pages < 0xffff; }
 
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {
   TcParams tp;
   tp.a = p;
-  tp.a.tile_tokens = BM / p.G;
+  tp.a.tile_tokens = p.sel ? sparse_tile_tokens(p.G) : BM / p.G;
+  tp.runs = reinterpret_cast<int32_t*>(p.partials);
   tp.seq_prefix = reinterpret_cast<int64_t*>(p.partials + run_bytes(dev.n_sm) / 4);
   tp.item_begin = reinterpret_cast<int32_t*>(tp.seq_prefix + p.n_seq + 1);
   tp.item_prefix = tp.item_begin + p.n_seq + 1;
-  tp.runs = reinterpret_cast<int32_t*>(p.partials);
   tp.n_cta = dev.n_sm;
-  tp.items = (int32_t)std::min<uint64_t>(plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq), INT32_MAX);
-  tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(tp.a.tile_tokens, p.n_tokens, p.n_seq)) / 4;
+  tp.items = (int32_t)plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq);
+  tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(p.G, p.Hkv, p.n_tokens, p.n_seq)) / 4;
   TcMaps maps;
   if (!paged_encode_pool(dev, &maps.k, pool.k, pool) || !paged_encode_pool(dev, &maps.v, pool.v, pool) || !paged_encode_q(dev, &maps.q, tp.a, pool))
     return cudaErrorInvalidValue;
   const bool fp16 = pool.dtype == HEATKV_DTYPE_FP16;
-  if (pool.d == 128) return fp16 ? launch<128, true>(tp, maps, dev.n_sm, stream) : launch<128, false>(tp, maps, dev.n_sm, stream);
-  return fp16 ? launch<64, true>(tp, maps, dev.n_sm, stream) : launch<64, false>(tp, maps, dev.n_sm, stream);
+  if (pool.d == 128) return fp16 ? launch_either<128, true>(tp, maps, dev.n_sm, stream) : launch_either<128, false>(tp, maps, dev.n_sm, stream);
+  return fp16 ? launch_either<64, true>(tp, maps, dev.n_sm, stream) : launch_either<64, false>(tp, maps, dev.n_sm, stream);
 }
 
 }  // namespace heatkv

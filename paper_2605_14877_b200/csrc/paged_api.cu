@@ -192,7 +192,7 @@ int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch*
   const SelectParams p = {q, q_tok, q_head, batch->q_begin, batch->kv_len, batch->block_table, batch->table_stride, pool->k_code, pool->k_scale, sel,
                           batch->n_seq, batch->table_pages, batch->n_tokens, pool->n_pages, pool->n_kv_heads, n_heads / pool->n_kv_heads, pool->d,
                           pool->dtype == HEATKV_DTYPE_FP16, sink, local, n_select};
-  return done(launch_paged_select(p, dev.n_sm, static_cast<cudaStream_t>(stream)));
+  return done(launch_paged_select(p, batch->max_new, dev.n_sm, static_cast<cudaStream_t>(stream)));
 }
 
 int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,

@@ -454,23 +454,25 @@ def test_sparse_attention_of_chunks_over_random_lists(hk, G, d, dtype, max_new):
     assert (out[q_begin[-1]:] == 7.0).all() and (lse[q_begin[-1]:] == 7.0).all()
 
 
-def test_select_of_a_long_context(hk):
-    """1500 pages, scores that are nearly all equal (three codes), and the score's sign."""
+@pytest.mark.parametrize("n_select", [8, 12, 50, 200])
+@pytest.mark.parametrize("tokens,codes", [(3, 1), (3, 127), (21, 1), (21, 127)])
+def test_select_of_a_long_context(hk, tokens, codes, n_select):
+    """1500 pages; scores of which many are equal (three codes) or hardly any, and of either sign."""
     n_pages, Hkv, d = 1500, 2, 64
     rng, g = np.random.default_rng(1), torch.Generator("cuda").manual_seed(1)
     pool, k, v, code, scale = _pool(hk, g, n_pages, Hkv, d, torch.bfloat16, fill=0.0)
-    code.copy_(torch.randint(-1, 2, code.shape, generator=g, device="cuda"))
+    code.copy_(torch.randint(-codes, codes + 1, code.shape, generator=g, device="cuda"))
     scale.copy_(2.0 ** torch.randint(-2, 1, scale.shape, generator=g, device="cuda"))
     kv = n_pages * PAGE - 5
-    b, table, _ = _batch(hk, rng, [(3, kv)], n_pages)
-    q = torch.randint(-1, 2, (3, 4, d), generator=g, device="cuda").to(torch.bfloat16)
+    b, table, _ = _batch(hk, rng, [(tokens, kv)], n_pages)
+    q = torch.randint(-codes, codes + 1, (tokens, 4, d), generator=g, device="cuda").to(torch.bfloat16)
     q[2] = 0
-    sel = torch.zeros(3, Hkv, 200, dtype=torch.int32, device="cuda")
+    sel = torch.zeros(tokens, Hkv, n_select, dtype=torch.int32, device="cuda")
     hk.heatkv_paged_select(pool, b, q, sel, 3, 4)
     pages, cn, sn = table[0, :n_pages], code.cpu().numpy(), scale.cpu().numpy()
-    for t in range(3):
+    for t in range(tokens):
         for h in range(Hkv):
-            assert sel[t, h].tolist() == P.select(_np(q)[t, 2 * h: 2 * h + 2], cn[pages, h], sn[pages, h], kv - 3 + t, 3, 4, 200)
+            assert sel[t, h].tolist() == P.select(_np(q)[t, 2 * h: 2 * h + 2], cn[pages, h], sn[pages, h], kv - tokens + t, 3, 4, n_select)
 
 
 def test_sparse_attention_over_lists_of_any_kind(hk):

@@ -65,15 +65,15 @@ enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV,
 
 struct TcParams {
   PagedParams a;
-  // the plan of the call: key tiles (of all heads) before every request; its first item; key tiles of one head before every item
-  int64_t* seq_prefix;        // [n_seq + 1]
-  int32_t* item_begin;        // [n_seq + 1]
-  int32_t* item_prefix;       // [items]; SPARSE: [items * Hkv + 1] key tiles before every item and kv head
+  // the plan of the call
+  int32_t* item_begin;        // [n_seq + 1] the request's first item
+  int32_t* item_prefix;       // what its items weigh, of one head, summed up; SPARSE: [items * Hkv + 1] every item's and kv head's key tiles
   int32_t* runs;              // [n_sm][RUN_WORDS] where every CTA's run starts
+  uint32_t* ticket;           // CTAs of union_kernel that are done; zero between launches
   int32_t items;              // room for the items
   int32_t n_cta;
 };
-enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_TILES, R_C0_FIRST, R_C1_FIRST, R_C1_LAST, RUN_WORDS };
+enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_UNITS, R_C0_FIRST, R_C1_FIRST, R_C1_LAST, RUN_WORDS };
 struct TcMaps {
   CUtensorMap q, k, v;
 };
@@ -133,241 +133,259 @@ struct Merge {
 // An item's lists into shared memory; entries that count for nothing become 0xffff.
 __device__ __forceinline__ void load_lists(const PagedParams& p, uint16_t* list, int tok0, int tokens, int pos0, int head, int lane) {
   const int total = tokens * p.n_sel;
-#pragma unroll 4
-  for (int i = lane; i < total; i += 32) {
-    const int t = i / p.n_sel;
-    const int place = __ldg(p.sel + ((int64_t)(tok0 + t) * p.Hkv + head) * p.n_sel + (i - t * p.n_sel)), pos = pos0 + t;
-    list[i] = place >= 0 && pos >= 0 && place <= pos / PAGE && place < p.table_pages ? (uint16_t)place : (uint16_t)0xffff;
+  constexpr int AHEAD = 8;
+  for (int base = lane; base < total; base += 32 * AHEAD) {
+    int place[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int i = base + 32 * u, t = i / p.n_sel;
+      place[u] = i < total ? __ldg(p.sel + ((int64_t)(tok0 + t) * p.Hkv + head) * p.n_sel + (i - t * p.n_sel)) : -1;
+      if (pos0 + t < 0 || place[u] > (pos0 + t) / PAGE || place[u] >= p.table_pages) place[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (base + 32 * u < total) list[base + 32 * u] = (uint16_t)place[u];
   }
   __syncwarp();
 }
 
-constexpr int PT = 1024;
-// One CTA: what every request's items weigh, and the sums that the attention kernel's CTAs look their run up in.  FIRST: only the items
-// of every request (selected pages: union_kernel then weighs them, and plan_runs_kernel sums that up).
-template <bool FIRST>
-__global__ void __launch_bounds__(PT) plan_kernel(const TcParams tp) {
+// An item weighs its key tiles and as much again as its end costs (rows out, the next one's first products), in tiles.
+constexpr int ITEM_END = 1;
+
+// The runs: CTA c's is the units bound(c) .. bound(c + 1) - 1 of all.
+struct Shares {
+  int64_t all;
+  int grid;                                                        // every share holds a unit
+  __device__ Shares(int64_t all_, int n_cta) : all(all_), grid((int)min((int64_t)n_cta, all_)) {}
+  __device__ int64_t bound(int c) const { return all * c / grid; }
+  // the CTA that holds unit y: the last c with bound(c) <= y
+  __device__ int owner(int64_t y) const {
+    int c = min((int)((double)y * grid / (double)all), grid - 1);  // (an estimate, put right without a division)
+    while (c + 1 < grid && all * (c + 1) < (y + 1) * grid) ++c;
+    while (c > 0 && all * c >= (y + 1) * grid) --c;
+    return c;
+  }
+};
+// CTA c's run.  `place(y)` says which item holds unit y; a run that would begin with an item's end begins with the next item.
+// All CTAs between an item's first and last tile have tiles of it: their bounds lie inside it.
+template <typename P>
+__device__ __forceinline__ void write_run(const TcParams& tp, const Shares& sh, int c, P place) {
+  int32_t* run = tp.runs + c * RUN_WORDS;
+  run[R_UNITS] = 0;
+  if (c >= sh.grid) return;
+  int64_t y0 = sh.bound(c);
+  const int64_t y1 = sh.bound(c + 1);
+  auto a = place(y0);
+  if (y0 - a.begin >= a.tiles) {
+    y0 = a.begin + a.tiles + ITEM_END;
+    if (y0 >= y1) return;
+    a = place(y0);
+  }
+  const auto z = place(y1 - 1);
+  run[R_SEQ] = a.seq;
+  run[R_HEAD] = a.head;
+  run[R_ITEM] = a.item;
+  run[R_J0] = (int)(y0 - a.begin);
+  run[R_UNITS] = (int)min(y1 - y0, (int64_t)INT32_MAX);
+  run[R_C0_FIRST] = sh.owner(a.begin);
+  run[R_C1_FIRST] = sh.owner(a.begin + a.tiles - 1);
+  run[R_C1_LAST] = sh.owner(z.begin + z.tiles - 1);
+}
+struct Place {
+  int seq, head, item, tiles;
+  int64_t begin;                                                   // the item's first unit
+};
+template <typename T, typename X>
+__device__ __forceinline__ int last_not_above(const T* a, int n, X x) {        // last i in [0, n) with a[i] <= x
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+// Exclusive sum over a CTA of WARPS warps.
+template <int WARPS>
+__device__ __forceinline__ int64_t exclusive(int64_t v, int64_t* sums, int64_t& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  __syncthreads();
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  int64_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    const int64_t x = sums[w];
+    if (w < warp) before += x;
+    all += x;
+  }
+  return before + inc - v;
+}
+
+// One CTA: what every request's items weigh, and the runs.  All sums stay in shared memory (the items' as far as they fit): the kernel is
+// a chain of look-ups, and through global memory it took 10 us.
+constexpr int PT = 512, PLAN_ITEMS = 16384;
+__global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcParams tp) {
+  extern __shared__ __align__(8) unsigned char plan_smem[];
   const PagedParams& p = tp.a;
-  __shared__ int64_t sums[PT / 32][2];
+  int64_t* seq_prefix = reinterpret_cast<int64_t*>(plan_smem);     // [n_seq + 1] units before the request
+  int32_t* item_begin = reinterpret_cast<int32_t*>(seq_prefix + p.n_seq + 1);  // [n_seq + 1]
+  int32_t* tokens = item_begin + p.n_seq + 1;                      // [n_seq]
+  int32_t* keys = tokens + p.n_seq;                                // [n_seq]
+  int32_t* item_prefix = tp.items <= PLAN_ITEMS ? keys + p.n_seq : tp.item_prefix;
+  __shared__ int64_t sums[PT / 32];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pair = 2 * p.tile_tokens;
-  auto scan = [&](int64_t v, int which, int64_t& all) {
-    int64_t inc = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    __syncthreads();
-    if (lane == 31) sums[warp][which] = inc;
-    __syncthreads();
-    int64_t before = 0;
-    all = 0;
-    for (int w = 0; w < PT / 32; ++w) {
-      if (w < warp) before += sums[w][which];
-      all += sums[w][which];
-    }
-    return before + inc - v;
-  };
-  // items of every request
-  const int per = (p.n_seq + PT - 1) / PT, i0 = min(tid * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
-  int64_t items = 0, all;
   int b;
-  for (int i = i0; i < i1; ++i) items += (request_tokens(p, i, b) + pair - 1) / pair;
-  int64_t at = scan(items, 0, all);
-  for (int i = i0; i < i1; ++i) {
-    tp.item_begin[i] = (int)min(at, (int64_t)tp.items);
-    at += (request_tokens(p, i, b) + pair - 1) / pair;
+  for (int i = tid; i < p.n_seq; i += PT) {
+    tokens[i] = request_tokens(p, i, b);
+    keys[i] = request_keys(p, i);
   }
-  if (tid == 0) tp.item_begin[p.n_seq] = (int)min(all, (int64_t)tp.items);
-  if (FIRST) return;
   __syncthreads();
-  // a warp per request: key tiles before every item
+  const int per = (p.n_seq + PT - 1) / PT, i0 = min(tid * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
+  int64_t mine = 0, all;
+  for (int i = i0; i < i1; ++i) mine += (tokens[i] + pair - 1) / pair;
+  int64_t at = exclusive<PT / 32>(mine, sums, all);
+  for (int i = i0; i < i1; ++i) {
+    tp.item_begin[i] = item_begin[i] = (int)min(at, (int64_t)tp.items);
+    at += (tokens[i] + pair - 1) / pair;
+  }
+  if (tid == 0) tp.item_begin[p.n_seq] = item_begin[p.n_seq] = (int)min(all, (int64_t)tp.items);
+  __syncthreads();
+  // a warp per request: units before every item
   for (int i = warp; i < p.n_seq; i += PT / 32) {
-    const int n = request_tokens(p, i, b), kv = request_keys(p, i), first = tp.item_begin[i], count = tp.item_begin[i + 1] - first;
+    const int first = item_begin[i], count = item_begin[i + 1] - first;
     int before = 0;
     for (int base = 0; base < count; base += 32) {
-      const int w = base + lane < count ? item_tiles(p, (base + lane) * pair, n, kv) : 0;
+      const int w = base + lane < count ? item_tiles(p, (base + lane) * pair, tokens[i], keys[i]) + ITEM_END : 0;
       int inc = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int up = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += up;
       }
-      if (base + lane < count) tp.item_prefix[first + base + lane] = before + inc - w;
+      if (base + lane < count) item_prefix[first + base + lane] = before + inc - w;
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
-    if (lane == 0) tp.seq_prefix[i] = (int64_t)before * p.Hkv;
+    if (lane == 0) seq_prefix[i] = before;                         // of one head, for now
   }
   __syncthreads();
-  int64_t w = 0;
-  for (int i = i0; i < i1; ++i) w += tp.seq_prefix[i];
-  int64_t x = scan(w, 1, all);
+  mine = 0;
+  for (int i = i0; i < i1; ++i) mine += seq_prefix[i] * p.Hkv;
+  at = exclusive<PT / 32>(mine, sums, all);
   for (int i = i0; i < i1; ++i) {
-    const int64_t v = tp.seq_prefix[i];
-    tp.seq_prefix[i] = x;
-    x += v;
+    const int64_t v = seq_prefix[i] * p.Hkv;
+    seq_prefix[i] = at;
+    at += v;
   }
-  if (tid == 0) tp.seq_prefix[p.n_seq] = all;
+  if (tid == 0) seq_prefix[p.n_seq] = all;
   __syncthreads();
-  // the runs: where each starts, and which CTAs hold the first and the last part of the items at its two ends
-  const int grid = (int)min((int64_t)tp.n_cta, all);               // every run holds a tile, so all CTAs between have a part
-  auto bound = [&](int c) { return all * c / grid; };
-  auto owner = [&](int64_t y) {
-    int c = (int)(y * grid / all);
-    while (c + 1 < grid && bound(c + 1) <= y) ++c;
-    while (c > 0 && bound(c) > y) --c;
-    return c;
-  };
-  struct Place {
-    int seq, head, item, j0, tiles;
-    int64_t begin;
-  };
-  auto place = [&](int64_t y) {
-    Place r;
-    int lo = 0, hi = p.n_seq - 1;                                  // last request that starts at or before y
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tp.seq_prefix[mid] <= y) lo = mid; else hi = mid - 1;
-    }
-    r.seq = lo;
-    const int64_t s0 = tp.seq_prefix[lo], per_head = (tp.seq_prefix[lo + 1] - s0) / p.Hkv;
-    r.head = (int)((y - s0) / per_head);
-    const int local = (int)(y - s0 - r.head * per_head);
-    const int first = tp.item_begin[r.seq];
-    lo = 0;
-    hi = tp.item_begin[r.seq + 1] - first - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tp.item_prefix[first + mid] <= local) lo = mid; else hi = mid - 1;
-    }
-    r.item = lo;
-    r.j0 = local - tp.item_prefix[first + lo];
-    r.begin = y - r.j0;
-    int b0;
-    const int n = request_tokens(p, r.seq, b0);
-    r.tiles = item_tiles(p, lo * pair, n, request_keys(p, r.seq));
-    return r;
-  };
-  for (int c = tid; c < tp.n_cta; c += PT) {
-    int32_t* run = tp.runs + c * RUN_WORDS;
-    if (c >= grid) {
-      run[R_TILES] = 0;
-      continue;
-    }
-    const int64_t y0 = bound(c), y1 = bound(c + 1);
-    const Place a = place(y0), z = place(y1 - 1);
-    run[R_SEQ] = a.seq;
-    run[R_HEAD] = a.head;
-    run[R_ITEM] = a.item;
-    run[R_J0] = a.j0;
-    run[R_TILES] = (int)min(y1 - y0, (int64_t)INT32_MAX);
-    run[R_C0_FIRST] = owner(a.begin);
-    run[R_C1_FIRST] = owner(a.begin + a.tiles - 1);
-    run[R_C1_LAST] = owner(z.begin + z.tiles - 1);
-  }
+  const Shares sh(all, tp.n_cta);
+  for (int c = tid; c < tp.n_cta; c += PT)
+    write_run(tp, sh, c, [&](int64_t y) {
+      Place r;
+      r.seq = last_not_above(seq_prefix, p.n_seq, y);
+      const int64_t s0 = seq_prefix[r.seq], per_head = (seq_prefix[r.seq + 1] - s0) / p.Hkv;
+      r.head = (int)((y - s0) / per_head);
+      const int local = (int)(y - s0 - r.head * per_head), first = item_begin[r.seq];
+      r.item = last_not_above(item_prefix + first, item_begin[r.seq + 1] - first, local);
+      r.begin = y - (local - item_prefix[first + r.item]);
+      r.tiles = item_tiles(p, r.item * pair, tokens[r.seq], keys[r.seq]);
+      return r;
+    });
 }
 
-// Key tiles of every item and kv head over selected pages: half of the pages that its tokens' lists give when merged.  A warp each.
-constexpr int UNION_WARPS = 4;
-__global__ void __launch_bounds__(UNION_WARPS * 32) union_kernel(const TcParams tp) {
-  extern __shared__ uint16_t lists[];
+// Key tiles of every item and kv head over selected pages: half of the pages that its tokens' lists give when merged, a warp each.  The
+// CTA that is done last sums them up and writes the runs.
+constexpr int UNION_WARPS = 4, UNION_THREADS = UNION_WARPS * 32;
+__global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_constant__ TcParams tp) {
+  extern __shared__ __align__(8) unsigned char union_smem[];
   const PagedParams& p = tp.a;
+  int32_t* item_begin = reinterpret_cast<int32_t*>(union_smem);    // [n_seq + 1]
+  uint16_t* lists = reinterpret_cast<uint16_t*>(item_begin + p.n_seq + 1);
+  __shared__ int64_t sums[UNION_WARPS];
+  __shared__ uint32_t ticket;
   pdl_trigger();
   pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = 2 * p.tile_tokens;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, pair = 2 * p.tile_tokens;
+  const int per = (p.n_seq + UNION_THREADS - 1) / UNION_THREADS, i0 = min(tid * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
+  int b;
+  int64_t mine = 0, all;
+  for (int i = i0; i < i1; ++i) mine += item_begin[i] = (request_tokens(p, i, b) + pair - 1) / pair;
+  int64_t at = exclusive<UNION_WARPS>(mine, sums, all);
+  for (int i = i0; i < i1; ++i) {
+    const int n = item_begin[i];
+    item_begin[i] = (int)min(at, (int64_t)tp.items);
+    at += n;
+  }
+  if (tid == 0) item_begin[p.n_seq] = (int)min(all, (int64_t)tp.items);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int i = tid; i <= p.n_seq; i += UNION_THREADS) tp.item_begin[i] = item_begin[i];
+  const int count = item_begin[p.n_seq] * p.Hkv;
   const int64_t x = (int64_t)blockIdx.x * UNION_WARPS + warp;
-  const int item = (int)(x / p.Hkv), head = (int)(x - (int64_t)item * p.Hkv);
-  if (item >= tp.item_begin[p.n_seq]) return;
-  int lo = 0, hi = p.n_seq - 1, b;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (tp.item_begin[mid] <= item) lo = mid; else hi = mid - 1;
+  if (x < count) {
+    const int item = (int)x / p.Hkv, head = (int)x - item * p.Hkv, seq = last_not_above(item_begin, p.n_seq, item);
+    const int n = request_tokens(p, seq, b), kv = request_keys(p, seq), tok = (item - item_begin[seq]) * pair, tokens = min(n - tok, pair);
+    uint16_t* list = lists + warp * pair * p.n_sel;
+    load_lists(p, list, b + tok, tokens, kv - n + tok, head, lane);
+    Merge merge;
+    merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
+    int pages = 0;
+    uint32_t bits_a, bits_b;
+    while (merge.next(bits_a, bits_b) < NO_PAGE) ++pages;
+    if (lane == 0) tp.item_prefix[x] = max(1, (pages + 1) / 2);
   }
-  const int n = request_tokens(p, lo, b), kv = request_keys(p, lo), tok = (item - tp.item_begin[lo]) * pair, tokens = min(n - tok, pair);
-  uint16_t* list = lists + warp * pair * p.n_sel;
-  load_lists(p, list, b + tok, tokens, kv - n + tok, head, lane);
-  Merge merge;
-  merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
-  int pages = 0;
-  uint32_t bits_a, bits_b;
-  while (merge.next(bits_a, bits_b) < NO_PAGE) ++pages;
-  if (lane == 0) tp.item_prefix[x] = max(1, (pages + 1) / 2);
-}
-
-// One CTA: the sums over items and kv heads, and the runs.
-__global__ void __launch_bounds__(PT) plan_runs_kernel(const TcParams tp) {
-  const PagedParams& p = tp.a;
-  __shared__ int64_t sums[PT / 32];
-  pdl_trigger();
-  pdl_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int count = tp.item_begin[p.n_seq] * p.Hkv, per = (count + PT - 1) / PT, i0 = min(tid * per, count), i1 = min(i0 + per, count);
-  int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += tp.item_prefix[i];
-  int64_t inc = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += up;
-  }
-  if (lane == 31) sums[warp] = inc;
+  __threadfence();
   __syncthreads();
-  int64_t at = inc - mine, all = 0;
-  for (int w = 0; w < PT / 32; ++w) {
-    if (w < warp) at += sums[w];
-    all += sums[w];
+  if (tid == 0) {
+    ticket = atomicAdd(tp.ticket, 1u);
+    if (ticket == gridDim.x - 1) *reinterpret_cast<volatile uint32_t*>(tp.ticket) = 0;         // ready for the next launch
   }
-  for (int i = i0; i < i1; ++i) {
-    const int v = tp.item_prefix[i];
+  __syncthreads();
+  if (ticket != gridDim.x - 1) return;
+  __threadfence();
+  const int each = (count + UNION_THREADS - 1) / UNION_THREADS, x0 = min(tid * each, count), x1 = min(x0 + each, count);
+  mine = 0;
+  for (int i = x0; i < x1; ++i) mine += __ldcg(tp.item_prefix + i) + ITEM_END;
+  at = exclusive<UNION_WARPS>(mine, sums, all);
+  for (int i = x0; i < x1; ++i) {
+    const int v = __ldcg(tp.item_prefix + i) + ITEM_END;
     tp.item_prefix[i] = (int)min(at, (int64_t)INT32_MAX);
     at += v;
   }
   if (tid == 0) tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
   __syncthreads();
-  all = min(all, (int64_t)INT32_MAX);
-  const int grid = (int)min((int64_t)tp.n_cta, all);
-  auto bound = [&](int c) { return all * c / grid; };
-  auto owner = [&](int64_t y) {
-    int c = (int)(y * grid / all);
-    while (c + 1 < grid && bound(c + 1) <= y) ++c;
-    while (c > 0 && bound(c) > y) --c;
-    return c;
-  };
-  auto item_of = [&](int64_t y) {
-    int lo = 0, hi = count - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tp.item_prefix[mid] <= y) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-  };
-  for (int c = tid; c < tp.n_cta; c += PT) {
-    int32_t* run = tp.runs + c * RUN_WORDS;
-    if (c >= grid) {
-      run[R_TILES] = 0;
-      continue;
-    }
-    const int64_t y0 = bound(c), y1 = bound(c + 1);
-    const int a = item_of(y0), z = item_of(y1 - 1);
-    int lo = 0, hi = p.n_seq - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tp.item_begin[mid] <= a / p.Hkv) lo = mid; else hi = mid - 1;
-    }
-    run[R_SEQ] = lo;
-    run[R_HEAD] = a % p.Hkv;
-    run[R_ITEM] = a / p.Hkv - tp.item_begin[lo];
-    run[R_J0] = (int)(y0 - tp.item_prefix[a]);
-    run[R_TILES] = (int)(y1 - y0);
-    run[R_C0_FIRST] = owner(tp.item_prefix[a]);
-    run[R_C1_FIRST] = owner(tp.item_prefix[a + 1] - 1);
-    run[R_C1_LAST] = owner(tp.item_prefix[z + 1] - 1);
-  }
+  const Shares sh(min(all, (int64_t)INT32_MAX), tp.n_cta);
+  for (int c = tid; c < tp.n_cta; c += UNION_THREADS)
+    write_run(tp, sh, c, [&](int64_t y) {
+      Place r;
+      const int i = last_not_above(tp.item_prefix, count, y), item = i / p.Hkv;
+      r.head = i - item * p.Hkv;
+      r.seq = last_not_above(item_begin, p.n_seq, item);
+      r.item = item - item_begin[r.seq];
+      r.begin = tp.item_prefix[i];
+      r.tiles = tp.item_prefix[i + 1] - tp.item_prefix[i] - ITEM_END;
+      return r;
+    });
 }
 
 __device__ __forceinline__ int ring_word(const volatile int32_t* ring, int word) { return __shfl_sync(0xffffffffu, ring[word], 0); }
+
+// Key tiles of row tile A in this part of an item: with B's tokens behind its own it may see fewer (at least one, if need be masked whole).
+template <bool SPARSE>
+__device__ __forceinline__ int tiles_of_a(const PagedParams& p, const volatile int32_t* ring, int n_tiles) {
+  if (SPARSE || !p.causal) return n_tiles;
+  const int sees = min(ring_word(ring, W_POS0) + p.tile_tokens, ring_word(ring, W_KV));
+  return max(1, min(n_tiles, (sees + BN - 1) / BN - ring_word(ring, W_J0)));
+}
 
 template <bool F16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -378,6 +396,25 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return pack_bf16(lo, hi);
 }
 
+// 2^x for a pair on the FMA units: x = n + f with n = round(x), f in [-1/2, 1/2]; the polynomial of degree 4 that is nearest to 2^f there
+// (relative error 2.7e-6 with its 32-bit steps) gets n added to its exponent.  x is clamped at -125: keys that a row does not see arrive as
+// minus infinity and give 2^-125.
+__device__ __forceinline__ void exp2_pair(uint64_t x, float& e0, float& e1) {
+  constexpr float MAGIC = 12582912.f;                  // 1.5 * 2^23: the sum's low mantissa bits hold round(x)
+  float x0, x1;
+  unpack2(x, x0, x1);
+  const uint64_t xc = pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f)), magic = pack2(MAGIC, MAGIC);
+  const uint64_t t = add2(xc, magic), f = sub2(xc, sub2(t, magic));
+  uint64_t q = fma2(pack2(0.00957010221f, 0.00957010221f), f, pack2(0.0559178591f, 0.0559178591f));
+  q = fma2(q, f, pack2(0.240247443f, 0.240247443f));
+  q = fma2(q, f, pack2(0.693121791f, 0.693121791f));
+  q = fma2(q, f, pack2(0.999999285f, 0.999999285f));
+  float t0, t1, q0, q1;
+  unpack2(t, t0, t1);
+  unpack2(q, q0, q1);
+  e0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
+  e1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+}
 template <int D, bool F16, bool SPARSE>
 __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
   using L = Layout<D>;
@@ -386,6 +423,10 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
   // How far (log2) a maximum may rise above the reference of its row's exponentials: bf16 and the 32-bit sums have room for 2^32,
   // fp16 probabilities for 2^15.
   constexpr float THRESHOLD = F16 ? 8.f : RESCALE_THRESHOLD;
+  // One pair of exponentials in four on the FMA units where the exponential unit is as busy as anything (64-wide heads: a chunk of 1500
+  // tokens behind 20 000, 40 heads, 452 us without, 411 with one pair in four, 440 with one in two; 128-wide heads, bound by the products:
+  // no difference, and 6 % slower with one in two).
+  constexpr bool POLY = D == 64;
   const PagedParams& p = tp.a;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -437,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       // ---------------------------------------------------------------- the CTA's run, and the copies
       const bool leader = elect_one();
       const int32_t* run = tp.runs + blockIdx.x * RUN_WORDS;
-      int left = run[R_TILES], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
+      int left = run[R_UNITS], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
       if (left > 0) {
         seq = run[R_SEQ];
         head = run[R_HEAD];
@@ -464,7 +505,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
         const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
         const int flat = SPARSE ? (tp.item_begin[seq] + item) * p.Hkv + head : 0;
-        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
+        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] - ITEM_END : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
         const int nq = tokens > p.tile_tokens ? 2 : 1;
         if (lane == 0) {
           ring[W_KIND] = 1;
@@ -482,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         }
         __syncwarp();
         if (leader) mbar_arrive(bar(ITEM_FULL + slot));
-        left -= n_tiles;
+        left -= n_tiles + (j0 + n_tiles == tiles ? ITEM_END : 0);
         const int32_t* table = p.block_table + seq * p.table_stride;
         const int n_pages = (kv + PAGE - 1) / PAGE;
         int pages = -1;
@@ -625,6 +666,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         if (!ok) break;
         if (ring_word(ring, W_KIND) == 0) break;
         const int nq = ring_word(ring, W_TOKENS) > p.tile_tokens ? 2 : 1, n_tiles = ring_word(ring, W_NT);
+        const int nt[2] = {tiles_of_a<SPARSE>(p, ring, n_tiles), n_tiles};
         const int kv_len = ring_word(ring, W_KV), kv_left = kv_len - ring_word(ring, W_J0) * BN;      // keys of the request from the item's first on
         // values of the tile: waited for, and rows without a key in the request's last page made zero
         auto values = [&](uint32_t st, uint32_t parity, int j) {
@@ -669,7 +711,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           for (int x = 0; x < nq; ++x) {
             issue_s(lead, x, st0);
             tc_commit(lead, bar(S_FULL + x));
-            if (n_tiles == 1) tc_commit(lead, bar(Q_EMPTY + x));
+            if (nt[x] == 1) tc_commit(lead, bar(Q_EMPTY + x));
           }
           tc_commit(lead, bar(K_EMPTY + st0));
         }
@@ -677,17 +719,20 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         for (int j = 0; j < n_tiles && ok; ++j) {
           const uint32_t st = (g + j) % KV_STAGES, stn = (g + j + 1) % KV_STAGES;
           const uint32_t parn = ((g + j + 1) / KV_STAGES) & 1;
-          const bool more = j + 1 < n_tiles;
+          const bool last = j + 1 == n_tiles;
+          bool keys = last;                                        // the next tile's keys are there (or not wanted)
           const uint32_t lead = elect_one();
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            if (x >= nq || !ok) continue;
+            if (x >= nq || j >= nt[x] || !ok) continue;
+            const bool more = j + 1 < nt[x];
             const uint32_t ph = (cx[x] + j) & 1;
             ok = mma_wait(P_FULL + 2 * x, ph);
             if (!ok) continue;
             tc_fence_after();
             issue_pv(lead, x, st, 0, j == 0);
-            if (more && x == 0) ok = mma_wait(K_FULL + stn, parn);
+            if (!keys) ok = mma_wait(K_FULL + stn, parn);
+            keys = true;
             if (!ok) continue;
             ok = mma_wait(P_FULL + 2 * x + 1, ph);
             if (!ok) continue;
@@ -696,22 +741,22 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             if (more) {
               issue_s(lead, x, stn);
               tc_commit(lead, bar(S_FULL + x));
-              if (j + 2 == n_tiles) tc_commit(lead, bar(Q_EMPTY + x));
+              if (j + 2 == nt[x]) tc_commit(lead, bar(Q_EMPTY + x));
             } else {
               tc_commit(lead, bar(PV_DONE + x));
             }
           }
           if (ok) {
             tc_commit(lead, bar(V_EMPTY + st));
-            if (more) tc_commit(lead, bar(K_EMPTY + stn));
+            if (!last) tc_commit(lead, bar(K_EMPTY + stn));
           }
-          if (ok && more) ok = values(stn, parn, j + 1);
+          if (ok && !last) ok = values(stn, parn, j + 1);
         }
         g += n_tiles;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
           if (x < nq) {
-            cx[x] += n_tiles;
+            cx[x] += nt[x];
             ++iq[x];
           }
         __syncwarp();
@@ -735,7 +780,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       ok = wait_all(bar(ITEM_FULL + slot), (it >> 1) & 1, abort_flag, p.status, 1 + ITEM_FULL);
       if (!ok) break;
       if (ring_word(ring, W_KIND) == 0) break;
-      const int n_tiles = ring_word(ring, W_NT), tokens = ring_word(ring, W_TOKENS);
+      const int all_tiles = ring_word(ring, W_NT), tokens = ring_word(ring, W_TOKENS);
+      const int n_tiles = x == 0 && tokens > p.tile_tokens ? tiles_of_a<SPARSE>(p, ring, all_tiles) : all_tiles;      // of this row tile
       if (x == 0 || tokens > p.tile_tokens) {
         const int kv = ring_word(ring, W_KV), pos0 = ring_word(ring, W_POS0), skipped = ring_word(ring, W_J0) * BN;
         const bool valid = row_tok < p.tile_tokens && x * p.tile_tokens + row_tok < tokens;
@@ -757,56 +803,64 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           tmem_ld32(t_s + 96, r3);
           tmem_wait_ld();
           bool sel0 = true, sel1 = true;                           // does the row see the tile's two pages at all
+          // keys of each half that the row sees, where some row of the warp does not see all of them (else more than it has)
+          int left0 = BN, left1 = BN;
           if (SPARSE) {
             const volatile int32_t* info = info_base + ((g + j) % INFO_RING) * INFO_WORDS;
             const int place0 = info[I_PLACE], place1 = info[I_PLACE + 1];
             sel0 = valid && ((uint32_t)info[I_BITS + 2 * x] >> row_tok & 1u);
             sel1 = valid && ((uint32_t)info[I_BITS + 2 * x + 1] >> row_tok & 1u);
             // (in pages that no row selected, and in the last one past the row's own position)
-            if (place0 * PAGE + PAGE > least) {
-              const int left = sees - place0 * PAGE;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                if (i >= left) r0[i] = 0xff800000u;
-                if (i + 32 >= left) r1[i] = 0xff800000u;
-              }
-            }
-            if (place1 * PAGE + PAGE > least) {
-              const int left = sees - place1 * PAGE;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                if (i >= left) r2[i] = 0xff800000u;
-                if (i + 32 >= left) r3[i] = 0xff800000u;
-              }
-            }
-          } else if ((j + 1) * BN > least) {                       // some row of the warp does not see the whole tile
-            const int left = lim - j * BN;
+            if (place0 * PAGE + PAGE > least) left0 = sees - place0 * PAGE;
+            if (place1 * PAGE + PAGE > least) left1 = sees - place1 * PAGE;
+          } else if ((j + 1) * BN > least) {
+            left0 = lim - j * BN;
+            left1 = left0 - PAGE;
+          }
+          auto mask = [](uint32_t (&a)[32], uint32_t (&b)[32], int left) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-              if (i >= left) r0[i] = 0xff800000u;
-              if (i + 32 >= left) r1[i] = 0xff800000u;
-              if (i + 64 >= left) r2[i] = 0xff800000u;
-              if (i + 96 >= left) r3[i] = 0xff800000u;
+              if (i >= left) a[i] = 0xff800000u;
+              if (i + 32 >= left) b[i] = 0xff800000u;
             }
-          }
-          float mq[8];
+          };
+          if (__any_sync(0xffffffffu, left0 < PAGE)) mask(r0, r1, left0);
+          if (__any_sync(0xffffffffu, left1 < PAGE)) mask(r2, r3, left1);
+          auto top_of = [](const uint32_t (&a)[32], const uint32_t (&b)[32]) {
+            float mq[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            mq[c] = fmaxf(__uint_as_float(r0[c]), __uint_as_float(r1[c]));
-            mq[4 + c] = fmaxf(__uint_as_float(r2[c]), __uint_as_float(r3[c]));
-          }
+            for (int c = 0; c < 4; ++c) mq[c] = fmaxf(__uint_as_float(a[c]), __uint_as_float(b[c]));
 #pragma unroll
-          for (int i = 4; i < 32; i += 4) {
+            for (int i = 4; i < 32; ++i) mq[i & 3] = fmax3(mq[i & 3], __uint_as_float(a[i]), __uint_as_float(b[i]));
+            return fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
+          };
+          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+          // (a page that the row did not select: every exponent minus infinity)
+          const uint64_t none2 = pack2(-INFINITY, -INFINITY);
+          uint64_t sum2 = pack2(0.f, 0.f);
+          auto exp_chunk = [&](const uint32_t (&rc)[32], uint64_t shift, int c) {
+            uint32_t pk[16];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              mq[c] = fmax3(mq[c], __uint_as_float(r0[i + c]), __uint_as_float(r1[i + c]));
-              mq[4 + c] = fmax3(mq[4 + c], __uint_as_float(r2[i + c]), __uint_as_float(r3[i + c]));
+            for (int i = 0; i < 32; i += 2) {
+              const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift);
+              float e0, e1;
+              if (POLY && (i >> 1 & 3) == 3) {
+                exp2_pair(xx, e0, e1);
+              } else {
+                float x0, x1;
+                unpack2(xx, x0, x1);
+                e0 = ex2_approx(x0);
+                e1 = ex2_approx(x1);
+              }
+              sum2 = add2(sum2, pack2(e0, e1));
+              pk[i >> 1] = pack16<F16>(e0, e1);
             }
-          }
-          const float mx0 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), mx1 = fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7]));
-          const float mx = (SPARSE ? fmaxf(sel0 ? mx0 : -INFINITY, sel1 ? mx1 : -INFINITY) : fmaxf(mx0, mx1)) * p.scale_log2;
-          const float m_new = fmaxf(m_ref, mx);
-          const bool grow = m_new > m_ref + THRESHOLD;             // also on the first tile with a key the row sees
+            tmem_st16(t_s + c * 16, pk);
+          };
+          const float mx0 = sel0 ? top_of(r0, r1) : -INFINITY, mx1 = sel1 ? top_of(r2, r3) : -INFINITY;
+          const float m_new = fmaxf(m_ref, fmaxf(mx0, mx1) * p.scale_log2);
+          // also on the first tile with a key the row sees; (rows that are none hold anything)
+          const bool grow = valid && m_new > m_ref + THRESHOLD;
           if (j > 0 && __any_sync(0xffffffffu, grow)) {
             // O is complete up to tile j - 1: the commit behind S_FULL covers every product issued before it
             const float f = grow ? exp2f(m_ref - m_new) : 1.f;
@@ -823,23 +877,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             l_sum *= f;
           }
           if (grow) m_ref = m_new;
-          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), shift2 = pack2(-m_ref, -m_ref);
-          // (a page that the row did not select: every exponent minus infinity)
-          const uint64_t none2 = pack2(-INFINITY, -INFINITY);
-          uint64_t sum2 = pack2(0.f, 0.f);
-          auto exp_chunk = [&](const uint32_t (&rc)[32], uint64_t shift, int c) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift);
-              float x0, x1;
-              unpack2(xx, x0, x1);
-              const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
-              sum2 = add2(sum2, pack2(e0, e1));
-              pk[i >> 1] = pack16<F16>(e0, e1);
-            }
-            tmem_st16(t_s + c * 16, pk);
-          };
+          const uint64_t shift2 = pack2(-m_ref, -m_ref);
           exp_chunk(r0, sel0 ? shift2 : none2, 0);
           exp_chunk(r1, sel0 ? shift2 : none2, 1);
           tmem_wait_st();
@@ -884,14 +922,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             __syncwarp();
           };
           auto finish = [&](float m, float l) {                    // 1 / sum, and the row's logarithm
-            const bool any = SPARSE ? l > 0.f : sees > 0;
+            const bool any = SPARSE ? l > 0.5f : sees > 0;             // (the key that set the reference counts 1)
             if (p.lse && valid) p.lse[(int64_t)tok * p.H + hd] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             const float inv = any ? 1.f / l : 0.f;
             __syncwarp();                                          // the loads of tensor memory that follow are the whole warp's
             return inv;
           };
           const int tiles = ring_word(ring, W_TILES);
-          if (n_tiles == tiles) {
+          if (all_tiles == tiles) {
             const float inv = finish(m_ref, l_sum);
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -942,11 +980,23 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
               __threadfence();
               // in key order, this warp's own part from tensor memory at its place
               auto m_of = [&](int c) { return c == me ? m_ref : __ldcg(part(c) + 2 * BM * D + x * BM + row); };
-              float m_all = NO_MAX;
-              for (int c = c0; c <= c1; ++c) m_all = fmaxf(m_all, m_of(c));
+              auto l_of = [&](int c) { return c == me ? l_sum : __ldcg(part(c) + 2 * BM * D + 2 * BM + x * BM + row); };
+              constexpr int FAST = 4;                              // parts whose two words are read once, all on their way together
+              float w4[FAST], l4[FAST];
+#pragma unroll
+              for (int i = 0; i < FAST; ++i) {
+                w4[i] = c0 + i <= c1 ? m_of(c0 + i) : NO_MAX;
+                l4[i] = c0 + i <= c1 ? l_of(c0 + i) : 0.f;
+              }
+              float m_all = fmaxf(fmaxf(w4[0], w4[1]), fmaxf(w4[2], w4[3]));
+              for (int c = c0 + FAST; c <= c1; ++c) m_all = fmaxf(m_all, m_of(c));
               float l_all = 0.f;
-              for (int c = c0; c <= c1; ++c)
-                l_all = fmaf(c == me ? l_sum : __ldcg(part(c) + 2 * BM * D + 2 * BM + x * BM + row), exp2f(m_of(c) - m_all), l_all);
+#pragma unroll
+              for (int i = 0; i < FAST; ++i) {
+                w4[i] = exp2f(w4[i] - m_all);                      // from here on: the part's weight
+                l_all = fmaf(l4[i], w4[i], l_all);
+              }
+              for (int c = c0 + FAST; c <= c1; ++c) l_all = fmaf(l_of(c), exp2f(m_of(c) - m_all), l_all);
               const float inv = finish(m_all, l_all);
 #pragma unroll 1
               for (int cc = 0; cc < D / 32; ++cc) {
@@ -958,7 +1008,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
                 for (int i = 0; i < 32; ++i) acc[i] = 0.f;
 #pragma unroll 1
                 for (int c = c0; c <= c1; ++c) {
-                  const float w = exp2f(m_of(c) - m_all);
+                  const int i4 = c - c0;
+                  const float w = i4 == 0 ? w4[0] : i4 == 1 ? w4[1] : i4 == 2 ? w4[2] : i4 == 3 ? w4[3] : exp2f(m_of(c) - m_all);
                   if (c == me) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) acc[i] = fmaf(__uint_as_float(r[i]), w, acc[i]);
@@ -981,7 +1032,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           tc_fence_before();                                       // orders this item's reads of O before the next one's products
         }
       }
-      g += n_tiles;
+      g += all_tiles;
       __syncwarp();
       if (ok && lane == 0) mbar_arrive(bar(ITEM_EMPTY + slot));
     }
@@ -1002,7 +1053,7 @@ uint64_t run_bytes(int n_sm) { return ((uint64_t)n_sm * RUN_WORDS * 4 + 255) / 2
 // (room for either kind of call: over selected pages every kv head's items count for themselves, and have at most 32 tokens a tile)
 uint64_t plan_bytes(int G, int Hkv, int n_tokens, int n_seq) {
   const uint64_t dense = plan_items(BM / G, n_tokens, n_seq), sparse = plan_items(sparse_tile_tokens(G), n_tokens, n_seq) * Hkv + 1;
-  return (12 * ((uint64_t)n_seq + 1) + 4 * std::max(dense, sparse) + 255) / 256 * 256;
+  return (4 * ((uint64_t)n_seq + 1) + 4 * std::max(dense, sparse) + 255) / 256 * 256;
 }
 
 template <int D, bool F16, bool SPARSE>
@@ -1016,17 +1067,20 @@ cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_
   rc = cudaFuncGetAttributes(&attr, kernel);
   if (rc != cudaSuccess) return rc;
   if (attr.numRegs * THREADS < 128 * REGS_SMALL + 256 * REGS_SOFTMAX) return cudaErrorLaunchOutOfResources;
-  rc = launch_pdl(plan_kernel<SPARSE>, dim3(1), dim3(PT), 0, stream, tp);
-  if (rc != cudaSuccess) return rc;
   if (SPARSE) {
-    const int lists = UNION_WARPS * 2 * tp.a.tile_tokens * tp.a.n_sel * 2;
-    rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, UNION_WARPS * LIST_ENTRIES * 2);
+    const int bytes = (tp.a.n_seq + 1) * 4 + UNION_WARPS * 2 * tp.a.tile_tokens * tp.a.n_sel * 2;
+    rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PAGED_MAX_SEQ + 1) * 4 + UNION_WARPS * LIST_ENTRIES * 2);
     if (rc != cudaSuccess) return rc;
-    rc = launch_pdl(union_kernel, dim3((unsigned)(((int64_t)tp.items * tp.a.Hkv + UNION_WARPS - 1) / UNION_WARPS)), dim3(UNION_WARPS * 32), lists, stream, tp);
+    const int64_t warps = (int64_t)tp.items * tp.a.Hkv;
+    rc = launch_pdl(union_kernel, dim3((unsigned)((warps + UNION_WARPS - 1) / UNION_WARPS)), dim3(UNION_THREADS), bytes, stream, tp);
+  } else {
+    constexpr int most = (PAGED_MAX_SEQ + 1) * 20 + PLAN_ITEMS * 4;
+    const int bytes = (tp.a.n_seq + 1) * 20 + (tp.items <= PLAN_ITEMS ? tp.items * 4 : 0);
+    rc = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (rc != cudaSuccess) return rc;
-    rc = launch_pdl(plan_runs_kernel, dim3(1), dim3(PT), 0, stream, tp);
-    if (rc != cudaSuccess) return rc;
+    rc = launch_pdl(plan_kernel, dim3(1), dim3(PT), bytes, stream, tp);
   }
+  if (rc != cudaSuccess) return rc;
   return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, stream, tp, maps);
 }
 template <int D, bool F16>
@@ -1048,8 +1102,8 @@ cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool,
   tp.a = p;
   tp.a.tile_tokens = p.sel ? sparse_tile_tokens(p.G) : BM / p.G;
   tp.runs = reinterpret_cast<int32_t*>(p.partials);
-  tp.seq_prefix = reinterpret_cast<int64_t*>(p.partials + run_bytes(dev.n_sm) / 4);
-  tp.item_begin = reinterpret_cast<int32_t*>(tp.seq_prefix + p.n_seq + 1);
+  tp.item_begin = reinterpret_cast<int32_t*>(p.partials + run_bytes(dev.n_sm) / 4);
+  tp.ticket = p.counters + PAGED_WS_CTRS * 8 - 1;
   tp.item_prefix = tp.item_begin + p.n_seq + 1;
   tp.n_cta = dev.n_sm;
   tp.items = (int32_t)plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq);

@@ -9,15 +9,20 @@ constexpr long long PAGED_WAIT_CYCLES = 4000000000ll;   // about two seconds: fa
 
 // Returns false when the CTA is leaving (this wait or another one ran out); the first to run out leaves its `code` in the status word.
 __device__ __forceinline__ bool timed_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status, uint32_t code) {
-  if (tc::mbar_try(bar, parity)) return true;
-  const long long begun = clock64();
+  uint32_t tries = 0;
+  long long begun = 0;
 #pragma unroll 1
   while (!tc::mbar_try(bar, parity)) {
     if (*abort_flag) return false;
-    if (clock64() - begun > PAGED_WAIT_CYCLES) {
-      *abort_flag = 1;
-      atomicCAS(status, 0u, code);
-      return false;
+    if ((++tries & 63u) == 0) {                        // (the clock is looked at seldom: a wait's end sits on the chain of every tile)
+      const long long now = clock64();
+      if (begun == 0) {
+        begun = now;
+      } else if (now - begun > PAGED_WAIT_CYCLES) {
+        *abort_flag = 1;
+        atomicCAS(status, 0u, code);
+        return false;
+      }
     }
   }
   return true;

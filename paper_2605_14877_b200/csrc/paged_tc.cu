@@ -5,7 +5,8 @@
 // order, are dealt out in equal runs, one per SM, so that every SM ends at the same time whatever the lengths; an item that a run's border
 // cuts leaves unnormalised rows in the workspace, where the warp that arrives last for its 32 rows adds the parts up in key order.
 // Warp roles as in attn_tc.cu:
-//   warp 0       walks the CTA's run, tells the others the items (a two-entry ring) and sends for Q, K and V (TMA);
+//   warp 2       walks the CTA's run and tells the others the items, one ahead (a two-entry ring);
+//   warp 0       sends for Q, K and V (TMA);
 //   warp 1       issues the products: S = Q K^T and O += P V, accumulators in tensor memory;
 //   warps 4-7    softmax of tile A, warps 8-11 of tile B, one thread a row; they write the item's rows, too.
 // Tensor memory: S_A/P_A 0..127, S_B/P_B 128..255, O_A 256..383, O_B 384..511.  Rows past a request's last key in its last page are
@@ -13,8 +14,8 @@
 //
 // Over selected pages (SPARSE) the keys of an item are the pages that any of its tokens selected, in ascending order, and a row sees a page
 // if its token is among those that did: neighbouring tokens select much the same pages, so a page is read and multiplied once for all of
-// them instead of once for each.  The copy warp merges the tokens' lists (in shared memory, a token per lane and tile) as it goes and
-// hands the tokens' bits to the softmax warps beside each tile.
+// them instead of once for each.  Warp 2 brings the tokens' lists into shared memory, the copy warp merges them as it goes (a
+// token per lane and tile) and hands the tokens' bits to the softmax warps beside each tile.
 // Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and leaves.
 #include <algorithm>
 
@@ -37,7 +38,9 @@ constexpr uint32_t HALF_COLS_BYTES = 128 * 128;        // one 64-column half of 
 constexpr uint32_t SLOT_BYTES = PAGE * 128;            // a page inside one column half
 constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 rows x 32 columns on their way out
 
-constexpr int LIST_ENTRIES = 8192;                     // 16-bit places of an item's lists
+// An item's lists of selected pages: 16-bit places, and a bit for every page of a context (0xffff stands for none).
+constexpr int LIST_ENTRIES = 2048, LIST_WORDS = 2048;
+constexpr uint32_t LIST_BYTES = LIST_ENTRIES * 2 + LIST_WORDS * 4;
 
 template <int D>
 struct Layout {
@@ -50,7 +53,7 @@ struct Layout {
   static constexpr uint32_t SM_BAR = SM_OUT + 8 * STAGE_BYTES;
   static constexpr uint32_t SM_LIST = SM_BAR + 512;
   static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;             // (and the lists where pages are selected)
-  static_assert(SM_ALLOC + LIST_ENTRIES * 2 <= 227 * 1024, "shared memory of one CTA");
+  static_assert(SM_ALLOC + LIST_BYTES + LIST_ENTRIES * 2 <= 227 * 1024, "shared memory of one CTA");
   // one part of a cut item: O of both tiles (groups of four columns outermost), then references and sums
   static constexpr int SLOT_FLOATS = 2 * BM * D + 2 * 2 * BM;
 };
@@ -61,7 +64,7 @@ enum Bar : uint32_t {
 constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256, BAR_INFO = 384;
 constexpr int INFO_RING = 4;                           // key tiles whose pages and bits are kept: the copy warp is at most two ahead of the softmax
 enum InfoWord : int { I_PLACE = 0, I_BITS = 2, INFO_WORDS = 8 };   // two places; bits of tile A for both, of tile B for both
-enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1 };
+enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1, W_SEEK };
 
 struct TcParams {
   PagedParams a;
@@ -95,22 +98,41 @@ __device__ __forceinline__ int item_tiles(const PagedParams& p, int tok, int n, 
 constexpr int NO_PAGE = 1 << 24;
 struct Merge {
   const uint16_t* list;
-  int n_sel, a, b, a_end, b_end, va, vb;
+  int a, b, a_end, b_end;                          // the next places to be read
+  int va, vb, va2, vb2;                            // the lists' next entries, and those behind them (read ahead)
   __device__ int entry(int& i, int end) const {
     int v = 0xffff;
-    while (i < end && (v = list[i]) == 0xffff) ++i;
-    return i < end ? v : NO_PAGE;
+    while (i < end && (v = list[i++]) == 0xffff) {}
+    return v == 0xffff ? NO_PAGE : v;
   }
-  __device__ void start(const uint16_t* l, int n, int tokens, int tile_tokens, int lane) {
+  __device__ void start(const uint16_t* l, int n_sel, int tokens, int tile_tokens, int lane) {
     list = l;
-    n_sel = n;
     const bool in_a = lane < min(tile_tokens, tokens), in_b = lane < tile_tokens && tile_tokens + lane < tokens;
-    a = lane * n;
-    a_end = in_a ? a + n : a;
-    b = (tile_tokens + lane) * n;
-    b_end = in_b ? b + n : b;
+    a = lane * n_sel;
+    a_end = in_a ? a + n_sel : a;
+    b = (tile_tokens + lane) * n_sel;
+    b_end = in_b ? b + n_sel : b;
+    refill();
+  }
+  __device__ void refill() {
     va = entry(a, a_end);
     vb = entry(b, b_end);
+    va2 = entry(a, a_end);
+    vb2 = entry(b, b_end);
+  }
+  // ascending lists: on to the first entries that are not below `page`
+  __device__ void seek(int page, int n_sel, int tile_tokens, int lane) {
+    auto first = [&](int from, int end) {
+      int lo = from, hi = end;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (list[mid] < page) lo = mid + 1; else hi = mid;
+      }
+      return lo;
+    };
+    a = first(min(lane * n_sel, a_end), a_end);
+    b = first(min((tile_tokens + lane) * n_sel, b_end), b_end);
+    refill();
   }
   // the next page (NO_PAGE: none is left) and the tokens of each tile that selected it
   __device__ int next(uint32_t& bits_a, uint32_t& bits_b) {
@@ -119,34 +141,84 @@ struct Merge {
     bits_a = __ballot_sync(0xffffffffu, ha);
     bits_b = __ballot_sync(0xffffffffu, hb);
     if (ha) {
-      ++a;
-      va = entry(a, a_end);
+      va = va2;
+      va2 = entry(a, a_end);
     }
     if (hb) {
-      ++b;
-      vb = entry(b, b_end);
+      vb = vb2;
+      vb2 = entry(b, b_end);
     }
     __syncwarp();
     return page;
   }
 };
-// An item's lists into shared memory; entries that count for nothing become 0xffff.
-__device__ __forceinline__ void load_lists(const PagedParams& p, uint16_t* list, int tok0, int tokens, int pos0, int head, int lane) {
-  const int total = tokens * p.n_sel;
-  constexpr int AHEAD = 8;
-  for (int base = lane; base < total; base += 32 * AHEAD) {
-    int place[AHEAD];
+// An item's lists into shared memory; entries that count for nothing become 0xffff.  Returns whether all lists ascend (with nothing but
+// such entries behind the last page), as heatkv_paged_select writes them.
+__device__ __forceinline__ bool load_lists(const PagedParams& p, uint16_t* list, int tok0, int tokens, int pos0, int head, int lane) {
+  // lanes: as many tokens at once as their lists fit a warp; longer lists in rounds
+  const int at_once = max(1, 32 / p.n_sel), t_lane = lane / p.n_sel, i_lane = at_once > 1 ? lane - t_lane * p.n_sel : lane;
+  const bool active = at_once == 1 || t_lane < at_once;
+  const int64_t stride = (int64_t)p.Hkv * p.n_sel;
+  bool ascend = true;
+  for (int i0 = 0; i0 < p.n_sel; i0 += 32) {
+    const int i = i0 + i_lane;
+    constexpr int AHEAD = 8;
+    for (int base = 0; base < tokens; base += at_once * AHEAD) {
+      int place[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int i = base + 32 * u, t = i / p.n_sel;
-      place[u] = i < total ? __ldg(p.sel + ((int64_t)(tok0 + t) * p.Hkv + head) * p.n_sel + (i - t * p.n_sel)) : -1;
-      if (pos0 + t < 0 || place[u] > (pos0 + t) / PAGE || place[u] >= p.table_pages) place[u] = -1;
+      for (int u = 0; u < AHEAD; ++u) {
+        const int t = base + t_lane + u * at_once;
+        place[u] = active && t < tokens && i < p.n_sel ? __ldg(p.sel + (tok0 + t) * stride + head * p.n_sel + i) : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int t = base + t_lane + u * at_once;
+        if (pos0 + t < 0 || place[u] > (pos0 + t) / PAGE || place[u] >= p.table_pages) place[u] = -1;
+        const int v = place[u] < 0 ? 0xffff : place[u], before = __shfl_up_sync(0xffffffffu, v, 1);
+        if (active && t < tokens && i < p.n_sel) {
+          list[t * p.n_sel + i] = (uint16_t)v;
+          if (i_lane > 0) ascend &= v == 0xffff || before < v;
+        }
+      }
     }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (base + 32 * u < total) list[base + 32 * u] = (uint16_t)place[u];
   }
   __syncwarp();
+  if (p.n_sel > 32)                                                // the seams between rounds
+    for (int t = lane; t < tokens; t += 32)
+      for (int i = 32; i < p.n_sel; i += 32) ascend &= list[t * p.n_sel + i] == 0xffff || list[t * p.n_sel + i - 1] < list[t * p.n_sel + i];
+  return __all_sync(0xffffffffu, ascend);
+}
+// A bit for every page that some list has; `words` of them.
+__device__ __forceinline__ void mark_pages(const uint16_t* list, int total, uint32_t* bits, int words, int lane) {
+  for (int i = lane; i < words; i += 32) bits[i] = 0;
+  __syncwarp();
+  for (int i = lane; i < total; i += 32)
+    if (list[i] != 0xffff) atomicOr(bits + (list[i] >> 5), 1u << (list[i] & 31));
+  __syncwarp();
+}
+__device__ __forceinline__ int pages_words(const PagedParams& p, int last_pos) { return min(max(last_pos, 0) / PAGE + 1, p.table_pages) / 32 + 1; }
+// the page with `rank` marked ones before it, by a warp (NO_PAGE: there are not so many)
+__device__ __forceinline__ int page_of_rank(const uint32_t* bits, int words, int rank, int lane) {
+  for (int base = 0; base < words; base += 32) {
+    uint32_t w = base + lane < words ? bits[base + lane] : 0;
+    int inc = __popc(w);
+    const int own = inc;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    const uint32_t reach = __ballot_sync(0xffffffffu, inc > rank);
+    if (reach) {
+      const int l = __ffs(reach) - 1;
+      int skip = rank - __shfl_sync(0xffffffffu, inc - own, l);
+      w = __shfl_sync(0xffffffffu, w, l);
+      for (; skip > 0; --skip) w &= w - 1;
+      return (base + l) * 32 + __ffs(w) - 1;
+    }
+    rank -= __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return NO_PAGE;
 }
 
 // An item weighs its key tiles and as much again as its end costs (rows out, the next one's first products), in tiles.
@@ -309,7 +381,7 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   extern __shared__ __align__(8) unsigned char union_smem[];
   const PagedParams& p = tp.a;
   int32_t* item_begin = reinterpret_cast<int32_t*>(union_smem);    // [n_seq + 1]
-  uint16_t* lists = reinterpret_cast<uint16_t*>(item_begin + p.n_seq + 1);
+  unsigned char* lists = union_smem + ((p.n_seq + 1) * 4 + 15) / 16 * 16;      // a warp's lists and bits each; at last the items' sums
   __shared__ int64_t sums[UNION_WARPS];
   __shared__ uint32_t ticket;
   pdl_trigger();
@@ -334,13 +406,20 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   if (x < count) {
     const int item = (int)x / p.Hkv, head = (int)x - item * p.Hkv, seq = last_not_above(item_begin, p.n_seq, item);
     const int n = request_tokens(p, seq, b), kv = request_keys(p, seq), tok = (item - item_begin[seq]) * pair, tokens = min(n - tok, pair);
-    uint16_t* list = lists + warp * pair * p.n_sel;
-    load_lists(p, list, b + tok, tokens, kv - n + tok, head, lane);
-    Merge merge;
-    merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
+    uint16_t* list = reinterpret_cast<uint16_t*>(lists + warp * LIST_BYTES);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(list + LIST_ENTRIES);
     int pages = 0;
-    uint32_t bits_a, bits_b;
-    while (merge.next(bits_a, bits_b) < NO_PAGE) ++pages;
+    if (load_lists(p, list, b + tok, tokens, kv - n + tok, head, lane)) {
+      const int words = pages_words(p, kv - n + tok + tokens - 1);
+      mark_pages(list, tokens * p.n_sel, bits, words, lane);
+      for (int i = lane; i < words; i += 32) pages += __popc(bits[i]);
+      pages = __reduce_add_sync(0xffffffffu, pages);
+    } else {                                                       // a page may come more than once
+      Merge merge;
+      merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
+      uint32_t bits_a, bits_b;
+      while (merge.next(bits_a, bits_b) < NO_PAGE) ++pages;
+    }
     if (lane == 0) tp.item_prefix[x] = max(1, (pages + 1) / 2);
   }
   __threadfence();
@@ -353,26 +432,33 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   if (ticket != gridDim.x - 1) return;
   __threadfence();
   const int each = (count + UNION_THREADS - 1) / UNION_THREADS, x0 = min(tid * each, count), x1 = min(x0 + each, count);
+  const bool fits = (count + 1) * 4 <= (int)(UNION_WARPS * LIST_BYTES);
+  int32_t* prefix = fits ? reinterpret_cast<int32_t*>(lists) : tp.item_prefix;
   mine = 0;
-  for (int i = x0; i < x1; ++i) mine += __ldcg(tp.item_prefix + i) + ITEM_END;
-  at = exclusive<UNION_WARPS>(mine, sums, all);
+#pragma unroll 4
   for (int i = x0; i < x1; ++i) {
     const int v = __ldcg(tp.item_prefix + i) + ITEM_END;
-    tp.item_prefix[i] = (int)min(at, (int64_t)INT32_MAX);
+    if (fits) prefix[i] = v;
+    mine += v;
+  }
+  at = exclusive<UNION_WARPS>(mine, sums, all);
+  for (int i = x0; i < x1; ++i) {
+    const int v = fits ? prefix[i] : __ldcg(tp.item_prefix + i) + ITEM_END;
+    prefix[i] = tp.item_prefix[i] = (int)min(at, (int64_t)INT32_MAX);
     at += v;
   }
-  if (tid == 0) tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
+  if (tid == 0) prefix[count] = tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
   __syncthreads();
   const Shares sh(min(all, (int64_t)INT32_MAX), tp.n_cta);
   for (int c = tid; c < tp.n_cta; c += UNION_THREADS)
     write_run(tp, sh, c, [&](int64_t y) {
       Place r;
-      const int i = last_not_above(tp.item_prefix, count, y), item = i / p.Hkv;
+      const int i = last_not_above(prefix, count, y), item = i / p.Hkv;
       r.head = i - item * p.Hkv;
       r.seq = last_not_above(item_begin, p.n_seq, item);
       r.item = item - item_begin[r.seq];
-      r.begin = tp.item_prefix[i];
-      r.tiles = tp.item_prefix[i + 1] - tp.item_prefix[i] - ITEM_END;
+      r.begin = prefix[i];
+      r.tiles = prefix[i + 1] - prefix[i] - ITEM_END;
       return r;
     });
 }
@@ -449,7 +535,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       mbar_init(bar(P_FULL + 2 * x + 1), BM);
       mbar_init(bar(PV_DONE + x), 1);
       mbar_init(bar(ITEM_FULL + x), 1);
-      mbar_init(bar(ITEM_EMPTY + x), 9);
+      mbar_init(bar(ITEM_EMPTY + x), 10);
     }
     for (int s = 0; s < KV_STAGES; ++s) {
       mbar_init(bar(K_FULL + s), 1);
@@ -475,16 +561,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
   if (warp < 4) {
     reg_dealloc<REGS_SMALL>();
     if (warp == 0) {
-      // ---------------------------------------------------------------- the CTA's run, and the copies
+      // ---------------------------------------------------------------- copies
       const bool leader = elect_one();
-      const int32_t* run = tp.runs + blockIdx.x * RUN_WORDS;
-      int left = run[R_UNITS], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
-      if (left > 0) {
-        seq = run[R_SEQ];
-        head = run[R_HEAD];
-        item = run[R_ITEM];
-        j0 = run[R_J0];
-      }
       uint32_t g = 0, iq[2] = {0, 0};                              // key tiles sent for; items that loaded query tile x
       uint32_t armed_k = 0, armed_v = 0, armed_q = 0, par_k = 0, par_v = 0, par_q = 0;
       const uint32_t q_bytes = (uint32_t)(p.tile_tokens * p.G) * 128;
@@ -492,48 +570,22 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       for (uint32_t it = 0; ok; ++it) {
         const uint32_t slot = it & 1;
         volatile int32_t* ring = ring_base + slot * 16;
-        if (it >= 2) ok = wait_all(bar(ITEM_EMPTY + slot), ((it >> 1) - 1) & 1, abort_flag, p.status, 1 + ITEM_EMPTY);
+        ok = wait_all(bar(ITEM_FULL + slot), (it >> 1) & 1, abort_flag, p.status, 1 + ITEM_FULL);
         if (!ok) break;
-        if (left <= 0) {
-          if (lane == 0) ring[W_KIND] = 0;
-          __syncwarp();
-          if (leader) mbar_arrive(bar(ITEM_FULL + slot));
-          break;
-        }
-        int q_first;
-        const int n_items = tp.item_begin[seq + 1] - tp.item_begin[seq];
-        const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
-        const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
-        const int flat = SPARSE ? (tp.item_begin[seq] + item) * p.Hkv + head : 0;
-        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] - ITEM_END : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
-        const int nq = tokens > p.tile_tokens ? 2 : 1;
-        if (lane == 0) {
-          ring[W_KIND] = 1;
-          ring[W_SEQ] = seq;
-          ring[W_HEAD] = head;
-          ring[W_TOK0] = q_first + tok;
-          ring[W_TOKENS] = tokens;
-          ring[W_POS0] = kv - n + tok;
-          ring[W_KV] = kv;
-          ring[W_J0] = j0;
-          ring[W_NT] = n_tiles;
-          ring[W_TILES] = tiles;
-          ring[W_C0] = it == 0 ? run[R_C0_FIRST] : (int)blockIdx.x;
-          ring[W_C1] = it == 0 ? run[R_C1_FIRST] : run[R_C1_LAST];
-        }
-        __syncwarp();
-        if (leader) mbar_arrive(bar(ITEM_FULL + slot));
-        left -= n_tiles + (j0 + n_tiles == tiles ? ITEM_END : 0);
-        const int32_t* table = p.block_table + seq * p.table_stride;
-        const int n_pages = (kv + PAGE - 1) / PAGE;
+        if (ring_word(ring, W_KIND) == 0) break;
+        const int head = ring_word(ring, W_HEAD), tok0 = ring_word(ring, W_TOK0), tokens = ring_word(ring, W_TOKENS), j0 = ring_word(ring, W_J0),
+                  n_tiles = ring_word(ring, W_NT), nq = tokens > p.tile_tokens ? 2 : 1;
+        const int32_t* table = p.block_table + ring_word(ring, W_SEQ) * p.table_stride;
+        const int n_pages = (ring_word(ring, W_KV) + PAGE - 1) / PAGE;
         int pages = -1;
         Merge merge;
         uint32_t bits[4];
         if (SPARSE) {
-          uint16_t* list = reinterpret_cast<uint16_t*>(sgen + L::SM_LIST);
-          load_lists(p, list, q_first + tok, tokens, kv - n + tok, head, lane);
-          merge.start(list, p.n_sel, tokens, p.tile_tokens, lane);
-          for (int i = 0; i < 2 * j0; ++i) merge.next(bits[0], bits[1]);      // pages of the parts before this one
+          merge.start(reinterpret_cast<const uint16_t*>(sgen + L::SM_LIST) + slot * LIST_ENTRIES, p.n_sel, tokens, p.tile_tokens, lane);
+          const int seek = ring_word(ring, W_SEEK);                // past the pages of the parts before this one
+          if (seek > 0) merge.seek(seek, p.n_sel, p.tile_tokens, lane);
+          if (seek < 0)
+            for (int i = 0; i < 2 * j0; ++i) merge.next(bits[0], bits[1]);
         }
         for (int j = 0; j < n_tiles && ok; ++j, ++g) {
           if (!SPARSE && (j & 15) == 0) {                          // page numbers of 16 tiles at a time, one per lane
@@ -589,7 +641,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
               if (leader) {
                 mbar_expect_tx(bar(Q_FULL + y), NCH * q_bytes);
                 for (int ch = 0; ch < NCH; ++ch)
-                  tma_load_4d(sbase + SM_Q + y * TILE_BYTES + ch * HALF_COLS_BYTES, &maps.q, ch * 64, head * p.G, q_first + tok + y * p.tile_tokens, 0,
+                  tma_load_4d(sbase + SM_Q + y * TILE_BYTES + ch * HALF_COLS_BYTES, &maps.q, ch * 64, head * p.G, tok0 + y * p.tile_tokens, 0,
                               bar(Q_FULL + y));
               }
             }
@@ -603,6 +655,76 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           __syncwarp();
         }
         __syncwarp();
+        if (ok && leader) mbar_arrive(bar(ITEM_EMPTY + slot));
+      }
+      if (!ok || *abort_flag) {
+        // leaving early: every copy under way lands before the CTA exits
+        for (int s = 0; s < KV_STAGES; ++s) {
+          if (armed_k & (1u << s))
+            settle(bar(K_FULL + s), (par_k >> s) & 1);
+          if (armed_v & (1u << s))
+            settle(bar(V_FULL + s), (par_v >> s) & 1);
+        }
+        for (int y = 0; y < 2; ++y)
+          if (armed_q & (1u << y))
+            settle(bar(Q_FULL + y), (par_q >> y) & 1);
+      }
+    } else if (warp == 2) {
+      // ---------------------------------------------------------------- the CTA's run
+      const bool leader = elect_one();
+      const int32_t* run = tp.runs + blockIdx.x * RUN_WORDS;
+      int left = run[R_UNITS], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
+      if (left > 0) {
+        seq = run[R_SEQ];
+        head = run[R_HEAD];
+        item = run[R_ITEM];
+        j0 = run[R_J0];
+      }
+      for (uint32_t it = 0;; ++it) {
+        const uint32_t slot = it & 1;
+        volatile int32_t* ring = ring_base + slot * 16;
+        if (it >= 2 && !wait_all(bar(ITEM_EMPTY + slot), ((it >> 1) - 1) & 1, abort_flag, p.status, 1 + ITEM_EMPTY)) break;
+        if (left <= 0) {
+          if (lane == 0) ring[W_KIND] = 0;
+          __syncwarp();
+          if (leader) mbar_arrive(bar(ITEM_FULL + slot));
+          break;
+        }
+        int q_first;
+        const int n_items = tp.item_begin[seq + 1] - tp.item_begin[seq];
+        const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
+        const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
+        const int flat = SPARSE ? (tp.item_begin[seq] + item) * p.Hkv + head : 0;
+        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] - ITEM_END : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
+        int seek = j0 > 0 ? -1 : 0;
+        if (SPARSE) {
+          uint16_t* list = reinterpret_cast<uint16_t*>(sgen + L::SM_LIST) + slot * LIST_ENTRIES;
+          const bool ascend = load_lists(p, list, q_first + tok, tokens, kv - n + tok, head, lane);
+          if (j0 > 0 && ascend) {                                  // (the run's first item alone)
+            uint32_t* marks = reinterpret_cast<uint32_t*>(sgen + L::SM_LIST + 2 * LIST_ENTRIES * 2);
+            const int words = pages_words(p, kv - n + tok + tokens - 1);
+            mark_pages(list, tokens * p.n_sel, marks, words, lane);
+            seek = page_of_rank(marks, words, 2 * j0, lane);
+          }
+        }
+        if (lane == 0) {
+          ring[W_KIND] = 1;
+          ring[W_SEQ] = seq;
+          ring[W_HEAD] = head;
+          ring[W_TOK0] = q_first + tok;
+          ring[W_TOKENS] = tokens;
+          ring[W_POS0] = kv - n + tok;
+          ring[W_KV] = kv;
+          ring[W_J0] = j0;
+          ring[W_NT] = n_tiles;
+          ring[W_TILES] = tiles;
+          ring[W_C0] = it == 0 ? run[R_C0_FIRST] : (int)blockIdx.x;
+          ring[W_C1] = it == 0 ? run[R_C1_FIRST] : run[R_C1_LAST];
+          ring[W_SEEK] = seek;
+        }
+        __syncwarp();
+        if (leader) mbar_arrive(bar(ITEM_FULL + slot));
+        left -= n_tiles + (j0 + n_tiles == tiles ? ITEM_END : 0);
         // the next item of the run: the request's next tokens, its next head, the next request with tokens
         // (over selected pages the heads come first: the order of the sums)
         j0 = 0;
@@ -624,18 +746,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           item = head = 0;
           do ++seq; while (left > 0 && seq + 1 < p.n_seq && tp.item_begin[seq + 1] == tp.item_begin[seq]);
         }
-      }
-      if (!ok || *abort_flag) {
-        // leaving early: every copy under way lands before the CTA exits
-        for (int s = 0; s < KV_STAGES; ++s) {
-          if (armed_k & (1u << s))
-            settle(bar(K_FULL + s), (par_k >> s) & 1);
-          if (armed_v & (1u << s))
-            settle(bar(V_FULL + s), (par_v >> s) & 1);
-        }
-        for (int y = 0; y < 2; ++y)
-          if (armed_q & (1u << y))
-            settle(bar(Q_FULL + y), (par_q >> y) & 1);
       }
     } else if (warp == 1) {
       // ---------------------------------------------------------------- products
@@ -1059,7 +1169,7 @@ uint64_t plan_bytes(int G, int Hkv, int n_tokens, int n_seq) {
 template <int D, bool F16, bool SPARSE>
 cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
   auto kernel = paged_tc_kernel<D, F16, SPARSE>;
-  constexpr int smem = (int)Layout<D>::SM_ALLOC + (SPARSE ? LIST_ENTRIES * 2 : 0);
+  constexpr int smem = (int)Layout<D>::SM_ALLOC + (SPARSE ? LIST_BYTES + LIST_ENTRIES * 2 : 0);
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (rc != cudaSuccess) return rc;
   // the register hand-over must fit in what the launch allocates, or it would wait for ever
@@ -1068,8 +1178,8 @@ cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_
   if (rc != cudaSuccess) return rc;
   if (attr.numRegs * THREADS < 128 * REGS_SMALL + 256 * REGS_SOFTMAX) return cudaErrorLaunchOutOfResources;
   if (SPARSE) {
-    const int bytes = (tp.a.n_seq + 1) * 4 + UNION_WARPS * 2 * tp.a.tile_tokens * tp.a.n_sel * 2;
-    rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PAGED_MAX_SEQ + 1) * 4 + UNION_WARPS * LIST_ENTRIES * 2);
+    const int bytes = ((tp.a.n_seq + 1) * 4 + 15) / 16 * 16 + UNION_WARPS * LIST_BYTES;
+    rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PAGED_MAX_SEQ + 4) * 4 + UNION_WARPS * LIST_BYTES);
     if (rc != cudaSuccess) return rc;
     const int64_t warps = (int64_t)tp.items * tp.a.Hkv;
     rc = launch_pdl(union_kernel, dim3((unsigned)((warps + UNION_WARPS - 1) / UNION_WARPS)), dim3(UNION_THREADS), bytes, stream, tp);

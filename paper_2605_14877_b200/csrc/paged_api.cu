@@ -173,8 +173,11 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
   rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);
   if (rc != HEATKV_OK) return rc;
   p.causal = causal != 0;
-  // up to 64 rows of the longest request: the warp-level kernel
-  const bool few = (int64_t)p.max_new * p.G <= 64;
+  // Up to 32 rows of the longest request: the warp-level kernel.  24 requests of 2000 tokens: 12 rows 44 us against 56 on the tensor-memory
+  // kernel, 21 rows 33 and 40, 32 rows 82 and 88, 36 rows 64 and 56, 63 rows 55 and 40.  Up to 48 rows, too, where there are fewer units
+  // than SMs (42 rows, 96 units of up to 2660 tokens: 18 and 34 us; 256 units of 1000 tokens: 56 and 46).
+  const int64_t rows = (int64_t)p.max_new * p.G;
+  const bool few = rows <= 32 || (rows <= 48 && p.G <= 16 && (int64_t)p.n_seq * p.Hkv < dev.n_sm);
   return done((few ? launch_paged_small : launch_paged_tc)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 
@@ -212,7 +215,8 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
   p.sel = sel;
   p.n_sel = n_select;
   // tokens of a chunk share the pages that they select: they are taken together
-  const bool chunk = p.max_new >= PAGED_SPARSE_CHUNK && paged_tc_takes_lists(p.G, n_select, p.table_pages);
+  const bool chunk = p.max_new >= PAGED_SPARSE_CHUNK && (int64_t)p.n_tokens * p.Hkv * n_select >= PAGED_SPARSE_PAGES &&
+                     paged_tc_takes_lists(p.G, n_select, p.table_pages);
   return done((chunk ? launch_paged_tc : launch_paged_small)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 

@@ -224,11 +224,16 @@ __device__ __forceinline__ int page_of_rank(const uint32_t* bits, int words, int
 // An item weighs its key tiles and as much again as its end costs (rows out, the next one's first products), in tiles.
 constexpr int ITEM_END = 1;
 
-// The runs: CTA c's is the units bound(c) .. bound(c + 1) - 1 of all.
+// The runs: CTA c's is the units bound(c) .. bound(c + 1) - 1 of all.  A run has at least MIN_SHARE units, and in a call of few and long items
+// more: P parts of an item of T tiles take about 1.35 T / P us, and half a microsecond each to add up, one behind another.
+constexpr int MIN_SHARE = 4;
 struct Shares {
   int64_t all;
-  int grid;                                                        // every share holds a unit
-  __device__ Shares(int64_t all_, int n_cta) : all(all_), grid((int)min((int64_t)n_cta, all_)) {}
+  int grid;
+  __device__ Shares(int64_t all_, int longest, int n_cta) : all(all_) {
+    const int64_t share = max(MIN_SHARE, (int)sqrtf(0.4f * (float)longest));
+    grid = (int)min((int64_t)n_cta, (all + share - 1) / share);
+  }
   __device__ int64_t bound(int c) const { return all * c / grid; }
   // the CTA that holds unit y: the last c with bound(c) <= y
   __device__ int owner(int64_t y) const {
@@ -312,10 +317,12 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
   int32_t* keys = tokens + p.n_seq;                                // [n_seq]
   int32_t* item_prefix = tp.items <= PLAN_ITEMS ? keys + p.n_seq : tp.item_prefix;
   __shared__ int64_t sums[PT / 32];
+  __shared__ int longest;
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pair = 2 * p.tile_tokens;
   int b;
+  if (tid == 0) longest = 1;
   for (int i = tid; i < p.n_seq; i += PT) {
     tokens[i] = request_tokens(p, i, b);
     keys[i] = request_keys(p, i);
@@ -346,7 +353,10 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
       if (base + lane < count) item_prefix[first + base + lane] = before + inc - w;
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
-    if (lane == 0) seq_prefix[i] = before;                         // of one head, for now
+    if (lane == 0) {
+      seq_prefix[i] = before;                                      // of one head, for now
+      if (count > 0) atomicMax(&longest, max(1, (keys[i] + BN - 1) / BN));
+    }
   }
   __syncthreads();
   mine = 0;
@@ -359,7 +369,7 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
   }
   if (tid == 0) seq_prefix[p.n_seq] = all;
   __syncthreads();
-  const Shares sh(all, tp.n_cta);
+  const Shares sh(all, longest, tp.n_cta);
   for (int c = tid; c < tp.n_cta; c += PT)
     write_run(tp, sh, c, [&](int64_t y) {
       Place r;
@@ -384,6 +394,7 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   unsigned char* lists = union_smem + ((p.n_seq + 1) * 4 + 15) / 16 * 16;      // a warp's lists and bits each; at last the items' sums
   __shared__ int64_t sums[UNION_WARPS];
   __shared__ uint32_t ticket;
+  __shared__ int longest;
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, pair = 2 * p.tile_tokens;
@@ -435,12 +446,17 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   const bool fits = (count + 1) * 4 <= (int)(UNION_WARPS * LIST_BYTES);
   int32_t* prefix = fits ? reinterpret_cast<int32_t*>(lists) : tp.item_prefix;
   mine = 0;
+  int most = 1;
+  if (tid == 0) longest = 1;
 #pragma unroll 4
   for (int i = x0; i < x1; ++i) {
     const int v = __ldcg(tp.item_prefix + i) + ITEM_END;
     if (fits) prefix[i] = v;
     mine += v;
+    most = max(most, v);
   }
+  __syncthreads();
+  atomicMax(&longest, most);
   at = exclusive<UNION_WARPS>(mine, sums, all);
   for (int i = x0; i < x1; ++i) {
     const int v = fits ? prefix[i] : __ldcg(tp.item_prefix + i) + ITEM_END;
@@ -449,7 +465,7 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   }
   if (tid == 0) prefix[count] = tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
   __syncthreads();
-  const Shares sh(min(all, (int64_t)INT32_MAX), tp.n_cta);
+  const Shares sh(min(all, (int64_t)INT32_MAX), longest, tp.n_cta);
   for (int c = tid; c < tp.n_cta; c += UNION_THREADS)
     write_run(tp, sh, c, [&](int64_t y) {
       Place r;

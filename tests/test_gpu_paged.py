@@ -429,28 +429,29 @@ def test_sparse_attention_any_group(hk, G):
 @pytest.mark.parametrize("max_new", [1, 100])
 def test_sparse_attention_of_chunks_over_random_lists(hk, G, d, dtype, max_new):
     """Lists of random lengths in random order with gaps, for chunks that end inside a tile; both kernels (max_new picks one)."""
-    lens = [(40, 700), (1, 65), (0, 0), (67, 67), (16, 1000)]
+    lens = [(90, 700), (1, 65), (0, 0), (67, 67), (40, 1000)]
+    Hkv, n_select = 4, 32                                  # as many lists as it takes for them to be merged
     rng, g = np.random.default_rng(G), torch.Generator("cuda").manual_seed(G)
     dt = DTYPES[dtype]
-    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, d, dt, spare=2)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, Hkv, d, dt, spare=2)
     b.max_new = max_new
-    sel = np.full((b.n_tokens, 2, 7), -1)
+    sel = np.full((b.n_tokens, Hkv, n_select), -1)
     chosen = []
     for i, (n, kv) in enumerate(lens):
-        mask = np.zeros((2, n, -(-kv // PAGE)), dtype=bool)
+        mask = np.zeros((Hkv, n, -(-kv // PAGE)), dtype=bool)
         for t in range(n):
-            for h in range(2):
+            for h in range(Hkv):
                 pages = rng.permutation((kv - n + t) // PAGE + 1)[: rng.integers(0, 7)]
-                sel[q_begin[i] + t, h, rng.permutation(7)[: len(pages)]] = pages
+                sel[q_begin[i] + t, h, rng.permutation(n_select)[: len(pages)]] = pages
                 mask[h, t, pages] = True
         chosen.append(mask)
-    q = torch.empty(b.n_tokens, 2 * G, d, dtype=dt, device="cuda").normal_(generator=g)
-    out, lse = torch.full_like(q, 7.0), torch.full((b.n_tokens, 2 * G), 7.0, device="cuda")
-    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 2 * G), dtype=torch.uint8, device="cuda")
+    q = torch.empty(b.n_tokens, Hkv * G, d, dtype=dt, device="cuda").normal_(generator=g)
+    out, lse = torch.full_like(q, 7.0), torch.full((b.n_tokens, Hkv * G), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, Hkv * G), dtype=torch.uint8, device="cuda")
     for _ in range(2):
         hk.heatkv_paged_sparse_attention(pool, b, q, _i32(sel), out, lse, ws)
     assert hk.heatkv_paged_status(ws) == 0
-    _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(d), dtype, chosen)
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype, chosen)
     assert (out[q_begin[-1]:] == 7.0).all() and (lse[q_begin[-1]:] == 7.0).all()
 
 

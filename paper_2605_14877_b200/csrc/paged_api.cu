@@ -26,7 +26,7 @@ bool paged_device(PagedDevice* out) {
       return false;
     encode.store(fn, std::memory_order_relaxed);
   }
-  out->n_sm = n;
+  out->n_sm = n < 240 ? n : 240;                       // (the workspace has arrival counters for so many)
   out->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   return true;
 }

@@ -5,7 +5,8 @@
 // requests: a unit of more than S pages is cut into equal pieces of at most S, S such that every CTA takes about PER_CTA pieces, and CTAs
 // take pieces from a counter until none is left (dealt out beforehand in equal shares, the SMs with the longest way to memory decided when
 // a call ended: SMs' active cycles differed by 15 %).  Pieces leave partial results (unnormalised O, maximum, sum) in the workspace, which a
-// second small kernel adds up in page order, a warp per row; neither the pieces nor that order depends on which CTA took what.
+// second small kernel adds up in page order; neither the pieces nor that order depends on which CTA took what.  (Added up by the CTA that
+// leaves a unit's last piece, with a fence and a counter behind every piece, a decode of 64 requests took 92 us instead of 71.)
 //
 // One warp takes pieces and looks up what they are, one ahead; the next sends for Q, K and V (TMA, K and V of one page per stage),
 // so that what a piece's beginning has to read (counter, lengths, table) is read while the pages before it arrive.  The others
@@ -31,13 +32,14 @@ constexpr float MOVE = 8.f;                    // a reference moves when a maxim
 // Pieces of fewer pages cost more to add up than they save: 64 requests of 500 tokens, 8 kv heads, take 34.3 us with pieces of 4 pages and
 // 30.4 of 8; where pieces of 8 would leave CTAs without one, 4 are better (24 requests of drafted tokens 26.9 us with 8, 24.8 with 4).
 constexpr int MIN_CHUNK = 4, FULL_CHUNK = 8;
+// (and units of up to FULL_CHUNK pages stay whole: a short request then needs no second kernel, 7.3 us instead of 10)
 constexpr int PER_CTA = 4;                     // pieces a CTA takes (64 requests of 1360 tokens: 70 us with 4, 73 with 6, 76 with 12)
 constexpr int MERGE_WARPS = 8;
 
 struct SmallParams {
   PagedParams a;
   uint32_t* counter;                           // pieces taken beyond every CTA's first; zero between launches
-  int32_t* n_slots;                            // partial results of this call
+  int32_t* n_slots;                            // partial results of this call, and most parts of a unit
   int4* cuts;                                  // [slot] {first token, rows, kv head, pieces} at a unit's first piece, else no rows
   int32_t stages;
 };
@@ -94,6 +96,8 @@ __device__ __forceinline__ void meet(int group) { asm volatile("bar.sync %0, 128
 // A partial result: rows of O, then their maxima and sums; whole 16-byte words.
 __host__ __device__ constexpr int64_t slot_floats(int rows, int d) { return ((int64_t)rows * (d + 2) + 3) & ~(int64_t)3; }
 
+__device__ __forceinline__ int pieces_of(int pages, int chunk) { return pages <= FULL_CHUNK ? pages > 0 : (pages + chunk - 1) / chunk; }
+
 enum RingWord : int { W_KIND = 0, W_HEAD, W_TOK0, W_ROWS, W_TILES, W_KV, W_POS0, W_SLOT, W_PIECE, W_PIECES, W_SEQ, W_TILE0, RING_WORDS = 12 };
 constexpr int RING = 2;                        // the piece at work and the next: more would be taken from CTAs that run out
 
@@ -104,6 +108,94 @@ __device__ __forceinline__ int find_last(const int32_t* a, int n, int x) {     /
     if (a[mid] <= x) lo = mid; else hi = mid - 1;
   }
   return lo;
+}
+
+// A part of a row's sum: columns lane * D / 32 .., relative to the maximum `top`.
+template <int D>
+struct RowSum {
+  static constexpr int N = D / 32;
+  float acc[N], top, l;
+  __device__ void clear() {
+    top = NO_MAX;
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = 0.f;
+  }
+};
+// A row's parts in the workspace (`first`: the unit's first slot).
+template <int D>
+struct Parts {
+  static constexpr int N = D / 32;
+  const float* first;
+  int64_t pitch;
+  int slot_rows, row, lane;
+  struct Columns {
+    float v[N];
+  };
+  __device__ float2 stats(int i) const { return __ldcg(reinterpret_cast<const float2*>(first + i * pitch + slot_rows * D) + row); }
+  __device__ Columns columns(int i) const {
+    Columns c;
+    const float* src = first + i * pitch + row * D + lane * N;
+    if (N == 4) {
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
+      c.v[0] = y.x, c.v[1] = y.y, c.v[N - 2] = y.z, c.v[N - 1] = y.w;
+    } else {
+      const float2 y = __ldcg(reinterpret_cast<const float2*>(src));
+      c.v[0] = y.x, c.v[1] = y.y;
+    }
+    return c;
+  }
+};
+constexpr int AHEAD = 4;
+// Parts begin .. end - 1, by a warp.  The first ones' columns come with the maxima and sums, not behind them.
+template <int D>
+__device__ __forceinline__ RowSum<D> sum_parts(const Parts<D>& p, int begin, int end) {
+  constexpr int N = D / 32;
+  RowSum<D> r;
+  r.clear();
+  const int n = end - begin;
+  typename Parts<D>::Columns ahead[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) ahead[i] = p.columns(begin + min(i, n - 1));
+  float2 ml = make_float2(NO_MAX, 0.f);                            // of part begin + lane
+  if (p.lane < n) ml = p.stats(begin + p.lane);
+  r.top = ml.x;
+  for (int i = p.lane + 32; i < n; i += 32) r.top = fmaxf(r.top, p.stats(begin + i).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+  for (int base = 0; base < n; base += 32) {
+    if (base > 0) ml = base + p.lane < n ? p.stats(begin + base + p.lane) : make_float2(NO_MAX, 0.f);
+    const float w = exp2f(ml.x - r.top), wl = ml.y * w;
+    const int m = min(32, n - base);
+    auto add = [&](int i, const typename Parts<D>::Columns& c) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      r.l += __shfl_sync(0xffffffffu, wl, i);
+#pragma unroll
+      for (int k = 0; k < N; ++k) r.acc[k] = fmaf(c.v[k], wi, r.acc[k]);
+    };
+    int i = 0;
+    if (base == 0) {
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (k < m) add(k, ahead[k]);
+      i = min(AHEAD, m);
+    }
+#pragma unroll 4
+    for (; i < m; ++i) add(i, p.columns(begin + base + i));
+  }
+  return r;
+}
+template <int D, bool F16>
+__device__ __forceinline__ void put_row(const PagedParams& p, const RowSum<D>& r, int tok, int hd, int lane) {
+  constexpr int N = D / 32;
+  const float inv = r.l > 0.f ? 1.f / r.l : 0.f;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head + lane * N);
+  if (N == 4) {
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack16<F16>(r.acc[0] * inv, r.acc[1] * inv), pack16<F16>(r.acc[N - 2] * inv, r.acc[N - 1] * inv));
+  } else {
+    *dst = pack16<F16>(r.acc[0] * inv, r.acc[1] * inv);
+  }
+  if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = r.l > 0.f ? (r.top + log2f(r.l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D, int MT, int GROUPS, bool F16, bool SPARSE>
@@ -126,6 +218,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   __shared__ int32_t page_of[MAX_STAGES];                                       // place in the request's table row of the page in a stage
   __shared__ uint32_t abort_word, leave_word[GROUPS];
   __shared__ int64_t sums[WARPS + 2];
+  __shared__ int longest;
   volatile uint32_t* abort_flag = &abort_word;
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int s) { return bar0 + s * 16; };
@@ -160,9 +253,12 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   if (SPARSE) {
     total = (int64_t)p.n_tokens * p.Hkv * p.n_sel;
     chunk = (int)max((int64_t)(total < (int64_t)gridDim.x * FULL_CHUNK ? MIN_CHUNK : FULL_CHUNK), (total + share - 1) / share);
-    const int pieces = (p.n_sel + chunk - 1) / chunk;
+    const int pieces = pieces_of(p.n_sel, chunk);
     n_chunks = (int)min((int64_t)p.n_tokens * p.Hkv * pieces, (int64_t)INT_MAX);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *sp.n_slots = pieces > 1 ? n_chunks : 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      sp.n_slots[0] = pieces > 1 ? n_chunks : 0;
+      sp.n_slots[1] = pieces;
+    }
     __syncthreads();
   } else {
     const int per = (p.n_seq + THREADS - 1) / THREADS, i0 = min((int)threadIdx.x * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
@@ -187,6 +283,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       return before + inc - v;
     };
     int64_t sum = 0;
+    int most = 0;                                                  // pages of the longest request
     for (int i = i0; i < i1; ++i) {
       const int b = max(p.q_begin[i], 0), n = max(min(p.q_begin[i + 1], p.n_tokens) - b, 0);
       const int kv = min(max(p.kv_len[i], 0), p.table_pages * PAGE);
@@ -194,20 +291,23 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       chunk_begin[i] = units;
       slot_begin[i] = tiles;
       sum += (int64_t)tiles * units;
+      if (units > 0) most = max(most, tiles);
     }
+    if (threadIdx.x == 0) longest = 0;
     scan(sum, total);
+    if (blockIdx.x == 0) atomicMax(&longest, most);                // (read by this CTA's first thread behind the next sum)
     chunk = (int)max((int64_t)(total < (int64_t)gridDim.x * FULL_CHUNK ? MIN_CHUNK : FULL_CHUNK), (total + share - 1) / share);
     // (both in one sum: pieces in the low 40 bits, partial results, of which there are few, above)
     constexpr int64_t LOW = ((int64_t)1 << 40) - 1;
     int64_t mine = 0, all;
     for (int i = i0; i < i1; ++i) {
-      const int pieces = (slot_begin[i] + chunk - 1) / chunk;
+      const int pieces = pieces_of(slot_begin[i], chunk);
       const int64_t c = (int64_t)chunk_begin[i] * pieces;
       mine += c + (pieces > 1 ? c << 40 : 0);
     }
     int64_t at = scan(mine, all);
     for (int i = i0; i < i1; ++i) {
-      const int pieces = (slot_begin[i] + chunk - 1) / chunk;
+      const int pieces = pieces_of(slot_begin[i], chunk);
       const int64_t c = (int64_t)chunk_begin[i] * pieces;
       chunk_begin[i] = (int)min((int64_t)(at & LOW), (int64_t)INT_MAX);
       slot_begin[i] = (int)(at >> 40);
@@ -216,7 +316,10 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
     n_chunks = (int)min((int64_t)(all & LOW), (int64_t)INT_MAX);
     if (threadIdx.x == 0) {
       chunk_begin[p.n_seq] = n_chunks;
-      if (blockIdx.x == 0) *sp.n_slots = (int)(all >> 40);
+      if (blockIdx.x == 0) {
+        sp.n_slots[0] = (int)(all >> 40);
+        sp.n_slots[1] = pieces_of(longest, chunk);
+      }
     }
     __syncthreads();
     for (int i = blockIdx.x; i < p.n_seq; i += gridDim.x) {
@@ -273,7 +376,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       const uint32_t next = ask();
       int seq, head, tok0, tokens, kv, pos0, tiles, piece, pieces, out_slot;
       if (SPARSE) {
-        pieces = (p.n_sel + chunk - 1) / chunk;
+        pieces = pieces_of(p.n_sel, chunk);
         const int unit = idx / pieces;
         piece = idx - unit * pieces;
         out_slot = pieces > 1 ? idx : -1;
@@ -290,7 +393,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
         const int b = max(p.q_begin[seq], 0), n = max(min(p.q_begin[seq + 1], p.n_tokens) - b, 0);
         kv = min(max(p.kv_len[seq], 0), p.table_pages * PAGE);
         tiles = (kv + PAGE - 1) / PAGE;
-        pieces = (tiles + chunk - 1) / chunk;
+        pieces = pieces_of(tiles, chunk);
         const int local = idx - chunk_begin[seq], unit = local / pieces;
         piece = local - unit * pieces;
         out_slot = pieces > 1 ? slot_begin[seq] + local : -1;
@@ -629,78 +732,57 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   }
 }
 
-// Adds up the parts of the units that were cut, a warp per row, in page order.
+// Adds up the parts of the units that were cut, in page order: a warp per row, or, where some unit has many, a CTA.
+constexpr int MANY_PARTS = 16;
 template <int D, bool F16>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ SmallParams sp) {
   const PagedParams& p = sp.a;
-  constexpr int N = D / 32;                                        // columns of a lane
+  constexpr int N = D / 32;
+  __shared__ float sums[MERGE_WARPS][D], tops[MERGE_WARPS], ls[MERGE_WARPS];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, slot_rows = p.tile_tokens * p.G;
-  const int64_t pairs = (int64_t)__ldcg(sp.n_slots) * slot_rows, pitch = slot_floats(slot_rows, D);
-  for (int64_t x = (int64_t)blockIdx.x * MERGE_WARPS + (threadIdx.x >> 5); x < pairs; x += (int64_t)gridDim.x * MERGE_WARPS) {
-    const int s0 = (int)(x / slot_rows), row = (int)(x - (int64_t)s0 * slot_rows);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot_rows = p.tile_tokens * p.G;
+  const int2 slots = __ldcg(reinterpret_cast<const int2*>(sp.n_slots));        // partial results, most parts of a unit
+  const int pairs = slots.x * slot_rows;                           // (slots and rows are few)
+  Parts<D> parts;
+  parts.pitch = slot_floats(slot_rows, D);
+  parts.slot_rows = slot_rows;
+  parts.lane = lane;
+  const bool many = slots.y > MANY_PARTS;
+  for (int x = many ? blockIdx.x : blockIdx.x * MERGE_WARPS + warp; x < pairs; x += gridDim.x * (many ? 1 : MERGE_WARPS)) {
+    const int s0 = x / slot_rows;
+    parts.row = x - s0 * slot_rows;
     const int4 cut = __ldcg(sp.cuts + s0);
-    if (row >= cut.y) continue;
-    const int n = cut.w;
-    const float* first = p.partials + s0 * pitch;
-    auto stats = [&](int i) { return __ldcg(reinterpret_cast<const float2*>(first + i * pitch + slot_rows * D) + row); };
-    struct Columns {
-      float v[N];
-    };
-    auto columns = [&](int i) {
-      Columns c;
-      const float* src = first + i * pitch + row * D + lane * N;
-      if (N == 4) {
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
-        c.v[0] = y.x, c.v[1] = y.y, c.v[N - 2] = y.z, c.v[N - 1] = y.w;
-      } else {
-        const float2 y = __ldcg(reinterpret_cast<const float2*>(src));
-        c.v[0] = y.x, c.v[1] = y.y;
-      }
-      return c;
-    };
-    // the first parts' columns come with the maxima and sums, not behind them
-    constexpr int AHEAD = 4;
-    Columns ahead[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) ahead[i] = columns(min(i, n - 1));
-    float2 ml = make_float2(NO_MAX, 0.f);                          // of part `lane`
-    if (lane < n) ml = stats(lane);
-    float top = ml.x;
-    for (int i = lane + 32; i < n; i += 32) top = fmaxf(top, stats(i).x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float acc[N] = {}, l = 0.f;
-    for (int base = 0; base < n; base += 32) {
-      if (base > 0) ml = base + lane < n ? stats(base + lane) : make_float2(NO_MAX, 0.f);
-      const float w = exp2f(ml.x - top), wl = ml.y * w;
-      const int m = min(32, n - base);
-      auto add = [&](int i, const Columns& c) {
-        const float wi = __shfl_sync(0xffffffffu, w, i);
-        l += __shfl_sync(0xffffffffu, wl, i);
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] = fmaf(c.v[k], wi, acc[k]);
-      };
-      int i = 0;
-      if (base == 0) {
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-          if (k < m) add(k, ahead[k]);
-        i = min(AHEAD, m);
-      }
-#pragma unroll 4
-      for (; i < m; ++i) add(i, columns(base + i));
+    if (parts.row >= cut.y) continue;
+    parts.first = p.partials + s0 * parts.pitch;
+    const int tok = cut.x + parts.row / p.G, hd = cut.z * p.G + parts.row % p.G;
+    if (!many) {
+      put_row<D, F16>(p, sum_parts<D>(parts, 0, cut.w), tok, hd, lane);
+      continue;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const int tok = cut.x + row / p.G, hd = cut.z * p.G + row % p.G;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head + lane * N);
-    if (N == 4) {
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack16<F16>(acc[0] * inv, acc[1] * inv), pack16<F16>(acc[N - 2] * inv, acc[N - 1] * inv));
-    } else {
-      *dst = pack16<F16>(acc[0] * inv, acc[1] * inv);
+    const int begin = cut.w * warp / MERGE_WARPS, end = cut.w * (warp + 1) / MERGE_WARPS;
+    RowSum<D> r;
+    r.clear();
+    if (begin < end) r = sum_parts<D>(parts, begin, end);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums[warp][lane * N + i] = r.acc[i];
+    if (lane == 0) {
+      tops[warp] = r.top;
+      ls[warp] = r.l;
     }
-    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = l > 0.f ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    __syncthreads();
+    if (warp == 0) {
+      r.clear();
+      for (int i = 0; i < MERGE_WARPS; ++i) r.top = fmaxf(r.top, tops[i]);
+      for (int i = 0; i < MERGE_WARPS; ++i) {
+        const float w = exp2f(tops[i] - r.top);
+        r.l = fmaf(ls[i], w, r.l);
+#pragma unroll
+        for (int j = 0; j < N; ++j) r.acc[j] = fmaf(sums[i][lane * N + j], w, r.acc[j]);
+      }
+      put_row<D, F16>(p, r, tok, hd, lane);
+    }
+    __syncthreads();
   }
 }
 
@@ -727,8 +809,8 @@ cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaSt
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (rc != cudaSuccess) return rc;
   rc = launch_pdl(kernel, dim3(n_sm * L::CTAS), dim3(L::THREADS), smem, stream, sp, maps);
-  // nothing can have been cut where no request has more pages than the shortest piece
-  if (rc != cudaSuccess || (SPARSE ? p.n_sel : p.table_pages) <= MIN_CHUNK) return rc;
+  // nothing can have been cut where no unit has more pages
+  if (rc != cudaSuccess || (SPARSE ? p.n_sel : p.table_pages) <= FULL_CHUNK) return rc;
   return launch_pdl(paged_merge_kernel<D, F16>, dim3(8 * n_sm), dim3(MERGE_WARPS * 32), 0, stream, sp);
 }
 template <int D, bool F16, bool SPARSE>

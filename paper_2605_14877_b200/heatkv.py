@@ -116,6 +116,26 @@ def _expect(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tens
     return x
 
 
+# The checks of the small calls, which take no longer on the GPU than in Python: no tuple or generator is built for an argument that
+# passes (a table call 13.7 -> 8 us).
+_I32 = torch.int32
+
+
+def _vector(x: torch.Tensor, n: int, what: str) -> int:
+    """Address of a contiguous int32 vector of n entries."""
+    if x.dtype is not _I32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous int32 vector of {n}, got {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _table(x: torch.Tensor, n: int):
+    """(address, row stride, columns) of a block table of n rows."""
+    if x.dtype is not _I32 or x.dim() != 2 or x.size(0) != n or x.stride(1) != 1:
+        raise ValueError(f"block_table: expected int32 [{n}, pages] with contiguous rows, got {x.dtype} {tuple(x.shape)}")
+    pages = x.size(1)
+    return x.data_ptr(), (x.stride(0) if n > 1 else pages), pages
+
+
 def _packed(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tensor:
     if not _expect(x, dtype, shape, what).is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor")
@@ -551,54 +571,38 @@ def heatkv_device_status(ctx: int, stream=None) -> int:
 def heatkv_paged_tables(new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map,
                         positions=None, stream=None) -> None:
     """Pages, slots and positions of a step's new tokens, from the requests' lengths (int32 tensors on the device)."""
-    n = new_tokens.shape[0]
-    i32 = torch.int32
-    _packed(new_tokens, i32, (n,), "new_tokens")
-    _packed(past_tokens, i32, (n,), "past_tokens")
-    _packed(free_pages, i32, (None,), "free_pages")
-    _packed(state, i32, (4,), "state")
-    _packed(state_out, i32, (4,), "state_out")
-    _packed(q_begin, i32, (n + 1,), "q_begin")
-    _packed(kv_len, i32, (n,), "kv_len")
-    _packed(slot_map, i32, (None,), "slot_map")
-    if _expect(block_table, i32, (n, None), "block_table").stride(1) != 1:
-        raise ValueError("block_table: expected contiguous rows")
-    if positions is not None:
-        _packed(positions, i32, slot_map.shape, "positions")
-    pages = block_table.shape[1]
-    _check(_lib.heatkv_paged_tables(new_tokens.data_ptr(), past_tokens.data_ptr(), n, free_pages.data_ptr(), free_pages.shape[0],
-                                    state.data_ptr(), state_out.data_ptr(), block_table.data_ptr(), block_table.stride(0) if n > 1 else pages,
-                                    pages, q_begin.data_ptr(), kv_len.data_ptr(), slot_map.data_ptr(), _ptr(positions), slot_map.shape[0],
-                                    _stream(stream)), "heatkv_paged_tables")
+    n, n_pages, n_tokens = new_tokens.numel(), free_pages.numel(), slot_map.numel()
+    table, stride, pages = _table(block_table, n)
+    rc = _lib.heatkv_paged_tables(_vector(new_tokens, n, "new_tokens"), _vector(past_tokens, n, "past_tokens"), n,
+                                  _vector(free_pages, n_pages, "free_pages"), n_pages, _vector(state, 4, "state"),
+                                  _vector(state_out, 4, "state_out"), table, stride, pages, _vector(q_begin, n + 1, "q_begin"),
+                                  _vector(kv_len, n, "kv_len"), _vector(slot_map, n_tokens, "slot_map"),
+                                  None if positions is None else _vector(positions, n_tokens, "positions"), n_tokens, _stream(stream))
+    if rc:
+        _check(rc, "heatkv_paged_tables")
 
 
 def heatkv_paged_release(kv_len, keep_len, block_table, free_pages, state, state_out, stream=None) -> None:
     """Gives back the pages that hold only tokens from keep_len on."""
-    n, i32 = kv_len.shape[0], torch.int32
-    _packed(kv_len, i32, (n,), "kv_len")
-    _packed(keep_len, i32, (n,), "keep_len")
-    _packed(free_pages, i32, (None,), "free_pages")
-    _packed(state, i32, (4,), "state")
-    _packed(state_out, i32, (4,), "state_out")
-    if _expect(block_table, i32, (n, None), "block_table").stride(1) != 1:
-        raise ValueError("block_table: expected contiguous rows")
-    pages = block_table.shape[1]
-    _check(_lib.heatkv_paged_release(kv_len.data_ptr(), keep_len.data_ptr(), n, block_table.data_ptr(),
-                                     block_table.stride(0) if n > 1 else pages, pages, free_pages.data_ptr(), free_pages.shape[0],
-                                     state.data_ptr(), state_out.data_ptr(), _stream(stream)), "heatkv_paged_release")
+    n, n_pages = kv_len.numel(), free_pages.numel()
+    table, stride, pages = _table(block_table, n)
+    _check(_lib.heatkv_paged_release(_vector(kv_len, n, "kv_len"), _vector(keep_len, n, "keep_len"), n, table, stride, pages,
+                                     _vector(free_pages, n_pages, "free_pages"), n_pages, _vector(state, 4, "state"),
+                                     _vector(state_out, 4, "state_out"), _stream(stream)), "heatkv_paged_release")
 
 
 def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> None:
     """K and V rows [n_tokens, n_kv_heads, d] (equal strides, d contiguous) to their slots, and the summaries of pages that fill up."""
-    shape = (slot_map.shape[0], pool.n_kv_heads, pool.d)
-    _packed(slot_map, torch.int32, (None,), "slot_map")
-    _expect(k_new, pool.torch_dtype, shape, "k_new")
-    _expect(v_new, pool.torch_dtype, shape, "v_new")
-    tok, head, one = k_new.stride()
-    if v_new.stride() != (tok, head, one) or one != 1:
+    n = slot_map.numel()
+    slots = _vector(slot_map, n, "slot_map")
+    _rows(k_new, pool, n, pool.n_kv_heads, "k_new")
+    _rows(v_new, pool, n, pool.n_kv_heads, "v_new")
+    strides = k_new.stride()
+    if v_new.stride() != strides or strides[2] != 1:
         raise ValueError("k_new, v_new: expected equal strides, the last dimension contiguous")
-    _check(_lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), tok, head, slot_map.data_ptr(), shape[0],
-                                   _stream(stream)), "heatkv_paged_store")
+    rc = _lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], slots, n, _stream(stream))
+    if rc:
+        _check(rc, "heatkv_paged_store")
 
 
 def heatkv_paged_workspace_bytes(pool: PagedPool, batch: PagedBatch, n_heads: int) -> int:
@@ -608,52 +612,69 @@ def heatkv_paged_workspace_bytes(pool: PagedPool, batch: PagedBatch, n_heads: in
     return out.value
 
 
+def _rows(x, pool, tokens, heads, what):
+    """Checks [tokens, heads, d] activations (heads None: any number)."""
+    if x.dtype is not pool.torch_dtype or x.dim() != 3 or x.size(0) != tokens or x.size(2) != pool.d or (heads is not None and x.size(1) != heads):
+        raise ValueError(f"{what}: expected {pool.torch_dtype} [{tokens}, {'heads' if heads is None else heads}, {pool.d}], got {x.dtype} {tuple(x.shape)}")
+
+
 def _token_strides(pool, batch, q, out):
     """Strides of q and out, None where both are packed."""
-    shape = (batch.n_tokens, None, pool.d)
-    _expect(q, pool.torch_dtype, shape, "q")
-    sq = q.stride()
-    if sq[2] != 1:
-        raise ValueError("q: expected the last dimension contiguous")
-    if out is None:
-        return None if q.is_contiguous() else C.byref(TokenStrides(sq[0], sq[1], sq[0], sq[1]))
-    _expect(out, pool.torch_dtype, q.shape, "out")
-    so = out.stride()
-    if so[2] != 1:
-        raise ValueError("out: expected the last dimension contiguous")
-    return None if q.is_contiguous() and out.is_contiguous() else C.byref(TokenStrides(sq[0], sq[1], so[0], so[1]))
+    tokens = batch.n_tokens
+    _rows(q, pool, tokens, None, "q")
+    if out is not None:
+        _rows(out, pool, tokens, q.size(1), "out")
+    if q.is_contiguous() and (out is None or out.is_contiguous()):
+        return None
+    sq, so = q.stride(), (q if out is None else out).stride()
+    if sq[2] != 1 or so[2] != 1:
+        raise ValueError("q, out: expected the last dimension contiguous")
+    return C.byref(TokenStrides(sq[0], sq[1], so[0], so[1]))
+
+
+def _lse(lse, q):
+    if lse is None:
+        return None
+    if lse.dtype is not torch.float32 or lse.dim() != 2 or lse.size(0) != q.size(0) or lse.size(1) != q.size(1) or not lse.is_contiguous():
+        raise ValueError(f"lse: expected contiguous float32 [{q.size(0)}, {q.size(1)}], got {lse.dtype} {tuple(lse.shape)}")
+    return lse.data_ptr()
+
+
+def _lists(sel, pool, batch):
+    if sel.dtype is not _I32 or sel.dim() != 3 or sel.size(0) != batch.n_tokens or sel.size(1) != pool.n_kv_heads or not sel.is_contiguous():
+        raise ValueError(f"sel: expected contiguous int32 [{batch.n_tokens}, {pool.n_kv_heads}, n_select], got {sel.dtype} {tuple(sel.shape)}")
+    return sel.data_ptr(), sel.size(2)
 
 
 def heatkv_paged_attention(pool: PagedPool, batch: PagedBatch, q, out, lse, workspace, causal: bool = True, sm_scale: float = 0.0,
                            stream=None) -> None:
     """out [n_tokens, n_heads, d] and (unless None) lse [n_tokens, n_heads] of the new tokens' attention over their requests' pages."""
     st = _token_strides(pool, batch, q, out)
-    if lse is not None:
-        _packed(lse, torch.float32, q.shape[:2], "lse")
-    _check(_lib.heatkv_paged_attention(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _ptr(lse),
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)),
-           "heatkv_paged_attention")
+    rc = _lib.heatkv_paged_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _lse(lse, q),
+                                     workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if rc:
+        _check(rc, "heatkv_paged_attention")
 
 
 def heatkv_paged_select(pool: PagedPool, batch: PagedBatch, q, sel, sink: int, local: int, stream=None) -> None:
     """sel [n_tokens, n_kv_heads, n_select]: the pages each new token attends to (places in its request's table row, ascending, -1
     after the last)."""
     st = _token_strides(pool, batch, q, None)
-    _packed(sel, torch.int32, (batch.n_tokens, pool.n_kv_heads, None), "sel")
-    _check(_lib.heatkv_paged_select(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, sink, local, sel.shape[2], sel.data_ptr(),
-                                    _stream(stream)), "heatkv_paged_select")
+    lists, n_select = _lists(sel, pool, batch)
+    rc = _lib.heatkv_paged_select(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, sink, local, n_select, lists, _stream(stream))
+    if rc:
+        _check(rc, "heatkv_paged_select")
 
 
 def heatkv_paged_sparse_attention(pool: PagedPool, batch: PagedBatch, q, sel, out, lse, workspace, sm_scale: float = 0.0,
                                   stream=None) -> None:
     """heatkv_paged_attention (causal) over the pages that sel lists for each token."""
     st = _token_strides(pool, batch, q, out)
-    _packed(sel, torch.int32, (batch.n_tokens, pool.n_kv_heads, None), "sel")
-    if lse is not None:
-        _packed(lse, torch.float32, q.shape[:2], "lse")
-    _check(_lib.heatkv_paged_sparse_attention(pool.addr, batch.addr, q.shape[1], q.data_ptr(), st, sel.data_ptr(), sel.shape[2], sm_scale,
-                                              out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                              _stream(stream)), "heatkv_paged_sparse_attention")
+    lists, n_select = _lists(sel, pool, batch)
+    rc = _lib.heatkv_paged_sparse_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, lists, n_select, sm_scale, out.data_ptr(),
+                                            _lse(lse, q), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if rc:
+        _check(rc, "heatkv_paged_sparse_attention")
 
 
 def heatkv_paged_status(workspace, stream=None) -> int:

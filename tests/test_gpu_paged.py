@@ -237,7 +237,7 @@ def _check(out, lse, q, k, v, lens, table, q_begin, Hkv, causal, scale, dtype, c
                     gl = lse[rows, h * G + g]
                     assert np.array_equal(np.isinf(gl), np.isinf(l))
                     fin = np.isfinite(l)
-                    assert (np.abs(gl - l)[fin] <= (off + 2.0**-22 * np.abs(l))[fin]).all(), (i, h, g)
+                    assert (np.abs(gl[fin] - l[fin]) <= (off + 2.0**-22 * np.abs(l))[fin]).all(), (i, h, g)
 
 
 LENS = {                                                   # (new tokens, tokens in all) per request
@@ -498,3 +498,66 @@ def test_sparse_attention_over_lists_of_any_kind(hk):
     hk.heatkv_paged_sparse_attention(pool, b, q, _i32(sel), out, lse, ws)
     _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(128), "bf16", chosen)
     assert (out[1, 4:] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ all together
+
+@pytest.mark.parametrize("pages", [0, 4])
+def test_serving_loop(hk, pages):
+    """Prompts of three requests, answers token by token, drafted tokens of which some are turned down, a request that ends and one that
+    takes its place and its pages: every step of two layers against attention over the tokens that each request really has."""
+    from paper_2605_14877_b200.paged import PagedCache
+    H, Hkv, d, layers = 8, 2, 64, 2
+    cache = PagedCache(layers, H, Hkv, d, n_pages=26, rows=3, max_pages=16, summaries=pages > 0)
+    g = torch.Generator("cuda").manual_seed(4)
+    kept = [[[np.zeros((0, Hkv, d))] * 2 for _ in range(layers)] for _ in range(3)]          # per request and layer: K, V rows
+    # (new tokens, tokens kept afterwards (None: all))
+    plan = [([300, 70, 0], None), ([1, 1, 0], None), ([1, 1, 640], None), ([4, 5, 1], (303, 73, 641)), ([1, 1, 1], None), ([0, 0, 1], (304, 0, 642)),
+            ([1, 500, 1], None), ([1, 1, 1], None)]
+    for new, keep in plan:
+        step = cache.begin(new)
+        lens = [len(kept[i][0][0]) for i in range(3)]
+        begin = np.concatenate([[0], np.cumsum(new)])
+        want_pos = np.concatenate([np.arange(lens[i], lens[i] + new[i]) for i in range(3)])
+        assert np.array_equal(step.positions.cpu().numpy(), want_pos)
+        assert cache.state.tolist()[2] == 0
+        for layer in range(layers):
+            T = sum(new)
+            q = torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+            kv = torch.empty(2, T, Hkv, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+            out, lse = torch.empty_like(q), torch.empty(T, H, device="cuda")
+            cache.attend(layer, step, q, kv[0], kv[1], out, lse, pages=pages)
+            for i in range(3):
+                rows = slice(begin[i], begin[i + 1])
+                for x in range(2):
+                    kept[i][layer][x] = np.concatenate([kept[i][layer][x], _np(kv[x, rows])])
+                K, V = kept[i][layer]
+                n, total = new[i], len(K)
+                at = np.arange(total - n, total)
+                for h in range(H):
+                    hk_ = h // (H // Hkv)
+                    seen = np.arange(total) <= at[:, None]
+                    if pages:
+                        got = np.zeros_like(seen)
+                        whole = [P.summary(K[p * PAGE:(p + 1) * PAGE, hk_].astype(np.float32)) for p in range(total // PAGE)] + [(np.zeros(d), 0.0)]
+                        codes, scales = np.array([c for c, _ in whole]), np.array([s for _, s in whole], dtype=np.float32)
+                        group = _np(q[rows, hk_ * 4: hk_ * 4 + 4])
+                        for t in range(n):
+                            for p in P.select(group[t], codes, scales, at[t], 1, 2, pages):
+                                got[t, p * PAGE:(p + 1) * PAGE] = True
+                        seen = seen & got
+                    o, l, pv, reach = P.attention(_np(q[rows, h]).astype(np.float64), K[:, hk_], V[:, hk_], seen, 0.125)
+                    off = (d + 8) * 2.0**-24 * reach + 2.0**-18
+                    tol = 2.0**-8 * np.abs(o) + (2.0**-8 + 2 * off)[:, None] * pv + 1e-30
+                    assert (np.abs(_np(out[rows, h]) - o) <= tol).all(), (new, layer, i, h)
+                    assert (np.abs(lse[rows, h].cpu().numpy() - l) <= off + 2.0**-22 * np.abs(l)).all()
+        if keep is not None:
+            cache.keep(keep)
+            for i in range(3):
+                for layer in range(layers):
+                    kept[i][layer] = [x[: keep[i]] for x in kept[i][layer]]
+    assert hk.heatkv_paged_status(cache.workspace) == 0
+    used = sum(-(-n // PAGE) for n in cache.lengths.tolist())
+    assert cache.state.tolist()[1] == 26 - used
+    cache.keep([0, 0, 0])
+    assert cache.state.tolist()[1] == 26 and sorted(cache.free.tolist()) == list(range(26))

@@ -492,7 +492,7 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
 /* Attention of every request's new tokens over its pages: out = softmax(sm_scale q K^T) V, with causal != 0 over the keys up to the
  * token's own position, else over all kv_len of the request (an image's scale, whose tokens see one another).  Sums and softmax
  * statistics in 32 bits, probabilities rounded to 16 before the product with V.
- *   q DEVICE [n_tokens][n_heads][d], out the same shape; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
+ *   q DEVICE [n_tokens][n_heads][d], out the same shape, not the same memory; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
  *   lse DEVICE fp32 [n_tokens][n_heads], the natural logarithm of the sum of exponentials, or NULL
  * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows past q_begin[n_seq] are left
  * as they are.  n_heads / n_kv_heads at most 128. */

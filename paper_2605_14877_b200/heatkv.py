@@ -142,6 +142,14 @@ def _packed(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tens
     return x
 
 
+def _one_device(tensors) -> int:
+    """The index of the device that all of them lie on (-1: host memory)."""
+    on = {x.get_device() for x in tensors}
+    if len(on) > 1:
+        raise ValueError("tensors on more than one device")
+    return on.pop()
+
+
 class PagedPool(C.Structure):
     """One layer's pages: k, v [n_pages, n_kv_heads, 64, d] views (d contiguous, any other strides) and, for page selection,
     their summaries.  Keeps the tensors alive."""
@@ -160,6 +168,7 @@ class PagedPool(C.Structure):
             raise ValueError("k, v: expected equal strides, the last dimension contiguous")
         p = cls()
         p.tensors = (k, v, k_code, k_scale)
+        p.device = _one_device(x for x in p.tensors if x is not None)
         p.k, p.v = k.data_ptr(), v.data_ptr()
         if k_code is not None:
             p.k_code = _packed(k_code, torch.int8, (k.shape[0], k.shape[1], k.shape[3]), "k_code").data_ptr()
@@ -187,6 +196,7 @@ class PagedBatch(C.Structure):
             raise ValueError("block_table: expected contiguous rows")
         b = cls()
         b.tensors = (q_begin, kv_len, block_table)
+        b.device = _one_device(b.tensors)
         b.q_begin, b.kv_len, b.block_table = q_begin.data_ptr(), kv_len.data_ptr(), block_table.data_ptr()
         b.table_stride = block_table.stride(0) if n > 1 else block_table.shape[1]
         b.n_seq, b.table_pages, b.n_tokens, b.max_new = n, block_table.shape[1], int(n_tokens), int(max_new)
@@ -577,7 +587,9 @@ def heatkv_paged_tables(new_tokens, past_tokens, free_pages, state, state_out, b
                                   _vector(free_pages, n_pages, "free_pages"), n_pages, _vector(state, 4, "state"),
                                   _vector(state_out, 4, "state_out"), table, stride, pages, _vector(q_begin, n + 1, "q_begin"),
                                   _vector(kv_len, n, "kv_len"), _vector(slot_map, n_tokens, "slot_map"),
-                                  None if positions is None else _vector(positions, n_tokens, "positions"), n_tokens, _stream(stream))
+                                  None if positions is None else _vector(positions, n_tokens, "positions"), n_tokens,
+                                  _on_device(stream, new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map,
+                                             positions))
     if rc:
         _check(rc, "heatkv_paged_tables")
 
@@ -588,7 +600,8 @@ def heatkv_paged_release(kv_len, keep_len, block_table, free_pages, state, state
     table, stride, pages = _table(block_table, n)
     _check(_lib.heatkv_paged_release(_vector(kv_len, n, "kv_len"), _vector(keep_len, n, "keep_len"), n, table, stride, pages,
                                      _vector(free_pages, n_pages, "free_pages"), n_pages, _vector(state, 4, "state"),
-                                     _vector(state_out, 4, "state_out"), _stream(stream)), "heatkv_paged_release")
+                                     _vector(state_out, 4, "state_out"),
+                                     _on_device(stream, kv_len, keep_len, block_table, free_pages, state, state_out)), "heatkv_paged_release")
 
 
 def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> None:
@@ -600,7 +613,8 @@ def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> 
     strides = k_new.stride()
     if v_new.stride() != strides or strides[2] != 1:
         raise ValueError("k_new, v_new: expected equal strides, the last dimension contiguous")
-    rc = _lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], slots, n, _stream(stream))
+    rc = _lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], slots, n,
+                                 _on_device(stream, pool, k_new, v_new, slot_map))
     if rc:
         _check(rc, "heatkv_paged_store")
 
@@ -610,6 +624,22 @@ def heatkv_paged_workspace_bytes(pool: PagedPool, batch: PagedBatch, n_heads: in
     out = C.c_uint64()
     _check(_lib.heatkv_paged_workspace_bytes(pool.addr, batch.addr, n_heads, C.byref(out)), "heatkv_paged_workspace_bytes")
     return out.value
+
+
+def _on_device(stream, *where) -> int:
+    """The stream's handle, after a look at where a call's tensors lie (tensors, pools and batches; None counts for nothing): an address
+    of the host or of another GPU would fault in the kernel."""
+    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    for x in where:
+        if x is not None and (x.get_device() if isinstance(x, torch.Tensor) else x.device) != here:
+            raise ValueError("a tensor that is not on the current CUDA device")
+    return _stream(stream)
+
+
+def _workspace(x) -> int:
+    if not x.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return x.data_ptr()
 
 
 def _rows(x, pool, tokens, heads, what):
@@ -651,7 +681,7 @@ def heatkv_paged_attention(pool: PagedPool, batch: PagedBatch, q, out, lse, work
     """out [n_tokens, n_heads, d] and (unless None) lse [n_tokens, n_heads] of the new tokens' attention over their requests' pages."""
     st = _token_strides(pool, batch, q, out)
     rc = _lib.heatkv_paged_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _lse(lse, q),
-                                     workspace.data_ptr(), workspace.nbytes, _stream(stream))
+                                     _workspace(workspace), workspace.nbytes, _on_device(stream, pool, batch, q, out, lse, workspace))
     if rc:
         _check(rc, "heatkv_paged_attention")
 
@@ -661,7 +691,8 @@ def heatkv_paged_select(pool: PagedPool, batch: PagedBatch, q, sel, sink: int, l
     after the last)."""
     st = _token_strides(pool, batch, q, None)
     lists, n_select = _lists(sel, pool, batch)
-    rc = _lib.heatkv_paged_select(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, sink, local, n_select, lists, _stream(stream))
+    rc = _lib.heatkv_paged_select(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, sink, local, n_select, lists,
+                                  _on_device(stream, pool, batch, q, sel))
     if rc:
         _check(rc, "heatkv_paged_select")
 
@@ -672,11 +703,11 @@ def heatkv_paged_sparse_attention(pool: PagedPool, batch: PagedBatch, q, sel, ou
     st = _token_strides(pool, batch, q, out)
     lists, n_select = _lists(sel, pool, batch)
     rc = _lib.heatkv_paged_sparse_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, lists, n_select, sm_scale, out.data_ptr(),
-                                            _lse(lse, q), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+                                            _lse(lse, q), _workspace(workspace), workspace.nbytes, _on_device(stream, pool, batch, q, sel, out, lse, workspace))
     if rc:
         _check(rc, "heatkv_paged_sparse_attention")
 
 
 def heatkv_paged_status(workspace, stream=None) -> int:
     """0, or -7 if a bounded wait of a kernel that used this workspace ran out (synchronises the stream)."""
-    return _lib.heatkv_paged_status(workspace.data_ptr(), _stream(stream))
+    return _lib.heatkv_paged_status(workspace.data_ptr(), _on_device(stream, workspace))

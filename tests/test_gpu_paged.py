@@ -561,3 +561,15 @@ def test_serving_loop(hk, pages):
     assert cache.state.tolist()[1] == 26 - used
     cache.keep([0, 0, 0])
     assert cache.state.tolist()[1] == 26 and sorted(cache.free.tolist()) == list(range(26))
+
+
+def test_a_host_tensor_is_refused(hk):
+    pool = hk.PagedPool.make(*(torch.zeros(4, 2, 64, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    slots = _i32([0, 1, 2])
+    for args in ((k.cpu(), k.cpu(), slots), (k, k, slots.cpu())):
+        with pytest.raises(ValueError, match="not on the current CUDA device"):
+            hk.heatkv_paged_store(pool, *args)
+    with pytest.raises(ValueError, match="more than one device"):
+        hk.PagedBatch.make(_i32([0, 3]), _i32([3]), _i32([[0]]).cpu(), 3, 3)
+    hk.heatkv_paged_store(pool, k, k, slots)

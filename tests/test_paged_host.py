@@ -135,6 +135,24 @@ def test_the_binding_says_what_is_wrong():
         hk.heatkv_paged_release(i(2), i(2), i(3, 5), i(9), i(4), i(4))
 
 
+def test_host_memory_never_reaches_a_kernel():
+    i = lambda *n: torch.zeros(*n, dtype=torch.int32)                                # noqa: E731
+    k, q = torch.zeros(4, 2, 64, 64, dtype=torch.bfloat16), torch.zeros(7, 4, 64, dtype=torch.bfloat16)
+    pool = hk.PagedPool.make(k, k.clone(), torch.zeros(4, 2, 64, dtype=torch.int8), torch.zeros(4, 2))
+    batch, ws = hk.PagedBatch.make(i(4), i(3), i(3, 5), 7, 2), torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (lambda: hk.heatkv_paged_tables(i(2), i(2), i(9), i(4), i(4), i(2, 5), i(3), i(2), i(4)),
+                 lambda: hk.heatkv_paged_release(i(2), i(2), i(2, 5), i(9), i(4), i(4)),
+                 lambda: hk.heatkv_paged_store(pool, q[:, :2], q[:, :2], i(7)),
+                 lambda: hk.heatkv_paged_attention(pool, batch, q, q.clone(), None, ws),
+                 lambda: hk.heatkv_paged_select(pool, batch, q, i(7, 2, 4), 1, 1),
+                 lambda: hk.heatkv_paged_sparse_attention(pool, batch, q, i(7, 2, 4), q.clone(), None, ws),
+                 lambda: hk.heatkv_paged_status(ws)):
+        with pytest.raises(ValueError, match="not on the current CUDA device"):
+            call()
+    with pytest.raises(ValueError, match="contiguous"):
+        hk.heatkv_paged_attention(pool, batch, q, q.clone(), None, ws[::2])
+
+
 def test_page_choice_by_hand():
     """Two heads of one group, d = 2: sums 3 and -1, codes 127 and -42."""
     q = np.array([[1.0, 0.0], [2.0, -1.0]], dtype=np.float32)

@@ -1,4 +1,5 @@
-"""Builds libheatkv.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc, and the call sequencer _native beside it."""
+"""Builds libheatkv.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc, and the CPython modules beside it: the call sequencer _native and
+the paged cache's calls, _paged."""
 from __future__ import annotations
 
 import os
@@ -11,14 +12,16 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheatkv.so")
 NATIVE = os.path.join(HERE, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+PAGED = os.path.join(HERE, os.path.basename(NATIVE).replace("_native", "_paged"))
 SOURCES = ["schedule.cpp", "plan.cpp", "split.cpp", "api.cu", "attn_generic.cu", "attn_tc.cu", "attn_pair.cu", "calib_tc.cu", "cache_kernels.cu",
            "paged_api.cu", "paged_tables.cu", "paged_select.cu", "paged_small.cu", "paged_tc.cu"]
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(NATIVE):
+    built = (LIB, NATIVE, PAGED)
+    if not all(os.path.exists(p) for p in built):
         return True
-    lib_t = min(os.path.getmtime(LIB), os.path.getmtime(NATIVE))
+    lib_t = min(os.path.getmtime(p) for p in built)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "heatkv.h")]
     return any(os.path.getmtime(p) > lib_t for p in deps)
 
@@ -51,9 +54,10 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("nvcc failed")
     link = [nvcc, "-shared", "-o", LIB] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-lcudart"]
     subprocess.run(link, check=True)
-    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
-                    "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "native_module.c"), "-o", NATIVE, "-L", HERE,
-                    "-l:libheatkv.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    for source, module in (("native_module.c", NATIVE), ("paged_calls.c", PAGED)):
+        subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                        "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, source), "-o", module, "-L", HERE,
+                        "-l:libheatkv.so", "-Wl,-rpath,$ORIGIN"], check=True)
     return LIB
 
 

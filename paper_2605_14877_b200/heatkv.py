@@ -116,14 +116,14 @@ def _expect(x: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tens
     return x
 
 
-# The checks of the small calls, which take no longer on the GPU than in Python: no tuple or generator is built for an argument that
-# passes (a table call 13.7 -> 8 us).
+# Checks of the paged calls.  The calls that a model's step repeats make the same checks in C first (_paged) and come here where one fails,
+# to say which (a table call 9.4 us from Python through ctypes, 6.1 from C).
 _I32 = torch.int32
 
 
 def _vector(x: torch.Tensor, n: int, what: str) -> int:
     """Address of a contiguous int32 vector of n entries."""
-    if x.dtype is not _I32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous():
+    if x.dtype is not _I32 or x.numel() != n or not x.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous int32 vector of {n}, got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
@@ -236,6 +236,8 @@ def _load() -> C.CDLL:
 
 
 _lib = _load()
+from . import _paged  # noqa: E402  (behind the library that it is linked to)
+
 _lib.heatkv_strerror.restype = C.c_char_p
 _lib.heatkv_strerror.argtypes = [C.c_int]
 _P = C.c_void_p
@@ -312,6 +314,9 @@ def _ptr(x) -> Optional[int]:
 def _check(rc: int, where: str) -> None:
     if rc != 0:
         raise HeatKVError(rc, where)
+
+
+_paged.set_hooks(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.int32, torch.float32)
 
 
 def _ids(seq_ids: Sequence[int]):
@@ -581,6 +586,9 @@ def heatkv_device_status(ctx: int, stream=None) -> int:
 def heatkv_paged_tables(new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map,
                         positions=None, stream=None) -> None:
     """Pages, slots and positions of a step's new tokens, from the requests' lengths (int32 tensors on the device)."""
+    rc = _paged.tables(new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map, positions, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_tables")
     n, n_pages, n_tokens = new_tokens.numel(), free_pages.numel(), slot_map.numel()
     table, stride, pages = _table(block_table, n)
     rc = _lib.heatkv_paged_tables(_vector(new_tokens, n, "new_tokens"), _vector(past_tokens, n, "past_tokens"), n,
@@ -590,8 +598,7 @@ def heatkv_paged_tables(new_tokens, past_tokens, free_pages, state, state_out, b
                                   None if positions is None else _vector(positions, n_tokens, "positions"), n_tokens,
                                   _on_device(stream, new_tokens, past_tokens, free_pages, state, state_out, block_table, q_begin, kv_len, slot_map,
                                              positions))
-    if rc:
-        _check(rc, "heatkv_paged_tables")
+    _check(rc, "heatkv_paged_tables")
 
 
 def heatkv_paged_release(kv_len, keep_len, block_table, free_pages, state, state_out, stream=None) -> None:
@@ -606,6 +613,9 @@ def heatkv_paged_release(kv_len, keep_len, block_table, free_pages, state, state
 
 def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> None:
     """K and V rows [n_tokens, n_kv_heads, d] (equal strides, d contiguous) to their slots, and the summaries of pages that fill up."""
+    rc = _paged.store(pool, k_new, v_new, slot_map, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_store")
     n = slot_map.numel()
     slots = _vector(slot_map, n, "slot_map")
     _rows(k_new, pool, n, pool.n_kv_heads, "k_new")
@@ -615,8 +625,7 @@ def heatkv_paged_store(pool: PagedPool, k_new, v_new, slot_map, stream=None) -> 
         raise ValueError("k_new, v_new: expected equal strides, the last dimension contiguous")
     rc = _lib.heatkv_paged_store(pool.addr, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], slots, n,
                                  _on_device(stream, pool, k_new, v_new, slot_map))
-    if rc:
-        _check(rc, "heatkv_paged_store")
+    _check(rc, "heatkv_paged_store")
 
 
 def heatkv_paged_workspace_bytes(pool: PagedPool, batch: PagedBatch, n_heads: int) -> int:
@@ -679,33 +688,39 @@ def _lists(sel, pool, batch):
 def heatkv_paged_attention(pool: PagedPool, batch: PagedBatch, q, out, lse, workspace, causal: bool = True, sm_scale: float = 0.0,
                            stream=None) -> None:
     """out [n_tokens, n_heads, d] and (unless None) lse [n_tokens, n_heads] of the new tokens' attention over their requests' pages."""
+    rc = _paged.attention(pool, batch, q, out, lse, workspace, causal, sm_scale, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_attention")
     st = _token_strides(pool, batch, q, out)
     rc = _lib.heatkv_paged_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _lse(lse, q),
                                      _workspace(workspace), workspace.nbytes, _on_device(stream, pool, batch, q, out, lse, workspace))
-    if rc:
-        _check(rc, "heatkv_paged_attention")
+    _check(rc, "heatkv_paged_attention")
 
 
 def heatkv_paged_select(pool: PagedPool, batch: PagedBatch, q, sel, sink: int, local: int, stream=None) -> None:
     """sel [n_tokens, n_kv_heads, n_select]: the pages each new token attends to (places in its request's table row, ascending, -1
     after the last)."""
+    rc = _paged.select(pool, batch, q, sel, sink, local, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_select")
     st = _token_strides(pool, batch, q, None)
     lists, n_select = _lists(sel, pool, batch)
     rc = _lib.heatkv_paged_select(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, sink, local, n_select, lists,
                                   _on_device(stream, pool, batch, q, sel))
-    if rc:
-        _check(rc, "heatkv_paged_select")
+    _check(rc, "heatkv_paged_select")
 
 
 def heatkv_paged_sparse_attention(pool: PagedPool, batch: PagedBatch, q, sel, out, lse, workspace, sm_scale: float = 0.0,
                                   stream=None) -> None:
     """heatkv_paged_attention (causal) over the pages that sel lists for each token."""
+    rc = _paged.sparse_attention(pool, batch, q, sel, out, lse, workspace, sm_scale, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_sparse_attention")
     st = _token_strides(pool, batch, q, out)
     lists, n_select = _lists(sel, pool, batch)
     rc = _lib.heatkv_paged_sparse_attention(pool.addr, batch.addr, q.size(1), q.data_ptr(), st, lists, n_select, sm_scale, out.data_ptr(),
                                             _lse(lse, q), _workspace(workspace), workspace.nbytes, _on_device(stream, pool, batch, q, sel, out, lse, workspace))
-    if rc:
-        _check(rc, "heatkv_paged_sparse_attention")
+    _check(rc, "heatkv_paged_sparse_attention")
 
 
 def heatkv_paged_status(workspace, stream=None) -> int:

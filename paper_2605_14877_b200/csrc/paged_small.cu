@@ -732,7 +732,8 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   }
 }
 
-// Adds up the parts of the units that were cut, in page order: a warp per row, or, where some unit has many, a CTA.
+// Adds up the parts of the units that were cut, in page order: a warp per row, or, where some unit has many, a CTA.  What bounds it is a chain of
+// loads behind the end of the kernel before (slots, cut, parts): about 7 us of a decode's 71, 4.6 MB of parts.
 constexpr int MANY_PARTS = 16;
 template <int D, bool F16>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ SmallParams sp) {

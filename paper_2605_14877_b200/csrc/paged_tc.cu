@@ -16,6 +16,9 @@
 // if its token is among those that did: neighbouring tokens select much the same pages, so a page is read and multiplied once for all of
 // them instead of once for each.  Warp 2 brings the tokens' lists into shared memory, the copy warp merges them as it goes (a
 // token per lane and tile) and hands the tokens' bits to the softmax warps beside each tile.
+// What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 us,
+// 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax (half the
+// products per exponential: 32 heads of the first shape 670 us, 800 TFLOP/s).
 // Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and leaves.
 #include <algorithm>
 

@@ -476,6 +476,31 @@ def test_select_of_a_long_context(hk, tokens, codes, n_select):
             assert sel[t, h].tolist() == P.select(_np(q)[t, 2 * h: 2 * h + 2], cn[pages, h], sn[pages, h], kv - tokens + t, 3, 4, n_select)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("codes", [1, 127])
+@pytest.mark.parametrize("requests", [3, 9, 18, 40, 100])
+def test_select_of_many_requests(hk, requests, codes, d):
+    """A token each, from so few that eight SMs share a token's pages to more than there are SMs; many equal scores or hardly any."""
+    n_pages, Hkv, G = 300, 2, 3
+    rng, g = np.random.default_rng(requests), torch.Generator("cuda").manual_seed(requests)
+    pool, _, _, code, scale = _pool(hk, g, n_pages, Hkv, d, torch.bfloat16, fill=0.0)
+    code.copy_(torch.randint(-codes, codes + 1, code.shape, generator=g, device="cuda"))
+    scale.copy_(2.0 ** torch.randint(-2, 1, scale.shape, generator=g, device="cuda"))
+    kv = [int(x) for x in rng.integers(1, n_pages * PAGE, requests)]
+    kv[0], kv[-1] = n_pages * PAGE, 1
+    table = _i32([rng.permutation(n_pages) for _ in range(requests)])                         # requests may share pages
+    b = hk.PagedBatch.make(_i32(range(requests + 1)), _i32(kv), table, requests, 1)
+    q = torch.randint(-codes, codes + 1, (requests, Hkv * G, d), generator=g, device="cuda").to(torch.bfloat16)
+    sel = torch.zeros(requests, Hkv, 21, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, 1, 2)
+    cn, sn, tn, qn = code.cpu().numpy(), scale.cpu().numpy(), table.cpu().numpy(), _np(q)
+    for t in range(requests):
+        pages = tn[t, : -(-kv[t] // PAGE)]
+        for h in range(Hkv):
+            want = P.select(qn[t, G * h: G * h + G], cn[pages, h], sn[pages, h], kv[t] - 1, 1, 2, 21)
+            assert sel[t, h].tolist() == want + [-1] * (21 - len(want)), (t, h)
+
+
 def test_sparse_attention_over_lists_of_any_kind(hk):
     """Gaps in a list, entries past the token's page and past the table, an empty list, pages out of order."""
     lens = [(2, 500), (1, 64 * 6)]

@@ -465,7 +465,8 @@ typedef struct {                 /* element strides of [n_tokens][n_heads][d] ac
  *             state, so that a step can be repeated
  *   block_table DEVICE, in and out: entries ceil(past_i / 64) .. are written for the fresh pages
  *   q_begin DEVICE [n_seq + 1], kv_len DEVICE [n_seq], slot_map DEVICE [n_tokens] (page * 64 + row, -1: none; also past the last token),
- *   positions DEVICE [n_tokens] (past_i + place among the new tokens) or NULL                                                  */
+ *   positions DEVICE [n_tokens] (past_i + place among the new tokens) or NULL
+ * What is written (state_out, block_table, q_begin, kv_len, slot_map, positions) shares no memory with the rest. */
 int heatkv_paged_tables(const int32_t* new_tokens, const int32_t* past_tokens, int n_seq, const int32_t* free_pages, int n_pages,
                         const int32_t* state, int32_t* state_out, int32_t* block_table, int64_t table_stride, int table_pages,
                         int32_t* q_begin, int32_t* kv_len, int32_t* slot_map, int32_t* positions, int n_tokens, void* stream);

@@ -126,6 +126,7 @@ int heatkv_paged_tables(const int32_t* new_tokens, const int32_t* past_tokens, i
     return HEATKV_ERR_INVALID_ARG;
   if (n_seq < 1 || n_pages < 1 || table_pages < 1 || table_stride < table_pages || n_tokens < 1 || state == state_out) return HEATKV_ERR_INVALID_ARG;
   if (n_seq > PAGED_MAX_SEQ || n_pages > PAGED_MAX_PAGES || table_pages > PAGED_MAX_TABLE) return HEATKV_ERR_TOO_LARGE;
+  if (kv_len == past_tokens || kv_len == new_tokens) return HEATKV_ERR_INVALID_ARG;      // (read by all CTAs while one writes)
   const TablesParams p = {new_tokens, past_tokens, free_pages, state,      state_out, block_table, q_begin, kv_len,
                           slot_map,   positions,   table_stride, n_seq, n_pages,   table_pages, n_tokens};
   return done(launch_paged_tables(p, static_cast<cudaStream_t>(stream)));

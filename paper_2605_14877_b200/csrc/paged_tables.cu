@@ -47,21 +47,25 @@ __device__ __forceinline__ int find_last(const int32_t* a, int n, int x) {
 // Every CTA takes the sums over all requests for itself (a few hundred lengths, read from L2) and then writes its share of the
 // tokens and of the fresh pages, so there is one launch and no CTA waits for another.  A page that this call hands out is looked
 // up in the ring, never in the table that another CTA is writing.  What bounds it is the chain of loads and sums before the first write:
-// 3 to 4 us for the 24 new tokens of 24 requests, 5.6 for 141 786 of 300 (1.2 MB; a thread with one token at a time 7.2).
+// 3.8 us for the 24 new tokens of 24 requests, 5.6 for 141 786 of 300 (1.2 MB; a thread with one token at a time and one sum behind
+// another 9.2).
 __global__ void __launch_bounds__(TT) tables_kernel(const TablesParams p) {
   extern __shared__ int32_t sm[];
   int32_t* begin = sm;                         // [n_seq + 1] first token
   int32_t* taken = sm + p.n_seq + 1;           // [n_seq + 1] pages handed out before the request
   int32_t* had = taken + p.n_seq + 1;          // [n_seq] pages it had; -1: refused
   int32_t* past = had + p.n_seq;               // [n_seq]
-  __shared__ int64_t warp_sums[TT / 32];
+  __shared__ int64_t warp_tokens[TT / 32], warp_pages[TT / 32];
+  __shared__ int handed, turned_down;
   pdl_trigger();
+  if (threadIdx.x == 0) handed = turned_down = 0;
   pdl_wait();
   const int per = (p.n_seq + TT - 1) / TT, i0 = min((int)threadIdx.x * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
   const int head = (p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages, free = min(max(p.state_in[1], 0), p.n_pages);
   int64_t tokens = 0, pages = 0;
+#pragma unroll 2
   for (int i = i0; i < i1; ++i) {
-    const int64_t a = max(p.past_tokens[i], 0), n = max(p.new_tokens[i], 0);
+    const int64_t a = max(__ldg(p.past_tokens + i), 0), n = max(__ldg(p.new_tokens + i), 0);
     const int64_t h0 = (a + PAGE - 1) / PAGE, h1 = (a + n + PAGE - 1) / PAGE;
     begin[i] = (int)n;
     past[i] = (int)a;
@@ -70,10 +74,34 @@ __global__ void __launch_bounds__(TT) tables_kernel(const TablesParams p) {
     tokens += n;
     pages += taken[i];
   }
-  int64_t all_tokens, all_pages;
-  int64_t t = block_exclusive(tokens, warp_sums, all_tokens);
-  int64_t r = block_exclusive(pages, warp_sums, all_pages);
-  int64_t refused = 0;
+  // both sums in one go: tokens and pages before this thread's requests
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t t = tokens, r = pages;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t t_up = __shfl_up_sync(0xffffffffu, t, o), r_up = __shfl_up_sync(0xffffffffu, r, o);
+    if (lane >= o) {
+      t += t_up;
+      r += r_up;
+    }
+  }
+  if (lane == 31) {
+    warp_tokens[warp] = t;
+    warp_pages[warp] = r;
+  }
+  __syncthreads();
+  t -= tokens;
+  r -= pages;
+  int64_t all_tokens = 0;
+#pragma unroll
+  for (int w = 0; w < TT / 32; ++w) {
+    all_tokens += warp_tokens[w];
+    if (w < warp) {
+      t += warp_tokens[w];
+      r += warp_pages[w];
+    }
+  }
+  int refused = 0;
   int granted = 0;                             // pages handed out up to this thread's last served request
   for (int i = i0; i < i1; ++i) {
     const int n = begin[i], need = taken[i];
@@ -88,16 +116,10 @@ __global__ void __launch_bounds__(TT) tables_kernel(const TablesParams p) {
     t += n;
     r += need;
   }
-  int64_t all_refused;
-  block_exclusive(refused, warp_sums, all_refused);
+  if (threadIdx.x == 0) begin[p.n_seq] = saturate(all_tokens);
   // served requests that take pages are the first ones: the most that any thread saw is what the call hands out
-  __shared__ int handed;
-  if (threadIdx.x == 0) {
-    handed = 0;
-    begin[p.n_seq] = saturate(all_tokens);
-  }
-  __syncthreads();
   if (granted > 0) atomicMax(&handed, granted);
+  if (refused > 0) atomicAdd(&turned_down, refused);
   __syncthreads();
   const int got = handed;
   auto page_of = [&](int rank) {                 // (rank < free <= n_pages)
@@ -154,7 +176,7 @@ __global__ void __launch_bounds__(TT) tables_kernel(const TablesParams p) {
   if (gid == 0) {
     p.state_out[0] = (int)(((int64_t)head + got) % p.n_pages);
     p.state_out[1] = free - got;
-    p.state_out[2] = (int)all_refused;
+    p.state_out[2] = turned_down;
     p.state_out[3] = begin[p.n_seq];
   }
 }

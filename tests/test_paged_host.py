@@ -94,6 +94,7 @@ def test_arguments_of_tables_release_and_store():
     for at, value, status in ((2, 0, INVALID), (2, 4097, LARGE), (4, 0, INVALID), (4, (1 << 25) + 1, LARGE), (6, A, INVALID), (8, 4, INVALID), (9, 0, INVALID),
                               (14, 0, INVALID)):
         assert call(ok[:at] + [value] + ok[at + 1:]) == status, (at, value)
+    assert call(ok) == INVALID and call([A + 64] + ok[1:]) == INVALID                # lengths written where they are read
     ok = [A, A, 3, A, 5, 5, A, 10, A, A + 64]
     call = lambda args: H._lib.heatkv_paged_release(*args, None)                    # noqa: E731
     for at in (0, 1, 3, 6, 8, 9):

@@ -87,7 +87,7 @@ cudaError_t launch_paged_release(const ReleaseParams& p, cudaStream_t stream);
 cudaError_t launch_paged_store(StoreParams p, cudaStream_t stream);
 cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cudaStream_t stream);
 // warp-level kernel: row tiles of up to 64 rows
-uint64_t paged_small_partial_bytes(int d, int n_sm);
+uint64_t paged_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens);
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 // tensor-memory kernel: row tiles of up to 128 rows
 uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, int n_seq);

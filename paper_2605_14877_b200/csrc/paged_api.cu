@@ -91,7 +91,7 @@ int attention_params(const heatkv_paged_pool* pool, const heatkv_paged_batch* b,
 }
 
 uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_tokens, int n_seq) {
-  const uint64_t a = paged_small_partial_bytes(d, dev.n_sm), b = paged_tc_partial_bytes(d, dev.n_sm, G, Hkv, n_tokens, n_seq);
+  const uint64_t a = paged_small_partial_bytes(d, dev.n_sm, Hkv, n_tokens), b = paged_tc_partial_bytes(d, dev.n_sm, G, Hkv, n_tokens, n_seq);
   return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 

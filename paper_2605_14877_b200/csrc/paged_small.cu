@@ -6,7 +6,7 @@
 // take pieces from a counter until none is left (dealt out beforehand in equal shares, the SMs with the longest way to memory decided when
 // a call ended: SMs' active cycles differed by 15 %).  Pieces leave partial results (unnormalised O, maximum, sum) in the workspace, which a
 // second small kernel adds up in page order; neither the pieces nor that order depends on which CTA took what.  (Added up by the CTA that
-// leaves a unit's last piece, with a fence and a counter behind every piece, a decode of 64 requests took 92 us instead of 71.)
+// leaves a unit's last piece, with a fence and a counter behind every piece, a decode of 64 requests took 92 us, with the second kernel 67.)
 //
 // One warp takes pieces and looks up what they are, one ahead; the next sends for Q, K and V (TMA, K and V of one page per stage),
 // so that what a piece's beginning has to read (counter, lengths, table) is read while the pages before it arrive.  The others
@@ -29,18 +29,19 @@ using namespace tc;
 
 constexpr int MAX_STAGES = 12;
 constexpr float MOVE = 8.f;                    // a reference moves when a maximum passes it by more than 2^MOVE (P fits fp16)
-// Pieces of fewer pages cost more to add up than they save: 64 requests of 500 tokens, 8 kv heads, take 34.3 us with pieces of 4 pages and
-// 30.4 of 8; where pieces of 8 would leave CTAs without one, 4 are better (24 requests of drafted tokens 26.9 us with 8, 24.8 with 4).
+// Pages of a piece.  In a small call every CTA takes one piece, of at least MIN_CHUNK pages (one token, 32 pages of 8 kv heads: 9.5 us with 4, 10.8
+// with 8) and at most FULL_CHUNK (24 requests of drafted tokens: 20.1 us in two rounds of 4, 16.7 in one of up to 8; 64 requests
+// of 500 tokens, 8 kv heads: 31.4 in pieces of 6, 28.5 of 8, which is whole units); in a large one PER_CTA, longer ones (64 requests of 1360 tokens on
+// average: 66.9 us with 4, 67.7 with 3, 68.1 with 6 or 8).
 constexpr int MIN_CHUNK = 4, FULL_CHUNK = 8;
 // (and units of up to FULL_CHUNK pages stay whole: a short request then needs no second kernel, 7.3 us instead of 10)
-constexpr int PER_CTA = 4;                     // pieces a CTA takes (64 requests of 1360 tokens: 70 us with 4, 73 with 6, 76 with 12)
+constexpr int PER_CTA = 4;
 constexpr int MERGE_WARPS = 8;
 
 struct SmallParams {
   PagedParams a;
   uint32_t* counter;                           // pieces taken beyond every CTA's first; zero between launches
-  int32_t* n_slots;                            // partial results of this call, and most parts of a unit
-  int4* cuts;                                  // [slot] {first token, rows, kv head, pieces} at a unit's first piece, else no rows
+  int2* cuts;                                  // [n_tokens][Hkv] {the unit's first slot, its pieces | the token's place in it << 16}; not cut: no pieces
   int32_t stages;
 };
 struct SmallMaps {
@@ -96,6 +97,13 @@ __device__ __forceinline__ void meet(int group) { asm volatile("bar.sync %0, 128
 // A partial result: rows of O, then their maxima and sums; whole 16-byte words.
 __host__ __device__ constexpr int64_t slot_floats(int rows, int d) { return ((int64_t)rows * (d + 2) + 3) & ~(int64_t)3; }
 
+__device__ __forceinline__ int chunk_of(int64_t pages, int units, int ctas) {
+  const int room = ctas - units / 2;                               // (a unit's last piece is half empty on average)
+  int chunk = FULL_CHUNK;
+  if (room > 0 && pages < (int64_t)room * FULL_CHUNK) chunk = max(((int)pages + room - 1) / room, MIN_CHUNK);
+  const int64_t share = (int64_t)ctas * PER_CTA;
+  return pages <= share * chunk ? chunk : (int)((pages + share - 1) / share);
+}
 __device__ __forceinline__ int pieces_of(int pages, int chunk) { return pages <= FULL_CHUNK ? pages > 0 : (pages + chunk - 1) / chunk; }
 
 enum RingWord : int { W_KIND = 0, W_HEAD, W_TOK0, W_ROWS, W_TILES, W_KV, W_POS0, W_SLOT, W_PIECE, W_PIECES, W_SEQ, W_TILE0, RING_WORDS = 12 };
@@ -146,8 +154,9 @@ struct Parts {
     return c;
   }
 };
-constexpr int AHEAD = 4;
-// Parts begin .. end - 1, by a warp.  The first ones' columns come with the maxima and sums, not behind them.
+// Parts begin .. end - 1, by a warp.  The first ones' columns come with the maxima and sums, not behind them (a decode of 64 requests, up to 16
+// parts: 69.1 us with 4 of them, 68.7 with 8, 66.9 with 12, 67.2 with 16; one request of 131 000 tokens 98.2, 97.8, 95.6, 96.1).
+constexpr int AHEAD = 12;
 template <int D>
 __device__ __forceinline__ RowSum<D> sum_parts(const Parts<D>& p, int begin, int end) {
   constexpr int N = D / 32;
@@ -156,7 +165,8 @@ __device__ __forceinline__ RowSum<D> sum_parts(const Parts<D>& p, int begin, int
   const int n = end - begin;
   typename Parts<D>::Columns ahead[AHEAD];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) ahead[i] = p.columns(begin + min(i, n - 1));
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < n) ahead[i] = p.columns(begin + i);
   float2 ml = make_float2(NO_MAX, 0.f);                            // of part begin + lane
   if (p.lane < n) ml = p.stats(begin + p.lane);
   r.top = ml.x;
@@ -218,7 +228,6 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   __shared__ int32_t page_of[MAX_STAGES];                                       // place in the request's table row of the page in a stage
   __shared__ uint32_t abort_word, leave_word[GROUPS];
   __shared__ int64_t sums[WARPS + 2];
-  __shared__ int longest;
   volatile uint32_t* abort_flag = &abort_word;
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int s) { return bar0 + s * 16; };
@@ -249,16 +258,11 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   // S, the pieces and the partial results.  (A request without keys has no pieces, and its rows get their zeros here.)
   int64_t total = 0;
   int chunk = 0, n_chunks = 0;
-  const int64_t share = (int64_t)gridDim.x * PER_CTA;
   if (SPARSE) {
     total = (int64_t)p.n_tokens * p.Hkv * p.n_sel;
-    chunk = (int)max((int64_t)(total < (int64_t)gridDim.x * FULL_CHUNK ? MIN_CHUNK : FULL_CHUNK), (total + share - 1) / share);
+    chunk = chunk_of(total, (int)min((int64_t)p.n_tokens * p.Hkv, (int64_t)INT_MAX), gridDim.x);
     const int pieces = pieces_of(p.n_sel, chunk);
     n_chunks = (int)min((int64_t)p.n_tokens * p.Hkv * pieces, (int64_t)INT_MAX);
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-      sp.n_slots[0] = pieces > 1 ? n_chunks : 0;
-      sp.n_slots[1] = pieces;
-    }
     __syncthreads();
   } else {
     const int per = (p.n_seq + THREADS - 1) / THREADS, i0 = min((int)threadIdx.x * per, p.n_seq), i1 = min(i0 + per, p.n_seq);
@@ -283,7 +287,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       return before + inc - v;
     };
     int64_t sum = 0;
-    int most = 0;                                                  // pages of the longest request
+    int units_mine = 0;
     for (int i = i0; i < i1; ++i) {
       const int b = max(p.q_begin[i], 0), n = max(min(p.q_begin[i + 1], p.n_tokens) - b, 0);
       const int kv = min(max(p.kv_len[i], 0), p.table_pages * PAGE);
@@ -291,12 +295,12 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       chunk_begin[i] = units;
       slot_begin[i] = tiles;
       sum += (int64_t)tiles * units;
-      if (units > 0) most = max(most, tiles);
+      if (tiles > 0) units_mine = min(units_mine + units, 4096);
     }
-    if (threadIdx.x == 0) longest = 0;
-    scan(sum, total);
-    if (blockIdx.x == 0) atomicMax(&longest, most);                // (read by this CTA's first thread behind the next sum)
-    chunk = (int)max((int64_t)(total < (int64_t)gridDim.x * FULL_CHUNK ? MIN_CHUNK : FULL_CHUNK), (total + share - 1) / share);
+    // pages, and above them the units, as many as matter
+    constexpr int64_t PAGES = ((int64_t)1 << 43) - 1;
+    scan(min(sum, PAGES / THREADS) + ((int64_t)min(units_mine, 4096) << 43), total);
+    chunk = chunk_of(total & PAGES, (int)(total >> 43), gridDim.x);
     // (both in one sum: pieces in the low 40 bits, partial results, of which there are few, above)
     constexpr int64_t LOW = ((int64_t)1 << 40) - 1;
     int64_t mine = 0, all;
@@ -314,13 +318,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       at += c + (pieces > 1 ? c << 40 : 0);
     }
     n_chunks = (int)min((int64_t)(all & LOW), (int64_t)INT_MAX);
-    if (threadIdx.x == 0) {
-      chunk_begin[p.n_seq] = n_chunks;
-      if (blockIdx.x == 0) {
-        sp.n_slots[0] = (int)(all >> 40);
-        sp.n_slots[1] = pieces_of(longest, chunk);
-      }
-    }
+    if (threadIdx.x == 0) chunk_begin[p.n_seq] = n_chunks;
     __syncthreads();
     for (int i = blockIdx.x; i < p.n_seq; i += gridDim.x) {
       if (chunk_begin[i + 1] != chunk_begin[i]) continue;
@@ -332,6 +330,7 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       }
       if (p.lse)
         for (int64_t j = threadIdx.x; j < n; j += THREADS) p.lse[b * (int64_t)p.H + j] = -INFINITY;
+      for (int64_t j = threadIdx.x; j < (int64_t)max(e - b, 0) * p.Hkv; j += THREADS) sp.cuts[b * (int64_t)p.Hkv + j] = make_int2(-1, 0);
     }
   }
 
@@ -702,7 +701,8 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
       }
     meet(group);
     const int out_slot = w[W_SLOT], tok0 = w[W_TOK0], head0 = w[W_HEAD] * p.G;
-    if (out_slot >= 0 && threadIdx.x == 0) sp.cuts[out_slot] = w[W_PIECE] == 0 ? make_int4(tok0, rows, w[W_HEAD], w[W_PIECES]) : make_int4(0, 0, 0, 0);
+    if (w[W_PIECE] == 0 && (int)threadIdx.x < rows / p.G)
+      sp.cuts[(int64_t)(tok0 + (int)threadIdx.x) * p.Hkv + w[W_HEAD]] = make_int2(out_slot, out_slot < 0 ? 0 : w[W_PIECES] | (int)threadIdx.x << 16);
     const int slot_rows = p.tile_tokens * p.G;
     float* part = p.partials + (int64_t)out_slot * slot_floats(slot_rows, D);
 #pragma unroll
@@ -732,36 +732,42 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
   }
 }
 
-// Adds up the parts of the units that were cut, in page order: a warp per row, or, where some unit has many, a CTA.  What bounds it is a chain of
-// loads behind the end of the kernel before (slots, cut, parts): about 7 us of a decode's 71, 4.6 MB of parts.
-constexpr int MANY_PARTS = 16;
-template <int D, bool F16>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ SmallParams sp) {
+// Partial results of a call: pieces of units of more than S pages, S at least pages / (CTAs * PER_CTA), so at most twice CTAs * PER_CTA
+// (a unit of x S pages, x > 1, has fewer than 2 x pieces).
+constexpr int MOST_CTAS = 240;                 // (SMs; at most twice as many CTAs)
+__host__ __device__ constexpr int max_slots(int n_sm) { return 2 * PER_CTA * 2 * n_sm; }
+static_assert(max_slots(MOST_CTAS) < 1 << 16, "pieces of a unit in 16 bits");
+
+// Adds up the parts of the rows whose units were cut, in page order: a CTA per row where the rows are few, else a warp.  What bounds it is a
+// chain of loads behind the end of the kernel before (cut, parts), and the start of its CTAs: one for every slot and row instead of one for 8 of
+// the call's rows, as it was first, made a decode of 64 requests 71 us instead of 67.
+template <int D, bool F16, bool WIDE>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ SmallParams sp, int slots) {
   const PagedParams& p = sp.a;
   constexpr int N = D / 32;
   __shared__ float sums[MERGE_WARPS][D], tops[MERGE_WARPS], ls[MERGE_WARPS];
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot_rows = p.tile_tokens * p.G;
-  const int2 slots = __ldcg(reinterpret_cast<const int2*>(sp.n_slots));        // partial results, most parts of a unit
-  const int pairs = slots.x * slot_rows;                           // (slots and rows are few)
+  const int begin_tok = __ldg(p.q_begin), end_tok = __ldg(p.q_begin + p.n_seq);
   Parts<D> parts;
   parts.pitch = slot_floats(slot_rows, D);
   parts.slot_rows = slot_rows;
   parts.lane = lane;
-  const bool many = slots.y > MANY_PARTS;
-  for (int x = many ? blockIdx.x : blockIdx.x * MERGE_WARPS + warp; x < pairs; x += gridDim.x * (many ? 1 : MERGE_WARPS)) {
-    const int s0 = x / slot_rows;
-    parts.row = x - s0 * slot_rows;
-    const int4 cut = __ldcg(sp.cuts + s0);
-    if (parts.row >= cut.y) continue;
-    parts.first = p.partials + s0 * parts.pitch;
-    const int tok = cut.x + parts.row / p.G, hd = cut.z * p.G + parts.row % p.G;
-    if (!many) {
-      put_row<D, F16>(p, sum_parts<D>(parts, 0, cut.w), tok, hd, lane);
+  const int64_t rows = (int64_t)p.n_tokens * p.H, step = (int64_t)gridDim.x * (WIDE ? 1 : MERGE_WARPS);
+  for (int64_t x = WIDE ? blockIdx.x : (int64_t)blockIdx.x * MERGE_WARPS + warp; x < rows; x += step) {
+    const int tok = (int)(x / p.H), hd = (int)(x - (int64_t)tok * p.H), head = hd / p.G;
+    const int2 cut = __ldcg(sp.cuts + (int64_t)tok * p.Hkv + head);
+    const int pieces = cut.y & 0xffff;
+    parts.row = (cut.y >> 16) * p.G + hd - head * p.G;
+    // (rows that are nobody's have an entry of some call before, or none)
+    if (pieces < 2 || tok < begin_tok || tok >= end_tok || cut.x < 0 || cut.x + pieces > slots || parts.row >= slot_rows) continue;
+    parts.first = p.partials + cut.x * parts.pitch;
+    if (!WIDE) {
+      put_row<D, F16>(p, sum_parts<D>(parts, 0, pieces), tok, hd, lane);
       continue;
     }
-    const int begin = cut.w * warp / MERGE_WARPS, end = cut.w * (warp + 1) / MERGE_WARPS;
+    const int begin = pieces * warp / MERGE_WARPS, end = pieces * (warp + 1) / MERGE_WARPS;
     RowSum<D> r;
     r.clear();
     if (begin < end) r = sum_parts<D>(parts, begin, end);
@@ -787,10 +793,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
   }
 }
 
-// Partial results of a call: pieces of units of more than S pages, S at least pages / (CTAs * PER_CTA), so at most twice CTAs * PER_CTA
-// (a unit of x S pages, x > 1, has fewer than 2 x pieces).
-int max_slots(int n_sm) { return 2 * PER_CTA * 2 * n_sm; }
-uint64_t cut_bytes(int n_sm) { return ((uint64_t)max_slots(n_sm) * 16 + 16 + 255) / 256 * 256; }
+uint64_t cut_bytes(int n_tokens, int Hkv) { return ((uint64_t)n_tokens * Hkv * 8 + 255) / 256 * 256; }
 
 template <int D, int MT, int GROUPS, bool F16, bool SPARSE>
 cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaStream_t stream) {
@@ -799,9 +802,8 @@ cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaSt
   SmallParams sp;
   sp.a = p;
   sp.counter = p.counters;
-  sp.cuts = reinterpret_cast<int4*>(p.partials);
-  sp.n_slots = reinterpret_cast<int32_t*>(sp.cuts + max_slots(n_sm));
-  sp.a.partials = p.partials + cut_bytes(n_sm) / 4;
+  sp.cuts = reinterpret_cast<int2*>(p.partials);
+  sp.a.partials = p.partials + cut_bytes(p.n_tokens, p.Hkv) / 4;
   // as many pages under way as the CTA's share of an SM's shared memory holds
   const int room = (L::CTAS == 2 ? 113 : 226) * 1024 - 768;
   sp.stages = std::max(2, std::min<int>(MAX_STAGES, (room - (int)fixed) / (int)(2 * L::TILE)));
@@ -812,7 +814,10 @@ cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaSt
   rc = launch_pdl(kernel, dim3(n_sm * L::CTAS), dim3(L::THREADS), smem, stream, sp, maps);
   // nothing can have been cut where no unit has more pages
   if (rc != cudaSuccess || (SPARSE ? p.n_sel : p.table_pages) <= FULL_CHUNK) return rc;
-  return launch_pdl(paged_merge_kernel<D, F16>, dim3(8 * n_sm), dim3(MERGE_WARPS * 32), 0, stream, sp);
+  const int64_t rows = (int64_t)p.n_tokens * p.H, pieces = (SPARSE ? p.n_sel : p.table_pages) / MIN_CHUNK;       // (of a unit, at most)
+  if (rows <= 8 * n_sm && pieces > AHEAD) return launch_pdl(paged_merge_kernel<D, F16, true>, dim3((unsigned)rows), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(n_sm));
+  const int64_t ctas = std::min<int64_t>((rows + MERGE_WARPS - 1) / MERGE_WARPS, 8 * n_sm);
+  return launch_pdl(paged_merge_kernel<D, F16, false>, dim3((unsigned)ctas), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(n_sm));
 }
 template <int D, bool F16, bool SPARSE>
 cudaError_t launch_rows(const PagedParams& p, int rows, const SmallMaps& maps, int n_sm, cudaStream_t stream) {
@@ -829,9 +834,9 @@ cudaError_t launch_typed(const PagedParams& p, bool fp16, int rows, const SmallM
 
 }  // namespace
 
-uint64_t paged_small_partial_bytes(int d, int n_sm) {
+uint64_t paged_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens) {
   // (twice the CTAs, at most 32 rows each, or once and 64)
-  return cut_bytes(n_sm) + (uint64_t)max_slots(n_sm) * 32 * (d + 2) * 4;
+  return cut_bytes(n_tokens, Hkv) + (uint64_t)max_slots(n_sm) * 32 * (d + 2) * 4;
 }
 
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {

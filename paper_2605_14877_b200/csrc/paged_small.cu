@@ -1,6 +1,7 @@
 // Attention of few query rows over a paged cache (decode, drafted tokens) and over selected pages, on warp-level MMA.
 //
-// A row tile is tile_tokens consecutive tokens of a request times the G query heads of one kv head, up to 32 rows (64 over selected pages); a unit is a row tile
+// A row tile is tile_tokens consecutive tokens of a request times the G query heads of one kv head, up to 32 rows (64 over selected pages; where a
+// request has more, several of 16); a unit is a row tile
 // of one request and kv head, its keys come page by page.  What bounds it is the reading of K and V, so the work is cut by pages, not by
 // requests: a unit of more than S pages is cut into equal pieces of at most S, S such that every CTA takes about PER_CTA pieces, and CTAs
 // take pieces from a counter until none is left (dealt out beforehand in equal shares, the SMs with the longest way to memory decided when
@@ -843,7 +844,7 @@ cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& po
   // rows of a tile: up to 16, 32 or 64
   const int tokens = p.sel ? 1 : std::max(1, p.max_new);
   const int64_t wanted = (int64_t)tokens * p.G;
-  // (33 to 48 rows come in tiles of 16: 42 rows, 96 units, 17.5 us against 21.0 in tiles of 32)
+  // (more than 32 rows come in tiles of 16: 42 rows, 96 units, 17.5 us against 21.0 in tiles of 32)
   const int rows = wanted <= 16 || (wanted > 32 && !p.sel && p.G <= 16) ? 16 : wanted <= 32 || !p.sel ? 32 : 64;
   PagedParams q = p;
   q.tile_tokens = p.sel ? 1 : rows / p.G;

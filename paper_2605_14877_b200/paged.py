@@ -38,6 +38,7 @@ class PagedCache:
         self.state = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=self.device)
         self.other_state = new(4)
         self.lengths = new(rows)                       # tokens of every row
+        self.at_most = [0] * rows                      # ... as far as the host knows: more where rows sat a step out
         self.workspace: Optional[torch.Tensor] = None
 
     def begin(self, new: Sequence[int]) -> Step:
@@ -50,7 +51,10 @@ class PagedCache:
         hk.heatkv_paged_tables(count, self.lengths, self.free, self.state, self.other_state, self.table, q_begin, kv_len, slots, positions)
         self.state, self.other_state = self.other_state, self.state
         self.lengths = torch.where(kv_len > 0, kv_len, self.lengths)
-        step = Step(hk.PagedBatch.make(q_begin, kv_len, self.table, tokens, longest), slots, positions)
+        self.at_most = [a + n for a, n in zip(self.at_most, new)]
+        # the calls get no more of the table than may be in use: its width is what they know of lengths beforehand
+        pages = min(max(-(-max(self.at_most) // hk.PAGE_TOKENS), 1), self.table.shape[1])
+        step = Step(hk.PagedBatch.make(q_begin, kv_len, self.table[:, :pages], tokens, longest), slots, positions)
         need = hk.heatkv_paged_workspace_bytes(self.pools[0], step.batch, self.n_heads)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
@@ -76,3 +80,4 @@ class PagedCache:
         hk.heatkv_paged_release(self.lengths, keep, self.table, self.free, self.state, self.other_state)
         self.state, self.other_state = self.other_state, self.state
         self.lengths = torch.minimum(self.lengths, keep)
+        self.at_most = [min(a, n) for a, n in zip(self.at_most, lengths)]

@@ -306,6 +306,24 @@ def test_attention_with_a_wrong_longest_request(hk, name, max_new):
     _check(out, lse, q, k, v, lens, table, q_begin, 4, True, 1 / math.sqrt(128), "bf16")
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(16, 16, 128, "bf16"), (32, 8, 128, "fp16"), (28, 4, 64, "bf16"), (5, 5, 64, "fp16"), (132, 4, 128, "bf16")])
+@pytest.mark.parametrize("name", ["one_key", "one_of_each", "no_keys", "drafts", "more_new_than_tokens", "short_prompts"])
+def test_attention_of_small_calls_as_if_large(hk, name, H, Hkv, d, dtype, causal):
+    """Few rows and short requests on the kernel that large calls take."""
+    lens = LENS[name]
+    rng, g = np.random.default_rng(len(name)), torch.Generator("cuda").manual_seed(len(name))
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, Hkv, d, DTYPES[dtype], spare=2)
+    b.max_new = 1 << 16
+    q = torch.empty(b.n_tokens, H, d, dtype=DTYPES[dtype], device="cuda").normal_(generator=g)
+    out, lse = torch.full_like(q, 7.0), torch.full((b.n_tokens, H), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws, causal=causal)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, causal, 1 / math.sqrt(d), dtype)
+    assert (out[q_begin[-1]:] == 7.0).all()
+
+
 @pytest.mark.parametrize("name", ["decode", "chunk_behind"])
 def test_attention_strides_streams_and_shifted_maxima(hk, name):
     """q inside a QKV tensor, out with a gap between heads, another stream than the tensors', and logits whose maximum rises by

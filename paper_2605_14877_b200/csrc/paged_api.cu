@@ -177,12 +177,14 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
   // Up to 32 rows of the longest request: the warp-level kernel.  24 requests of 2000 tokens: 12 rows 44 us against 56 on the tensor-memory
   // kernel, 21 rows 33 and 40, 32 rows 82 and 88, 36 rows 64 and 56, 63 rows 55 and 40.  Up to 48 rows, too, where there are fewer units
   // than SMs (42 rows, 96 units of up to 2660 tokens: 18 and 34 us; 256 units of 1000 tokens: 56 and 46).
-  // And up to eight tiles of 16 rows where there is little to do in all: a tile of `table_pages` pages weighs six more (its own beginning and end).  One request
-  // of 8 kv heads, 14 new tokens of 4 heads each behind 500 or 8000: 10 and 25 us, 22 and 53 on the tensor-memory kernel; 4 requests of 28 behind 1000
-  // (weight 5152) 25 and 24, 16 of 20 behind 300 (7040) 19 and 16, 16 of 28 (10 752) 32 and 17; 150 shapes measured, none up to 6000 loses more than 4 %.
+  // And any number of tiles of 16 rows where there is little to do in all: a tile of `table_pages` pages weighs six more (its own beginning and
+  // end).  One request of 8 kv heads with 4 heads each, 14 new tokens behind 500 or 8000: 10 and 25 us, 22 and 53 on the tensor-memory kernel; a
+  // prompt of 100: 8 and 17; two kv heads, a prompt of 400 (weight 2600): 13 and 23, 100 behind 1500 with 8 heads each (3100): 19 and 28; 4 requests of 28
+  // behind 1000 (5152) 25 and 24, 16 of 20 behind 300 (7040) 19 and 16.  Of 250 shapes measured none up to 6000 loses more than 4 %.
   const int64_t rows = (int64_t)p.max_new * p.G, units = (int64_t)p.n_seq * p.Hkv;
-  const int64_t tiles = p.G <= 16 ? ((int64_t)p.max_new + 16 / p.G - 1) / (16 / p.G) : 9;
-  const bool few = rows <= 32 || (rows <= 48 && p.G <= 16 && units < dev.n_sm) || (tiles <= 8 && units * tiles * ((int64_t)p.table_pages + 6) <= 6000);
+  const int64_t tiles = p.G <= 16 ? ((int64_t)p.max_new + 16 / p.G - 1) / (16 / p.G) : 0;
+  const bool little = units <= 6000 && tiles <= 6000 && units * tiles * ((int64_t)p.table_pages + 6) <= 6000;
+  const bool few = rows <= 32 || (p.G <= 16 && ((rows <= 48 && units < dev.n_sm) || little));
   return done((few ? launch_paged_small : launch_paged_tc)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 

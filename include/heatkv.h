@@ -442,7 +442,8 @@ typedef struct {                 /* one layer's pool                            
 } heatkv_paged_pool;
 
 typedef struct {                 /* the requests of a step                                                             */
-  const int32_t* q_begin;        /* DEVICE [n_seq + 1] first new token of every request, and their number              */
+  const int32_t* q_begin;        /* DEVICE [n_seq + 1] first new token of every request, and the last one's end; the first may be
+                                    other than 0 (a part of a larger batch's requests: its pointers moved on, n_tokens as it was) */
   const int32_t* kv_len;         /* DEVICE [n_seq] tokens of the request, the new ones included; 0: none               */
   const int32_t* block_table;    /* DEVICE [n_seq][table_pages] page numbers, rows table_stride elements apart         */
   int64_t table_stride;
@@ -495,8 +496,8 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
  * statistics in 32 bits, probabilities rounded to 16 before the product with V.
  *   q DEVICE [n_tokens][n_heads][d], out the same shape, not the same memory; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
  *   lse DEVICE fp32 [n_tokens][n_heads], the natural logarithm of the sum of exponentials, or NULL
- * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows past q_begin[n_seq] are left
- * as they are.  n_heads / n_kv_heads at most 128. */
+ * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows in front of q_begin[0] and
+ * past q_begin[n_seq] are left as they are.  n_heads / n_kv_heads at most 128. */
 int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
                            uint64_t workspace_bytes, void* stream);
@@ -505,7 +506,8 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
  * page is among them) and, up to n_select in all, those between whose summary scores highest against the query's: the sum of the
  * group's query heads in 32 bits, in head order, as 8-bit codes like a page's; score = (whole-number dot product of the codes) * the
  * page's scale, ties to the lower page.  sel DEVICE int32 [n_tokens][n_kv_heads][n_select]: page places in the request's table row,
- * ascending, -1 after the last.  n_select >= sink + local.  Pages between must have summaries (they are whole by then). */
+ * ascending, -1 after the last (nothing but -1 for tokens that are no request's).  n_select >= sink + local.  Pages between must have
+ * summaries (they are whole by then). */
 int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                         const heatkv_token_strides* st, int sink, int local, int n_select, int32_t* sel, void* stream);
 

@@ -358,8 +358,9 @@ __global__ void __launch_bounds__(ROWS_THREADS, 4) select_rows_kernel(const __gr
   while (t < t_end) {                                         // the requests that the 16 tokens belong to
     while (seq + 1 < p.n_seq && p.q_begin[seq + 1] <= t) ++seq;
     const int b = p.q_begin[seq], e = p.q_begin[seq + 1], kv = p.kv_len[seq];
-    const bool nobody = t < b || t >= e;
-    const int t_next = nobody ? t_end : min(e, t_end);
+    // tokens in front of the first request and behind the last one are nobody's (all requests between begin where the one before ends)
+    const bool before = t < b, nobody = before || t >= e;
+    const int t_next = before ? min(b, t_end) : nobody ? t_end : min(e, t_end);
     const Range widest(p, nobody ? -1 : kv - e + t_next - 1);
     const int32_t* table = p.block_table + seq * p.table_stride;
     // scores of all rows against the request's pages, 8 pages a product

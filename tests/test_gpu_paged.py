@@ -616,3 +616,48 @@ def test_a_host_tensor_is_refused(hk):
     with pytest.raises(ValueError, match="more than one device"):
         hk.PagedBatch.make(_i32([0, 3]), _i32([3]), _i32([[0]]).cpu(), 3, 3)
     hk.heatkv_paged_store(pool, k, k, slots)
+
+
+# ------------------------------------------------------------------------------------------------ batches that begin behind token 0
+
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(16, 16, 128, "bf16"), (14, 2, 64, "fp16")])
+@pytest.mark.parametrize("max_new", [1, 1000])
+@pytest.mark.parametrize("ahead", [1, 5, 37])
+@pytest.mark.parametrize("name", ["decode", "no_keys", "chunk_behind", "mixed"])
+def test_batch_that_begins_behind_token_0(hk, name, ahead, max_new, H, Hkv, d, dtype):
+    """q_begin[0] > 0 (the later requests of a larger batch): every form of selection and attention takes the requests' tokens and leaves those
+    in front of them as they are."""
+    lens = LENS[name]
+    rng, g = np.random.default_rng(ahead), torch.Generator("cuda").manual_seed(ahead)
+    dt, sink, local, n_select = DTYPES[dtype], 1, 2, 30
+    pool, b0, table, q_begin, k, v, code, scale = _filled(hk, g, rng, lens, Hkv, d, dt, spare=2)
+    for i, (_, kv) in enumerate(lens):
+        _summaries(k, code, scale, table[i, : kv // PAGE])
+    q_begin = q_begin + ahead
+    T, G = b0.n_tokens + ahead, H // Hkv
+    b = hk.PagedBatch.make(_i32(q_begin), *b0.tensors[1:], T, max_new)
+    q = torch.empty(T, H, d, dtype=dt, device="cuda").normal_(generator=g)
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype)
+    assert (out[:ahead] == 7.0).all() and (out[q_begin[-1]:] == 7.0).all()
+    sel = torch.full((T, Hkv, n_select), -9, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, sink, local)
+    got, qf, cn, sn = sel.cpu().numpy(), _np(q), code.cpu().numpy(), scale.cpu().numpy()
+    chosen = []
+    for i, (n, kv) in enumerate(lens):
+        pages = table[i, : -(-kv // PAGE)]
+        mask = np.zeros((Hkv, n, len(pages)), dtype=bool)
+        for t in range(n):
+            for h in range(Hkv):
+                want = P.select(qf[q_begin[i] + t, h * G:(h + 1) * G], cn[pages, h], sn[pages, h], kv - n + t, sink, local, n_select) if kv - n + t >= 0 else []
+                assert got[q_begin[i] + t, h].tolist() == want + [-1] * (n_select - len(want)), (i, t, h)
+                mask[h, t, want] = True
+        chosen.append(mask)
+    assert (got[:ahead] == -1).all() and (got[q_begin[-1]:] == -1).all()
+    out.fill_(7.0), lse.fill_(7.0)
+    hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype, chosen)
+    assert (out[:ahead] == 7.0).all() and (out[q_begin[-1]:] == 7.0).all() and (lse[:ahead] == 7.0).all()

@@ -27,7 +27,7 @@ constexpr int PAGED_WS_PARTIALS = (PAGED_WS_HEAD_WORDS + PAGED_WS_CTRS * 8) * 4;
 
 struct PagedDevice {
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
-  int n_sm = 0;
+  int n_sm = 0, index = 0;
 };
 
 struct TablesParams {
@@ -94,24 +94,33 @@ uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, i
 bool paged_tc_takes_lists(int G, int n_sel, int table_pages);
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 
+// A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.  The driver's encoder wants a current context, and a thread that has made
+// no CUDA call yet has none: where it fails the runtime makes the device's own current, and the map is asked for once more.
+inline bool paged_encode(const PagedDevice& dev, CUtensorMap* m, void* base, int dtype, const cuuint64_t* dims, const cuuint64_t* strides,
+                         const cuuint32_t* box) {
+  const cuuint32_t unit[4] = {1, 1, 1, 1};
+  auto made = [&] {
+    return dev.encode(m, dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box,
+                      unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  return made() || (cudaSetDevice(dev.index) == cudaSuccess && made());
+}
+
 // boxes of 64 columns x 64 rows of one page and head: (column, row, head, page)
 inline bool paged_encode_pool(const PagedDevice& dev, CUtensorMap* m, void* base, const heatkv_paged_pool& pool) {
   const cuuint64_t dims[4] = {(cuuint64_t)pool.d, PAGE, (cuuint64_t)pool.n_kv_heads, (cuuint64_t)pool.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)pool.row_stride * 2, (cuuint64_t)pool.head_stride * 2, (cuuint64_t)pool.page_stride * 2};
-  const cuuint32_t box[4] = {64, PAGE, 1, 1}, unit[4] = {1, 1, 1, 1};
-  return dev.encode(m, pool.dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base,
-                    dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[4] = {64, PAGE, 1, 1};
+  return paged_encode(dev, m, base, pool.dtype, dims, strides, box);
 }
 
 // query rows: boxes of 64 columns x the G heads of a kv head x tile_tokens tokens: (column, head, token)
 inline bool paged_encode_q(const PagedDevice& dev, CUtensorMap* m, const PagedParams& p, const heatkv_paged_pool& pool) {
   const cuuint64_t dims[4] = {(cuuint64_t)pool.d, (cuuint64_t)p.H, (cuuint64_t)p.n_tokens, 1};
   const cuuint64_t strides[3] = {(cuuint64_t)p.q_head * 2, (cuuint64_t)p.q_tok * 2, 16};
-  const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens, 1}, unit[4] = {1, 1, 1, 1};
-  return dev.encode(m, pool.dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
-                    const_cast<void*>(p.q), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens, 1};
+  return paged_encode(dev, m, const_cast<void*>(p.q), pool.dtype, dims, strides, box);
 }
 
 }  // namespace heatkv

@@ -661,3 +661,31 @@ def test_batch_that_begins_behind_token_0(hk, name, ahead, max_new, H, Hkv, d, d
     assert hk.heatkv_paged_status(ws) == 0
     _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype, chosen)
     assert (out[:ahead] == 7.0).all() and (out[q_begin[-1]:] == 7.0).all() and (lse[:ahead] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------------ threads
+
+@pytest.mark.parametrize("max_new", [1, 1 << 16])
+def test_the_first_cuda_call_of_a_thread(hk, max_new):
+    """A thread that has made no CUDA call of its own yet attends (by either kernel) as any other does."""
+    import threading
+    lens = [(2, 300), (1, 65)]
+    rng, g = np.random.default_rng(11), torch.Generator("cuda").manual_seed(11)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, 128, torch.bfloat16)
+    b.max_new = max_new
+    q = torch.empty(b.n_tokens, 4, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_tokens, 4, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 4), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    raised = []
+
+    def attend():
+        try:
+            hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+        except Exception as e:                             # noqa: BLE001
+            raised.append(e)
+    thread = threading.Thread(target=attend)
+    thread.start()
+    thread.join()
+    assert not raised, raised
+    _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(128), "bf16")

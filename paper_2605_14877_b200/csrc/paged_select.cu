@@ -534,9 +534,11 @@ __global__ void __launch_bounds__(ROWS_THREADS, 4) select_rows_kernel(const __gr
 }  // namespace
 
 cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cudaStream_t stream) {
-  auto go = [&](auto kernel, int64_t units, int threads, size_t smem, int ctas, auto... more) {
+  // (a kernel's limit is the process's: always set to the most that any call takes, or another thread's smaller call, between this one's
+  // limit and its launch, would have the launch refused)
+  auto go = [&](auto kernel, int64_t units, int threads, size_t smem, int most, int ctas, auto... more) {
     if (smem > 24 * 1024) {
-      const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
       if (rc != cudaSuccess) return rc;
     }
     cudaLaunchConfig_t cfg = {};
@@ -555,19 +557,22 @@ cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cu
     return cudaLaunchKernelEx(&cfg, kernel, p, more...);
   };
   if (max_new >= SEL_ROWS_FROM && p.table_pages <= SEL_ROWS_PAGES) {
-    const int pitch = (p.table_pages + 7) / 8 * 8 + 4;        // (eight pages a product may run past the last; odd multiples of 16 bytes spread the rows over the banks)
+    // (eight pages a product may run past the last; odd multiples of 16 bytes spread the rows over the banks)
+    auto pitch_of = [](int pages) { return (pages + 7) / 8 * 8 + 4; };
+    const int pitch = pitch_of(p.table_pages), most = SEL_ROWS * pitch_of(SEL_ROWS_PAGES) * 4;
     const int64_t units = (int64_t)((p.n_tokens + SEL_ROWS - 1) / SEL_ROWS) * p.Hkv;
     const size_t smem = (size_t)SEL_ROWS * pitch * 4;
-    return p.d == 128 ? go(select_rows_kernel<128>, units, ROWS_THREADS, smem, 1, pitch) : go(select_rows_kernel<64>, units, ROWS_THREADS, smem, 1, pitch);
+    return p.d == 128 ? go(select_rows_kernel<128>, units, ROWS_THREADS, smem, most, 1, pitch) : go(select_rows_kernel<64>, units, ROWS_THREADS, smem, most, 1, pitch);
   }
   const int64_t units = (int64_t)p.n_tokens * p.Hkv;
   const size_t smem = ((size_t)p.table_pages + 3) / 4 * 16;
+  constexpr int most = (PAGED_MAX_SELECT_PAGES + 3) / 4 * 16;
   // few tokens: more of a context's codes on their way at once (without a cluster 1024 threads: 16 requests of 8 kv heads 14.9 us, 15.4 with 256)
   int ctas = 8;
   while (ctas > 1 && units * ctas > n_sm) ctas /= 2;
-  if (ctas > 1) return p.d == 128 ? go(select_kernel<128, 512, true>, units, 512, smem, ctas) : go(select_kernel<64, 512, true>, units, 512, smem, ctas);
-  if (units <= n_sm) return p.d == 128 ? go(select_kernel<128, 1024, false>, units, 1024, smem, 1) : go(select_kernel<64, 1024, false>, units, 1024, smem, 1);
-  return p.d == 128 ? go(select_kernel<128, 256, false>, units, 256, smem, 1) : go(select_kernel<64, 256, false>, units, 256, smem, 1);
+  if (ctas > 1) return p.d == 128 ? go(select_kernel<128, 512, true>, units, 512, smem, most, ctas) : go(select_kernel<64, 512, true>, units, 512, smem, most, ctas);
+  if (units <= n_sm) return p.d == 128 ? go(select_kernel<128, 1024, false>, units, 1024, smem, most, 1) : go(select_kernel<64, 1024, false>, units, 1024, smem, most, 1);
+  return p.d == 128 ? go(select_kernel<128, 256, false>, units, 256, smem, most, 1) : go(select_kernel<64, 256, false>, units, 256, smem, most, 1);
 }
 
 }  // namespace heatkv

@@ -802,18 +802,21 @@ uint64_t cut_bytes(int n_tokens, int Hkv) { return ((uint64_t)n_tokens * Hkv * 8
 template <int D, int MT, int GROUPS, bool F16, bool SPARSE>
 cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaStream_t stream) {
   using L = SmallLayout<D, MT, GROUPS>;
-  const uint32_t fixed = L::FIXED + (SPARSE ? 0 : (p.n_seq + 1) * 8) + 1024;
+  auto fixed_of = [](int n_seq) { return (int)(L::FIXED + (SPARSE ? 0 : (n_seq + 1) * 8) + 1024); };
+  const int fixed = fixed_of(p.n_seq);
   SmallParams sp;
   sp.a = p;
   sp.counter = p.counters;
   sp.cuts = reinterpret_cast<int2*>(p.partials);
   sp.a.partials = p.partials + cut_bytes(p.n_tokens, p.Hkv) / 4;
   // as many pages under way as the CTA's share of an SM's shared memory holds
-  const int room = (L::CTAS == 2 ? 113 : 226) * 1024 - 768;
-  sp.stages = std::max(2, std::min<int>(MAX_STAGES, (room - (int)fixed) / (int)(2 * L::TILE)));
-  const int smem = (int)fixed + sp.stages * 2 * (int)L::TILE;
+  constexpr int room = (L::CTAS == 2 ? 113 : 226) * 1024 - 768, stage = 2 * (int)L::TILE;
+  sp.stages = std::max(2, std::min(MAX_STAGES, (room - fixed) / stage));
+  const int smem = fixed + sp.stages * stage;
+  // (the kernel's limit is the process's: always the most that any call takes, as another thread may set it between this line and the launch)
+  const int most = std::max(room, fixed_of(PAGED_MAX_SEQ) + 2 * stage);
   auto kernel = paged_small_kernel<D, MT, GROUPS, F16, SPARSE>;
-  cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   if (rc != cudaSuccess) return rc;
   rc = launch_pdl(kernel, dim3(n_sm * L::CTAS), dim3(L::THREADS), smem, stream, sp, maps);
   // nothing can have been cut where no unit has more pages

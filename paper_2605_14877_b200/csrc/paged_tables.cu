@@ -341,7 +341,8 @@ cudaError_t launch_paged_tables(const TablesParams& p, cudaStream_t stream) {
   const int grid = (int)std::min<int64_t>(296, std::max<int64_t>(1, (work + TT * 4 - 1) / (TT * 4)));
   const size_t smem = (4 * (size_t)p.n_seq + 2) * sizeof(int32_t);
   if (smem > 48 * 1024) {
-    const cudaError_t rc = cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (the most that any call takes: the limit is the process's, and another thread may set it before this launch)
+    const cudaError_t rc = cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * PAGED_MAX_SEQ + 2) * (int)sizeof(int32_t));
     if (rc != cudaSuccess) return rc;
   }
   return launch_pdl(tables_kernel, dim3(grid), dim3(TT), smem, stream, p);

@@ -689,3 +689,64 @@ def test_the_first_cuda_call_of_a_thread(hk, max_new):
     thread.join()
     assert not raised, raised
     _check(out, lse, q, k, v, lens, table, q_begin, 2, True, 1 / math.sqrt(128), "bf16")
+
+
+def _in_two_threads(calls, rounds):
+    """calls[i]() again and again in thread i, all at once; what they raised."""
+    import threading
+    raised, start = [], threading.Barrier(len(calls))
+
+    def loop(call):
+        stream = torch.cuda.Stream()
+        start.wait()
+        try:
+            for _ in range(rounds):
+                call(stream)
+        except Exception as e:                             # noqa: BLE001  (reported by the caller)
+            raised.append(e)
+        stream.synchronize()
+    threads = [threading.Thread(target=loop, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    return raised
+
+
+@pytest.mark.parametrize("what", ["tables", "attention", "select", "select_chunk"])
+def test_calls_of_two_threads(hk, what):
+    """Calls of different sizes from two threads, each with buffers and a stream of its own: every one is made, and gives what it gives alone."""
+    g = torch.Generator("cuda").manual_seed(6)
+    Hkv, d = 2, 128
+    pool, *_ = _pool(hk, g, 8, Hkv, d, torch.bfloat16, fill=0.0)
+    calls, results = [], []
+    for n, width in ((4000, 6000), (3300, 3200)) if what == "tables" else ((600, 3000), (20, 2000)) if what == "select_chunk" else ((1000, 24000), (20, 9000)):
+        if what == "tables":
+            out = [_i32([0] * 4), torch.full((n, 4), -1, dtype=torch.int32, device="cuda"), _i32([0] * (n + 1)), _i32([0] * n), _i32([0] * n)]
+            args = _i32([1] * n), _i32([0] * n), _i32(range(n)), _i32([0, n, 0, 0])
+            calls.append(lambda s, a=args, o=out: hk.heatkv_paged_tables(*a, *o, stream=s))
+            results.append(out)
+            continue
+        rows = 20 if what == "select_chunk" else 1
+        kv = width * PAGE if what != "attention" else 8 * PAGE - 5
+        table = _i32([list(range(8)) + [-1] * (width - 8)] * (n // rows)) if what != "attention" else _i32([list(range(8))] * n)
+        b = hk.PagedBatch.make(_i32(range(0, n + 1, rows)), _i32([kv] * (n // rows)), table, n, rows)
+        q = torch.empty(n, 4, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        if what == "attention":
+            out = torch.zeros_like(q)
+            ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 4), dtype=torch.uint8, device="cuda")
+            calls.append(lambda s, b=b, q=q, o=out, w=ws: hk.heatkv_paged_attention(pool, b, q, o, None, w, stream=s))
+        else:
+            out = torch.zeros(n, Hkv, 12, dtype=torch.int32, device="cuda")
+            calls.append(lambda s, b=b, q=q, o=out: hk.heatkv_paged_select(pool, b, q, o, 1, 2, stream=s))
+        results.append([out])
+    alone = []
+    torch.cuda.synchronize()
+    for call, out in zip(calls, results):
+        call(None)
+        alone.append([x.clone() for x in out])
+    torch.cuda.synchronize()
+    raised = _in_two_threads(calls, 1500)
+    assert not raised, raised
+    for a, r in zip(alone, results):
+        assert all(torch.equal(x, y) for x, y in zip(a, r))

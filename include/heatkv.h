@@ -496,8 +496,9 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
  * statistics in 32 bits, probabilities rounded to 16 before the product with V.
  *   q DEVICE [n_tokens][n_heads][d], out the same shape, not the same memory; strides NULL: packed.  sm_scale <= 0: 1 / sqrt(d)
  *   lse DEVICE fp32 [n_tokens][n_heads], the natural logarithm of the sum of exponentials, or NULL
- * A row that sees no key (kv_len 0, or shorter than the new tokens) is zero, its lse minus infinity.  Rows in front of q_begin[0] and
- * past q_begin[n_seq] are left as they are.  n_heads / n_kv_heads at most 128. */
+ * A row that sees no key (kv_len 0, or shorter than the new tokens), or whose logits are all minus infinity, is zero, its lse minus
+ * infinity.  NaN in a query row, or a logit of plus infinity, makes that row and its lse NaN, and no other row.  Rows in front of
+ * q_begin[0] and past q_begin[n_seq] are left as they are.  n_heads / n_kv_heads at most 128. */
 int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
                            uint64_t workspace_bytes, void* stream);

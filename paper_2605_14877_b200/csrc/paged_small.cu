@@ -199,14 +199,14 @@ __device__ __forceinline__ RowSum<D> sum_parts(const Parts<D>& p, int begin, int
 template <int D, bool F16>
 __device__ __forceinline__ void put_row(const PagedParams& p, const RowSum<D>& r, int tok, int hd, int lane) {
   constexpr int N = D / 32;
-  const float inv = r.l > 0.f ? 1.f / r.l : 0.f;
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;                  // (0: no key; a sum that is NaN stays one, here and in the logarithm)
   uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head + lane * N);
   if (N == 4) {
     *reinterpret_cast<uint2*>(dst) = make_uint2(pack16<F16>(r.acc[0] * inv, r.acc[1] * inv), pack16<F16>(r.acc[N - 2] * inv, r.acc[N - 1] * inv));
   } else {
     *dst = pack16<F16>(r.acc[0] * inv, r.acc[1] * inv);
   }
-  if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = r.l > 0.f ? (r.top + log2f(r.l)) * 0.6931471805599453f : -INFINITY;
+  if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = r.l == 0.f ? -INFINITY : (r.top + log2f(r.l)) * 0.6931471805599453f;
 }
 
 template <int D, int MT, int GROUPS, bool F16, bool SPARSE>
@@ -719,12 +719,12 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
         const float l = (t[0] + t[16 * MT]) + (t[32 * MT] + t[48 * MT]);
         const int col = quarter * (D / 4) + qd * 2;
         if (out_slot < 0) {
-          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const float inv = l == 0.f ? 0.f : 1.f / l;
           const int64_t tok = tok0 + row_tok[m][i], hd = head0 + row_head[m][i];
           uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + tok * p.o_tok + hd * p.o_head + col);
 #pragma unroll
           for (int n = 0; n < NT; ++n) dst[n * 4] = pack16<F16>(o[m][n][2 * i] * inv, o[m][n][2 * i + 1] * inv);
-          if (p.lse && quarter == 0 && qd == 0) p.lse[tok * p.H + hd] = l > 0.f ? (m_ref[m][i] + log2f(l)) * 0.6931471805599453f : -INFINITY;
+          if (p.lse && quarter == 0 && qd == 0) p.lse[tok * p.H + hd] = l == 0.f ? -INFINITY : (m_ref[m][i] + log2f(l)) * 0.6931471805599453f;
         } else {
 #pragma unroll
           for (int n = 0; n < NT; ++n) __stcg(reinterpret_cast<float2*>(part + row * D + col + n * 8), make_float2(o[m][n][2 * i], o[m][n][2 * i + 1]));

@@ -1051,7 +1051,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             __syncwarp();
           };
           auto finish = [&](float m, float l) {                    // 1 / sum, and the row's logarithm
-            const bool any = SPARSE ? l > 0.5f : sees > 0;             // (the key that set the reference counts 1)
+            // the key that set the reference counts 1, so a sum below that has no key, or none with a weight; one that is NaN stays NaN
+            const bool any = !(l <= 0.5f);
             if (p.lse && valid) p.lse[(int64_t)tok * p.H + hd] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             const float inv = any ? 1.f / l : 0.f;
             __syncwarp();                                          // the loads of tensor memory that follow are the whole warp's

@@ -750,3 +750,84 @@ def test_calls_of_two_threads(hk, what):
     assert not raised, raised
     for a, r in zip(alone, results):
         assert all(torch.equal(x, y) for x, y in zip(a, r))
+
+
+# ------------------------------------------------------------------------------------------------ NaN and infinity in a query
+
+@pytest.mark.parametrize("form", ["small", "large", "selected", "selected_chunk"])
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "bf16"), (64, "fp16")])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_that_is_no_number_shows(hk, form, d, dtype, bad):
+    """A row whose query holds NaN or an infinity is NaN, its logarithm too: minus infinity would say that it saw no key.  Rows beside it and
+    rows without keys are as ever."""
+    lens = [(9, 700), (1, 65), (3, 0), (20, 20), (1, 5000)]
+    Hkv, G, n_select = 2, 4, 96
+    rng, g = np.random.default_rng(8), torch.Generator("cuda").manual_seed(8)
+    dt = DTYPES[dtype]
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, Hkv, d, dt)
+    for x in k:                                            # (an infinity times keys of either sign is minus infinity for half of them)
+        x[..., 0].abs_()
+    T, H = b.n_tokens, Hkv * G
+    q = torch.empty(T, H, d, dtype=dt, device="cuda").normal_(generator=g)
+    clean = q.clone()
+    hit = [(q_begin[0] + 4, 5), (q_begin[1], 0), (q_begin[2] + 1, 2), (q_begin[3], 7), (q_begin[3] + 19, 1), (q_begin[4], 3)]
+    for t, h in hit:
+        q[t, h, 0] = bad
+    b.max_new = 1 << 16 if form in ("large", "selected_chunk") else 1
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+    chosen = None
+    if form in ("small", "large"):
+        hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    else:
+        n_select = 2048 // (2 * 32) if form == "selected_chunk" else n_select
+        sel = np.tile(np.concatenate([np.arange(n_select - 1), [-1]]), (T, Hkv, 1))
+        if form == "selected_chunk":                       # as many lists as it takes for them to be merged
+            hk_rows = 24576 // (Hkv * n_select) + 1
+            pad = max(hk_rows - T, 0)
+            b = hk.PagedBatch.make(*b.tensors, T + pad, 1 << 16)
+            q, sel = torch.cat([q, q.new_zeros(pad, H, d)]), np.concatenate([sel, np.full((pad, Hkv, n_select), -1)])
+            clean = torch.cat([clean, clean.new_zeros(pad, H, d)])
+            out, lse = torch.full_like(q, 7.0), torch.full((T + pad, H), 7.0, device="cuda")
+            ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+        chosen = [np.broadcast_to(np.arange(-(-kv // PAGE)) < n_select - 1, (Hkv, n, -(-kv // PAGE))) for n, kv in lens]
+        hk.heatkv_paged_sparse_attention(pool, b, q, _i32(sel), out, lse, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    for t, h in hit:
+        if q_begin[2] <= t < q_begin[3]:                   # no keys
+            assert (out[t, h] == 0).all() and lse[t, h].item() == -math.inf
+        else:
+            assert out[t, h].isnan().all() and lse[t, h].isnan(), (t, h, out[t, h, :4], lse[t, h])
+        out[t, h], lse[t, h] = 0.0, 0.0                    # (the rest against 64 bits; these rows' queries see nothing there)
+    for t, h in hit:
+        clean[t, h] = 0
+    rest = torch.ones(T, H, dtype=torch.bool, device="cuda")
+    for t, h in hit:
+        rest[t, h] = False
+    # the rows beside them: the same bits as without the bad ones
+    want, want_lse = torch.full_like(out, 7.0), torch.full_like(lse, 7.0)
+    if chosen is None:
+        hk.heatkv_paged_attention(pool, b, clean, want, want_lse, ws)
+    else:
+        hk.heatkv_paged_sparse_attention(pool, b, clean, _i32(sel), want, want_lse, ws)
+    _check(want[:T], want_lse[:T], clean[:T], k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(d), dtype, chosen)
+    assert torch.equal(out[:T][rest], want[:T][rest]) and torch.equal(lse[:T][rest], want_lse[:T][rest])
+
+
+@pytest.mark.parametrize("form", ["small", "large"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_of_minus_infinity(hk, form, d):
+    """A row all of whose logits are minus infinity: no weight anywhere, zero and minus infinity, whichever kernel has it."""
+    lens = [(3, 200), (1, 3000)]
+    rng, g = np.random.default_rng(9), torch.Generator("cuda").manual_seed(9)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, d, torch.bfloat16)
+    k[..., 0] = 1.0
+    b.max_new = 1 << 16 if form == "large" else 1
+    q = torch.empty(4, 4, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    q[1, 2, 0] = q[3, 0, 0] = -math.inf
+    out, lse = torch.full_like(q, 7.0), torch.full((4, 4), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 4), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    for t, h in ((1, 2), (3, 0)):
+        assert (out[t, h] == 0).all() and lse[t, h].item() == -math.inf
+    assert out.isfinite().all() and lse.isfinite().sum() == 14

@@ -502,14 +502,13 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 }
 
 // 2^x for a pair on the FMA units: x = n + f with n = round(x), f in [-1/2, 1/2]; the polynomial of degree 4 that is nearest to 2^f there
-// (relative error 2.7e-6 with its 32-bit steps) gets n added to its exponent.  x is clamped at -125: keys that a row does not see arrive as
-// minus infinity and give 2^-125.
+// (relative error 2.7e-6 with its 32-bit steps) gets n added to its exponent.  Below -125, where the exponent would leave its range, the result
+// is zero: keys that a row does not see arrive as minus infinity, and times a value near the type's largest even 2^-125 would show.
 __device__ __forceinline__ void exp2_pair(uint64_t x, float& e0, float& e1) {
   constexpr float MAGIC = 12582912.f;                  // 1.5 * 2^23: the sum's low mantissa bits hold round(x)
   float x0, x1;
   unpack2(x, x0, x1);
-  const uint64_t xc = pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f)), magic = pack2(MAGIC, MAGIC);
-  const uint64_t t = add2(xc, magic), f = sub2(xc, sub2(t, magic));
+  const uint64_t magic = pack2(MAGIC, MAGIC), t = add2(x, magic), f = sub2(x, sub2(t, magic));
   uint64_t q = fma2(pack2(0.00957010221f, 0.00957010221f), f, pack2(0.0559178591f, 0.0559178591f));
   q = fma2(q, f, pack2(0.240247443f, 0.240247443f));
   q = fma2(q, f, pack2(0.693121791f, 0.693121791f));
@@ -517,8 +516,8 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& e0, float& e1) {
   float t0, t1, q0, q1;
   unpack2(t, t0, t1);
   unpack2(q, q0, q1);
-  e0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
-  e1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+  e0 = x0 >= -125.f ? __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23)) : 0.f;
+  e1 = x1 >= -125.f ? __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23)) : 0.f;
 }
 template <int D, bool F16, bool SPARSE>
 __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {

@@ -831,3 +831,25 @@ def test_logits_of_minus_infinity(hk, form, d):
     for t, h in ((1, 2), (3, 0)):
         assert (out[t, h] == 0).all() and lse[t, h].item() == -math.inf
     assert out.isfinite().all() and lse.isfinite().sum() == 14
+
+
+@pytest.mark.parametrize("max_new", [1, 1 << 16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_key_that_a_row_does_not_see_has_no_weight(hk, d, max_new):
+    """Values near the type's largest behind a row's own position leave it as it is: their weight is zero,
+    not merely small."""
+    lens = [(150, 300), (70, 70)]
+    rng, g = np.random.default_rng(10), torch.Generator("cuda").manual_seed(10)
+    pool, b, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, 2, d, torch.bfloat16)
+    b.max_new = max_new
+    for i, (n, kv) in enumerate(lens):                     # the last 40 tokens' values
+        for p in range(kv - 40, kv):
+            v[table[i, p // PAGE], :, p % PAGE] = 3e38
+    q = torch.empty(b.n_tokens, 4, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_tokens, 4, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, 4), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    # the requests without their last 40 tokens
+    short = [(n - 40, kv - 40) for n, kv in lens]
+    begin = [q_begin[0], q_begin[1]]
+    _check(out, lse, q, k, v, short, table, begin, 2, True, 1 / math.sqrt(d), "bf16")

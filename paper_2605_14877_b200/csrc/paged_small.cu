@@ -738,9 +738,9 @@ paged_small_kernel(const __grid_constant__ SmallParams sp, const __grid_constant
 
 // Partial results of a call: pieces of units of more than S pages, S at least pages / (CTAs * PER_CTA), so at most twice CTAs * PER_CTA
 // (a unit of x S pages, x > 1, has fewer than 2 x pieces).
-constexpr int MOST_CTAS = 240;                 // (SMs; at most twice as many CTAs)
-__host__ __device__ constexpr int max_slots(int n_sm) { return 2 * PER_CTA * 2 * n_sm; }
-static_assert(max_slots(MOST_CTAS) < 1 << 16, "pieces of a unit in 16 bits");
+constexpr int MOST_SMS = 240;                  // (at most two CTAs each)
+__host__ __device__ constexpr int max_slots(int ctas) { return 2 * PER_CTA * ctas; }
+static_assert(max_slots(2 * MOST_SMS) < 1 << 16, "pieces of a unit in 16 bits");
 
 // Adds up the parts of the rows whose units were cut, in page order: a CTA per row where the rows are few, else a warp.  What bounds it is a
 // chain of loads behind the end of the kernel before (cut, parts), and the start of its CTAs: one for every slot and row instead of one for 8 of
@@ -764,8 +764,11 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
     const int2 cut = __ldcg(sp.cuts + (int64_t)tok * p.Hkv + head);
     const int pieces = cut.y & 0xffff;
     parts.row = (cut.y >> 16) * p.G + hd - head * p.G;
-    // (rows that are nobody's have an entry of some call before, or none)
-    if (pieces < 2 || tok < begin_tok || tok >= end_tok || cut.x < 0 || cut.x + pieces > slots || parts.row >= slot_rows) continue;
+    // (Rows that are nobody's have an entry of some call before, or none; in a call that gave up, a request's own may be whatever the other
+    // kernel left there.  No such entry leads out of the workspace.)
+    if (tok < begin_tok || tok >= end_tok || pieces < 2 || pieces > slots || cut.x < 0 || cut.x > slots - pieces ||
+        (uint32_t)parts.row >= (uint32_t)slot_rows)
+      continue;
     parts.first = p.partials + cut.x * parts.pitch;
     if (!WIDE) {
       put_row<D, F16>(p, sum_parts<D>(parts, 0, pieces), tok, hd, lane);
@@ -822,9 +825,9 @@ cudaError_t launch(const PagedParams& p, const SmallMaps& maps, int n_sm, cudaSt
   // nothing can have been cut where no unit has more pages
   if (rc != cudaSuccess || (SPARSE ? p.n_sel : p.table_pages) <= FULL_CHUNK) return rc;
   const int64_t rows = (int64_t)p.n_tokens * p.H, pieces = (SPARSE ? p.n_sel : p.table_pages) / MIN_CHUNK;       // (of a unit, at most)
-  if (rows <= 8 * n_sm && pieces > AHEAD) return launch_pdl(paged_merge_kernel<D, F16, true>, dim3((unsigned)rows), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(n_sm));
+  if (rows <= 8 * n_sm && pieces > AHEAD) return launch_pdl(paged_merge_kernel<D, F16, true>, dim3((unsigned)rows), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(L::CTAS * n_sm));
   const int64_t ctas = std::min<int64_t>((rows + MERGE_WARPS - 1) / MERGE_WARPS, 8 * n_sm);
-  return launch_pdl(paged_merge_kernel<D, F16, false>, dim3((unsigned)ctas), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(n_sm));
+  return launch_pdl(paged_merge_kernel<D, F16, false>, dim3((unsigned)ctas), dim3(MERGE_WARPS * 32), 0, stream, sp, max_slots(L::CTAS * n_sm));
 }
 template <int D, bool F16, bool SPARSE>
 cudaError_t launch_rows(const PagedParams& p, int rows, const SmallMaps& maps, int n_sm, cudaStream_t stream) {
@@ -843,7 +846,7 @@ cudaError_t launch_typed(const PagedParams& p, bool fp16, int rows, const SmallM
 
 uint64_t paged_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens) {
   // (twice the CTAs, at most 32 rows each, or once and 64)
-  return cut_bytes(n_tokens, Hkv) + (uint64_t)max_slots(n_sm) * 32 * (d + 2) * 4;
+  return cut_bytes(n_tokens, Hkv) + (uint64_t)max_slots(2 * n_sm) * 32 * (d + 2) * 4;
 }
 
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {

@@ -853,3 +853,41 @@ def test_a_key_that_a_row_does_not_see_has_no_weight(hk, d, max_new):
     short = [(n - 40, kv - 40) for n, kv in lens]
     begin = [q_begin[0], q_begin[1]]
     _check(out, lse, q, k, v, short, table, begin, 2, True, 1 / math.sqrt(d), "bf16")
+
+
+# ------------------------------------------------------------------------------------------------ calls that give up
+
+@pytest.mark.parametrize("G,max_new", [(4, 1), (64, 1)])
+def test_calls_on_a_workspace_whose_status_is_set(hk, G, max_new):
+    """After a wait has run out, calls on the workspace end at once whatever the kernels before have left in it; zeroed, it serves again."""
+    lens = [(1, 3000), (3, 700), (1, 64 * 40)]
+    Hkv, n_select = 2, 32
+    rng, g = np.random.default_rng(12), torch.Generator("cuda").manual_seed(12)
+    pool, b0, table, q_begin, k, v, _, _ = _filled(hk, g, rng, lens, Hkv, 128, torch.bfloat16)
+    T = 5 if max_new == 1 else 400                         # (rows that are nobody's: as many lists as it takes for them to be merged)
+    b = hk.PagedBatch.make(*b0.tensors, T, max_new)
+    q = torch.empty(T, Hkv * G, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    sel = np.full((T, Hkv, n_select), -1)
+    sel[:5] = np.arange(n_select)
+    sel, chosen = _i32(sel), [np.broadcast_to(np.arange(-(-kv // PAGE)) < n_select, (Hkv, n, -(-kv // PAGE))) for n, kv in lens]
+    out, lse = torch.full_like(q, 7.0), torch.full((T, Hkv * G), 7.0, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, Hkv * G), dtype=torch.uint8, device="cuda")
+    words = ws.view(torch.int32)
+    head = 64 + 8192                                       # status and counters; behind them what kernels hand to one another
+    for entry in ([2**31 - 5, 20], [5, -2**31 + 7], [2**30, 40000], [3, 2**31 - 60000], [900, 300], None):
+        words.zero_()
+        if entry is None:
+            words[head:] = torch.randint(-2**31, 2**31 - 1, (len(words) - head,), generator=g, device="cuda").int()
+        else:
+            words[head: head + 2 * (len(words[head:]) // 2)].view(-1, 2)[:] = _i32(entry)
+        words[0] = 1
+        hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+        hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
+        assert hk.heatkv_paged_status(ws) == -7
+    words.zero_()
+    out.fill_(7.0), lse.fill_(7.0)
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(128), "bf16")
+    hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
+    _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(128), "bf16", chosen)
+    assert hk.heatkv_paged_status(ws) == 0

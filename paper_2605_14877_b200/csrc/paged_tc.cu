@@ -19,7 +19,7 @@
 // What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 us,
 // 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax (half the
 // products per exponential: 32 heads of the first shape 670 us, 800 TFLOP/s).
-// Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and leaves.
+// Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and its products end, and leaves.
 #include <algorithm>
 
 #include <cuda_fp16.h>
@@ -62,7 +62,7 @@ struct Layout {
 };
 enum Bar : uint32_t {
   Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 6, V_FULL = 8, V_EMPTY = 10, S_FULL = 12, P_FULL = 14, PV_DONE = 18, ITEM_FULL = 20, ITEM_EMPTY = 22,
-  N_BARS = 24
+  DRAIN = 24, N_BARS
 };
 constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256, BAR_INFO = 384;
 constexpr int INFO_RING = 4;                           // key tiles whose pages and bits are kept: the copy warp is at most two ahead of the softmax
@@ -561,6 +561,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       mbar_init(bar(V_FULL + s), 1);
       mbar_init(bar(V_EMPTY + s), 1);
     }
+    mbar_init(bar(DRAIN), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -889,6 +890,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           }
         __syncwarp();
         if (ok && elect_one()) mbar_arrive(bar(ITEM_EMPTY + slot));
+      }
+      if (!ok) {
+        // leaving early: products under way end before their operands and the tensor memory are given back
+        __syncwarp();
+        tc_commit(elect_one(), bar(DRAIN));
+        settle(bar(DRAIN), 0);
       }
     }
   } else {

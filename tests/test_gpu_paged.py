@@ -857,7 +857,7 @@ def test_a_key_that_a_row_does_not_see_has_no_weight(hk, d, max_new):
 
 # ------------------------------------------------------------------------------------------------ calls that give up
 
-@pytest.mark.parametrize("G,max_new", [(4, 1), (64, 1)])
+@pytest.mark.parametrize("G,max_new", [(4, 1), (64, 1), (4, 1 << 16)])
 def test_calls_on_a_workspace_whose_status_is_set(hk, G, max_new):
     """After a wait has run out, calls on the workspace end at once whatever the kernels before have left in it; zeroed, it serves again."""
     lens = [(1, 3000), (3, 700), (1, 64 * 40)]

@@ -91,7 +91,7 @@ uint64_t paged_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens);
 cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 // tensor-memory kernel: row tiles of up to 128 rows
 uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, int n_seq);
-bool paged_tc_takes_lists(int G, int n_sel, int table_pages);
+bool paged_tc_takes_lists(int G, int Hkv, int n_sel, int table_pages, int n_tokens, int n_seq);
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 
 // A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.  The driver's encoder wants a current context, and a thread that has made

@@ -224,7 +224,7 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
   p.n_sel = n_select;
   // tokens of a chunk share the pages that they select: they are taken together
   const bool chunk = p.max_new >= PAGED_SPARSE_CHUNK && (int64_t)p.n_tokens * p.Hkv * n_select >= PAGED_SPARSE_PAGES &&
-                     paged_tc_takes_lists(p.G, n_select, p.table_pages);
+                     paged_tc_takes_lists(p.G, p.Hkv, n_select, p.table_pages, p.n_tokens, p.n_seq);
   return done((chunk ? launch_paged_tc : launch_paged_small)(p, *pool, dev, static_cast<cudaStream_t>(stream)));
 }
 

@@ -73,13 +73,15 @@ struct TcParams {
   PagedParams a;
   // the plan of the call
   int32_t* item_begin;        // [n_seq + 1] the request's first item
-  int32_t* item_prefix;       // what its items weigh, of one head, summed up; SPARSE: [items * Hkv + 1] every item's and kv head's key tiles
+  int64_t* item_units;        // [items] what a request's items weigh, of one head, summed up (a long prompt of many heads a group passes 2^31)
+  int32_t* item_prefix;       // SPARSE (in the same place): [items * Hkv + 1] every item's and kv head's key tiles, summed up
   int32_t* runs;              // [n_sm][RUN_WORDS] where every CTA's run starts
   uint32_t* ticket;           // CTAs of union_kernel that are done; zero between launches
   int32_t items;              // room for the items
   int32_t n_cta;
 };
-enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_UNITS, R_C0_FIRST, R_C1_FIRST, R_C1_LAST, RUN_WORDS };
+enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_UNITS, R_C0_FIRST = R_UNITS + 2, R_C1_FIRST, R_C1_LAST, RUN_WORDS = 10 };
+static_assert(R_UNITS % 2 == 0 && RUN_WORDS % 2 == 0 && R_C1_LAST < RUN_WORDS, "a run's units are a 64-bit number");
 struct TcMaps {
   CUtensorMap q, k, v;
 };
@@ -251,7 +253,8 @@ struct Shares {
 template <typename P>
 __device__ __forceinline__ void write_run(const TcParams& tp, const Shares& sh, int c, P place) {
   int32_t* run = tp.runs + c * RUN_WORDS;
-  run[R_UNITS] = 0;
+  int64_t* units = reinterpret_cast<int64_t*>(run + R_UNITS);
+  *units = 0;
   if (c >= sh.grid) return;
   int64_t y0 = sh.bound(c);
   const int64_t y1 = sh.bound(c + 1);
@@ -266,7 +269,7 @@ __device__ __forceinline__ void write_run(const TcParams& tp, const Shares& sh, 
   run[R_HEAD] = a.head;
   run[R_ITEM] = a.item;
   run[R_J0] = (int)(y0 - a.begin);
-  run[R_UNITS] = (int)min(y1 - y0, (int64_t)INT32_MAX);
+  *units = y1 - y0;
   run[R_C0_FIRST] = sh.owner(a.begin);
   run[R_C1_FIRST] = sh.owner(a.begin + a.tiles - 1);
   run[R_C1_LAST] = sh.owner(z.begin + z.tiles - 1);
@@ -314,11 +317,12 @@ constexpr int PT = 512, PLAN_ITEMS = 16384;
 __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcParams tp) {
   extern __shared__ __align__(8) unsigned char plan_smem[];
   const PagedParams& p = tp.a;
-  int64_t* seq_prefix = reinterpret_cast<int64_t*>(plan_smem);     // [n_seq + 1] units before the request
+  const bool fits = tp.items <= PLAN_ITEMS;
+  int64_t* item_units = fits ? reinterpret_cast<int64_t*>(plan_smem) : tp.item_units;
+  int64_t* seq_prefix = reinterpret_cast<int64_t*>(plan_smem) + (fits ? tp.items : 0);         // [n_seq + 1] units before the request
   int32_t* item_begin = reinterpret_cast<int32_t*>(seq_prefix + p.n_seq + 1);  // [n_seq + 1]
   int32_t* tokens = item_begin + p.n_seq + 1;                      // [n_seq]
   int32_t* keys = tokens + p.n_seq;                                // [n_seq]
-  int32_t* item_prefix = tp.items <= PLAN_ITEMS ? keys + p.n_seq : tp.item_prefix;
   __shared__ int64_t sums[PT / 32];
   __shared__ int longest;
   pdl_trigger();
@@ -344,7 +348,7 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
   // a warp per request: units before every item
   for (int i = warp; i < p.n_seq; i += PT / 32) {
     const int first = item_begin[i], count = item_begin[i + 1] - first;
-    int before = 0;
+    int64_t before = 0;
     for (int base = 0; base < count; base += 32) {
       const int w = base + lane < count ? item_tiles(p, (base + lane) * pair, tokens[i], keys[i]) + ITEM_END : 0;
       int inc = w;
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
         const int up = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += up;
       }
-      if (base + lane < count) item_prefix[first + base + lane] = before + inc - w;
+      if (base + lane < count) item_units[first + base + lane] = before + inc - w;
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
     if (lane == 0) {
@@ -379,9 +383,10 @@ __global__ void __launch_bounds__(PT) plan_kernel(const __grid_constant__ TcPara
       r.seq = last_not_above(seq_prefix, p.n_seq, y);
       const int64_t s0 = seq_prefix[r.seq], per_head = (seq_prefix[r.seq + 1] - s0) / p.Hkv;
       r.head = (int)((y - s0) / per_head);
-      const int local = (int)(y - s0 - r.head * per_head), first = item_begin[r.seq];
-      r.item = last_not_above(item_prefix + first, item_begin[r.seq + 1] - first, local);
-      r.begin = y - (local - item_prefix[first + r.item]);
+      const int64_t local = y - s0 - r.head * per_head;
+      const int first = item_begin[r.seq];
+      r.item = last_not_above(item_units + first, item_begin[r.seq + 1] - first, local);
+      r.begin = y - (local - item_units[first + r.item]);
       r.tiles = item_tiles(p, r.item * pair, tokens[r.seq], keys[r.seq]);
       return r;
     });
@@ -463,12 +468,12 @@ __global__ void __launch_bounds__(UNION_THREADS) union_kernel(const __grid_const
   at = exclusive<UNION_WARPS>(mine, sums, all);
   for (int i = x0; i < x1; ++i) {
     const int v = fits ? prefix[i] : __ldcg(tp.item_prefix + i) + ITEM_END;
-    prefix[i] = tp.item_prefix[i] = (int)min(at, (int64_t)INT32_MAX);
+    prefix[i] = tp.item_prefix[i] = (int)at;                       // (paged_tc_takes_lists: all of them are below 2^31)
     at += v;
   }
-  if (tid == 0) prefix[count] = tp.item_prefix[count] = (int)min(all, (int64_t)INT32_MAX);
+  if (tid == 0) prefix[count] = tp.item_prefix[count] = (int)all;
   __syncthreads();
-  const Shares sh(min(all, (int64_t)INT32_MAX), longest, tp.n_cta);
+  const Shares sh(all, longest, tp.n_cta);
   for (int c = tid; c < tp.n_cta; c += UNION_THREADS)
     write_run(tp, sh, c, [&](int64_t y) {
       Place r;
@@ -692,7 +697,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       // ---------------------------------------------------------------- the CTA's run
       const bool leader = elect_one();
       const int32_t* run = tp.runs + blockIdx.x * RUN_WORDS;
-      int left = run[R_UNITS], seq = 0, head = 0, item = 0, j0 = 0;    // what is left of the run, and where it goes on
+      int64_t left = *reinterpret_cast<const int64_t*>(run + R_UNITS); // what is left of the run
+      int seq = 0, head = 0, item = 0, j0 = 0;                         // where it goes on
       if (left > 0) {
         seq = run[R_SEQ];
         head = run[R_HEAD];
@@ -714,7 +720,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         const int n = request_tokens(p, seq, q_first), kv = request_keys(p, seq);
         const int tok = item * 2 * p.tile_tokens, tokens = min(n - tok, 2 * p.tile_tokens);
         const int flat = SPARSE ? (tp.item_begin[seq] + item) * p.Hkv + head : 0;
-        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] - ITEM_END : item_tiles(p, tok, n, kv), n_tiles = min(tiles - j0, left);
+        const int tiles = SPARSE ? tp.item_prefix[flat + 1] - tp.item_prefix[flat] - ITEM_END : item_tiles(p, tok, n, kv),
+                  n_tiles = (int)min((int64_t)(tiles - j0), left);
         int seek = j0 > 0 ? -1 : 0;
         if (SPARSE) {
           uint16_t* list = reinterpret_cast<uint16_t*>(sgen + L::SM_LIST) + slot * LIST_ENTRIES;
@@ -1186,10 +1193,11 @@ uint64_t plan_items(int tile_tokens, int n_tokens, int n_seq) { return (uint64_t
 // tokens of a row tile over selected pages: a bit each in a word
 int sparse_tile_tokens(int G) { return std::min(32, BM / G); }
 uint64_t run_bytes(int n_sm) { return ((uint64_t)n_sm * RUN_WORDS * 4 + 255) / 256 * 256; }
+uint64_t item_words(int n_seq) { return ((uint64_t)n_seq + 2) & ~1ull; }      // of item_begin: 64-bit numbers follow it
 // (room for either kind of call: over selected pages every kv head's items count for themselves, and have at most 32 tokens a tile)
 uint64_t plan_bytes(int G, int Hkv, int n_tokens, int n_seq) {
   const uint64_t dense = plan_items(BM / G, n_tokens, n_seq), sparse = plan_items(sparse_tile_tokens(G), n_tokens, n_seq) * Hkv + 1;
-  return (4 * ((uint64_t)n_seq + 1) + 4 * std::max(dense, sparse) + 255) / 256 * 256;
+  return (4 * item_words(n_seq) + std::max(8 * dense, 4 * sparse) + 255) / 256 * 256;
 }
 
 template <int D, bool F16, bool SPARSE>
@@ -1210,8 +1218,8 @@ cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_
     const int64_t warps = (int64_t)tp.items * tp.a.Hkv;
     rc = launch_pdl(union_kernel, dim3((unsigned)((warps + UNION_WARPS - 1) / UNION_WARPS)), dim3(UNION_THREADS), bytes, stream, tp);
   } else {
-    constexpr int most = (PAGED_MAX_SEQ + 1) * 20 + PLAN_ITEMS * 4;
-    const int bytes = (tp.a.n_seq + 1) * 20 + (tp.items <= PLAN_ITEMS ? tp.items * 4 : 0);
+    constexpr int most = (PAGED_MAX_SEQ + 1) * 20 + PLAN_ITEMS * 8;
+    const int bytes = (tp.a.n_seq + 1) * 20 + (tp.items <= PLAN_ITEMS ? tp.items * 8 : 0);
     rc = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (rc != cudaSuccess) return rc;
     rc = launch_pdl(plan_kernel, dim3(1), dim3(PT), bytes, stream, tp);
@@ -1231,7 +1239,12 @@ uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, i
   return run_bytes(n_sm) + plan_bytes(G, Hkv, n_tokens, n_seq) + 2 * (uint64_t)n_sm * floats * 4;
 }
 
-bool paged_tc_takes_lists(int G, int n_sel, int table_pages) { return 2 * sparse_tile_tokens(G) * n_sel <= LIST_ENTRIES && table_pages < 0xffff; }
+bool paged_tc_takes_lists(int G, int Hkv, int n_sel, int table_pages, int n_tokens, int n_seq) {
+  const int tile_tokens = sparse_tile_tokens(G);
+  if (2 * tile_tokens * (int64_t)n_sel > LIST_ENTRIES || table_pages >= 0xffff) return false;
+  // the plan sums up key tiles in 32 bits: an item has half as many as its lists have pages, at most one more, and its end
+  return ((int64_t)n_tokens * n_sel / 2 + (int64_t)plan_items(tile_tokens, n_tokens, n_seq) * (1 + ITEM_END)) * Hkv <= INT32_MAX;
+}
 
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {
   TcParams tp;
@@ -1240,7 +1253,8 @@ cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool,
   tp.runs = reinterpret_cast<int32_t*>(p.partials);
   tp.item_begin = reinterpret_cast<int32_t*>(p.partials + run_bytes(dev.n_sm) / 4);
   tp.ticket = p.counters + PAGED_WS_CTRS * 8 - 1;
-  tp.item_prefix = tp.item_begin + p.n_seq + 1;
+  tp.item_prefix = tp.item_begin + item_words(p.n_seq);
+  tp.item_units = reinterpret_cast<int64_t*>(tp.item_prefix);
   tp.n_cta = dev.n_sm;
   tp.items = (int32_t)plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq);
   tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(p.G, p.Hkv, p.n_tokens, p.n_seq)) / 4;

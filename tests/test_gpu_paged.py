@@ -891,3 +891,37 @@ def test_calls_on_a_workspace_whose_status_is_set(hk, G, max_new):
     hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
     _check(out, lse, q, k, v, lens, table, q_begin, Hkv, True, 1 / math.sqrt(128), "bf16", chosen)
     assert hk.heatkv_paged_status(ws) == 0
+
+
+def test_plan_of_a_call_whose_key_tiles_pass_32_bits(hk):
+    """Half a million new tokens of 128 heads a group behind a million and a half: 3.8e9 key tiles a kv head.  The call is made on a workspace whose
+    status is set, so that its plan is made and nothing else (the attention would take minutes); every SM's run of the plan is looked at."""
+    n, kv, Hkv, G = 1 << 19, 1 << 21, 2, 128
+    k, v = (torch.zeros(1, Hkv, PAGE, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    pool = hk.PagedPool.make(k, v)
+    b = hk.PagedBatch.make(_i32([0, n]), _i32([kv]), torch.full((1, kv // PAGE), -1, dtype=torch.int32, device="cuda"), n, n)
+    q, out = (torch.zeros((n + Hkv * G) * 64, dtype=torch.bfloat16, device="cuda").as_strided((n, Hkv * G, 64), (64, 64, 1)) for _ in range(2))
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, Hkv * G), dtype=torch.uint8, device="cuda")
+    words = ws.view(torch.int32)
+    words[0] = 1
+    hk.heatkv_paged_attention(pool, b, q, out, None, ws)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    runs = words[64 + 8192:][: sms * 10].view(sms, 10).cpu().numpy()             # behind the status and the counters
+    # what the plan has to say: items of two tokens, a unit for each of their key tiles and one for their end
+    upto = kv - n + 2 * (np.arange(n // 2, dtype=np.int64) + 1)
+    tiles = -(-upto // 128)
+    begin = np.concatenate([[0], np.cumsum(tiles + 1)])
+    per_head = int(begin[-1])
+    assert per_head > 2**31
+    bound = [per_head * Hkv * c // sms for c in range(sms + 1)]
+    for c in range(sms):
+        seq, head, item, j0 = (int(x) for x in runs[c, :4])
+        units = int(runs[c, 4:6].copy().view(np.int64)[0])
+        y = head * per_head + int(begin[item]) + j0
+        h, at = divmod(bound[c], per_head)
+        i = int(np.searchsorted(begin, at, side="right")) - 1
+        ends = at - int(begin[i]) == tiles[i]              # a run that would begin with an item's end begins with the next item
+        assert (seq, y, units) == (0, bound[c] + ends, bound[c + 1] - bound[c] - ends), c
+        assert 0 <= head < Hkv and 0 <= j0 < tiles[item]
+        first = [x for x in range(sms) if bound[x] <= head * per_head + begin[item] < bound[x + 1]]
+        assert [int(runs[c, 6])] == first

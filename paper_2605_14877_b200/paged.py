@@ -63,8 +63,10 @@ class PagedCache:
     def attend(self, layer: int, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                lse: Optional[torch.Tensor] = None, causal: bool = True, sm_scale: float = 0.0, pages: int = 0, sink: int = 1,
                local: int = 2) -> None:
-        """Stores k, v [tokens, n_kv_heads, d] and writes to out the attention of q [tokens, n_heads, d]: over everything, or (pages > 0)
-        over that many pages of each token's choice."""
+        """Stores k, v [tokens, n_kv_heads, d] and writes to out the attention of q [tokens, n_heads, d]: over everything, or (pages > 0, always
+        causal) over that many pages of each token's choice."""
+        if pages > 0 and not causal:
+            raise ValueError("attention over selected pages is causal: a token's choice ends with its own page")
         pool = self.pools[layer]
         hk.heatkv_paged_store(pool, k, v, step.slots)
         if pages == 0:

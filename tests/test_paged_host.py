@@ -165,3 +165,13 @@ def test_page_choice_by_hand():
     assert P.select(q, codes, scales, 63, 0, 1, 4) == [0]
     c, s = P.summary(np.tile(np.array([[1.0, -0.5, 0.0]], dtype=np.float32), (64, 1)))
     assert c.tolist() == [127, -64, 0] and s == np.float32(1) / np.float32(127)
+
+
+def test_the_cache_refuses_selected_pages_that_see_what_is_behind():
+    """Attention over selected pages is causal; asked for without, it is refused and nothing is stored."""
+    from paper_2605_14877_b200.paged import PagedCache
+    cache = PagedCache(1, 4, 2, 64, n_pages=4, rows=1, max_pages=4, summaries=True, device="cpu")
+    q, kv = torch.ones(3, 4, 64, dtype=torch.bfloat16), torch.ones(3, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="causal"):
+        cache.attend(0, None, q, kv, kv, torch.empty_like(q), causal=False, pages=2)
+    assert (cache.pools[0].tensors[0] == 0).all()

@@ -11,10 +11,11 @@ from . import heatkv as hk
 
 
 class Step:
-    """The new tokens of one model step: `positions` for the position encoding, `batch` and `slots` for the calls."""
+    """The new tokens of one model step: `positions` for the position encoding, `batch` and `slots` for the calls, and `kv_len`, the tokens
+    that every row attends to (int32, on the device): 0 for a row whose new tokens were refused."""
 
-    def __init__(self, batch: hk.PagedBatch, slots: torch.Tensor, positions: torch.Tensor):
-        self.batch, self.slots, self.positions = batch, slots, positions
+    def __init__(self, batch: hk.PagedBatch, slots: torch.Tensor, positions: torch.Tensor, kv_len: torch.Tensor):
+        self.batch, self.slots, self.positions, self.kv_len = batch, slots, positions, kv_len
 
 
 class PagedCache:
@@ -42,8 +43,12 @@ class PagedCache:
         self.workspace: Optional[torch.Tensor] = None
 
     def begin(self, new: Sequence[int]) -> Step:
-        """Pages and slots of a step with new[i] new tokens in row i.  Rows that find no free pages get none and sit the step out: their
-        rows of the attention are zero, and their length stays (`state[2]` says how many there were)."""
+        """Pages and slots of a step with new[i] new tokens in row i (0: none).  Pages are wanted in row order, and from the first row that the free
+        ones do not suffice for, every row that needs one is refused; a row that would outgrow `max_pages` is refused alone.  Refused rows
+        sit the step out: their new tokens are stored nowhere, their rows of the attention are zero, their length stays.  The step's `kv_len` is
+        0 for them, and `state[2]` counts them: their tokens have to come again."""
+        if len(new) != self.rows or min(new) < 0 or sum(new) == 0:
+            raise ValueError(f"new: expected {self.rows} numbers of tokens, none below 0 and not all 0, got {list(new)}")
         tokens, longest = sum(new), max(new)
         count = torch.tensor(list(new), dtype=torch.int32, device=self.device)
         q_begin, kv_len = torch.empty(self.rows + 1, dtype=torch.int32, device=self.device), torch.empty_like(count)
@@ -54,7 +59,7 @@ class PagedCache:
         self.at_most = [a + n for a, n in zip(self.at_most, new)]
         # the calls get no more of the table than may be in use: its width is what they know of lengths beforehand
         pages = min(max(-(-max(self.at_most) // hk.PAGE_TOKENS), 1), self.table.shape[1])
-        step = Step(hk.PagedBatch.make(q_begin, kv_len, self.table[:, :pages], tokens, longest), slots, positions)
+        step = Step(hk.PagedBatch.make(q_begin, kv_len, self.table[:, :pages], tokens, longest), slots, positions, kv_len)
         need = hk.heatkv_paged_workspace_bytes(self.pools[0], step.batch, self.n_heads)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
@@ -77,7 +82,9 @@ class PagedCache:
         hk.heatkv_paged_sparse_attention(pool, step.batch, q, sel, out, lse, self.workspace, sm_scale)
 
     def keep(self, lengths: Sequence[int]) -> None:
-        """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free)."""
+        """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free; more than it has: it stays as it is)."""
+        if len(lengths) != self.rows or min(lengths) < 0:
+            raise ValueError(f"lengths: expected {self.rows} numbers of tokens, none below 0, got {list(lengths)}")
         keep = torch.tensor(list(lengths), dtype=torch.int32, device=self.device)
         hk.heatkv_paged_release(self.lengths, keep, self.table, self.free, self.state, self.other_state)
         self.state, self.other_state = self.other_state, self.state

@@ -925,3 +925,47 @@ def test_plan_of_a_call_whose_key_tiles_pass_32_bits(hk):
         assert 0 <= head < Hkv and 0 <= j0 < tiles[item]
         first = [x for x in range(sms) if bound[x] <= head * per_head + begin[item] < bound[x + 1]]
         assert [int(runs[c, 6])] == first
+
+
+def test_cache_of_rows_that_are_refused(hk):
+    """Rows that find no pages, or would outgrow their row of the table, sit a step out and say so; the others go on, and the tokens may come again."""
+    from paper_2605_14877_b200.paged import PagedCache
+    H, Hkv, d, rows = 4, 2, 64, 4
+    cache = PagedCache(1, H, Hkv, d, n_pages=6, rows=rows, max_pages=5)
+    g = torch.Generator("cuda").manual_seed(13)
+    kept = [[np.zeros((0, Hkv, d))] * 2 for _ in range(rows)]
+
+    def step_of(new, refused):
+        step, before = cache.begin(new), [len(x[0]) for x in kept]
+        T, begin = sum(new), np.concatenate([[0], np.cumsum(new)])
+        served = [0 if i in refused else before[i] + new[i] for i in range(rows)]
+        assert step.kv_len.tolist() == served and cache.state.tolist()[2] == len(refused)
+        assert cache.lengths.tolist() == [before[i] if i in refused else served[i] for i in range(rows)]
+        assert ((step.slots == -1).cpu().numpy() == np.isin(np.repeat(np.arange(rows), new), refused)).all()
+        q = torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        kv = torch.empty(2, T, Hkv, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        out, lse = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+        cache.attend(0, step, q, kv[0], kv[1], out, lse)
+        for i in range(rows):
+            at = slice(begin[i], begin[i + 1])
+            if i in refused:
+                assert (out[at] == 0).all() and (lse[at] == -math.inf).all()
+                continue
+            kept[i] = [np.concatenate([x, _np(kv[j, at])]) for j, x in enumerate(kept[i])]
+            K, V = kept[i]
+            seen = np.arange(len(K)) <= np.arange(len(K) - new[i], len(K))[:, None]
+            for h in range(H):
+                o, l, pv, reach = P.attention(_np(q[at, h]).astype(np.float64), K[:, h // 2], V[:, h // 2], seen, 0.125)
+                off = (d + 8) * 2.0**-24 * reach + 2.0**-18
+                assert (np.abs(_np(out[at, h]) - o) <= 2.0**-8 * np.abs(o) + (2.0**-8 + 2 * off)[:, None] * pv + 1e-30).all()
+                assert (np.abs(lse[at, h].cpu().numpy() - l) <= off + 2.0**-22 * np.abs(l)).all()
+
+    step_of([60, 100, 0, 64], [])                          # 1 + 2 + 1 pages of 6
+    step_of([3, 200, 65, 1], [1, 2, 3])                    # row 0 has room in its page; row 1 wants 3 pages of 2, and all behind it are refused
+    step_of([300, 1, 65, 1], [0, 3])                       # row 0 would outgrow its row; row 1 has room, row 2 takes the last two pages
+    cache.keep([63, 0, 65, 64])
+    kept[1] = [x[:0] for x in kept[1]]
+    step_of([1, 70, 1, 1], [3])                            # row 1 takes the two pages that came back
+    assert cache.state.tolist()[1] == 0
+    cache.keep([0, 0, 0, 0])
+    assert sorted(cache.free.tolist()) == list(range(6)) and cache.state.tolist()[1] == 6

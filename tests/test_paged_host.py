@@ -175,3 +175,16 @@ def test_the_cache_refuses_selected_pages_that_see_what_is_behind():
     with pytest.raises(ValueError, match="causal"):
         cache.attend(0, None, q, kv, kv, torch.empty_like(q), causal=False, pages=2)
     assert (cache.pools[0].tensors[0] == 0).all()
+
+
+def test_the_cache_refuses_numbers_of_tokens_that_are_none():
+    """Negative numbers would shorten the step's tensors, or a row's length, silently."""
+    from paper_2605_14877_b200.paged import PagedCache
+    cache = PagedCache(1, 4, 2, 64, n_pages=4, rows=2, max_pages=4, device="cpu")
+    for bad in ([3, -1], [0, 0], [1], [1, 2, 3]):
+        with pytest.raises(ValueError, match="new: expected 2 numbers"):
+            cache.begin(bad)
+    for bad in ([3, -1], [1], [1, 2, 3]):
+        with pytest.raises(ValueError, match="lengths: expected 2 numbers"):
+            cache.keep(bad)
+    assert cache.at_most == [0, 0] and cache.lengths.tolist() == [0, 0]

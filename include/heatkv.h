@@ -520,8 +520,15 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
                                   float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Reads the workspace's status word (synchronises `stream`): HEATKV_OK, or HEATKV_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel
- * ran out; the workspace must then be zeroed again. */
+ * ran out.  From the call whose wait ran out on, attention on this workspace leaves rows unwritten, although the calls return HEATKV_OK (they
+ * do not wait for the device): results since the last look are not to be used, and the workspace must be zeroed again. */
 int heatkv_paged_status(const void* workspace /*DEVICE*/, void* stream);
+
+/* Exercises the bounded waits of the paged kernels as heatkv_selftest_wait_expiry does those of the others: one warp waits, with a short limit,
+ * on a barrier that nothing will ever signal.  Synchronises `stream`.  workspace: at least 256 bytes, the status zero.
+ * HEATKV_ERR_DEVICE_TIMEOUT when the waits gave up and set the status as designed (the expected outcome; the workspace must then be
+ * zeroed again), HEATKV_OK if one claimed success, HEATKV_ERR_CUDA on any other outcome.  Nothing faults, traps or hangs. */
+int heatkv_paged_selftest_wait_expiry(void* workspace /*DEVICE*/, void* stream);
 
 #ifdef __cplusplus
 }

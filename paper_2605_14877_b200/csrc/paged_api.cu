@@ -1,7 +1,7 @@
 // Entry points of the paged cache: checks of arguments and kernel choice.
 #include <atomic>
 
-#include "paged.h"
+#include "paged_wait.cuh"
 
 namespace heatkv {
 namespace {
@@ -111,6 +111,25 @@ int done(cudaError_t rc) {
     return HEATKV_ERR_CUDA;
   }
   return HEATKV_OK;
+}
+
+// The paged kernels' waits on a barrier that nothing will ever signal, with limits of well under a millisecond.  result: 2 where the first gave up,
+// left its code and raised the CTA's flag, the second ended because of that flag, and the one for copies under way ended, too; 1: one of them
+// claimed success.
+constexpr uint32_t EXPIRY_CODE = 64;
+__global__ void __launch_bounds__(32) paged_wait_expiry_kernel(uint32_t* status, uint32_t* result) {
+  constexpr long long LIMIT = 1 << 20;
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ uint32_t abort_word;
+  const uint32_t at = smem_u32(&bar);
+  if (threadIdx.x == 0) {
+    tc::mbar_init(at, 1);
+    abort_word = 0;
+  }
+  __syncthreads();
+  const bool first = wait_all(at, 0, &abort_word, status, EXPIRY_CODE, LIMIT), second = wait_all(at, 0, &abort_word, status, EXPIRY_CODE + 1);
+  settle(at, 0, LIMIT);
+  if (threadIdx.x == 0) *result = first || second ? 1 : *const_cast<volatile uint32_t*>(&abort_word) ? 2 : 3;
 }
 
 }  // namespace
@@ -235,6 +254,20 @@ int heatkv_paged_status(const void* workspace, void* stream) {
   if (cudaMemcpyAsync(&word, workspace, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
     return done(cudaErrorUnknown);
   return word ? HEATKV_ERR_DEVICE_TIMEOUT : HEATKV_OK;
+}
+
+int heatkv_paged_selftest_wait_expiry(void* workspace, void* stream) {
+  if (!workspace || !aligned(workspace, 256)) return HEATKV_ERR_INVALID_ARG;
+  uint32_t* words = static_cast<uint32_t*>(workspace);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  constexpr int RESULT = 1;                            // word behind the status: no kernel reads it
+  uint32_t host[2] = {0, 0};
+  paged_wait_expiry_kernel<<<1, 32, 0, s>>>(words, words + RESULT);
+  if (cudaGetLastError() != cudaSuccess || cudaMemcpyAsync(host, words, sizeof(host), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaMemsetAsync(words + RESULT, 0, 4, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
+    return done(cudaErrorUnknown);
+  if (host[RESULT] == 1) return HEATKV_OK;
+  return host[RESULT] == 2 && host[0] == EXPIRY_CODE ? HEATKV_ERR_DEVICE_TIMEOUT : HEATKV_ERR_CUDA;
 }
 
 }  // extern "C"

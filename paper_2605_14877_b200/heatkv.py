@@ -28,7 +28,7 @@ __all__ = [
     "heatkv_selftest_wait_expiry", "heatkv_device_status", "heatkv_strerror", "heatkv_attention_split", "arena_bytes_for",
     "PagedPool", "PagedBatch", "TokenStrides", "DTYPE_BF16", "DTYPE_FP16", "PAGED_MAX_SEQ", "PAGED_MAX_SELECT", "heatkv_paged_tables",
     "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention", "heatkv_paged_select",
-    "heatkv_paged_sparse_attention", "heatkv_paged_status",
+    "heatkv_paged_sparse_attention", "heatkv_paged_status", "heatkv_paged_selftest_wait_expiry",
 ]
 
 MAX_K, MAX_BATCH, PAGE_TOKENS = 16, 128, 64
@@ -224,7 +224,7 @@ def exported_symbols():
             "heatkv_kernel_launches", "heatkv_pair_launches", "heatkv_lone_launches", "heatkv_last_attention", "heatkv_rank_dispersion", "heatkv_selftest_wait_expiry", "heatkv_device_status",
             "heatkv_strerror",
             "heatkv_paged_tables", "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention",
-            "heatkv_paged_select", "heatkv_paged_sparse_attention", "heatkv_paged_status"]
+            "heatkv_paged_select", "heatkv_paged_sparse_attention", "heatkv_paged_status", "heatkv_paged_selftest_wait_expiry"]
 
 
 def _load() -> C.CDLL:
@@ -289,6 +289,7 @@ _lib.heatkv_paged_attention.argtypes = [_P, _P, _I, _P, _P, _I, C.c_float, _P, _
 _lib.heatkv_paged_select.argtypes = [_P, _P, _I, _P, _P, _I, _I, _I, _P, _P]
 _lib.heatkv_paged_sparse_attention.argtypes = [_P, _P, _I, _P, _P, _P, _I, C.c_float, _P, _P, _P, C.c_uint64, _P]
 _lib.heatkv_paged_status.argtypes = [_P, _P]
+_lib.heatkv_paged_selftest_wait_expiry.argtypes = [_P, _P]
 for _n in exported_symbols():
     if _n != "heatkv_strerror":
         getattr(_lib, _n).restype = C.c_int
@@ -724,5 +725,13 @@ def heatkv_paged_sparse_attention(pool: PagedPool, batch: PagedBatch, q, sel, ou
 
 
 def heatkv_paged_status(workspace, stream=None) -> int:
-    """0, or -7 if a bounded wait of a kernel that used this workspace ran out (synchronises the stream)."""
+    """0, or -7 if a bounded wait of a kernel that used this workspace ran out (synchronises the stream): results since the last look are then
+    not to be used, and the workspace is to be zeroed."""
     return _lib.heatkv_paged_status(workspace.data_ptr(), _on_device(stream, workspace))
+
+
+def heatkv_paged_selftest_wait_expiry(workspace, stream=None) -> int:
+    """-7 when the paged kernels' bounded waits, tried on a barrier that nothing signals, give up as they should; leaves the status set."""
+    if workspace.nbytes < 256:
+        raise ValueError("workspace: expected at least 256 bytes")
+    return _lib.heatkv_paged_selftest_wait_expiry(_workspace(workspace), _on_device(stream, workspace))

@@ -62,7 +62,10 @@ class PagedCache:
         step = Step(hk.PagedBatch.make(q_begin, kv_len, self.table[:, :pages], tokens, longest), slots, positions, kv_len)
         need = hk.heatkv_paged_workspace_bytes(self.pools[0], step.batch, self.n_heads)
         if self.workspace is None or self.workspace.numel() < need:
-            self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            grown = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            if self.workspace is not None:
+                grown[:4] = self.workspace[:4]         # (the status, for the next `check`)
+            self.workspace = grown
         return step
 
     def attend(self, layer: int, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -80,6 +83,15 @@ class PagedCache:
         sel = torch.empty(step.batch.n_tokens, pool.n_kv_heads, pages, dtype=torch.int32, device=self.device)
         hk.heatkv_paged_select(pool, step.batch, q, sel, sink, local)
         hk.heatkv_paged_sparse_attention(pool, step.batch, q, sel, out, lse, self.workspace, sm_scale)
+
+    def check(self) -> None:
+        """Raises HeatKVError if a bounded wait inside a kernel ran out since the last look: what `attend` wrote since then is not to be used.  The
+        workspace is zeroed, so that the steps can be attended to again (K and V are stored whatever happens there).  Waits for the device."""
+        status = hk.heatkv_paged_status(self.workspace) if self.workspace is not None else 0
+        if status != 0:
+            if status == -7:                           # HEATKV_ERR_DEVICE_TIMEOUT
+                self.workspace.zero_()
+            raise hk.HeatKVError(status, "PagedCache.check")
 
     def keep(self, lengths: Sequence[int]) -> None:
         """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free; more than it has: it stays as it is)."""

@@ -969,3 +969,44 @@ def test_cache_of_rows_that_are_refused(hk):
     assert cache.state.tolist()[1] == 0
     cache.keep([0, 0, 0, 0])
     assert sorted(cache.free.tolist()) == list(range(6)) and cache.state.tolist()[1] == 6
+
+
+def test_a_wait_that_runs_out(hk):
+    """The paged kernels' own bounded waits, on a barrier that nothing signals: they give up, the status says so until the workspace is zeroed, and
+    a cache's check raises once and leaves a cache that serves, also where its workspace grew in between."""
+    from paper_2605_14877_b200.paged import PagedCache
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    assert hk.heatkv_paged_status(ws) == 0
+    assert hk.heatkv_paged_selftest_wait_expiry(ws) == -7 and hk.heatkv_paged_status(ws) == -7
+    assert (ws[4:] == 0).all()
+    assert hk.heatkv_paged_selftest_wait_expiry(ws) == -7      # (the first code stays)
+    ws.zero_()
+    assert hk.heatkv_paged_status(ws) == 0
+
+    H, Hkv, d = 4, 2, 64
+    cache = PagedCache(1, H, Hkv, d, n_pages=210, rows=2, max_pages=200)
+    cache.check()                                              # nothing has run yet
+    g = torch.Generator("cuda").manual_seed(14)
+    rows = lambda n, heads: torch.empty(n, heads, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)      # noqa: E731
+    step = cache.begin([1, 1])
+    q, k, v = rows(2, H), rows(2, Hkv), rows(2, Hkv)
+    cache.attend(0, step, q, k, v, torch.empty_like(q))
+    cache.check()
+    for again in range(2):
+        assert hk.heatkv_paged_selftest_wait_expiry(cache.workspace) == -7
+        size = cache.workspace.numel()
+        step = cache.begin([6000, 1 + again])                  # (its workspace is larger the first time)
+        assert again == 1 or cache.workspace.numel() > size
+        q, k, v = rows(6001 + again, H), rows(6001 + again, Hkv), rows(6001 + again, Hkv)
+        out = torch.full_like(q, 7.0)
+        cache.attend(0, step, q, k, v, out)
+        with pytest.raises(hk.HeatKVError, match="-7"):
+            cache.check()
+        cache.check()
+        cache.attend(0, step, q, k, v, out)
+        cache.check()
+        want = torch.zeros_like(out)
+        pool = cache.pools[0]
+        hk.heatkv_paged_attention(pool, step.batch, q, want, None,
+                                  torch.zeros(hk.heatkv_paged_workspace_bytes(pool, step.batch, H), dtype=torch.uint8, device="cuda"))
+        assert torch.equal(out, want) and (out != 7.0).any(-1).all()

@@ -188,3 +188,11 @@ def test_the_cache_refuses_numbers_of_tokens_that_are_none():
         with pytest.raises(ValueError, match="lengths: expected 2 numbers"):
             cache.keep(bad)
     assert cache.at_most == [0, 0] and cache.lengths.tolist() == [0, 0]
+
+
+def test_arguments_of_the_waits_self_test():
+    assert H._lib.heatkv_paged_selftest_wait_expiry(None, None) == INVALID and H._lib.heatkv_paged_selftest_wait_expiry(A + 16, None) == INVALID
+    with pytest.raises(ValueError, match="256"):
+        hk.heatkv_paged_selftest_wait_expiry(torch.zeros(255, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="not on the current CUDA device"):
+        hk.heatkv_paged_selftest_wait_expiry(torch.zeros(256, dtype=torch.uint8))

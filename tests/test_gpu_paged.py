@@ -1010,3 +1010,168 @@ def test_a_wait_that_runs_out(hk):
         hk.heatkv_paged_attention(pool, step.batch, q, want, None,
                                   torch.zeros(hk.heatkv_paged_workspace_bytes(pool, step.batch, H), dtype=torch.uint8, device="cuda"))
         assert torch.equal(out, want) and (out != 7.0).any(-1).all()
+
+
+# ------------------------------------------------------------------------------------------------ many requests
+
+def _many(hk, seed, new, kv, Hkv, d, dt):
+    """A pool of requests' pages in random order, NaN past every request's last key; everything by whole tensors."""
+    g, rng = torch.Generator("cuda").manual_seed(seed), np.random.default_rng(seed)
+    held = -(-np.asarray(kv) // PAGE)
+    n_pages, width = int(held.sum()) + 2, int(held.max()) + 1
+    table = np.full((len(kv), width), -1)
+    row, col = np.repeat(np.arange(len(kv)), held), np.concatenate([np.arange(h) for h in held])
+    table[row, col] = rng.permutation(n_pages)[: len(row)]
+    pool, k, v, code, scale = _pool(hk, g, n_pages, Hkv, d, dt)
+    empty = torch.ones(n_pages, PAGE, dtype=torch.bool, device="cuda")
+    pages = torch.tensor(table[row, col], device="cuda")
+    left = torch.tensor(np.asarray(kv)[row] - col * PAGE, device="cuda")
+    empty[pages] = torch.arange(PAGE, device="cuda") >= left[:, None]
+    for x in (k, v):
+        x.normal_(generator=g)
+        x.masked_fill_(empty[:, None, :, None], math.nan)
+    q_begin = np.concatenate([[0], np.cumsum(new)])
+    b = hk.PagedBatch.make(_i32(q_begin), _i32(kv), _i32(table), int(q_begin[-1]), int(max(new)))
+    return pool, b, k, v, code, scale, g
+
+
+def _check_many(out, lse, q, k, v, b, dtype, sel=None):
+    """_check by whole tensors on the device, causal, 1 / sqrt(d): every row of every request against 64 bits."""
+    u = 2.0**-8 if dtype == "bf16" else 2.0**-11
+    q_begin, kv, table = (x.long() for x in b.tensors)
+    T, H, d = q.shape
+    Hkv = k.shape[1]
+    G, scale, new = H // Hkv, 1 / math.sqrt(d), q_begin[1:] - q_begin[:-1]
+    for lo in range(0, len(kv), 64):
+        ids = slice(lo, min(lo + 64, len(kv)))
+        n, most, pages = new[ids], max(int(new[ids].max()), 1), max(-(-int(kv[ids].max()) // PAGE), 1)
+        t = torch.arange(most, device="cuda")
+        at = (q_begin[:-1][ids, None] + t).clamp(max=T - 1)
+        keys, values = (x[table[ids, :pages].clamp(min=0)].transpose(1, 2).flatten(2, 3).double().nan_to_num() for x in (k, v))     # [r, Hkv, keys, d]
+        qq = q[at].double().view(len(n), most, Hkv, G, d)
+        j = torch.arange(pages * PAGE, device="cuda")
+        pos = (kv[ids] - n)[:, None] + t                                         # [r, t]
+        seen = ((j < kv[ids, None])[:, None] & (j <= pos[..., None]))[:, None, None]   # [r, 1, 1, t, keys]
+        if sel is not None:
+            took = torch.zeros(len(n), most, Hkv, pages + 1, dtype=torch.bool, device="cuda")
+            place = sel[at].long()
+            took.scatter_(3, torch.where((place < 0) | (place >= pages), pages, place), True)
+            seen = seen & took[..., :pages].repeat_interleave(PAGE, -1).permute(0, 2, 1, 3)[:, :, None]
+        logits = torch.einsum("rthgd,rhkd->rhgtk", qq, keys).mul_(scale).masked_fill_(~seen, -math.inf)
+        want_lse = torch.logsumexp(logits, -1)
+        p = torch.exp(logits - want_lse.clamp(min=-1e300)[..., None])
+        o, pv = torch.einsum("rhgtk,rhkd->rthgd", p, values), torch.einsum("rhgtk,rhkd->rthgd", p, values.abs())
+        reach = (torch.einsum("rthgd,rhkd->rhgtk", qq.abs(), keys.abs()) * scale * seen).amax(-1).permute(0, 3, 1, 2)
+        want_lse = want_lse.permute(0, 3, 1, 2)
+        off = (d + 8) * 2.0**-24 * reach + 2.0**-18
+        small = pages * PAGE * 2.0**-25 * values.abs().max() if dtype == "fp16" else 0.0
+        tol = u * o.abs() + (u + 2 * off)[..., None] * pv + small + 1e-30
+        real = t < n[:, None]
+        got, got_lse = out[at].double().view_as(o), lse[at].double().view_as(want_lse)
+        assert got[real].isfinite().all()
+        assert ((got - o).abs() <= tol)[real].all(), lo
+        assert torch.equal(got_lse.isinf()[real], want_lse.isinf()[real])
+        fine = (got_lse - want_lse).abs() <= off + 2.0**-22 * want_lse.abs()
+        assert (fine | want_lse.isinf())[real].all(), lo
+
+
+MANY = {
+    # more requests than threads that plan, most short, a few long, some without keys or new tokens
+    "few_tokens": dict(n=4096, new=(0, 3), H=8, Hkv=2, d=64, dtype="bf16"),
+    "wide_group": dict(n=1500, new=(1, 4), H=48, Hkv=3, d=128, dtype="fp16"),
+    # more items than the plan keeps in shared memory
+    "many_items": dict(n=4096, new=(6, 8), H=128, Hkv=1, d=64, dtype="bf16"),
+}
+
+
+def _many_lens(c, seed):
+    rng = np.random.default_rng(seed)
+    new = rng.integers(c["new"][0], c["new"][1] + 1, c["n"])
+    kv = new + rng.integers(0, 150, c["n"])
+    kv[:: 97] = 1200 + rng.integers(0, 400, len(kv[:: 97]))
+    kv[5:: 301] = 0
+    kv[7:: 301] = 1                                        # (fewer than the new tokens)
+    return new, kv
+
+
+@pytest.mark.parametrize("max_new", [1, 1 << 16])
+@pytest.mark.parametrize("name", MANY)
+def test_attention_of_many_requests(hk, name, max_new):
+    c = MANY[name]
+    new, kv = _many_lens(c, 21)
+    pool, b, k, v, _, _, g = _many(hk, 21, new, kv, c["Hkv"], c["d"], DTYPES[c["dtype"]])
+    b.max_new = max_new
+    q = torch.empty(b.n_tokens, c["H"], c["d"], dtype=DTYPES[c["dtype"]], device="cuda").normal_(generator=g)
+    out, lse = torch.full_like(q, math.nan), torch.full((b.n_tokens, c["H"]), math.nan, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, c["H"]), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attention(pool, b, q, out, lse, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check_many(out, lse, q, k, v, b, c["dtype"])
+
+
+@pytest.mark.parametrize("max_new", [1, 1 << 16])
+@pytest.mark.parametrize("Hkv,G,d", [(4, 2, 64), (8, 1, 128), (2, 16, 128)])
+def test_sparse_attention_of_many_requests(hk, Hkv, G, d, max_new):
+    """As many lists (4096 requests, 2 or more kv heads) as their sums do not fit shared memory for, with gaps and in any order; both kernels."""
+    new, kv = _many_lens(dict(n=4096, new=(0, 3)), 22)
+    pool, b, k, v, _, _, g = _many(hk, 22, new, kv, Hkv, d, torch.bfloat16)
+    b.max_new = max_new
+    T, H, n_select = b.n_tokens, Hkv * G, 9
+    q = torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    order = torch.rand(T, Hkv, 26, generator=g, device="cuda").argsort(-1)[..., :n_select]      # distinct pages, some past the request's last
+    sel = torch.where(torch.rand(T, Hkv, n_select, generator=g, device="cuda") < 0.2, -1, order).int().contiguous()
+    out, lse = torch.full_like(q, math.nan), torch.full((T, H), math.nan, device="cuda")
+    ws = torch.zeros(hk.heatkv_paged_workspace_bytes(pool, b, H), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_sparse_attention(pool, b, q, sel, out, lse, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check_many(out, lse, q, k, v, b, "bf16", sel)
+
+
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(14, 2, 64, "fp16"), (16, 4, 128, "bf16")])
+def test_select_of_single_tokens_between_chunks(hk, H, Hkv, d, dtype):
+    """Chunks and single tokens in one batch, more requests than 16 tokens have: both forms of selection give the definition's pages."""
+    new = np.array([1, 40, 1, 1, 0, 1, 17, 1, 1, 1, 2, 0, 0, 1, 1, 16, 1] + [1] * 40 + [33])
+    rng = np.random.default_rng(23)
+    kv = new + rng.integers(0, 3000, len(new))
+    kv[[3, 6]] = 0, 5                                      # no keys, and fewer than the new tokens
+    pool, b, k, v, code, scale, g = _many(hk, 23, new, kv, Hkv, d, DTYPES[dtype])
+    code.copy_(torch.randint(-127, 128, code.shape, generator=g, device="cuda"))
+    scale.uniform_(0.5, 2.0, generator=g)
+    q = torch.empty(b.n_tokens, H, d, dtype=DTYPES[dtype], device="cuda").normal_(generator=g)
+    q_begin, _, table = (x.cpu().numpy() for x in b.tensors)
+    qf, cn, sn, G, n_select = _np(q), code.cpu().numpy(), scale.cpu().numpy(), H // Hkv, 12
+    for max_new in (1, 40):
+        b.max_new = max_new
+        sel = torch.full((b.n_tokens, Hkv, n_select), -9, dtype=torch.int32, device="cuda")
+        hk.heatkv_paged_select(pool, b, q, sel, 2, 3)
+        got = sel.cpu().numpy()
+        for i, n in enumerate(new):
+            pages = table[i, : -(-kv[i] // PAGE)]
+            for t in range(n):
+                at = kv[i] - n + t
+                for h in range(Hkv):
+                    want = P.select(qf[q_begin[i] + t, h * G:(h + 1) * G], cn[pages, h], sn[pages, h], at, 2, 3, n_select) if at >= 0 else []
+                    assert got[q_begin[i] + t, h].tolist() == want + [-1] * (n_select - len(want)), (max_new, i, t, h)
+
+
+def test_one_workspace_for_calls_of_all_kinds(hk):
+    """A workspace of the largest batch serves smaller ones of either kernel in any order, with the bits that one of its own gives."""
+    H, Hkv, d = 16, 4, 128
+    cases = []
+    for seed, (n, new, more) in enumerate(((40, (30, 90), 3000), (7, (1, 1), 9000), (300, (1, 4), 500), (3, (200, 300), 100), (60, (1, 1), 4000))):
+        rng = np.random.default_rng(seed)
+        lens = rng.integers(new[0], new[1] + 1, n)
+        pool, b, k, v, _, _, g = _many(hk, seed, lens, lens + rng.integers(0, more, n), Hkv, d, torch.bfloat16)
+        q = torch.empty(b.n_tokens, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        sel = torch.rand(b.n_tokens, Hkv, 47, generator=g, device="cuda").argsort(-1)[..., :32].int().contiguous()
+        cases.append((pool, b, q, sel, hk.heatkv_paged_workspace_bytes(pool, b, H)))
+    ws = torch.zeros(max(c[-1] for c in cases), dtype=torch.uint8, device="cuda")
+    order = [0, 1, 2, 3, 4, 1, 0, 4, 3, 2, 0]
+    for i in order:
+        pool, b, q, sel, size = cases[i]
+        own = torch.zeros(size, dtype=torch.uint8, device="cuda")
+        got, want = ([torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")] for _ in range(2))
+        for call in (lambda o, w: hk.heatkv_paged_attention(pool, b, q, *o, w), lambda o, w: hk.heatkv_paged_sparse_attention(pool, b, q, sel, *o, w)):
+            call(got, ws), call(want, own)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and (want[1] != 7.0).all(), i
+    assert hk.heatkv_paged_status(ws) == 0

@@ -449,7 +449,7 @@ typedef struct {                 /* the requests of a step                      
   int64_t table_stride;
   int32_t n_seq, table_pages;
   int32_t n_tokens;              /* rows of the token tensors, at least q_begin[n_seq]                                 */
-  int32_t max_new;               /* new tokens of the longest request: picks the kernel, with table_pages; any value gives right results */
+  int32_t max_new;               /* new tokens of the longest request: picks the kernel, with the other sizes; any value gives right results */
 } heatkv_paged_batch;
 
 typedef struct {                 /* element strides of [n_tokens][n_heads][d] activations: at least d, multiples of 8 */

@@ -22,9 +22,8 @@ namespace {
 
 constexpr int ROWS_THREADS = 256, ROWS_WARPS = ROWS_THREADS / 32;
 constexpr int LIST = 256, ROW_LIST = 128;                     // pages that are ranked: of one token by a CTA, by a warp
-constexpr int SEL_ROWS = 16;                                  // tokens of a CTA where requests have many
-constexpr int SEL_ROWS_FROM = 8;                              // ... new tokens of the longest request
-constexpr int SEL_ROWS_PAGES = 3200;                          // ... pages whose scores fit shared memory for all of them
+constexpr int SEL_ROWS = 16;                                  // tokens of a CTA where requests have many (sixteen_at_once)
+constexpr int SEL_ROWS_PAGES = 3200;                          // pages whose scores fit shared memory for all of them
 
 __device__ __forceinline__ float load_half(const void* p, int64_t i, bool fp16) {
   return fp16 ? __half2float(static_cast<const __half*>(p)[i]) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
@@ -533,6 +532,18 @@ __global__ void __launch_bounds__(ROWS_THREADS, 4) select_rows_kernel(const __gr
 
 }  // namespace
 
+// Whether 16 tokens share a CTA.  That takes 7 us or so for every request among the 16, one behind another, where a CTA or cluster of its own for
+// every token and kv head takes 14 ns of the whole device.  How many requests 16 tokens belong to is known to the host on average only: the tokens
+// beside the longest request's are taken to be spread evenly over the others.  Contexts of 20 000 tokens, 8 kv heads of 4 heads, us with a
+// token a CTA and with 16: 1 request of 16 new tokens 8.1 and 14, 8 of them 19 and 14.5, 64 126 and 25; 64 of 4 36 and 37; a chunk of 8 beside
+// 64 single tokens 11 and 108, of 256 43 and 113, of 1024 131 and 132, of 2048 252 and 162; 2048 beside one 231 and 40.  Two kv heads: 64 of 8
+// 20 and 18, 2048 beside 8 62 and 58, beside 32 64 and 111.  Of 132 shapes measured two lose more than 5 % (9.0 us for 7.0).
+bool sixteen_at_once(const SelectParams& p, int max_new) {
+  const int64_t units = (int64_t)p.n_tokens * p.Hkv, others = std::max(p.n_tokens - max_new, 0), n = p.n_seq;
+  const int64_t requests = std::min<int64_t>(std::min<int64_t>(n, SEL_ROWS), 1 + (SEL_ROWS - 1) * (n - 1) / std::max<int64_t>(std::max(others, n - 1), 1));
+  return p.table_pages <= SEL_ROWS_PAGES && units > 200 + 400 * requests;
+}
+
 cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cudaStream_t stream) {
   // (a kernel's limit is the process's: always set to the most that any call takes, or another thread's smaller call, between this one's
   // limit and its launch, would have the launch refused)
@@ -556,7 +567,7 @@ cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cu
     cfg.numAttrs = ctas > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, p, more...);
   };
-  if (max_new >= SEL_ROWS_FROM && p.table_pages <= SEL_ROWS_PAGES) {
+  if (sixteen_at_once(p, max_new)) {
     // (eight pages a product may run past the last; odd multiples of 16 bytes spread the rows over the banks)
     auto pitch_of = [](int pages) { return (pages + 7) / 8 * 8 + 4; };
     const int pitch = pitch_of(p.table_pages), most = SEL_ROWS * pitch_of(SEL_ROWS_PAGES) * 4;

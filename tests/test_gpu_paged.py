@@ -1175,3 +1175,69 @@ def test_one_workspace_for_calls_of_all_kinds(hk):
             call(got, ws), call(want, own)
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and (want[1] != 7.0).all(), i
     assert hk.heatkv_paged_status(ws) == 0
+
+
+def _check_select(pool_codes, b, q, lens, Hkv, sel, sink, local, tokens=None):
+    """Every token's list (or those of `tokens`) against the definition."""
+    code, scale = (x.cpu().numpy() for x in pool_codes)
+    (q_begin, _, table), qf, got, G, n_select = (x.cpu().numpy() for x in b.tensors), _np(q), sel.cpu().numpy(), q.shape[1] // Hkv, sel.shape[2]
+    for i, (n, kv) in enumerate(lens):
+        pages = table[i, : -(-kv // PAGE)]
+        for t in range(n):
+            if tokens is not None and q_begin[i] + t not in tokens:
+                continue
+            for h in range(Hkv):
+                at = kv - n + t
+                want = P.select(qf[q_begin[i] + t, h * G:(h + 1) * G], code[pages, h], scale[pages, h], at, sink, local, n_select) if at >= 0 else []
+                assert got[q_begin[i] + t, h].tolist() == want + [-1] * (n_select - len(want)), (i, t, h)
+
+
+def _select_batch(hk, seed, lens, Hkv, G, d, codes=127):
+    pool, b, _, _, code, scale, g = _many(hk, seed, [n for n, _ in lens], [kv for _, kv in lens], Hkv, d, torch.bfloat16)
+    code.copy_(torch.randint(-codes, codes + 1, code.shape, generator=g, device="cuda"))
+    scale.copy_(2.0 ** torch.randint(-2, 1, scale.shape, generator=g, device="cuda"))
+    q = torch.randint(-codes, codes + 1, (b.n_tokens, Hkv * G, d), generator=g, device="cuda").to(torch.bfloat16)
+    return pool, b, q, (code, scale)
+
+
+@pytest.mark.parametrize("n_select", [8, 40, 100, 200])
+@pytest.mark.parametrize("codes", [1, 127])
+def test_select_of_a_long_context_by_many_tokens(hk, codes, n_select):
+    """1500 pages chosen from by as many tokens as it takes for 16 of them to share a CTA; many equal scores or hardly any."""
+    lens = [(333, 1500 * PAGE - 5)]
+    pool, b, q, summaries = _select_batch(hk, 31, lens, 2, 2, 64, codes)
+    q[2] = 0
+    sel = torch.zeros(333, 2, n_select, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, 3, 4)
+    _check_select(summaries, b, q, lens, 2, sel, 3, 4, set(range(0, 333, 4)) | {2, 331, 332})
+
+
+def test_select_of_a_chunk_beside_as_many_single_tokens_as_share_a_cta(hk):
+    """A chunk long enough that 16 tokens share a CTA whosever they are, single tokens in front of it and behind it."""
+    lens = [(1, 500 + 37 * i) for i in range(20)] + [(0, 77), (600, 3000), (1, 0), (2, 1)] + [(1, 64 * i + 1) for i in range(37)] + [(3, 900)]
+    pool, b, q, summaries = _select_batch(hk, 32, lens, 16, 1, 64)
+    sel = torch.zeros(b.n_tokens, 16, 9, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(pool, b, q, sel, 1, 2)
+    _check_select(summaries, b, q, lens, 16, sel, 1, 2, set(range(0, 30)) | set(range(30, 600, 50)) | set(range(600, b.n_tokens)))
+
+
+def test_select_of_a_chunk_beside_single_tokens_takes_no_longer_than_both(hk):
+    """One request of 8 new tokens among 64 of one: all of them had been sent through the form in which 16 tokens share a CTA, which takes a request
+    after another (108 us where a token a CTA takes 11).  Four times the single tokens' own time is far above any noise."""
+    times = []
+    for lens in ([(1, 20000)] * 64, [(8, 20000)] + [(1, 20000)] * 64):
+        pool, b, q, _ = _select_batch(hk, 33, lens, 8, 4, 128)
+        sel = torch.zeros(b.n_tokens, 8, 16, dtype=torch.int32, device="cuda")
+        for _ in range(3):
+            hk.heatkv_paged_select(pool, b, q, sel, 1, 2)
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        best = math.inf
+        for _ in range(5):
+            begin.record()
+            for _ in range(30):
+                hk.heatkv_paged_select(pool, b, q, sel, 1, 2)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        times.append(best)
+    assert times[1] < 4 * times[0], times

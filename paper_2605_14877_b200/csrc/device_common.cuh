@@ -149,6 +149,15 @@ __device__ __forceinline__ void prefetch_rows(const void* first, int64_t stride,
   for (int i = tid; i < rows * lines; i += threads)
     prefetch_l2(static_cast<const char*>(first) + (int64_t)(i / lines) * stride + (i % lines) * 128);
 }
+
+// encode(): makes a tensor map, and says whether it did.  The driver's encoder wants a current context, and a thread that has made no CUDA call
+// yet has none: where it fails, the runtime makes that of the thread's device current, and the map is asked for once more.
+template <typename F>
+bool encode_in_context(F encode) {
+  int dev = 0;
+  return encode() || (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode());
+}
+
 template <typename... P, typename... A>
 cudaError_t launch_pdl(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A&... args) {
   cudaLaunchConfig_t cfg = {};

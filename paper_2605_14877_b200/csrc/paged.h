@@ -6,6 +6,7 @@
 
 #include <cstdint>
 
+#include "device_common.cuh"
 #include "heatkv.h"
 
 namespace heatkv {
@@ -27,7 +28,7 @@ constexpr int PAGED_WS_PARTIALS = (PAGED_WS_HEAD_WORDS + PAGED_WS_CTRS * 8) * 4;
 
 struct PagedDevice {
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
-  int n_sm = 0, index = 0;
+  int n_sm = 0;
 };
 
 struct TablesParams {
@@ -94,17 +95,15 @@ uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, i
 bool paged_tc_takes_lists(int G, int Hkv, int n_sel, int table_pages, int n_tokens, int n_seq);
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
 
-// A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.  The driver's encoder wants a current context, and a thread that has made
-// no CUDA call yet has none: where it fails the runtime makes the device's own current, and the map is asked for once more.
+// A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.
 inline bool paged_encode(const PagedDevice& dev, CUtensorMap* m, void* base, int dtype, const cuuint64_t* dims, const cuuint64_t* strides,
                          const cuuint32_t* box) {
   const cuuint32_t unit[4] = {1, 1, 1, 1};
-  auto made = [&] {
+  return encode_in_context([&] {
     return dev.encode(m, dtype == HEATKV_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box,
                       unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-  };
-  return made() || (cudaSetDevice(dev.index) == cudaSuccess && made());
+  });
 }
 
 // boxes of 64 columns x 64 rows of one page and head: (column, row, head, page)

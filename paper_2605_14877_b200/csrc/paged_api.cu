@@ -27,7 +27,6 @@ bool paged_device(PagedDevice* out) {
     encode.store(fn, std::memory_order_relaxed);
   }
   out->n_sm = n < 240 ? n : 240;                       // (the workspace has arrival counters for so many)
-  out->index = dev;
   out->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   return true;
 }

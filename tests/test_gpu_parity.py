@@ -1582,3 +1582,56 @@ def test_config2_graph_replay_sampled_heads(hk):
                 _check_attention(outs[step - 1][s_, h], want, ("graph", s_, h, step), stats)
         stats.check()
         hk.heatkv_schedule_free(sch)
+
+
+def test_tensor_memory_kernels_from_a_thread_that_has_made_no_cuda_call(hk):
+    """Calibration, a context's creation and a whole generation, each as the first CUDA call of a thread of its own: as from any other thread, on the
+    tensor-memory kernels."""
+    import threading
+
+    from paper_2605_14877_b200.sweep import Session
+    sh = W.Shape("thread", L=1, H=2, d=128, sides=W.SIDES_13[:11], n_seq=1, s=3)
+    q, k, v = W.qkv_layer(sh, 7, 0, device="cuda")
+    out, want = torch.zeros_like(q), torch.zeros_like(q)
+    scores, raised = W.synthetic_scas(sh, 2), []
+
+    def in_a_thread(f):
+        def guarded():
+            try:
+                f()
+            except Exception as e:                             # noqa: BLE001
+                raised.append(e)
+        torch.cuda.synchronize()
+        thread = threading.Thread(target=guarded)
+        thread.start()
+        thread.join()
+        torch.cuda.synchronize()
+        assert not raised, raised
+
+    def generate(ses, where):
+        sid = hk.heatkv_seq_open(ses.ctx, ses.schedule(scas=scores, b=1.0))
+        return lambda: ses.generate([sid], lambda l: (q, k, v), lambda l: where, fused=True)
+
+    def made():
+        ses = Session(sh.L, sh.H, sh.d, sh.t, sh.s, pool_rows=1 << 15, kernel=hk.KERNEL_TCGEN05)
+        contexts.append(ses)
+
+    contexts = []
+    with Session(sh.L, sh.H, sh.d, sh.t, sh.s, pool_rows=1 << 15, kernel=hk.KERNEL_TCGEN05) as ses:
+        beta, beta_want = (torch.zeros(sh.L, sh.H, sh.K, sh.K, device="cuda") for _ in range(2))
+        lo, hi = ses.step_slices(sh.K - 1)
+        qs, ks = q[:, :, lo:hi], k[:, :, :hi]
+        calibrate = lambda x: hk.heatkv_calibrate_scores(ses.ctx, 0, sh.K - 1, 1, qs, ks, None, hk.Strides.of(qs, ks), None, x, None)    # noqa: E731
+        calibrate(beta_want)
+        in_a_thread(lambda: calibrate(beta))
+        assert ((beta - beta_want).abs() <= RTOL_BETA * beta_want).all() and (beta != 0).any()      # (the sums' order is not fixed)
+        generate(ses, want)()
+        in_a_thread(generate(ses, out))
+        assert torch.equal(out, want) and (out != 0).any()
+        assert hk.heatkv_device_status(ses.ctx) == 0
+    in_a_thread(made)
+    with contexts[0] as ses:
+        out.zero_()
+        generate(ses, out)()
+        st = hk.heatkv_kernel_launches(ses.ctx)
+        assert torch.equal(out, want) and st.attention_generic == 0 and st.attention_tcgen05 == sh.K

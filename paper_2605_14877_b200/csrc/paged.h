@@ -18,13 +18,21 @@ constexpr int PAGED_MAX_PAGES = 1 << 25;       // pages of a pool: slot numbers 
 constexpr int PAGED_MAX_SELECT_PAGES = 32768;  // pages of a context whose scores one CTA keeps in shared memory
 
 // Selected pages are attended to for many tokens at once from so many new tokens a request and selected pages in all: 8 requests x 32 tokens
-// x 4 heads x 16 pages take 59 us token by token and 64 together, x 64 tokens 100 and 69, 16 heads x 16 tokens 98 and 81.
+// x 4 heads x 16 pages take 59 us token by token and 64 together, x 64 tokens 100 and 69, 16 heads x 16 tokens 98 and 81.  What is gained hangs on how
+// much the lists of neighbouring tokens have in common, which no size says.  2001 tokens, 4 kv heads of 8 heads, 16 of 500 pages: where 40 neighbours
+// have the same list 396 and 84 us, where every token has a list of its own 370 and 490 (heads of their own, G = 1: 337 and 76, 335 and 346);
+// a chunk of 300 beside 64 single tokens, 8 kv heads of 4 heads: 153 and 112, 150 and 179.
 constexpr int PAGED_SPARSE_CHUNK = 8, PAGED_SPARSE_PAGES = 24576;
 
 // Workspace: 64 words (word 0: status of bounded waits), then arrival counters, then partial results.
 constexpr int PAGED_WS_HEAD_WORDS = 64;
-constexpr int PAGED_WS_CTRS = 1024;            // one per CTA of a launch and group of 32 rows at most
+constexpr int PAGED_WS_CTRS = 1024;            // times 8: one for every run of paged_tc_kernel and 32 rows; the first also counts pieces (paged_small_kernel),
+                                               // the last CTAs (union_kernel)
 constexpr int PAGED_WS_PARTIALS = (PAGED_WS_HEAD_WORDS + PAGED_WS_CTRS * 8) * 4;
+
+// SMs that a launch is laid out for at most: a run's counters and, in paged_small_kernel, pieces of a unit (16 bits) are counted by it.
+constexpr int PAGED_MOST_SMS = 240;
+static_assert(PAGED_MOST_SMS < PAGED_WS_CTRS, "counters of every run, and a ticket");
 
 struct PagedDevice {
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;

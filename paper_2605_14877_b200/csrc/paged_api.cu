@@ -26,7 +26,7 @@ bool paged_device(PagedDevice* out) {
       return false;
     encode.store(fn, std::memory_order_relaxed);
   }
-  out->n_sm = n < 240 ? n : 240;                       // (the workspace has arrival counters for so many)
+  out->n_sm = n < PAGED_MOST_SMS ? n : PAGED_MOST_SMS;
   out->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   return true;
 }
@@ -195,7 +195,10 @@ int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_bat
   p.causal = causal != 0;
   // Up to 32 rows of the longest request: the warp-level kernel.  24 requests of 2000 tokens: 12 rows 44 us against 56 on the tensor-memory
   // kernel, 21 rows 33 and 40, 32 rows 82 and 88, 36 rows 64 and 56, 63 rows 55 and 40.  Up to 48 rows, too, where there are fewer units
-  // than SMs (42 rows, 96 units of up to 2660 tokens: 18 and 34 us; 256 units of 1000 tokens: 56 and 46).
+  // than SMs: 34 to 48 rows at 2 to 16 heads a group, 32 units of 500 tokens 16 and 24 us, of 2500 24 and 39, 64 of 2500 36 and 39; 42 rows, 96 units of
+  // 40 to 8000 tokens 17 and 34; 192 units of 500 36 and 33, of 2500 90 and 66.  (Few units of long contexts lose: 64 of 8000 83 and 69, 128 of
+  // 2500 57 and 52, of 8000 147 and 109.  Lengths are not known here, and a table is as wide as its longest request.)  49 to 64 rows: 32 units
+  // of 2500 30 and 38, of 8000 64 and 54, 64 of 2500 48 and 39.
   // And any number of tiles of 16 rows where there is little to do in all: a tile of `table_pages` pages weighs six more (its own beginning and
   // end).  One request of 8 kv heads with 4 heads each, 14 new tokens behind 500 or 8000: 10 and 25 us, 22 and 53 on the tensor-memory kernel; a
   // prompt of 100: 8 and 17; two kv heads, a prompt of 400 (weight 2600): 13 and 23, 100 behind 1500 with 8 heads each (3100): 19 and 28; 4 requests of 28

@@ -304,8 +304,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) select_kernel
 
 // ------------------------------------------------------------------------------------------------ 16 tokens, one CTA
 // A request's tokens share its pages: their codes are read once for 16 tokens and multiplied on the matrix units (as fp16, in which the
-// codes, and in 32 bits their products' sums, are exact); a warp then chooses for two tokens.  What bounds it is that choice, a chain of
-// counts: 2001 tokens, 4 kv heads, 500 pages take 28.5 us with four CTAs on an SM (64 registers), 33.8 with the two that 109 registers allow.
+// codes, and in 32 bits their products' sums, are exact); a warp then chooses for two tokens.  What bounds it is that choice (a
+// warp reads a token's scores from shared memory for the groups' maxima and again for the list, and ranks both): issue slots 56 %, the matrix unit
+// 6 %, the DRAM 6 %.  2001 tokens, 4 kv heads, 500 pages take 28.5 us with four CTAs on an SM (64 registers), 33.8 with the two that 109 registers allow.
 template <int D>
 __global__ void __launch_bounds__(ROWS_THREADS, 4) select_rows_kernel(const __grid_constant__ SelectParams p, int pitch) {
   extern __shared__ __align__(16) uint32_t keys[];            // [16][pitch] scores; 0: not to be chosen

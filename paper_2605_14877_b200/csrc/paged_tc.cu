@@ -16,9 +16,10 @@
 // if its token is among those that did: neighbouring tokens select much the same pages, so a page is read and multiplied once for all of
 // them instead of once for each.  Warp 2 brings the tokens' lists into shared memory, the copy warp merges them as it goes (a
 // token per lane and tile) and hands the tokens' bits to the softmax warps beside each tile.
-// What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 us,
-// 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax (half the
-// products per exponential: 32 heads of the first shape 670 us, 800 TFLOP/s).
+// (A tile has at most 32 tokens there, one a bit of a word, so that groups of one or two heads fill a quarter or half of its 128 rows.)
+// What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 to 470 us,
+// 1160 to 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax warps'
+// waits for tensor memory (half the products per exponential: 32 heads of the first shape 666 us, 815 TFLOP/s; no unit is busy more than 57 %).
 // Every wait is bounded in time; on expiry the CTA records which wait it was, lets its own copies land and its products end, and leaves.
 #include <algorithm>
 
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
   // fp16 probabilities for 2^15.
   constexpr float THRESHOLD = F16 ? 8.f : RESCALE_THRESHOLD;
   // One pair of exponentials in four on the FMA units where the exponential unit is as busy as anything (64-wide heads: a chunk of 1500
-  // tokens behind 20 000, 40 heads, 452 us without, 411 with one pair in four, 440 with one in two; 128-wide heads, bound by the products:
+  // tokens behind 20 000, 40 heads, 439 us without, 396 with one pair in four, 438 with one in two; 128-wide heads, bound by the products:
   // no difference, and 6 % slower with one in two).
   constexpr bool POLY = D == 64;
   const PagedParams& p = tp.a;
@@ -977,6 +978,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             return fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
           };
           const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+          // The sum takes the probabilities as 32-bit numbers; for the product with V they are rounded to the 16 bits of the matrix unit's operand in
+          // tensor memory: the result's error is then 1.3 times that of its own rounding, and a product for the low halves would be as long again.
           // (a page that the row did not select: every exponent minus infinity)
           const uint64_t none2 = pack2(-INFINITY, -INFINITY);
           uint64_t sum2 = pack2(0.f, 0.f);

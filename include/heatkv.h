@@ -530,6 +530,76 @@ int heatkv_paged_status(const void* workspace /*DEVICE*/, void* stream);
  * zeroed again), HEATKV_OK if one claimed success, HEATKV_ERR_CUDA on any other outcome.  Nothing faults, traps or hangs. */
 int heatkv_paged_selftest_wait_expiry(void* workspace /*DEVICE*/, void* stream);
 
+/* ---- a cache in 4 bits
+ * The same pages with K and V as 4-bit codes: a value is code * scale * 2^exp, whole codes from -7 to 7 kept as code + 8, one scale (an 8-bit e4m3
+ * number, not negative) for sixteen neighbouring columns of a row, exp the pool's.  72 bytes a row and head for d = 128 instead of 256.  Every
+ * such value with exp 0 is a bf16 and an fp16 number exactly.  scale = e4m3(max |x| 2^-exp * (1 / 7)), to nearest even, at most 448; code = x 2^-exp / scale
+ * to the nearest whole number, ties to even, within -7 .. 7; all 0 where the scale is 0.  Rows that are stored must be finite.
+ * A page of one head is one block of bytes: codes of K [64][d / 2], codes of V, scales of K [64][d / 16], scales of V.  In every four bytes (a word, lowest
+ * byte first, columns c .. c + 7) bits 4 i .. 4 i + 3 hold column c + 2 i for i < 4 and column c + 2 (i - 4) + 1 for the others. */
+typedef struct {                 /* one layer's pool                                                                       */
+  void* blocks;                  /* DEVICE [n_pages][n_kv_heads][64 (d + d / 8)] bytes, 16-byte aligned; strides below     */
+  int64_t page_stride, head_stride;               /* bytes, multiples of 16                                                */
+  int32_t n_pages, n_kv_heads;
+  int32_t d;                     /* 64 or 128                                                                              */
+  int32_t dtype;                 /* heatkv_dtype of the activations that go with it                                        */
+  int32_t k_exp, v_exp;          /* from -64 to 64                                                                         */
+} heatkv_paged4_pool;
+
+/* K and V rows of new tokens to their slots; arguments as heatkv_paged_store. */
+int heatkv_paged4_store(const heatkv_paged4_pool* pool /*HOST*/, const void* k_new, const void* v_new, int64_t tok_stride, int64_t head_stride,
+                        const int32_t* slot_map, int n_tokens, void* stream);
+
+/* The reverse: rows of some slots as 16-bit numbers, to k_out, v_out DEVICE [n_tokens][n_kv_heads][d] (strides at least d, multiples of 8; not the
+ * same memory).  Tokens with a slot outside of the pool get zeros; a slot may occur more than once. */
+int heatkv_paged4_load(const heatkv_paged4_pool* pool /*HOST*/, const int32_t* slot_map, int n_tokens, void* k_out, void* v_out,
+                       int64_t tok_stride, int64_t head_stride, void* stream);
+
+/* heatkv_paged_workspace_bytes and heatkv_paged_attention for a cache in 4 bits: the same arguments and results; what the pool holds
+ * past kv_len and in pages that no table lists may be any bytes.  heatkv_paged_status looks at this workspace, too. */
+int heatkv_paged4_workspace_bytes(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, uint64_t* bytes);
+int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
+                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
+                            uint64_t workspace_bytes, void* stream);
+
+/* ---- rows between steps
+ * Requests may list the same page as long as it is full for all of them: a page that is not full, where the next token goes, is listed by one row
+ * alone.  The two calls below keep it so.  They read the old lengths and table and write new ones (other buffers, so that a step can be
+ * repeated; entries past a row's pages become -1), take pages from the ring's head where rows need fresh ones and append to its end, in page
+ * order, those that the old table lists and the new one does not.  Neither touches K and V: the moves (from and to slots, -1: none) are for
+ * heatkv_paged_move or heatkv_paged4_move on every layer's pool, before anything else writes to the pools.
+ * heatkv_paged_release must not be used while rows share pages (it would give them back for all): heatkv_paged_fork does its work, too.
+ *   lengths DEVICE [n_seq] tokens of every row; block_table, table_out DEVICE [n_seq][table_pages], rows table_stride and out_stride apart
+ *   free_pages DEVICE [n_pages] in and out, state, state_out DEVICE int32[4] as in heatkv_paged_tables
+ *   workspace DEVICE, heatkv_paged_rows_workspace_bytes, 16-byte aligned, zero before its first use; for calls that do not overlap */
+int heatkv_paged_rows_workspace_bytes(int n_seq, int table_pages, int n_pages, uint64_t* bytes);
+
+/* Row i goes on as a copy of row parents[i] (its own number: as it is; none of 0 .. n_seq - 1: it is over) with its first keep_len[i] tokens at most
+ * (negative counts as 0; keep_len NULL: all).  Whole pages are shared.  A page that is not full stays with one row: the lowest of those that go
+ * on from themselves, else the lowest; every other row, and all of them where some row has all of the page, get a fresh page, in row order, and its
+ * tokens' moves: entries 64 i .. of move_from and move_to, DEVICE [64 n_seq].  Where the free pages end, rows lose the tokens of that page: lengths_out
+ * says how many they have.  state_out: {place and entries of the ring, rows that lost tokens, pages given back} */
+int heatkv_paged_fork(const int32_t* parents, const int32_t* keep_len, const int32_t* lengths, int n_seq, const int32_t* block_table,
+                      int64_t table_stride, int table_pages, int32_t* free_pages, int n_pages, const int32_t* state, int32_t* lengths_out,
+                      int32_t* table_out, int64_t out_stride, int32_t* state_out, int32_t* move_from, int32_t* move_to, void* workspace,
+                      uint64_t workspace_bytes, void* stream);
+
+/* Token t of row i leaves the cache where stays[i][t] (DEVICE bytes, rows stays_stride apart, stays_width of each) is 0; tokens past the width stay.
+ * Pages before the first token that leaves stay as they are; the tokens behind move together into fresh pages, in order.  Rows take their fresh
+ * pages in row order; from the first row on for which the free ones, or the n_moves entries of move_from and move_to, do not suffice, every
+ * row that needs some is left as it is.  The moves lie one after another, row by row, token by token; -1 past the last.
+ * state_out: {place and entries of the ring, rows left as they are, tokens moved}.  A row's K keep the positions that they were encoded
+ * with, while the places that heatkv_paged_tables counts go on from the new length. */
+int heatkv_paged_compact(const uint8_t* stays, int64_t stays_stride, int stays_width, const int32_t* lengths, int n_seq,
+                         const int32_t* block_table, int64_t table_stride, int table_pages, int32_t* free_pages, int n_pages,
+                         const int32_t* state, int32_t* lengths_out, int32_t* table_out, int64_t out_stride, int32_t* state_out,
+                         int32_t* move_from, int32_t* move_to, int n_moves, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* K and V of all heads from slot from[i] to slot to[i], DEVICE [n_moves]; nothing where either lies outside of the pool.  No slot may occur twice
+ * in `to`, nor in both.  With page summaries kept, pages whose last row is among `to` get theirs. */
+int heatkv_paged_move(const heatkv_paged_pool* pool /*HOST*/, const int32_t* from, const int32_t* to, int n_moves, void* stream);
+int heatkv_paged4_move(const heatkv_paged4_pool* pool /*HOST*/, const int32_t* from, const int32_t* to, int n_moves, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

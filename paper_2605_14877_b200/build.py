@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libheatkv.so")
 NATIVE = os.path.join(HERE, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 PAGED = os.path.join(HERE, os.path.basename(NATIVE).replace("_native", "_paged"))
 SOURCES = ["schedule.cpp", "plan.cpp", "split.cpp", "api.cu", "attn_generic.cu", "attn_tc.cu", "attn_pair.cu", "calib_tc.cu", "cache_kernels.cu",
-           "paged_api.cu", "paged_tables.cu", "paged_select.cu", "paged_small.cu", "paged_tc.cu"]
+           "paged_api.cu", "paged_tables.cu", "paged_select.cu", "paged_small.cu", "paged_tc.cu",
+           "paged_rows.cu", "paged4_rows.cu", "paged4_small.cu"]
 
 
 def _stale() -> bool:

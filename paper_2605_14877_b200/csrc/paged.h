@@ -91,9 +91,26 @@ struct PagedParams {
   int32_t max_new;
 };
 
+// the 4-bit cache
+struct Store4Params {
+  const void *k_new, *v_new;        // (read back: written)
+  unsigned char* blocks;
+  const int32_t* slot_map;
+  int64_t tok, head, page_stride, head_stride;      // strides of the blocks in bytes
+  int32_t n_tokens, n_pages, Hkv, fp16, k_exp, v_exp;
+};
+struct Paged4Params {
+  PagedParams a;                    // scale_log2 holds what the numbers of K are to be multiplied by
+  const unsigned char* blocks;
+  int64_t page_stride, head_stride; // bytes
+  float v_unit;                     // .. and those of V
+  int32_t fp16;                     // type of q and out
+};
+
 cudaError_t launch_paged_tables(const TablesParams& p, cudaStream_t stream);
 cudaError_t launch_paged_release(const ReleaseParams& p, cudaStream_t stream);
 cudaError_t launch_paged_store(StoreParams p, cudaStream_t stream);
+cudaError_t launch_paged_summaries(const StoreParams& p, cudaStream_t stream);
 cudaError_t launch_paged_select(const SelectParams& p, int max_new, int n_sm, cudaStream_t stream);
 // warp-level kernel: row tiles of up to 64 rows
 uint64_t paged_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens);
@@ -102,6 +119,10 @@ cudaError_t launch_paged_small(const PagedParams& p, const heatkv_paged_pool& po
 uint64_t paged_tc_partial_bytes(int d, int n_sm, int G, int Hkv, int n_tokens, int n_seq);
 bool paged_tc_takes_lists(int G, int Hkv, int n_sel, int table_pages, int n_tokens, int n_seq);
 cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream);
+
+cudaError_t launch_paged4_rows(const Store4Params& p, bool load, int d, cudaStream_t stream);
+uint64_t paged4_small_partial_bytes(int d, int n_sm, int Hkv, int n_tokens);
+cudaError_t launch_paged4_small(const Paged4Params& p, int d, const PagedDevice& dev, cudaStream_t stream);
 
 // A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.
 inline bool paged_encode(const PagedDevice& dev, CUtensorMap* m, void* base, int dtype, const cuuint64_t* dims, const cuuint64_t* strides,

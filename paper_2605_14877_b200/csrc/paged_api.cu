@@ -1,6 +1,7 @@
 // Entry points of the paged cache: checks of arguments and kernel choice.
 #include <atomic>
 
+#include "paged_rows.cuh"
 #include "paged_wait.cuh"
 
 namespace heatkv {
@@ -43,7 +44,18 @@ int check_pool(const heatkv_paged_pool* p) {
   return HEATKV_OK;
 }
 
-int check_batch(const heatkv_paged_pool* pool, const heatkv_paged_batch* b, int n_heads) {
+int check_pool(const heatkv_paged4_pool* p) {
+  if (!p || !p->blocks || p->n_pages < 1 || p->n_kv_heads < 1) return HEATKV_ERR_INVALID_ARG;
+  if ((p->d != 64 && p->d != 128) || (p->dtype != HEATKV_DTYPE_BF16 && p->dtype != HEATKV_DTYPE_FP16)) return HEATKV_ERR_INVALID_ARG;
+  if (p->n_pages > PAGED_MAX_PAGES || p->n_kv_heads > 4096) return HEATKV_ERR_TOO_LARGE;
+  if (!aligned(p->blocks, 16) || ((p->page_stride | p->head_stride) & 15)) return HEATKV_ERR_INVALID_ARG;
+  if (p->page_stride < block4_bytes(p->d) || p->head_stride < block4_bytes(p->d)) return HEATKV_ERR_INVALID_ARG;
+  if (p->k_exp < -64 || p->k_exp > 64 || p->v_exp < -64 || p->v_exp > 64) return HEATKV_ERR_INVALID_ARG;
+  return HEATKV_OK;
+}
+
+template <typename Pool>
+int check_batch(const Pool* pool, const heatkv_paged_batch* b, int n_heads) {
   const int rc = check_pool(pool);
   if (rc != HEATKV_OK) return rc;
   if (!b || !b->q_begin || !b->kv_len || !b->block_table || b->n_seq < 1 || b->n_tokens < 1 || b->table_pages < 1 || b->max_new < 1)
@@ -56,7 +68,8 @@ int check_batch(const heatkv_paged_pool* pool, const heatkv_paged_batch* b, int 
 }
 
 // Fills the part of the parameters that all calls over a batch share.
-int attention_params(const heatkv_paged_pool* pool, const heatkv_paged_batch* b, int n_heads, const void* q, const heatkv_token_strides* st,
+template <typename Pool>
+int attention_params(const Pool* pool, const heatkv_paged_batch* b, int n_heads, const void* q, const heatkv_token_strides* st,
                      float sm_scale, void* out, float* lse, PagedParams* p) {
   const int rc = check_batch(pool, b, n_heads);
   if (rc != HEATKV_OK) return rc;
@@ -95,9 +108,15 @@ uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_to
   return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 
-int place_workspace(const PagedDevice& dev, const heatkv_paged_pool* pool, void* ws, uint64_t bytes, PagedParams* p) {
+uint64_t workspace4_bytes(const PagedDevice& dev, int d, int, int Hkv, int n_tokens, int) {
+  return PAGED_WS_PARTIALS + paged4_small_partial_bytes(d, dev.n_sm, Hkv, n_tokens);
+}
+
+uint64_t needed_bytes(const PagedDevice& dev, int d, const PagedParams& p) { return workspace_bytes(dev, d, p.G, p.Hkv, p.n_tokens, p.n_seq); }
+
+int place_workspace(uint64_t need, void* ws, uint64_t bytes, PagedParams* p) {
   if (!ws || !aligned(ws, 256)) return HEATKV_ERR_INVALID_ARG;
-  if (bytes < workspace_bytes(dev, pool->d, p->G, p->Hkv, p->n_tokens, p->n_seq)) return HEATKV_ERR_TOO_LARGE;
+  if (bytes < need) return HEATKV_ERR_TOO_LARGE;
   p->status = static_cast<uint32_t*>(ws);
   p->counters = p->status + PAGED_WS_HEAD_WORDS;
   p->partials = reinterpret_cast<float*>(static_cast<char*>(ws) + PAGED_WS_PARTIALS);
@@ -184,13 +203,13 @@ int heatkv_paged_workspace_bytes(const heatkv_paged_pool* pool, const heatkv_pag
 
 int heatkv_paged_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,
-                           uint64_t workspace_bytes, void* stream) {
+                           uint64_t bytes, void* stream) {
   PagedParams p;
   int rc = attention_params(pool, batch, n_heads, q, st, sm_scale, out, lse, &p);
   if (rc != HEATKV_OK) return rc;
   PagedDevice dev;
   if (!paged_device(&dev)) return done(cudaErrorInitializationError);
-  rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);
+  rc = place_workspace(needed_bytes(dev, pool->d, p), workspace, bytes, &p);
   if (rc != HEATKV_OK) return rc;
   p.causal = causal != 0;
   // Up to 32 rows of the longest request: the warp-level kernel.  24 requests of 2000 tokens: 12 rows 44 us against 56 on the tensor-memory
@@ -229,7 +248,7 @@ int heatkv_paged_select(const heatkv_paged_pool* pool, const heatkv_paged_batch*
 
 int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                                   const heatkv_token_strides* st, const int32_t* sel, int n_select, float sm_scale, void* out, float* lse,
-                                  void* workspace, uint64_t workspace_bytes, void* stream) {
+                                  void* workspace, uint64_t bytes, void* stream) {
   PagedParams p;
   int rc = attention_params(pool, batch, n_heads, q, st, sm_scale, out, lse, &p);
   if (rc != HEATKV_OK) return rc;
@@ -238,7 +257,7 @@ int heatkv_paged_sparse_attention(const heatkv_paged_pool* pool, const heatkv_pa
   if ((int64_t)p.n_tokens * p.Hkv * ((n_select + 3) / 4) > (1 << 30)) return HEATKV_ERR_TOO_LARGE;
   PagedDevice dev;
   if (!paged_device(&dev)) return done(cudaErrorInitializationError);
-  rc = place_workspace(dev, pool, workspace, workspace_bytes, &p);
+  rc = place_workspace(needed_bytes(dev, pool->d, p), workspace, bytes, &p);
   if (rc != HEATKV_OK) return rc;
   p.causal = 1;
   p.sel = sel;
@@ -270,6 +289,162 @@ int heatkv_paged_selftest_wait_expiry(void* workspace, void* stream) {
     return done(cudaErrorUnknown);
   if (host[RESULT] == 1) return HEATKV_OK;
   return host[RESULT] == 2 && host[0] == EXPIRY_CODE ? HEATKV_ERR_DEVICE_TIMEOUT : HEATKV_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- 4 bits
+namespace {
+int rows4(const heatkv_paged4_pool* pool, const void* k, const void* v, int64_t tok_stride, int64_t head_stride, const int32_t* slot_map, int n_tokens,
+          bool load, void* stream) {
+  const int rc = check_pool(pool);
+  if (rc != HEATKV_OK) return rc;
+  if (!k || !v || !slot_map || n_tokens < 1 || !aligned(k, 16) || !aligned(v, 16) || ((tok_stride | head_stride) & 7) || tok_stride < 0 || head_stride < 0)
+    return HEATKV_ERR_INVALID_ARG;
+  if (load && (tok_stride < pool->d || head_stride < pool->d)) return HEATKV_ERR_INVALID_ARG;      // (rows that are written share no memory)
+  const Store4Params p = {k, v, static_cast<unsigned char*>(pool->blocks), slot_map, tok_stride, head_stride, pool->page_stride, pool->head_stride,
+                          n_tokens, pool->n_pages, pool->n_kv_heads, pool->dtype == HEATKV_DTYPE_FP16, pool->k_exp, pool->v_exp};
+  return done(launch_paged4_rows(p, load, pool->d, static_cast<cudaStream_t>(stream)));
+}
+}  // namespace
+
+int heatkv_paged4_store(const heatkv_paged4_pool* pool, const void* k_new, const void* v_new, int64_t tok_stride, int64_t head_stride,
+                        const int32_t* slot_map, int n_tokens, void* stream) {
+  return rows4(pool, k_new, v_new, tok_stride, head_stride, slot_map, n_tokens, false, stream);
+}
+
+int heatkv_paged4_load(const heatkv_paged4_pool* pool, const int32_t* slot_map, int n_tokens, void* k_out, void* v_out, int64_t tok_stride,
+                       int64_t head_stride, void* stream) {
+  if (k_out == v_out) return HEATKV_ERR_INVALID_ARG;
+  return rows4(pool, k_out, v_out, tok_stride, head_stride, slot_map, n_tokens, true, stream);
+}
+
+int heatkv_paged4_workspace_bytes(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, uint64_t* bytes) {
+  const int rc = check_batch(pool, batch, n_heads);
+  if (rc != HEATKV_OK) return rc;
+  PagedDevice dev;
+  if (!bytes) return HEATKV_ERR_INVALID_ARG;
+  if (!paged_device(&dev)) return done(cudaErrorInitializationError);
+  *bytes = workspace4_bytes(dev, pool->d, n_heads / pool->n_kv_heads, pool->n_kv_heads, batch->n_tokens, batch->n_seq);
+  return HEATKV_OK;
+}
+
+int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
+                            const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace, uint64_t bytes,
+                            void* stream) {
+  Paged4Params p;
+  int rc = attention_params(pool, batch, n_heads, q, st, sm_scale, out, lse, &p.a);
+  if (rc != HEATKV_OK) return rc;
+  PagedDevice dev;
+  if (!paged_device(&dev)) return done(cudaErrorInitializationError);
+  rc = place_workspace(workspace4_bytes(dev, pool->d, p.a.G, p.a.Hkv, p.a.n_tokens, p.a.n_seq), workspace, bytes, &p.a);
+  if (rc != HEATKV_OK) return rc;
+  p.a.causal = causal != 0;
+  p.a.scale_log2 *= ldexpf(VALUES4_UNIT, pool->k_exp);
+  p.v_unit = ldexpf(VALUES4_UNIT, pool->v_exp);
+  p.blocks = static_cast<const unsigned char*>(pool->blocks);
+  p.page_stride = pool->page_stride;
+  p.head_stride = pool->head_stride;
+  p.fp16 = pool->dtype == HEATKV_DTYPE_FP16;
+  return done(launch_paged4_small(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------- rows between steps
+namespace {
+int rearrange(RowsParams* p, void* workspace, uint64_t bytes, bool compact, void* stream) {
+  if (!p->lengths || !p->table || !p->free_pages || !p->state_in || !p->lengths_out || !p->table_out || !p->state_out || !p->move_from || !p->move_to ||
+      !workspace || !aligned(workspace, 16))
+    return HEATKV_ERR_INVALID_ARG;
+  if (p->n_seq < 1 || p->n_pages < 1 || p->table_pages < 1 || p->table_stride < p->table_pages || p->out_stride < p->table_pages || p->n_moves < 1)
+    return HEATKV_ERR_INVALID_ARG;
+  // (read by all CTAs while one writes)
+  if (p->lengths == p->lengths_out || p->table == p->table_out || p->state_in == p->state_out || p->move_from == p->move_to) return HEATKV_ERR_INVALID_ARG;
+  if (p->n_seq > PAGED_MAX_SEQ || p->n_pages > PAGED_MAX_PAGES || p->table_pages > PAGED_MAX_TABLE) return HEATKV_ERR_TOO_LARGE;
+  if (bytes < rows_workspace_bytes(p->n_seq, p->table_pages, p->n_pages)) return HEATKV_ERR_TOO_LARGE;
+  place_rows_workspace(workspace, p);
+  return done((compact ? launch_paged_compact : launch_paged_fork)(*p, static_cast<cudaStream_t>(stream)));
+}
+}  // namespace
+
+int heatkv_paged_rows_workspace_bytes(int n_seq, int table_pages, int n_pages, uint64_t* bytes) {
+  if (!bytes || n_seq < 1 || table_pages < 1 || n_pages < 1) return HEATKV_ERR_INVALID_ARG;
+  if (n_seq > PAGED_MAX_SEQ || n_pages > PAGED_MAX_PAGES || table_pages > PAGED_MAX_TABLE) return HEATKV_ERR_TOO_LARGE;
+  *bytes = rows_workspace_bytes(n_seq, table_pages, n_pages);
+  return HEATKV_OK;
+}
+
+int heatkv_paged_fork(const int32_t* parents, const int32_t* keep_len, const int32_t* lengths, int n_seq, const int32_t* block_table,
+                      int64_t table_stride, int table_pages, int32_t* free_pages, int n_pages, const int32_t* state, int32_t* lengths_out,
+                      int32_t* table_out, int64_t out_stride, int32_t* state_out, int32_t* move_from, int32_t* move_to, void* workspace,
+                      uint64_t workspace_bytes, void* stream) {
+  if (!parents) return HEATKV_ERR_INVALID_ARG;
+  RowsParams p = {};
+  p.parents = parents;
+  p.keep_len = keep_len;
+  p.lengths = lengths;
+  p.table = block_table;
+  p.state_in = state;
+  p.table_stride = table_stride;
+  p.out_stride = out_stride;
+  p.free_pages = free_pages;
+  p.lengths_out = lengths_out;
+  p.table_out = table_out;
+  p.state_out = state_out;
+  p.move_from = move_from;
+  p.move_to = move_to;
+  p.n_seq = n_seq;
+  p.table_pages = table_pages;
+  p.n_pages = n_pages;
+  p.n_moves = n_seq > 0 && n_seq <= PAGED_MAX_SEQ ? n_seq * PAGE : 0;
+  return rearrange(&p, workspace, workspace_bytes, false, stream);
+}
+
+int heatkv_paged_compact(const uint8_t* stays, int64_t stays_stride, int stays_width, const int32_t* lengths, int n_seq, const int32_t* block_table,
+                         int64_t table_stride, int table_pages, int32_t* free_pages, int n_pages, const int32_t* state, int32_t* lengths_out,
+                         int32_t* table_out, int64_t out_stride, int32_t* state_out, int32_t* move_from, int32_t* move_to, int n_moves,
+                         void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!stays || stays_width < 0 || stays_stride < stays_width) return HEATKV_ERR_INVALID_ARG;
+  RowsParams p = {};
+  p.mask = stays;
+  p.mask_stride = stays_stride;
+  p.mask_width = stays_width;
+  p.lengths = lengths;
+  p.table = block_table;
+  p.state_in = state;
+  p.table_stride = table_stride;
+  p.out_stride = out_stride;
+  p.free_pages = free_pages;
+  p.lengths_out = lengths_out;
+  p.table_out = table_out;
+  p.state_out = state_out;
+  p.move_from = move_from;
+  p.move_to = move_to;
+  p.n_seq = n_seq;
+  p.table_pages = table_pages;
+  p.n_pages = n_pages;
+  p.n_moves = n_moves;
+  return rearrange(&p, workspace, workspace_bytes, true, stream);
+}
+
+int heatkv_paged_move(const heatkv_paged_pool* pool, const int32_t* from, const int32_t* to, int n_moves, void* stream) {
+  const int rc = check_pool(pool);
+  if (rc != HEATKV_OK) return rc;
+  if (!from || !to || n_moves < 1) return HEATKV_ERR_INVALID_ARG;
+  const MoveParams p = {pool->k, pool->v, from, to, pool->page_stride, pool->head_stride, pool->row_stride, n_moves, pool->n_pages, pool->n_kv_heads,
+                        pool->d};
+  cudaError_t rc2 = launch_paged_move(p, 16, static_cast<cudaStream_t>(stream));
+  if (rc2 == cudaSuccess && pool->k_code) {
+    const StoreParams s = {nullptr, nullptr, pool->k, pool->v, pool->k_code, pool->k_scale, to, 0, 0, pool->page_stride, pool->head_stride, pool->row_stride,
+                           n_moves, pool->n_pages, pool->n_kv_heads, pool->d, pool->dtype == HEATKV_DTYPE_FP16, 0};
+    rc2 = launch_paged_summaries(s, static_cast<cudaStream_t>(stream));
+  }
+  return done(rc2);
+}
+
+int heatkv_paged4_move(const heatkv_paged4_pool* pool, const int32_t* from, const int32_t* to, int n_moves, void* stream) {
+  const int rc = check_pool(pool);
+  if (rc != HEATKV_OK) return rc;
+  if (!from || !to || n_moves < 1) return HEATKV_ERR_INVALID_ARG;
+  const MoveParams p = {pool->blocks, nullptr, from, to, pool->page_stride, pool->head_stride, 0, n_moves, pool->n_pages, pool->n_kv_heads, pool->d};
+  return done(launch_paged_move(p, 4, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -232,51 +232,21 @@ __device__ __forceinline__ float2 widen(uint32_t w, bool fp16) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
-// Blocks 0 .. copy_blocks - 1 copy rows, 16 bytes at a time; the others look for pages whose row 63 is written by this call and
-// write the summary of each: mean key as 8-bit codes and a scale.  The mean is a tree (rows i and i + 32, then i and i + 16, ..), so
-// its value depends on the page's rows alone.  Rows that this call writes are read from the caller's tensor, since the pool's may not be
-// there yet: a request's tokens lie one after another in position order.  6 356 rows of 16 kv heads, 128 columns (104 MB read and written) take
-// 21.6 us, 4.8 TB/s, a decode's 64 rows 2.1.  What bounds it is waiting for loads (a word's address stands behind its slot's load and two 64-bit
-// divisions; four words of K and of V are on their way per thread): the DRAM is busy 42 % of the time, the issue slots 44 %.
-template <int D>
-__global__ void __launch_bounds__(ST) store_kernel(const StoreParams p) {
+__device__ __forceinline__ const __nv_bfloat16* pool_row(const StoreParams& p, int page, int row, int h) {
+  return static_cast<const __nv_bfloat16*>(p.k) + (int64_t)page * p.page_stride + h * p.head_stride + (int64_t)row * p.row_stride;
+}
+
+// Pages whose row 63 is among the slots of 64 tokens, for one head: mean key as 8-bit codes and a scale.  row_at(token, slot, row, head): where row `row` of
+// the page lies whose last row is the token's.
+template <int D, typename Row>
+__device__ __forceinline__ void summaries(const StoreParams& p, int unit, Row row_at) {
   constexpr int CH = D / 8;
-  pdl_trigger();
-  pdl_wait();
-  const uint32_t n_slots = (uint32_t)p.n_pages * PAGE;
-  if ((int)blockIdx.x < p.copy_blocks) {
-    const int64_t total = (int64_t)p.n_tokens * p.Hkv * CH;
-    const int64_t base = (int64_t)blockIdx.x * (ST * STORE_UNROLL) + threadIdx.x;
-    int4 k[STORE_UNROLL], v[STORE_UNROLL];
-    int64_t dst[STORE_UNROLL];
-#pragma unroll
-    for (int u = 0; u < STORE_UNROLL; ++u) {
-      const int64_t i = base + u * ST;
-      dst[u] = -1;
-      if (i >= total) continue;
-      const int ch = (int)(i % CH);
-      const int64_t th = i / CH;
-      const int h = (int)(th % p.Hkv);
-      const int64_t t = th / p.Hkv;
-      const uint32_t slot = (uint32_t)p.slot_map[t];
-      const int64_t src = t * p.tok + h * p.head + ch * 8;
-      k[u] = __ldg(reinterpret_cast<const int4*>(static_cast<const __nv_bfloat16*>(p.k_new) + src));
-      v[u] = __ldg(reinterpret_cast<const int4*>(static_cast<const __nv_bfloat16*>(p.v_new) + src));
-      if (slot < n_slots) dst[u] = (int64_t)(slot / PAGE) * p.page_stride + h * p.head_stride + (int64_t)(slot % PAGE) * p.row_stride + ch * 8;
-    }
-#pragma unroll
-    for (int u = 0; u < STORE_UNROLL; ++u) {
-      if (dst[u] < 0) continue;
-      *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.k) + dst[u]) = k[u];
-      *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.v) + dst[u]) = v[u];
-    }
-    return;
-  }
   __shared__ float part[8][D];
   __shared__ float tops[ST / 32];
   __shared__ int found[SUMMARY_TOKENS];
   __shared__ int n_found;
-  const int unit = blockIdx.x - p.copy_blocks, h = unit % p.Hkv, t0 = unit / p.Hkv * SUMMARY_TOKENS;
+  const uint32_t n_slots = (uint32_t)p.n_pages * PAGE;
+  const int h = unit % p.Hkv, t0 = unit / p.Hkv * SUMMARY_TOKENS;
   if (threadIdx.x == 0) n_found = 0;
   __syncthreads();
   if (threadIdx.x < SUMMARY_TOKENS && t0 + (int)threadIdx.x < p.n_tokens) {
@@ -292,11 +262,7 @@ __global__ void __launch_bounds__(ST) store_kernel(const StoreParams p) {
       int4 w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int row = rg + 8 * j, tt = t - (PAGE - 1 - row);
-        const bool fresh = tt >= 0 && p.slot_map[tt] == slot - (PAGE - 1 - row);
-        const __nv_bfloat16* src = fresh ? static_cast<const __nv_bfloat16*>(p.k_new) + (int64_t)tt * p.tok + h * p.head
-                                         : static_cast<const __nv_bfloat16*>(p.k) + (int64_t)page * p.page_stride + h * p.head_stride + (int64_t)row * p.row_stride;
-        w[j] = *reinterpret_cast<const int4*>(src + ch * 8);
+        w[j] = *reinterpret_cast<const int4*>(row_at(t, slot, rg + 8 * j, h) + ch * 8);
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -337,6 +303,61 @@ __global__ void __launch_bounds__(ST) store_kernel(const StoreParams p) {
   }
 }
 
+// Blocks 0 .. copy_blocks - 1 copy rows, 16 bytes at a time; the others look for pages whose row 63 is written by this call and
+// write the summary of each: mean key as 8-bit codes and a scale.  The mean is a tree (rows i and i + 32, then i and i + 16, ..), so
+// its value depends on the page's rows alone.  Rows that this call writes are read from the caller's tensor, since the pool's may not be
+// there yet: a request's tokens lie one after another in position order.  6 356 rows of 16 kv heads, 128 columns (104 MB read and written) take
+// 21.6 us, 4.8 TB/s, a decode's 64 rows 2.1.  What bounds it is waiting for loads (a word's address stands behind its slot's load and two 64-bit
+// divisions; four words of K and of V are on their way per thread): the DRAM is busy 42 % of the time, the issue slots 44 %.
+template <int D>
+__global__ void __launch_bounds__(ST) store_kernel(const StoreParams p) {
+  constexpr int CH = D / 8;
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t n_slots = (uint32_t)p.n_pages * PAGE;
+  if ((int)blockIdx.x < p.copy_blocks) {
+    const int64_t total = (int64_t)p.n_tokens * p.Hkv * CH;
+    const int64_t base = (int64_t)blockIdx.x * (ST * STORE_UNROLL) + threadIdx.x;
+    int4 k[STORE_UNROLL], v[STORE_UNROLL];
+    int64_t dst[STORE_UNROLL];
+#pragma unroll
+    for (int u = 0; u < STORE_UNROLL; ++u) {
+      const int64_t i = base + u * ST;
+      dst[u] = -1;
+      if (i >= total) continue;
+      const int ch = (int)(i % CH);
+      const int64_t th = i / CH;
+      const int h = (int)(th % p.Hkv);
+      const int64_t t = th / p.Hkv;
+      const uint32_t slot = (uint32_t)p.slot_map[t];
+      const int64_t src = t * p.tok + h * p.head + ch * 8;
+      k[u] = __ldg(reinterpret_cast<const int4*>(static_cast<const __nv_bfloat16*>(p.k_new) + src));
+      v[u] = __ldg(reinterpret_cast<const int4*>(static_cast<const __nv_bfloat16*>(p.v_new) + src));
+      if (slot < n_slots) dst[u] = (int64_t)(slot / PAGE) * p.page_stride + h * p.head_stride + (int64_t)(slot % PAGE) * p.row_stride + ch * 8;
+    }
+#pragma unroll
+    for (int u = 0; u < STORE_UNROLL; ++u) {
+      if (dst[u] < 0) continue;
+      *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.k) + dst[u]) = k[u];
+      *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.v) + dst[u]) = v[u];
+    }
+    return;
+  }
+  summaries<D>(p, (int)blockIdx.x - p.copy_blocks, [&](int t, int slot, int row, int h) {
+    const int tt = t - (PAGE - 1 - row);
+    const bool fresh = tt >= 0 && p.slot_map[tt] == slot - (PAGE - 1 - row);
+    return fresh ? static_cast<const __nv_bfloat16*>(p.k_new) + (int64_t)tt * p.tok + h * p.head : pool_row(p, slot / PAGE, row, h);
+  });
+}
+
+// The summaries alone, of pages whose last row is among the slots: all rows are in the pool.
+template <int D>
+__global__ void __launch_bounds__(ST) summary_kernel(const StoreParams p) {
+  pdl_trigger();
+  pdl_wait();
+  summaries<D>(p, (int)blockIdx.x, [&](int, int slot, int row, int h) { return pool_row(p, slot / PAGE, row, h); });
+}
+
 }  // namespace
 
 cudaError_t launch_paged_tables(const TablesParams& p, cudaStream_t stream) {
@@ -363,6 +384,13 @@ cudaError_t launch_paged_store(StoreParams p, cudaStream_t stream) {
   p.copy_blocks = (int)copy;
   const dim3 grid((unsigned)(copy + sums));
   return p.d == 128 ? launch_pdl(store_kernel<128>, grid, dim3(ST), 0, stream, p) : launch_pdl(store_kernel<64>, grid, dim3(ST), 0, stream, p);
+}
+
+cudaError_t launch_paged_summaries(const StoreParams& p, cudaStream_t stream) {
+  const int64_t blocks = (int64_t)((p.n_tokens + SUMMARY_TOKENS - 1) / SUMMARY_TOKENS) * p.Hkv;
+  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
+  return p.d == 128 ? launch_pdl(summary_kernel<128>, grid, dim3(ST), 0, stream, p) : launch_pdl(summary_kernel<64>, grid, dim3(ST), 0, stream, p);
 }
 
 }  // namespace heatkv

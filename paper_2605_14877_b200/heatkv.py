@@ -29,6 +29,8 @@ __all__ = [
     "PagedPool", "PagedBatch", "TokenStrides", "DTYPE_BF16", "DTYPE_FP16", "PAGED_MAX_SEQ", "PAGED_MAX_SELECT", "heatkv_paged_tables",
     "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention", "heatkv_paged_select",
     "heatkv_paged_sparse_attention", "heatkv_paged_status", "heatkv_paged_selftest_wait_expiry",
+    "PagedPool4", "heatkv_paged4_store", "heatkv_paged4_load", "heatkv_paged4_workspace_bytes", "heatkv_paged4_attention", "heatkv_paged4_move",
+    "heatkv_paged_rows_workspace_bytes", "heatkv_paged_fork", "heatkv_paged_compact", "heatkv_paged_move",
 ]
 
 MAX_K, MAX_BATCH, PAGE_TOKENS = 16, 128, 64
@@ -180,6 +182,35 @@ class PagedPool(C.Structure):
         return p
 
 
+class PagedPool4(C.Structure):
+    """One layer's pages in 4 bits: blocks uint8 [n_pages, n_kv_heads, 64 * (d + d // 8)] (a block's bytes contiguous, any other strides that are
+    multiples of 16), dtype of the activations that go with them; values are code * scale * 2^exp.  Keeps the tensor alive."""
+    _fields_ = [("blocks", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("d", C.c_int32), ("dtype", C.c_int32), ("k_exp", C.c_int32), ("v_exp", C.c_int32)]
+
+    @classmethod
+    def make(cls, blocks: torch.Tensor, d: int, dtype: torch.dtype, k_exp: int = 0, v_exp: int = 0) -> "PagedPool4":
+        if dtype not in _DTYPES:
+            raise ValueError(f"dtype: expected bfloat16 or float16, got {dtype}")
+        _expect(blocks, torch.uint8, (None, None, cls.block_bytes(d)), "blocks")
+        if blocks.stride(2) != 1:
+            raise ValueError("blocks: expected the last dimension contiguous")
+        p = cls()
+        p.tensors = (blocks,)
+        p.device = blocks.get_device()
+        p.blocks = blocks.data_ptr()
+        p.page_stride, p.head_stride = blocks.stride()[:2]
+        p.n_pages, p.n_kv_heads, p.d, p.dtype = blocks.shape[0], blocks.shape[1], int(d), _DTYPES[dtype]
+        p.k_exp, p.v_exp = int(k_exp), int(v_exp)
+        p.torch_dtype, p.addr4 = dtype, C.addressof(p)             # (not `addr`: the calls over 16-bit pools take that for their own)
+        return p
+
+    @staticmethod
+    def block_bytes(d: int) -> int:
+        """Bytes of a page of one head."""
+        return PAGE_TOKENS * (d + d // 8)
+
+
 class PagedBatch(C.Structure):
     """The requests of a step: int32 tensors q_begin [n_seq + 1], kv_len [n_seq], block_table [n_seq, pages]; n_tokens rows in the token
     tensors, max_new new tokens in the longest request.  Keeps the tensors alive."""
@@ -224,7 +255,9 @@ def exported_symbols():
             "heatkv_kernel_launches", "heatkv_pair_launches", "heatkv_lone_launches", "heatkv_last_attention", "heatkv_rank_dispersion", "heatkv_selftest_wait_expiry", "heatkv_device_status",
             "heatkv_strerror",
             "heatkv_paged_tables", "heatkv_paged_release", "heatkv_paged_store", "heatkv_paged_workspace_bytes", "heatkv_paged_attention",
-            "heatkv_paged_select", "heatkv_paged_sparse_attention", "heatkv_paged_status", "heatkv_paged_selftest_wait_expiry"]
+            "heatkv_paged_select", "heatkv_paged_sparse_attention", "heatkv_paged_status", "heatkv_paged_selftest_wait_expiry",
+            "heatkv_paged4_store", "heatkv_paged4_load", "heatkv_paged4_workspace_bytes", "heatkv_paged4_attention",
+            "heatkv_paged_rows_workspace_bytes", "heatkv_paged_fork", "heatkv_paged_compact", "heatkv_paged_move", "heatkv_paged4_move"]
 
 
 def _load() -> C.CDLL:
@@ -290,6 +323,15 @@ _lib.heatkv_paged_select.argtypes = [_P, _P, _I, _P, _P, _I, _I, _I, _P, _P]
 _lib.heatkv_paged_sparse_attention.argtypes = [_P, _P, _I, _P, _P, _P, _I, C.c_float, _P, _P, _P, C.c_uint64, _P]
 _lib.heatkv_paged_status.argtypes = [_P, _P]
 _lib.heatkv_paged_selftest_wait_expiry.argtypes = [_P, _P]
+_lib.heatkv_paged4_store.argtypes = [_P, _P, _P, _L, _L, _P, _I, _P]
+_lib.heatkv_paged4_load.argtypes = [_P, _P, _I, _P, _P, _L, _L, _P]
+_lib.heatkv_paged4_workspace_bytes.argtypes = [_P, _P, _I, C.POINTER(C.c_uint64)]
+_lib.heatkv_paged4_attention.argtypes = [_P, _P, _I, _P, _P, _I, C.c_float, _P, _P, _P, C.c_uint64, _P]
+_lib.heatkv_paged_rows_workspace_bytes.argtypes = [_I, _I, _I, C.POINTER(C.c_uint64)]
+_lib.heatkv_paged_fork.argtypes = [_P, _P, _P, _I, _P, _L, _I, _P, _I, _P, _P, _P, _L, _P, _P, _P, _P, C.c_uint64, _P]
+_lib.heatkv_paged_compact.argtypes = [_P, _L, _I, _P, _I, _P, _L, _I, _P, _I, _P, _P, _P, _L, _P, _P, _P, _I, _P, C.c_uint64, _P]
+_lib.heatkv_paged_move.argtypes = [_P, _P, _P, _I, _P]
+_lib.heatkv_paged4_move.argtypes = [_P, _P, _P, _I, _P]
 for _n in exported_symbols():
     if _n != "heatkv_strerror":
         getattr(_lib, _n).restype = C.c_int
@@ -735,3 +777,123 @@ def heatkv_paged_selftest_wait_expiry(workspace, stream=None) -> int:
     if workspace.nbytes < 256:
         raise ValueError("workspace: expected at least 256 bytes")
     return _lib.heatkv_paged_selftest_wait_expiry(_workspace(workspace), _on_device(stream, workspace))
+
+
+# ---------------------------------------------------------------------------------------------- the same in 4 bits
+def _same_rows(k, v, pool, n, what):
+    """Checks K and V rows of n tokens; their strides."""
+    _rows(k, pool, n, pool.n_kv_heads, f"k_{what}")
+    _rows(v, pool, n, pool.n_kv_heads, f"v_{what}")
+    if v.stride() != k.stride() or k.stride(2) != 1:
+        raise ValueError(f"k_{what}, v_{what}: expected equal strides, the last dimension contiguous")
+    return k.stride(0), k.stride(1)
+
+
+def _pool_kind(pool, kind):
+    if not isinstance(pool, kind):
+        raise ValueError(f"pool: expected a {kind.__name__}, got {type(pool).__name__}")
+
+
+def heatkv_paged4_store(pool: PagedPool4, k_new, v_new, slot_map, stream=None) -> None:
+    """K and V rows [n_tokens, n_kv_heads, d] (equal strides, d contiguous) to their slots, as 4-bit codes and scales."""
+    _pool_kind(pool, PagedPool4)
+    n = slot_map.numel()
+    slots = _vector(slot_map, n, "slot_map")
+    tok, head = _same_rows(k_new, v_new, pool, n, "new")
+    rc = _lib.heatkv_paged4_store(pool.addr4, k_new.data_ptr(), v_new.data_ptr(), tok, head, slots, n,
+                                  _on_device(stream, pool, k_new, v_new, slot_map))
+    _check(rc, "heatkv_paged4_store")
+
+
+def heatkv_paged4_load(pool: PagedPool4, slot_map, k_out, v_out, stream=None) -> None:
+    """Rows of some slots back as 16-bit numbers, to k_out, v_out [n_tokens, n_kv_heads, d]; zeros where a slot is outside of the pool."""
+    _pool_kind(pool, PagedPool4)
+    n = slot_map.numel()
+    slots = _vector(slot_map, n, "slot_map")
+    tok, head = _same_rows(k_out, v_out, pool, n, "out")
+    rc = _lib.heatkv_paged4_load(pool.addr4, slots, n, k_out.data_ptr(), v_out.data_ptr(), tok, head,
+                                 _on_device(stream, pool, k_out, v_out, slot_map))
+    _check(rc, "heatkv_paged4_load")
+
+
+def heatkv_paged4_workspace_bytes(pool: PagedPool4, batch: PagedBatch, n_heads: int) -> int:
+    """heatkv_paged_workspace_bytes for heatkv_paged4_attention."""
+    _pool_kind(pool, PagedPool4)
+    out = C.c_uint64()
+    _check(_lib.heatkv_paged4_workspace_bytes(pool.addr4, batch.addr, n_heads, C.byref(out)), "heatkv_paged4_workspace_bytes")
+    return out.value
+
+
+def heatkv_paged4_attention(pool: PagedPool4, batch: PagedBatch, q, out, lse, workspace, causal: bool = True, sm_scale: float = 0.0,
+                            stream=None) -> None:
+    """heatkv_paged_attention over a cache in 4 bits."""
+    _pool_kind(pool, PagedPool4)
+    st = _token_strides(pool, batch, q, out)
+    rc = _lib.heatkv_paged4_attention(pool.addr4, batch.addr, q.size(1), q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _lse(lse, q),
+                                      _workspace(workspace), workspace.nbytes, _on_device(stream, pool, batch, q, out, lse, workspace))
+    _check(rc, "heatkv_paged4_attention")
+
+
+# ---------------------------------------------------------------------------------------------- rows between steps
+def heatkv_paged_rows_workspace_bytes(n_seq: int, table_pages: int, n_pages: int) -> int:
+    """Bytes of workspace that heatkv_paged_fork and heatkv_paged_compact need (a zeroed uint8 tensor; it may be used again and again)."""
+    out = C.c_uint64()
+    _check(_lib.heatkv_paged_rows_workspace_bytes(n_seq, table_pages, n_pages, C.byref(out)), "heatkv_paged_rows_workspace_bytes")
+    return out.value
+
+
+def _old_and_new(lengths, block_table, free_pages, state, lengths_out, table_out, state_out):
+    """Checks what both calls read and write; their arguments from lengths on, the old ones and the new ones."""
+    n, n_pages = lengths.numel(), free_pages.numel()
+    table, stride, pages = _table(block_table, n)
+    new_table, new_stride, new_pages = _table(table_out, n)
+    if new_pages != pages:
+        raise ValueError(f"table_out: expected {pages} columns, got {new_pages}")
+    return ((_vector(lengths, n, "lengths"), n, table, stride, pages, _vector(free_pages, n_pages, "free_pages"), n_pages, _vector(state, 4, "state")),
+            (_vector(lengths_out, n, "lengths_out"), new_table, new_stride, _vector(state_out, 4, "state_out")))
+
+
+def heatkv_paged_fork(parents, keep_len, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace,
+                      stream=None) -> None:
+    """Row i goes on as a copy of row parents[i] (-1: it is over), with its first keep_len[i] tokens at most (keep_len None: all).  move_from, move_to
+    [64 * rows]: the moves for heatkv_paged_move."""
+    old, new = _old_and_new(lengths, block_table, free_pages, state, lengths_out, table_out, state_out)
+    n = lengths.numel()
+    rc = _lib.heatkv_paged_fork(_vector(parents, n, "parents"), None if keep_len is None else _vector(keep_len, n, "keep_len"), *old, *new,
+                                _vector(move_from, n * PAGE_TOKENS, "move_from"), _vector(move_to, n * PAGE_TOKENS, "move_to"), _workspace(workspace),
+                                workspace.nbytes, _on_device(stream, parents, keep_len, lengths, block_table, free_pages, state, lengths_out, table_out,
+                                                             state_out, move_from, move_to, workspace))
+    _check(rc, "heatkv_paged_fork")
+
+
+def heatkv_paged_compact(stays, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace,
+                         stream=None) -> None:
+    """Tokens with stays[row, token] False (bool or uint8 [rows, width]) leave the cache, the others move together.  move_from, move_to (of one
+    length, as many entries as may move): the moves for heatkv_paged_move."""
+    old, new = _old_and_new(lengths, block_table, free_pages, state, lengths_out, table_out, state_out)
+    n, n_moves = lengths.numel(), move_from.numel()
+    if stays.dtype not in (torch.bool, torch.uint8) or stays.dim() != 2 or stays.size(0) != n or (stays.stride(1) != 1 and stays.size(1) > 1):
+        raise ValueError(f"stays: expected bool or uint8 [{n}, tokens] with contiguous rows, got {stays.dtype} {tuple(stays.shape)}")
+    rc = _lib.heatkv_paged_compact(stays.data_ptr(), stays.stride(0) if n > 1 else stays.size(1), stays.size(1), *old, *new,
+                                   _vector(move_from, n_moves, "move_from"), _vector(move_to, n_moves, "move_to"), n_moves, _workspace(workspace),
+                                   workspace.nbytes, _on_device(stream, stays, lengths, block_table, free_pages, state, lengths_out, table_out, state_out,
+                                                                move_from, move_to, workspace))
+    _check(rc, "heatkv_paged_compact")
+
+
+def heatkv_paged_move(pool: PagedPool, move_from, move_to, stream=None) -> None:
+    """K and V of all heads from slot move_from[i] to slot move_to[i] (either -1: nothing), and the summaries of pages whose last row is among those."""
+    _pool_kind(pool, PagedPool)
+    n = move_from.numel()
+    rc = _lib.heatkv_paged_move(pool.addr, _vector(move_from, n, "move_from"), _vector(move_to, n, "move_to"), n,
+                                _on_device(stream, pool, move_from, move_to))
+    _check(rc, "heatkv_paged_move")
+
+
+def heatkv_paged4_move(pool: PagedPool4, move_from, move_to, stream=None) -> None:
+    """heatkv_paged_move in a cache in 4 bits."""
+    _pool_kind(pool, PagedPool4)
+    n = move_from.numel()
+    rc = _lib.heatkv_paged4_move(pool.addr4, _vector(move_from, n, "move_from"), _vector(move_to, n, "move_to"), n,
+                                 _on_device(stream, pool, move_from, move_to))
+    _check(rc, "heatkv_paged4_move")

@@ -5,7 +5,7 @@
 // CTA, and a run's pages in equal ranges, one a warp.  A warp works through its range by itself, from the copies that it sends for (9216 bytes, a ring of
 // its own) to the product with V, and never waits for another: units that lie in its range whole it writes out, of the at most two that its
 // range's ends cut it leaves unnormalised rows, which the CTA's warps add up when all are done, in page order.  A unit that a run's border cuts leaves
-// the sum in the workspace, which a second small kernel adds up.  (With page x of a run taken by warp x mod 8, so that the warps met wherever a unit
+// the sum in the workspace, and the CTA that leaves the last part of it adds them up, in page order again.  (With page x of a run taken by warp x mod 8, so that the warps met wherever a unit
 // ended, a decode of 64 requests took 68 us: a unit's end and beginning cost 6000 cycles, and the SM with the shortest units was the last.)
 //
 // The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that the cache is the operand with 16 rows and the queries the one with 8: a group of up to
@@ -28,7 +28,7 @@ constexpr int WARPS = 8, THREADS = WARPS * 32;
 constexpr int MAX_STAGES = 6;
 constexpr float MOVE = 8.f;                    // a reference moves when a maximum passes it by more than 2^MOVE (P fits fp16)
 #ifndef V_SHARE
-#define V_SHARE 8
+#define V_SHARE 4
 #endif
 constexpr int SHARE = V_SHARE;                      // pages of a run at least
 constexpr int WHOLE = 8;                       // units of up to so many pages are never cut by a run's border
@@ -37,7 +37,6 @@ constexpr int UNIT_END = 1;                    // what a unit weighs beyond its 
 
 struct Small4Params {
   Paged4Params q;
-  int2* cuts;                                  // [n_tokens][H] {the CTA with the unit's first page, its parts | the row's place in it << 16}; no parts: not cut
   float* ends;                                 // [CTAs][WARPS] rows of the unit that a warp's range begins inside of
   int32_t stages;
 };
@@ -84,17 +83,14 @@ struct Requests {
 };
 // The runs: CTA c's begins where what came before weighs raw(c), or near there.
 struct Runs {
-  int64_t all;
+  int64_t all, share;                          // a run's share in 2^-16
   int grid;
-  uint32_t each, rest;
   __device__ void deal(int64_t all_, int grid_) {
     all = all_;
     grid = grid_;
-    const int64_t e = all / grid;
-    each = (uint32_t)min(e, (int64_t)UINT_MAX);
-    rest = (uint32_t)(all - e * grid);
+    share = (all << 16) / grid;
   }
-  __device__ int64_t raw(int c) const { return (int64_t)each * c + rest * (uint32_t)c / (uint32_t)grid; }
+  __device__ int64_t raw(int c) const { return share * c >> 16; }
   // a border inside a unit of `pages` pages from `begin` on: not near its ends, not in a short one
   __device__ static int64_t snap(int64_t y, int64_t begin, int pages) {
     const int64_t at = y - begin, end = begin + pages + UNIT_END;
@@ -149,6 +145,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * MAX_STAGES];
   __shared__ uint32_t abort_word;
+  __shared__ int2 final_parts[2];                                  // of the run's first and last unit: the CTAs whose parts are there, if this one is to add them up
   __shared__ int64_t sums[WARPS];
   __shared__ int4 records[2 * WARPS];                              // a warp's two ends: {request, head, tile, what is cut}
   volatile uint32_t* abort_flag = &abort_word;
@@ -161,6 +158,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   pdl_trigger();
   if (threadIdx.x < WARPS * MAX_STAGES) mbar_init(bar0 + threadIdx.x * 8, 1);
   if (threadIdx.x < 2 * WARPS) records[threadIdx.x] = make_int4(-1, 0, 0, 0);
+  if (threadIdx.x < 2) final_parts[threadIdx.x] = make_int2(0, -1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_wait();
   if (threadIdx.x == 0) *abort_flag = *reinterpret_cast<volatile uint32_t*>(p.status) != 0;
@@ -228,10 +226,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
       const int64_t t = b + j / ((int64_t)p.H * D), hd = j / D % p.H;
       static_cast<uint16_t*>(p.out)[t * p.o_tok + hd * p.o_head + j % D] = 0;
     }
-    for (int64_t j = threadIdx.x; j < n; j += THREADS) {
-      if (p.lse) p.lse[b * p.H + j] = -INFINITY;
-      sp.cuts[b * p.H + j] = make_int2(-1, 0);
-    }
+    if (p.lse)
+      for (int64_t j = threadIdx.x; j < n; j += THREADS) p.lse[b * p.H + j] = -INFINITY;
   }
   if ((int)blockIdx.x >= runs.grid || runs.all == 0) return;
   // pages before the border of CTA c
@@ -248,8 +244,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     const int64_t at = Runs::snap(y, begin, pages) - begin;
     return req.pages(lo) + (int64_t)unit * pages + min(at, (int64_t)pages);
   };
-  const int64_t first_page = border(blockIdx.x);
-  const int n_run = (int)min(border(blockIdx.x + 1) - first_page, (int64_t)INT_MAX / 16);
+  const int64_t a_border = border(blockIdx.x + (lane & 1)), first_page = __shfl_sync(0xffffffffu, a_border, 0);        // (both at once)
+  const int n_run = (int)min(__shfl_sync(0xffffffffu, a_border, 1) - first_page, (int64_t)INT_MAX / 16);
   if (n_run <= 0) return;
   const int x0 = n_run * warp / WARPS, x1 = n_run * (warp + 1) / WARPS;
   Unit<ROWS> unit;
@@ -276,10 +272,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   unsigned char* ring = smem + warp * stages * B::BYTES;
   Unit<ROWS> ahead = unit;                                         // the page to be sent for next: number ahead_j of this unit
   int ahead_x = x0, ahead_j = j0, ahead_len = min(unit.pages - j0, x1 - x0), ahead_stop = min(j0 + ahead_len, unit.seen);
-  int ahead_page = -1, ahead_stage = 0, sent = 0;
+  int entry = -1, entries = 0, ahead_stage = 0, sent = 0;          // lane l: the table's entry for page `entries` + l of the unit
   bool more = true;
-  auto look_up = [&]() {                                           // on to a page that is seen, and its number
+  auto look_up = [&]() {                                           // on to a page that is seen
+    bool fresh = sent == 0;
     while (ahead_j >= ahead_stop) {
+      fresh = true;
       ahead_x += ahead_len;
       if (ahead_x >= x1) {
         more = false;
@@ -290,11 +288,15 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
       ahead_len = min(ahead.pages, x1 - ahead_x);
       ahead_stop = min(ahead_len, ahead.seen);
     }
-    ahead_page = __ldg(p.block_table + ahead.seq * p.table_stride + ahead_j);
+    if (fresh || ahead_j - entries == 32) {
+      entries = ahead_j;
+      entry = ahead_j + lane < ahead_stop ? __ldg(p.block_table + ahead.seq * p.table_stride + ahead_j + lane) : -1;
+    }
   };
   auto send = [&]() {
     if (!more) return;
     unsigned char* dst = ring + ahead_stage * B::BYTES;
+    const int ahead_page = __shfl_sync(0xffffffffu, entry, ahead_j - entries);
     if (ahead_page >= 0 && ahead_page < p.n_pages) {
       if (lane == 0) {
         mbar_expect_tx(full(ahead_stage), B::BYTES);
@@ -312,11 +314,34 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     ++ahead_j;
     look_up();
   };
-  if (x0 < x1) look_up(); else more = false;
+  // a unit's query rows: they are asked for before the pages that would be in front of them, the next unit's are brought to L2
+  const int gr = lane >> 2, qd = lane & 3;
+  uint4 q_rows[NT][WORDS];
+  auto row_at = [&](const Unit<ROWS>& u, int r) {
+    const int row = u.row0 + r, tok = row / p.G;
+    return static_cast<const __half*>(p.q) + (int64_t)(u.tok0 + tok) * p.q_tok + (int64_t)(u.head * p.G + row - tok * p.G) * p.q_head;
+  };
+  auto load_rows = [&]() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) q_rows[nt][i] = make_uint4(0, 0, 0, 0);
+      if (nt * 8 + gr < unit.rows) {
+        const uint4* src = reinterpret_cast<const uint4*>(row_at(unit, nt * 8 + gr) + qd * (D / 4));
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) q_rows[nt][i] = __ldg(src + i);
+      }
+    }
+  };
+  if (x0 < x1) {
+    look_up();
+    load_rows();
+  } else {
+    more = false;
+  }
   for (int s = 0; s < stages; ++s) send();
 
   // ------------------------------------------------------------------ products and softmax
-  const int gr = lane >> 2, qd = lane & 3;
   const int key_of = gr ^ ((gr >> 1) & 1);                         // keys of a block of eight in the order in which neither K's nor V's reads meet in a bank
   const int v0 = (2 * qd) ^ (qd & 1), v1 = v0 ^ 1;                 // the keys of the operands' columns 2 qd and 2 qd + 1
   int st = 0;
@@ -328,22 +353,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     int lim[NT][2], least = 0;                                     // keys that a row may see; the fewest
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int row = unit.row0 + nt * 8 + gr, tok = row / p.G;
-      uint4 y[WORDS];
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) y[i] = make_uint4(0, 0, 0, 0);
-      if (nt * 8 + gr < unit.rows) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __half*>(p.q) + (int64_t)(unit.tok0 + tok) * p.q_tok +
-                                                          (int64_t)(unit.head * p.G + row - tok * p.G) * p.q_head + qd * (D / 4));
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) y[i] = __ldg(src + i);
-      }
 #pragma unroll
       for (int i = 0; i < WORDS; ++i) {
-        qf[nt][4 * i] = y[i].x;
-        qf[nt][4 * i + 1] = y[i].y;
-        qf[nt][4 * i + 2] = y[i].z;
-        qf[nt][4 * i + 3] = y[i].w;
+        qf[nt][4 * i] = q_rows[nt][i].x;
+        qf[nt][4 * i + 1] = q_rows[nt][i].y;
+        qf[nt][4 * i + 2] = q_rows[nt][i].z;
+        qf[nt][4 * i + 3] = q_rows[nt][i].w;
       }
       float down = 1.f;                                        // of row `row`: what it was divided by
       if (!F16) {
@@ -546,10 +561,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
             for (int i = 0; i < 4; ++i) y[i] = pack_out<F16>(o[4 * c + i][nt][e] * inv, o[4 * c + i][nt][2 + e] * inv);
             dst[c] = make_uint4(y[0], y[1], y[2], y[3]);
           }
-          if (gr == 0) {
-            if (p.lse) p.lse[(int64_t)tok * p.H + hd] = l == 0.f ? -INFINITY : (m_ref[nt][e] + log2f(l)) * 0.6931471805599453f;
-            sp.cuts[(int64_t)tok * p.H + hd] = make_int2(-1, 0);
-          }
+          if (p.lse && gr == 0) p.lse[(int64_t)tok * p.H + hd] = l == 0.f ? -INFINITY : (m_ref[nt][e] + log2f(l)) * 0.6931471805599453f;
         }
     } else {
       // (a unit that goes on behind the range is its last one: all copies have landed, the ring is free)
@@ -570,7 +582,10 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     }
     x += len;
     j0 = 0;
-    if (x < x1) unit.next(req, p);
+    if (x < x1) {
+      unit.next(req, p);
+      load_rows();
+    }
   }
   if (*abort_flag) {
     // leaving early: every copy under way lands before the CTA exits
@@ -579,10 +594,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   // ------------------------------------------------------------------ units that ranges' ends cut: added up by all warps, a row each
   __syncthreads();
   const int4 mine = lane < 2 * WARPS ? records[lane] : make_int4(-1, 0, 0, 0);
-  // a lane's rows (their order is the pages'), as 64-bit addresses: those of unit.begins in shared memory, the others not
-  const float* my_rows = lane & 1 ? reinterpret_cast<const float*>(smem + (lane >> 1) * stages * B::BYTES)
-                                  : sp.ends + ((int64_t)blockIdx.x * WARPS + (lane >> 1)) * slot_floats(ROWS, D);
-  uint32_t left = __ballot_sync(0xffffffffu, mine.x >= 0);
+  const uint32_t met = __ballot_sync(0xffffffffu, mine.x >= 0);
+  uint32_t left = met;
   int turn = 0;
   while (left) {
     const int head_lane = __ffs(left) - 1;
@@ -591,57 +604,45 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     unit.tile = __shfl_sync(0xffffffffu, mine.z, head_lane);
     const uint32_t parties = __ballot_sync(0xffffffffu, mine.x == unit.seq && mine.y == unit.head && mine.z == unit.tile);
     left &= ~parties;
-    const bool goes_on = __shfl_sync(0xffffffffu, mine.w, 31 - __clz(parties)) & 2, began = __shfl_sync(0xffffffffu, mine.w, head_lane) & 1;
+    const bool on = __shfl_sync(0xffffffffu, mine.w, 31 - __clz(parties)) & 2, from_before = __shfl_sync(0xffffffffu, mine.w, head_lane) & 1;
     unit.set(req, p);
-    int parts = 0;
-    if (goes_on && !began) {                                       // the part with the unit's first page says how many there are
-      const int64_t begin = req.pre[unit.seq] + ((int64_t)unit.head * unit.tiles + unit.tile) * (unit.pages + UNIT_END), end = begin + unit.pages + UNIT_END;
-      int lo = blockIdx.x + 1, hi = runs.grid - 1;                 // the last CTA whose run begins inside
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        const int64_t y = runs.raw(mid);
-        if (y < end && Runs::snap(y, begin, unit.pages) < end) lo = mid; else hi = mid - 1;
-      }
-      parts = lo - (int)blockIdx.x + 1;
-    }
-    const bool cut = goes_on || began, party = parties >> lane & 1;
-    float* slot = p.partials + (2 * (int64_t)blockIdx.x + (began ? 0 : 1)) * slot_floats(ROWS, D);
+    const bool cut = on || from_before;
+    // a warp has at most one part of a unit: in its ring where the unit begins in its range, else in the workspace
+    auto rows_of = [&](int w) {
+      return parties >> (2 * w + 1) & 1 ? reinterpret_cast<const float*>(smem + w * stages * B::BYTES)
+                                        : sp.ends + ((int64_t)blockIdx.x * WARPS + w) * slot_floats(ROWS, D);
+    };
+    float* slot = p.partials + (2 * (int64_t)blockIdx.x + (from_before ? 0 : 1)) * slot_floats(ROWS, D);
     constexpr int LANES = D / 4, AT_ONCE = 32 / LANES;             // lanes of a row, rows at once
     const int my = lane % LANES;
     for (int r0 = 0; r0 < unit.rows; r0 += AT_ONCE, ++turn) {
       if (turn % WARPS != warp) continue;
       const int row = r0 + lane / LANES;
-      float m[AT_ONCE], f[AT_ONCE], l[AT_ONCE];                    // of the rows at once: maximum; lane i: party i's weight; sum
+      float4 c[WARPS];
+      float2 ml[WARPS];
 #pragma unroll
-      for (int a = 0; a < AT_ONCE; ++a) {
-        float2 ml = make_float2(NO_MAX, 0.f);
-        if (party) ml = reinterpret_cast<const float2*>(my_rows + ROWS * D)[r0 + a];
-        m[a] = ml.x;
-#pragma unroll
-        for (int i = 16; i > 0; i >>= 1) m[a] = fmaxf(m[a], __shfl_xor_sync(0xffffffffu, m[a], i));
-        f[a] = exp2f(ml.x - m[a]);
-        l[a] = ml.y * f[a];
-#pragma unroll
-        for (int i = 16; i > 0; i >>= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], i);
+      for (int w = 0; w < WARPS; ++w) {
+        ml[w] = make_float2(NO_MAX, 0.f);
+        c[w] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!(parties >> (2 * w) & 3)) continue;
+        const float* from = rows_of(w);
+        ml[w] = reinterpret_cast<const float2*>(from + ROWS * D)[row];
+        c[w] = reinterpret_cast<const float4*>(from + row * D)[my];
       }
+      float top = ml[0].x, sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) top = fmaxf(top, ml[w].x);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (uint32_t rest = parties; rest; rest &= rest - 1) {
-        const int i = __ffs(rest) - 1;
-        const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_rows), i));
-        float weight = __shfl_sync(0xffffffffu, f[0], i);
-        if (AT_ONCE == 2) {
-          const float other = __shfl_sync(0xffffffffu, f[AT_ONCE - 1], i);
-          if (lane >= LANES) weight = other;
-        }
-        const float4 c = reinterpret_cast<const float4*>(from + row * D)[my];
-        acc.x = fmaf(c.x, weight, acc.x);
-        acc.y = fmaf(c.y, weight, acc.y);
-        acc.z = fmaf(c.z, weight, acc.z);
-        acc.w = fmaf(c.w, weight, acc.w);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float f = exp2f(ml[w].x - top);
+        sum = fmaf(ml[w].y, f, sum);
+        acc.x = fmaf(c[w].x, f, acc.x);
+        acc.y = fmaf(c[w].y, f, acc.y);
+        acc.z = fmaf(c[w].z, f, acc.z);
+        acc.w = fmaf(c[w].w, f, acc.w);
       }
       if (row >= unit.rows) continue;
-      const float top = lane < LANES ? m[0] : m[AT_ONCE - 1], sum = lane < LANES ? l[0] : l[AT_ONCE - 1];
       const int col = (my ^ ((row >> 1) & 3)) * 4, of = unit.row0 + row, tok = unit.tok0 + of / p.G, hd = unit.head * p.G + of % p.G;
       if (cut) {
         __stcg(reinterpret_cast<float4*>(slot + row * D + col), acc);
@@ -652,101 +653,101 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
         *reinterpret_cast<uint2*>(dst) = make_uint2(pack_out<F16>(acc.x * inv, acc.y * inv), pack_out<F16>(acc.z * inv, acc.w * inv));
         if (p.lse && my == 0) p.lse[(int64_t)tok * p.H + hd] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
       }
-      if (!began && my == 0) sp.cuts[(int64_t)tok * p.H + hd] = make_int2(blockIdx.x, parts | row << 16);
+    }
+  }
+  // ------------------------------------------------------------------ units that the run's borders cut: added up by the CTA that leaves their last part
+  const int first_lane = __ffs(met) - 1, last_lane = 31 - __clz(met);
+  const bool began = met && __shfl_sync(0xffffffffu, mine.w, first_lane) & 1, goes_on = met && __shfl_sync(0xffffffffu, mine.w, last_lane) & 2;
+  if (!began && !goes_on) return;
+  auto unit_of = [&](int of) {
+    unit.seq = __shfl_sync(0xffffffffu, mine.x, of);
+    unit.head = __shfl_sync(0xffffffffu, mine.y, of);
+    unit.tile = __shfl_sync(0xffffffffu, mine.z, of);
+    unit.set(req, p);
+  };
+  __threadfence();
+  __syncthreads();
+  if (warp < 2 && (warp == 0 ? began : goes_on)) {                 // warp 0 sees to the first unit, warp 1 to the last; one that is both is the first
+    unit_of(warp == 0 ? first_lane : last_lane);
+    const int64_t begin = req.pre[unit.seq] + ((int64_t)unit.head * unit.tiles + unit.tile) * (unit.pages + UNIT_END), end = begin + unit.pages + UNIT_END;
+    // the last CTA whose run begins before `y`, a place of this unit (at its beginning: not behind it)
+    auto last_before = [&](int64_t y) {
+      auto before = [&](int c) {
+        const int64_t raw = runs.raw(c);
+        return raw < begin || (raw < end && Runs::snap(raw, begin, unit.pages) < y);
+      };
+      int c = min(max((int)((float)y * 65536.f / (float)runs.share), 0), runs.grid - 1);
+      while (c + 1 < runs.grid && before(c + 1)) ++c;
+      while (c > 0 && !before(c)) --c;
+      return c;
+    };
+    const bool both = warp == 0 && goes_on && __shfl_sync(0xffffffffu, (int)(mine.x == unit.seq && mine.y == unit.head && mine.z == unit.tile), last_lane);
+    const bool other = warp == 1 && began && __shfl_sync(0xffffffffu, (int)(mine.x == unit.seq && mine.y == unit.head && mine.z == unit.tile), first_lane);
+    const int c0 = warp == 0 ? last_before(begin + 1) : (int)blockIdx.x, c1 = warp == 1 || both ? last_before(end) : (int)blockIdx.x;
+    if (lane == 0 && !other) {
+      const uint32_t old = atomicAdd(p.counters + c0, 1u);
+      const bool last = old == (uint32_t)(c1 - c0);
+      if (last) *reinterpret_cast<volatile uint32_t*>(p.counters + c0) = 0;              // ready for the next launch
+      final_parts[warp] = last ? make_int2(c0, c1) : make_int2(0, -1);
+      __threadfence();
+    }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int u = 0; u < 2; ++u) {
+    const int c0 = final_parts[u].x, c1 = final_parts[u].y;
+    if (c1 < c0) continue;
+    unit_of(u == 0 ? first_lane : last_lane);
+    for (int row = warp; row < unit.rows; row += WARPS) {
+      constexpr int N = D / 32, AHEAD = 8;
+      auto part = [&](int c) { return p.partials + (2 * (int64_t)c + (c == c0)) * slot_floats(ROWS, D); };
+      float acc[N], l = 0.f, top = NO_MAX;
+#pragma unroll
+      for (int k = 0; k < N; ++k) acc[k] = 0.f;
+      for (int base = c0; base <= c1; base += AHEAD) {
+        float c[AHEAD][N];
+        float2 ml[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          ml[i] = make_float2(NO_MAX, 0.f);
+#pragma unroll
+          for (int k = 0; k < N; ++k) c[i][k] = 0.f;
+          if (base + i > c1) continue;
+          const float* s = part(base + i);
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(s + ROWS * D) + row);
+          if (N == 4) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(s + row * D) + lane);
+            c[i][0] = y.x, c[i][1] = y.y, c[i][N - 2] = y.z, c[i][N - 1] = y.w;
+          } else {
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(s + row * D) + lane);
+            c[i][0] = y.x, c[i][1] = y.y;
+          }
+        }
+        float t = top;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) t = fmaxf(t, ml[i].x);
+        const float f0 = exp2f(top - t);
+        top = t;
+        l *= f0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] *= f0;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const float f = exp2f(ml[i].x - top);
+          l = fmaf(ml[i].y, f, l);
+#pragma unroll
+          for (int k = 0; k < N; ++k) acc[k] = fmaf(c[i][k], f, acc[k]);
+        }
+      }
+      const int of = unit.row0 + row, tok = unit.tok0 + of / p.G, hd = unit.head * p.G + of % p.G;
+      const float inv = l == 0.f ? 0.f : q4.v_unit / l;
+      uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__half*>(p.out) + (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head + lane * N);
+#pragma unroll
+      for (int k = 0; k < N; k += 2) dst[k / 2] = pack_out<F16>(acc[k] * inv, acc[k + 1] * inv);
+      if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
     }
   }
 }
-
-// Adds up the parts of the rows whose units were cut, in page order: a CTA per row where the rows are few, else a warp.
-constexpr int MERGE_WARPS = 8;
-template <int D, bool F16, bool WIDE>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) paged4_merge_kernel(const __grid_constant__ Small4Params sp, int rows_of_slot, int n_cta) {
-  const PagedParams& p = sp.q.a;
-  constexpr int N = D / 32, AHEAD = 8;
-  __shared__ float sums[MERGE_WARPS][D], tops[MERGE_WARPS], ls[MERGE_WARPS];
-  pdl_trigger();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int begin_tok = __ldg(p.q_begin), end_tok = __ldg(p.q_begin + p.n_seq);
-  const int64_t pitch = slot_floats(rows_of_slot, D), rows = (int64_t)p.n_tokens * p.H;
-  for (int64_t x = WIDE ? blockIdx.x : (int64_t)blockIdx.x * MERGE_WARPS + warp; x < rows; x += (int64_t)gridDim.x * (WIDE ? 1 : MERGE_WARPS)) {
-    const int2 cut = __ldcg(sp.cuts + x);
-    const int tok = divide(x, p.H), hd = (int)(x - (int64_t)tok * p.H);
-    const int parts = cut.y & 0xffff, row = cut.y >> 16;
-    // (rows that are nobody's have an entry of some call before, or none; no entry leads out of the workspace)
-    if (tok < begin_tok || tok >= end_tok || parts < 2 || cut.x < 0 || cut.x > n_cta - parts || (uint32_t)row >= (uint32_t)rows_of_slot) continue;
-    auto slot = [&](int i) { return p.partials + (2 * (int64_t)(cut.x + i) + (i == 0)) * pitch; };
-    const int begin = WIDE ? parts * warp / MERGE_WARPS : 0, end = WIDE ? parts * (warp + 1) / MERGE_WARPS : parts;
-    float acc[N], l = 0.f, top = NO_MAX;
-#pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = 0.f;
-    for (int base = begin; base < end; base += AHEAD) {
-      float c[AHEAD][N];
-      float2 ml[AHEAD];
-      float t = top;
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        ml[i] = make_float2(NO_MAX, 0.f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) c[i][k] = 0.f;
-        if (base + i >= end) continue;
-        const float* s = slot(base + i);
-        ml[i] = __ldcg(reinterpret_cast<const float2*>(s + rows_of_slot * D) + row);
-        if (N == 4) {
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(s + row * D) + lane);
-          c[i][0] = y.x, c[i][1] = y.y, c[i][N - 2] = y.z, c[i][N - 1] = y.w;
-        } else {
-          const float2 y = __ldcg(reinterpret_cast<const float2*>(s + row * D) + lane);
-          c[i][0] = y.x, c[i][1] = y.y;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) t = fmaxf(t, ml[i].x);
-      const float f0 = exp2f(top - t);
-      top = t;
-      l *= f0;
-#pragma unroll
-      for (int k = 0; k < N; ++k) acc[k] *= f0;
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const float f = exp2f(ml[i].x - top);
-        l = fmaf(ml[i].y, f, l);
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] = fmaf(c[i][k], f, acc[k]);
-      }
-    }
-    if (WIDE) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) sums[warp][lane * N + k] = acc[k];
-      if (lane == 0) {
-        tops[warp] = top;
-        ls[warp] = l;
-      }
-      __syncthreads();
-      if (warp == 0) {
-        for (int i = 0; i < MERGE_WARPS; ++i) top = fmaxf(top, tops[i]);
-        l = 0.f;
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] = 0.f;
-        for (int i = 0; i < MERGE_WARPS; ++i) {
-          const float f = exp2f(tops[i] - top);
-          l = fmaf(ls[i], f, l);
-#pragma unroll
-          for (int k = 0; k < N; ++k) acc[k] = fmaf(sums[i][lane * N + k], f, acc[k]);
-        }
-      }
-      __syncthreads();
-      if (warp > 0) continue;
-    }
-    const float inv = l == 0.f ? 0.f : sp.q.v_unit / l;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__half*>(p.out) + (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head + lane * N);
-#pragma unroll
-    for (int k = 0; k < N; k += 2) dst[k / 2] = pack_out<F16>(acc[k] * inv, acc[k + 1] * inv);
-    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.H + hd] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
-  }
-}
-
-uint64_t cut_bytes(int n_tokens, int H) { return ((uint64_t)n_tokens * H * 8 + 255) / 256 * 256; }
 
 uint64_t slot_bytes(int d, int rows, int slots) { return ((uint64_t)slots * slot_floats(rows, d) * 4 + 255) / 256 * 256; }
 
@@ -756,23 +757,14 @@ cudaError_t launch(const Paged4Params& q, int n_sm, cudaStream_t stream) {
   const int fixed = Requests::bytes(q.a.n_seq);
   Small4Params sp;
   sp.q = q;
-  sp.cuts = reinterpret_cast<int2*>(q.a.partials);
-  sp.q.a.partials = q.a.partials + cut_bytes(q.a.n_tokens, q.a.H) / 4;
-  sp.ends = sp.q.a.partials + slot_bytes(D, 8 * NT, 2 * n_sm) / 4;
+  sp.ends = q.a.partials + slot_bytes(D, 8 * NT, 2 * n_sm) / 4;
   // as many pages under way as shared memory holds (of a call of 3200 requests and more one a warp)
   sp.stages = std::max(1, std::min(MAX_STAGES, (room - fixed) / stage));
   auto kernel = paged4_small_kernel<D, NT, F16>;
   // (the kernel's limit is the process's: always the most that any call takes, as another thread may set it between this line and the launch)
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room);
   if (rc != cudaSuccess) return rc;
-  rc = launch_pdl(kernel, dim3(n_sm), dim3(THREADS), fixed + sp.stages * stage, stream, sp);
-  // nothing can have been cut where no unit has more pages
-  if (rc != cudaSuccess || q.a.table_pages <= WHOLE) return rc;
-  const int64_t rows = (int64_t)q.a.n_tokens * q.a.H;
-  if (rows <= 8 * n_sm && q.a.table_pages > 8 * MIN_PART)
-    return launch_pdl(paged4_merge_kernel<D, F16, true>, dim3((unsigned)rows), dim3(MERGE_WARPS * 32), 0, stream, sp, 8 * NT, n_sm);
-  const int64_t ctas = std::min<int64_t>((rows + MERGE_WARPS - 1) / MERGE_WARPS, 8 * n_sm);
-  return launch_pdl(paged4_merge_kernel<D, F16, false>, dim3((unsigned)ctas), dim3(MERGE_WARPS * 32), 0, stream, sp, 8 * NT, n_sm);
+  return launch_pdl(kernel, dim3(n_sm), dim3(THREADS), fixed + sp.stages * stage, stream, sp);
 }
 template <int D>
 cudaError_t launch_typed(const Paged4Params& q, int rows, int n_sm, cudaStream_t stream) {
@@ -782,7 +774,7 @@ cudaError_t launch_typed(const Paged4Params& q, int rows, int n_sm, cudaStream_t
 
 }  // namespace
 
-uint64_t paged4_small_partial_bytes(int d, int n_sm, int H, int n_tokens) { return cut_bytes(n_tokens, H) + slot_bytes(d, 16, 2 * n_sm) + slot_bytes(d, 16, WARPS * n_sm); }
+uint64_t paged4_small_partial_bytes(int d, int n_sm) { return slot_bytes(d, 16, 2 * n_sm) + slot_bytes(d, 16, WARPS * n_sm); }
 
 cudaError_t launch_paged4_small(const Paged4Params& p, int d, const PagedDevice& dev, cudaStream_t stream) {
   const int rows = (int64_t)std::max(1, p.a.max_new) * p.a.G <= 8 ? 8 : 16;

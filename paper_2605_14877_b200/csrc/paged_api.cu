@@ -108,9 +108,7 @@ uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_to
   return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 
-uint64_t workspace4_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_tokens, int) {
-  return PAGED_WS_PARTIALS + paged4_small_partial_bytes(d, dev.n_sm, G * Hkv, n_tokens);
-}
+uint64_t workspace4_bytes(const PagedDevice& dev, int d, int, int, int, int) { return PAGED_WS_PARTIALS + paged4_small_partial_bytes(d, dev.n_sm); }
 
 uint64_t needed_bytes(const PagedDevice& dev, int d, const PagedParams& p) { return workspace_bytes(dev, d, p.G, p.Hkv, p.n_tokens, p.n_seq); }
 

@@ -122,6 +122,7 @@ cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool,
 
 cudaError_t launch_paged4_rows(const Store4Params& p, bool load, int d, cudaStream_t stream);
 uint64_t paged4_small_partial_bytes(int d, int n_sm);
+cudaError_t launch_paged4_tc(const Paged4Params& p, int d, const PagedDevice& dev, cudaStream_t stream);
 cudaError_t launch_paged4_small(const Paged4Params& p, int d, const PagedDevice& dev, cudaStream_t stream);
 
 // A tensor map with four dimensions of 16-bit numbers, 128-byte swizzle.

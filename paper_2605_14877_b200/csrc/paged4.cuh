@@ -59,6 +59,30 @@ __device__ __forceinline__ void values4(uint32_t w, const Steps4& s, uint32_t (&
   out[2] = as_word(__hfma2(as_half2(fields_lo(up)), s.lo, s.lo8));
   out[3] = as_word(__hfma2(as_half2(fields_hi(up)), s.hi, s.hi8));
 }
+// The same in bf16: 128 + c is a number of 8 bits, of a half's fields one at a time, and (c - 8) s' with s' = s / 256 is exact as 136 s' = 17 * 8 s' has 8
+// bits.  The scale's byte, shifted by 4, is s' 2^-112.
+struct Steps4Bf16 {
+  __nv_bfloat162 s, s8;                                          // s', -136 s'
+  __device__ __forceinline__ explicit Steps4Bf16(uint32_t bytes) {
+    const uint32_t x = bytes << 4;
+    s = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), __float2bfloat162_rn(5.192296858534828e33f));      // 2^112
+    s8 = __hmul2(s, __float2bfloat162_rn(-136.f));
+  }
+};
+__device__ __forceinline__ void values4(uint32_t w, const Steps4Bf16& s, uint32_t (&out)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t x;
+    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(x) : "r"(w >> (4 * i)));
+    const __nv_bfloat162 y = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x), s.s, s.s8);
+    out[i] = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+// A copy of contiguous bytes (a multiple of 16) from global to shared memory, counted by a barrier there.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 constexpr float VALUES4_UNIT = 256.f;                            // what values4's numbers are to be multiplied by
 
 }  // namespace heatkv

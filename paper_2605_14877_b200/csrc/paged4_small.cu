@@ -60,10 +60,6 @@ template <bool F16>
 __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
   return F16 ? pack_half(lo, hi) : pack_bf16(lo, hi);
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
 
 __host__ __device__ constexpr int64_t slot_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
 

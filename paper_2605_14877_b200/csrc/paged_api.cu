@@ -108,7 +108,10 @@ uint64_t workspace_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_to
   return PAGED_WS_PARTIALS + (a > b ? a : b);
 }
 
-uint64_t workspace4_bytes(const PagedDevice& dev, int d, int, int, int, int) { return PAGED_WS_PARTIALS + paged4_small_partial_bytes(d, dev.n_sm); }
+uint64_t workspace4_bytes(const PagedDevice& dev, int d, int G, int Hkv, int n_tokens, int n_seq) {
+  const uint64_t a = paged4_small_partial_bytes(d, dev.n_sm), b = paged_tc_partial_bytes(d, dev.n_sm, G, Hkv, n_tokens, n_seq);
+  return PAGED_WS_PARTIALS + (a > b ? a : b);
+}
 
 uint64_t needed_bytes(const PagedDevice& dev, int d, const PagedParams& p) { return workspace_bytes(dev, d, p.G, p.Hkv, p.n_tokens, p.n_seq); }
 
@@ -342,7 +345,8 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
   p.page_stride = pool->page_stride;
   p.head_stride = pool->head_stride;
   p.fp16 = pool->dtype == HEATKV_DTYPE_FP16;
-  return done(launch_paged4_small(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
+  const int64_t rows = (int64_t)p.a.max_new * p.a.G;
+  return done((rows <= 64 ? launch_paged4_small : launch_paged4_tc)(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
 }
 
 // ---------------------------------------------------------------- rows between steps

@@ -17,6 +17,9 @@
 // them instead of once for each.  Warp 2 brings the tokens' lists into shared memory, the copy warp merges them as it goes (a
 // token per lane and tile) and hands the tokens' bits to the softmax warps beside each tile.
 // (A tile has at most 32 tokens there, one a bit of a word, so that groups of one or two heads fill a quarter or half of its 128 rows.)
+// Over a cache in 4 bits (CODES) warp 0 sends for whole blocks (codes and scales of K and V of a page and head), which four more warps, 12-15, turn into
+// the tiles of 16-bit numbers that TMA brings otherwise, exactly (paged4.cuh); rows go out without a detour through shared memory, whose place the
+// blocks take.
 // What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 to 470 us,
 // 1160 to 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax warps'
 // waits for tensor memory (half the products per exponential: 32 heads of the first shape 666 us, 815 TFLOP/s; no unit is busy more than 57 %).
@@ -25,6 +28,7 @@
 
 #include <cuda_fp16.h>
 
+#include "paged4.cuh"
 #include "paged_wait.cuh"
 
 namespace heatkv {
@@ -38,6 +42,9 @@ constexpr int KV_STAGES = 2;
 // Register hand-over between warpgroups, inside what the launch allocates (checked against the compiled kernel before it runs).
 constexpr int REGS_LAUNCH = 168, REGS_SMALL = 72, REGS_SOFTMAX = 216;
 static_assert(128 * REGS_SMALL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register hand-over exceeds the CTA's allocation");
+// .. of the kernel over 4 bits, with four warps more
+constexpr int THREADS4 = 512, REGS4_LAUNCH = 128, REGS4_SMALL = 48, REGS4_SOFTMAX = 200, REGS4_CODES = 64;
+static_assert(128 * (REGS4_SMALL + REGS4_CODES) + 256 * REGS4_SOFTMAX <= THREADS4 * REGS4_LAUNCH, "register hand-over exceeds the CTA's allocation");
 constexpr uint32_t HALF_COLS_BYTES = 128 * 128;        // one 64-column half of a 128-row tile
 constexpr uint32_t SLOT_BYTES = PAGE * 128;            // a page inside one column half
 constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 rows x 32 columns on their way out
@@ -46,7 +53,7 @@ constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 r
 constexpr int LIST_ENTRIES = 2048, LIST_WORDS = 2048;
 constexpr uint32_t LIST_BYTES = LIST_ENTRIES * 2 + LIST_WORDS * 4;
 
-template <int D>
+template <int D, bool CODES = false>
 struct Layout {
   static constexpr int NCH = D / 64;
   static constexpr uint32_t TILE_BYTES = NCH * HALF_COLS_BYTES;
@@ -54,18 +61,22 @@ struct Layout {
   static constexpr uint32_t SM_K = SM_Q + 2 * TILE_BYTES;
   static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;
   static constexpr uint32_t SM_OUT = SM_V + KV_STAGES * TILE_BYTES;
-  static constexpr uint32_t SM_BAR = SM_OUT + 8 * STAGE_BYTES;
+  // CODES: blocks of the cache instead of rows on their way out
+  static constexpr uint32_t RAW_STAGES = D == 128 ? 3 : 6;
+  static constexpr uint32_t SM_BAR = SM_OUT + (CODES ? RAW_STAGES * block4_bytes(D) : 8 * STAGE_BYTES);
   static constexpr uint32_t SM_LIST = SM_BAR + 512;
   static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;             // (and the lists where pages are selected)
-  static_assert(SM_ALLOC + LIST_BYTES + LIST_ENTRIES * 2 <= 227 * 1024, "shared memory of one CTA");
+  static_assert(SM_ALLOC + (CODES ? 0 : LIST_BYTES + LIST_ENTRIES * 2) <= 227 * 1024, "shared memory of one CTA");
   // one part of a cut item: O of both tiles (groups of four columns outermost), then references and sums
   static constexpr int SLOT_FLOATS = 2 * BM * D + 2 * 2 * BM;
 };
 enum Bar : uint32_t {
   Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 6, V_FULL = 8, V_EMPTY = 10, S_FULL = 12, P_FULL = 14, PV_DONE = 18, ITEM_FULL = 20, ITEM_EMPTY = 22,
-  DRAIN = 24, N_BARS
+  DRAIN = 24, N_BARS,
+  RAW_FULL = 48, RAW_EMPTY = 54                        // CODES: where SPARSE has its tiles' pages
 };
 constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256, BAR_INFO = 384;
+static_assert(RAW_FULL * 8 == BAR_INFO && RAW_EMPTY - RAW_FULL >= 6 && (RAW_EMPTY + 6) * 8 <= 512, "barriers of up to six blocks");
 constexpr int INFO_RING = 4;                           // key tiles whose pages and bits are kept: the copy warp is at most two ahead of the softmax
 enum InfoWord : int { I_PLACE = 0, I_BITS = 2, INFO_WORDS = 8 };   // two places; bits of tile A for both, of tile B for both
 enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1, W_SEEK };
@@ -80,6 +91,10 @@ struct TcParams {
   uint32_t* ticket;           // CTAs of union_kernel that are done; zero between launches
   int32_t items;              // room for the items
   int32_t n_cta;
+  // CODES: the blocks, strides in bytes; what the numbers of V are to be multiplied by
+  const unsigned char* blocks;
+  int64_t page_stride, head_stride;
+  float v_unit;
 };
 enum RunWord : int { R_SEQ = 0, R_HEAD, R_ITEM, R_J0, R_UNITS, R_C0_FIRST = R_UNITS + 2, R_C1_FIRST, R_C1_LAST, RUN_WORDS = 10 };
 static_assert(R_UNITS % 2 == 0 && RUN_WORDS % 2 == 0 && R_C1_LAST < RUN_WORDS, "a run's units are a 64-bit number");
@@ -525,9 +540,10 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& e0, float& e1) {
   e0 = x0 >= -125.f ? __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23)) : 0.f;
   e1 = x1 >= -125.f ? __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23)) : 0.f;
 }
-template <int D, bool F16, bool SPARSE>
-__global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
-  using L = Layout<D>;
+template <int D, bool F16, bool SPARSE, bool CODES>
+__global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
+  using L = Layout<D, CODES>;
+  using B = Block4<D>;
   constexpr int NCH = L::NCH;
   constexpr uint32_t TILE_BYTES = L::TILE_BYTES, SM_Q = L::SM_Q, SM_K = L::SM_K, SM_V = L::SM_V, SM_OUT = L::SM_OUT, SM_BAR = L::SM_BAR;
   // How far (log2) a maximum may rise above the reference of its row's exponentials: bf16 and the 32-bit sums have room for 2^32,
@@ -559,14 +575,19 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
       mbar_init(bar(P_FULL + 2 * x + 1), BM);
       mbar_init(bar(PV_DONE + x), 1);
       mbar_init(bar(ITEM_FULL + x), 1);
-      mbar_init(bar(ITEM_EMPTY + x), 10);
+      mbar_init(bar(ITEM_EMPTY + x), CODES ? 14 : 10);
     }
     for (int s = 0; s < KV_STAGES; ++s) {
-      mbar_init(bar(K_FULL + s), 1);
+      mbar_init(bar(K_FULL + s), CODES ? 4 : 1);
       mbar_init(bar(K_EMPTY + s), 1);
-      mbar_init(bar(V_FULL + s), 1);
+      mbar_init(bar(V_FULL + s), CODES ? 4 : 1);
       mbar_init(bar(V_EMPTY + s), 1);
     }
+    if (CODES)
+      for (uint32_t s = 0; s < L::RAW_STAGES; ++s) {
+        mbar_init(bar(RAW_FULL + s), 1);
+        mbar_init(bar(RAW_EMPTY + s), 4);
+      }
     mbar_init(bar(DRAIN), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -584,12 +605,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_smem, 0);
 
   if (warp < 4) {
-    reg_dealloc<REGS_SMALL>();
+    reg_dealloc<CODES ? REGS4_SMALL : REGS_SMALL>();
     if (warp == 0) {
       // ---------------------------------------------------------------- copies
       const bool leader = elect_one();
       uint32_t g = 0, iq[2] = {0, 0};                              // key tiles sent for; items that loaded query tile x
       uint32_t armed_k = 0, armed_v = 0, armed_q = 0, par_k = 0, par_v = 0, par_q = 0;
+      uint32_t raw = 0;                                            // CODES: blocks sent for
       const uint32_t q_bytes = (uint32_t)(p.tile_tokens * p.G) * 128;
       bool ok = true;
       for (uint32_t it = 0; ok; ++it) {
@@ -631,6 +653,29 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             pg0 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15));
             pg1 = __shfl_sync(0xffffffffu, pages, 2 * (j & 15) + 1);
           }
+          if (CODES) {
+#pragma unroll 1
+            for (int h = 0; h < 2 && ok; ++h, ++raw) {
+              const uint32_t rs = raw % L::RAW_STAGES, round = raw / L::RAW_STAGES;
+              if (round > 0) ok = wait_all(bar(RAW_EMPTY + rs), (round - 1) & 1, abort_flag, p.status, 1 + RAW_EMPTY);
+              if (!ok) break;
+              unsigned char* dst = sgen + L::SM_OUT + rs * B::BYTES;
+              const int pg = h ? pg1 : pg0;
+              if (pg >= 0) {
+                if (leader) {
+                  mbar_expect_tx(bar(RAW_FULL + rs), B::BYTES);
+                  bulk_load(smem_u32(dst), tp.blocks + pg * tp.page_stride + head * tp.head_stride, B::BYTES, bar(RAW_FULL + rs));
+                }
+              } else {                                             // no page of the pool: zeros
+                for (int i = lane; i < B::BYTES / 16; i += 32) reinterpret_cast<int4*>(dst)[i] = make_int4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // (before the stage's next copy)
+                __syncwarp();
+                if (leader) mbar_arrive(bar(RAW_FULL + rs));
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+          }
           const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
           auto load = [&](uint32_t smem, const CUtensorMap* map, uint32_t full) {
             if (!leader) return;
@@ -641,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
               tma_load_4d(smem + ch * HALF_COLS_BYTES + SLOT_BYTES, map, ch * 64, 0, head, pg1, full);
             }
           };
-          if (use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
+          if (!CODES && use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
           if (!ok) break;
           if (SPARSE && lane == 0) {
             volatile int32_t* info = info_base + (g % INFO_RING) * INFO_WORDS;
@@ -651,9 +696,11 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             for (int i = 0; i < 4; ++i) info[I_BITS + i] = (int32_t)bits[i];
           }
           __syncwarp();
-          armed_k |= 1u << st;
-          par_k = (par_k & ~(1u << st)) | ((use & 1) << st);
-          load(sbase + SM_K + st * TILE_BYTES, &maps.k, bar(K_FULL + st));
+          if (!CODES) {
+            armed_k |= 1u << st;
+            par_k = (par_k & ~(1u << st)) | ((use & 1) << st);
+            load(sbase + SM_K + st * TILE_BYTES, &maps.k, bar(K_FULL + st));
+          }
           if (j == 0) {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
@@ -672,6 +719,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
             }
             if (!ok) break;
           }
+          if (CODES) continue;
           if (use > 0) ok = wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
           if (!ok) break;
           armed_v |= 1u << st;
@@ -693,6 +741,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         for (int y = 0; y < 2; ++y)
           if (armed_q & (1u << y))
             settle(bar(Q_FULL + y), (par_q >> y) & 1);
+        if (CODES)
+          for (uint32_t s = 0; s < L::RAW_STAGES; ++s)
+            if (raw > s) settle(bar(RAW_FULL + s), ((raw - s + L::RAW_STAGES - 1) / L::RAW_STAGES - 1) & 1);
       }
     } else if (warp == 2) {
       // ---------------------------------------------------------------- the CTA's run
@@ -906,8 +957,79 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
         settle(bar(DRAIN), 0);
       }
     }
+  } else if (CODES && warp >= 12) {
+    // ------------------------------------------------------------------ codes to numbers
+    reg_dealloc<REGS4_CODES>();
+    // a thread takes half of a row of K and of V of a page: D / 16 words; at 128 columns a half is a 128-byte row of the tile's half (chunks of 16
+    // bytes, swizzled), and the two threads of a row begin at different ends of it, so that they do not meet in a bank
+    constexpr int W = D / 16;
+    const int t = threadIdx.x - 384, row = t >> 1, half = t & 1, swap = D == 128 ? half : 0;
+    const int from = row * B::ROW + half * (D / 4);
+    const uint32_t to = (D == 128 ? half * HALF_COLS_BYTES : 0) + row * 128;
+    auto convert = [&](const unsigned char* codes, const unsigned char* scales, unsigned char* tile) {
+      uint32_t w[W], s[W / 2];
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const uint4 y = *reinterpret_cast<const uint4*>(codes + from + (i ^ swap) * 16);
+        w[4 * i] = y.x, w[4 * i + 1] = y.y, w[4 * i + 2] = y.z, w[4 * i + 3] = y.w;
+      }
+      uint32_t bytes = D == 128 ? *reinterpret_cast<const uint32_t*>(scales + row * B::SCALES + half * 4)
+                                : *reinterpret_cast<const uint16_t*>(scales + row * B::SCALES + half * 2);
+      if (swap) bytes = bytes << 16 | bytes >> 16;
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) s[i] = __byte_perm(bytes, 0, 0x4040 + 0x0101 * i);       // a scale's byte in both halves
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        uint32_t v[4];
+        if (F16) {
+          const Steps4 steps(s[i / 2]);
+          values4(w[i], steps, v);
+        } else {
+          const Steps4Bf16 steps(s[i / 2]);
+          values4(w[i], steps, v);
+        }
+        const int chunk = D == 128 ? i ^ (swap << 2) : half * W + i;
+        *reinterpret_cast<uint4*>(tile + to + ((chunk ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    };
+    uint32_t g = 0, raw = 0;
+    bool ok = true;
+    for (uint32_t it = 0; ok; ++it) {
+      const uint32_t slot = it & 1;
+      volatile int32_t* ring = ring_base + slot * 16;
+      ok = wait_all(bar(ITEM_FULL + slot), (it >> 1) & 1, abort_flag, p.status, 1 + ITEM_FULL);
+      if (!ok) break;
+      if (ring_word(ring, W_KIND) == 0) break;
+      const int n_tiles = ring_word(ring, W_NT);
+      for (int j = 0; j < n_tiles && ok; ++j, ++g) {
+        const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
+#pragma unroll 1
+        for (int h = 0; h < 2 && ok; ++h, ++raw) {
+          const uint32_t rs = raw % L::RAW_STAGES;
+          const unsigned char* block = sgen + L::SM_OUT + rs * B::BYTES;
+          ok = wait_all(bar(RAW_FULL + rs), (raw / L::RAW_STAGES) & 1, abort_flag, p.status, 1 + RAW_FULL);
+          if (ok && h == 0 && use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
+          if (!ok) break;
+          convert(block + B::K, block + B::KS, sgen + SM_K + st * TILE_BYTES + h * SLOT_BYTES);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (h == 1 && lane == 0) mbar_arrive(bar(K_FULL + st));
+          if (h == 0 && use > 0) ok = wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
+          if (!ok) break;
+          convert(block + B::V, block + B::VS, sgen + SM_V + st * TILE_BYTES + h * SLOT_BYTES);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (h == 1) mbar_arrive(bar(V_FULL + st));
+            mbar_arrive(bar(RAW_EMPTY + rs));
+          }
+        }
+      }
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(bar(ITEM_EMPTY + slot));
+    }
   } else {
-    reg_alloc<REGS_SOFTMAX>();
+    reg_alloc<CODES ? REGS4_SOFTMAX : REGS_SOFTMAX>();
     // ------------------------------------------------------------------ softmax and results
     const int x = (warp - 4) >> 2;
     const int row = (warp & 3) * 32 + lane;                        // row of the tile == TMEM lane
@@ -1046,31 +1168,41 @@ __global__ void __launch_bounds__(THREADS, 1) paged_tc_kernel(const __grid_const
           const int64_t o_at = (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head;
           // 32 columns of the warp's rows, through shared memory so that four lanes write 64 bytes of a row
           auto store_rows = [&](const float (&acc)[32], float inv, int c) {
+            if constexpr (CODES) {                                           // (the blocks have the place: a lane writes 64 bytes of its row)
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              int4 v;
-              v.x = (int)pack16<F16>(acc[i] * inv, acc[i + 1] * inv);
-              v.y = (int)pack16<F16>(acc[i + 2] * inv, acc[i + 3] * inv);
-              v.z = (int)pack16<F16>(acc[i + 4] * inv, acc[i + 5] * inv);
-              v.w = (int)pack16<F16>(acc[i + 6] * inv, acc[i + 7] * inv);
-              *reinterpret_cast<int4*>(stage + lane * 64 + (((i >> 3) ^ ((lane >> 1) & 3)) << 4)) = v;
-            }
-            __syncwarp();
+              for (int i = 0; i < 32; i += 8)
+                if (valid)
+                  *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + o_at + c * 32 + i) =
+                      make_uint4(pack16<F16>(acc[i] * inv, acc[i + 1] * inv), pack16<F16>(acc[i + 2] * inv, acc[i + 3] * inv),
+                                 pack16<F16>(acc[i + 4] * inv, acc[i + 5] * inv), pack16<F16>(acc[i + 6] * inv, acc[i + 7] * inv));
+              __syncwarp();
+            } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int r = k * 8 + (lane >> 2), ch = lane & 3;
-              const int4 v = *reinterpret_cast<const int4*>(stage + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
-              const int64_t at = __shfl_sync(0xffffffffu, o_at, r);
-              if (__shfl_sync(0xffffffffu, (int)valid, r))
-                *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.out) + at + c * 32 + ch * 8) = v;
+              for (int i = 0; i < 32; i += 8) {
+                int4 v;
+                v.x = (int)pack16<F16>(acc[i] * inv, acc[i + 1] * inv);
+                v.y = (int)pack16<F16>(acc[i + 2] * inv, acc[i + 3] * inv);
+                v.z = (int)pack16<F16>(acc[i + 4] * inv, acc[i + 5] * inv);
+                v.w = (int)pack16<F16>(acc[i + 6] * inv, acc[i + 7] * inv);
+                *reinterpret_cast<int4*>(stage + lane * 64 + (((i >> 3) ^ ((lane >> 1) & 3)) << 4)) = v;
+              }
+              __syncwarp();
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int r = k * 8 + (lane >> 2), ch = lane & 3;
+                const int4 v = *reinterpret_cast<const int4*>(stage + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
+                const int64_t at = __shfl_sync(0xffffffffu, o_at, r);
+                if (__shfl_sync(0xffffffffu, (int)valid, r))
+                  *reinterpret_cast<int4*>(static_cast<__nv_bfloat16*>(p.out) + at + c * 32 + ch * 8) = v;
+              }
+              __syncwarp();
             }
-            __syncwarp();
           };
           auto finish = [&](float m, float l) {                    // 1 / sum, and the row's logarithm
             // the key that set the reference counts 1, so a sum below that has no key, or none with a weight; one that is NaN stays NaN
             const bool any = !(l <= 0.5f);
             if (p.lse && valid) p.lse[(int64_t)tok * p.H + hd] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-            const float inv = any ? 1.f / l : 0.f;
+            const float inv = any ? (CODES ? tp.v_unit : 1.f) / l : 0.f;
             __syncwarp();                                          // the loads of tensor memory that follow are the whole warp's
             return inv;
           };
@@ -1203,17 +1335,18 @@ uint64_t plan_bytes(int G, int Hkv, int n_tokens, int n_seq) {
   return (4 * item_words(n_seq) + std::max(8 * dense, 4 * sparse) + 255) / 256 * 256;
 }
 
-template <int D, bool F16, bool SPARSE>
+template <int D, bool F16, bool SPARSE, bool CODES = false>
 cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
-  auto kernel = paged_tc_kernel<D, F16, SPARSE>;
-  constexpr int smem = (int)Layout<D>::SM_ALLOC + (SPARSE ? LIST_BYTES + LIST_ENTRIES * 2 : 0);
+  auto kernel = paged_tc_kernel<D, F16, SPARSE, CODES>;
+  constexpr int threads = CODES ? THREADS4 : THREADS, smem = (int)Layout<D, CODES>::SM_ALLOC + (SPARSE ? LIST_BYTES + LIST_ENTRIES * 2 : 0);
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (rc != cudaSuccess) return rc;
   // the register hand-over must fit in what the launch allocates, or it would wait for ever
   cudaFuncAttributes attr;
   rc = cudaFuncGetAttributes(&attr, kernel);
   if (rc != cudaSuccess) return rc;
-  if (attr.numRegs * THREADS < 128 * REGS_SMALL + 256 * REGS_SOFTMAX) return cudaErrorLaunchOutOfResources;
+  constexpr int wanted = CODES ? 128 * (REGS4_SMALL + REGS4_CODES) + 256 * REGS4_SOFTMAX : 128 * REGS_SMALL + 256 * REGS_SOFTMAX;
+  if (attr.numRegs * threads < wanted) return cudaErrorLaunchOutOfResources;
   if (SPARSE) {
     const int bytes = ((tp.a.n_seq + 1) * 4 + 15) / 16 * 16 + UNION_WARPS * LIST_BYTES;
     rc = cudaFuncSetAttribute(union_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PAGED_MAX_SEQ + 4) * 4 + UNION_WARPS * LIST_BYTES);
@@ -1228,7 +1361,7 @@ cudaError_t launch(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_
     rc = launch_pdl(plan_kernel, dim3(1), dim3(PT), bytes, stream, tp);
   }
   if (rc != cudaSuccess) return rc;
-  return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, stream, tp, maps);
+  return launch_pdl(kernel, dim3(grid), dim3(threads), smem, stream, tp, maps);
 }
 template <int D, bool F16>
 cudaError_t launch_either(const TcParams& tp, const TcMaps& maps, int grid, cudaStream_t stream) {
@@ -1249,8 +1382,10 @@ bool paged_tc_takes_lists(int G, int Hkv, int n_sel, int table_pages, int n_toke
   return ((int64_t)n_tokens * n_sel / 2 + (int64_t)plan_items(tile_tokens, n_tokens, n_seq) * (1 + ITEM_END)) * Hkv <= INT32_MAX;
 }
 
-cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {
-  TcParams tp;
+// what the calls of either kind of cache share: places in the workspace
+namespace {
+TcParams place_plan(const PagedParams& p, const PagedDevice& dev) {
+  TcParams tp = {};
   tp.a = p;
   tp.a.tile_tokens = p.sel ? sparse_tile_tokens(p.G) : BM / p.G;
   tp.runs = reinterpret_cast<int32_t*>(p.partials);
@@ -1261,12 +1396,33 @@ cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool,
   tp.n_cta = dev.n_sm;
   tp.items = (int32_t)plan_items(tp.a.tile_tokens, p.n_tokens, p.n_seq);
   tp.a.partials = p.partials + (run_bytes(dev.n_sm) + plan_bytes(p.G, p.Hkv, p.n_tokens, p.n_seq)) / 4;
+  return tp;
+}
+}  // namespace
+
+cudaError_t launch_paged_tc(const PagedParams& p, const heatkv_paged_pool& pool, const PagedDevice& dev, cudaStream_t stream) {
+  const TcParams tp = place_plan(p, dev);
   TcMaps maps;
   if (!paged_encode_pool(dev, &maps.k, pool.k, pool) || !paged_encode_pool(dev, &maps.v, pool.v, pool) || !paged_encode_q(dev, &maps.q, tp.a, pool))
     return cudaErrorInvalidValue;
   const bool fp16 = pool.dtype == HEATKV_DTYPE_FP16;
   if (pool.d == 128) return fp16 ? launch_either<128, true>(tp, maps, dev.n_sm, stream) : launch_either<128, false>(tp, maps, dev.n_sm, stream);
   return fp16 ? launch_either<64, true>(tp, maps, dev.n_sm, stream) : launch_either<64, false>(tp, maps, dev.n_sm, stream);
+}
+
+cudaError_t launch_paged4_tc(const Paged4Params& q, int d, const PagedDevice& dev, cudaStream_t stream) {
+  TcParams tp = place_plan(q.a, dev);
+  tp.blocks = q.blocks;
+  tp.page_stride = q.page_stride;
+  tp.head_stride = q.head_stride;
+  tp.v_unit = q.v_unit;
+  TcMaps maps = {};
+  heatkv_paged_pool shape = {};
+  shape.d = d;
+  shape.dtype = q.fp16 ? HEATKV_DTYPE_FP16 : HEATKV_DTYPE_BF16;
+  if (!paged_encode_q(dev, &maps.q, tp.a, shape)) return cudaErrorInvalidValue;
+  if (d == 128) return q.fp16 ? launch<128, true, false, true>(tp, maps, dev.n_sm, stream) : launch<128, false, false, true>(tp, maps, dev.n_sm, stream);
+  return q.fp16 ? launch<64, true, false, true>(tp, maps, dev.n_sm, stream) : launch<64, false, false, true>(tp, maps, dev.n_sm, stream);
 }
 
 }  // namespace heatkv

@@ -345,8 +345,14 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
   p.page_stride = pool->page_stride;
   p.head_stride = pool->head_stride;
   p.fp16 = pool->dtype == HEATKV_DTYPE_FP16;
-  const int64_t rows = (int64_t)p.a.max_new * p.a.G;
-  return done((rows <= 64 ? launch_paged4_small : launch_paged4_tc)(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
+  // Up to two tiles of 16 rows: the warp-level kernel (8 kv heads of 4 heads; 32 requests of 10 000 tokens, 16 rows 117 us and 254 on the tensor-memory
+  // kernel, 32 rows 219 and 254, 48 rows 318 and 255).  More where there is little to do in all, a tile of `table_pages` pages weighing eight more: one
+  // request of 10 000, 96 rows (7920) 37 and 63, of 300 11.9 and 16.8; 8 requests of 2500, 64 rows (12 288) 44.8 and 39.6; 32 of 300, 64 rows (14 336) 37.4
+  // and 33.9.  Three tiles up to four times as much, as a batch's requests are mostly shorter than its table is wide: 24 of 40 to 8000 tokens, 42 rows
+  // (38 900) 20.8 and 35.9; 8 of 10 000, 48 rows (31 700) 91 and 83.
+  const int64_t tiles = ((int64_t)p.a.max_new * p.a.G + 15) / 16, units = (int64_t)p.a.n_seq * p.a.Hkv, little = tiles == 3 ? 40000 : 10000;
+  const bool few = tiles <= 2 || (units <= little && tiles <= little && units * tiles * ((int64_t)p.a.table_pages + 8) <= little);
+  return done((few ? launch_paged4_small : launch_paged4_tc)(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
 }
 
 // ---------------------------------------------------------------- rows between steps
@@ -395,7 +401,7 @@ int heatkv_paged_fork(const int32_t* parents, const int32_t* keep_len, const int
   p.n_seq = n_seq;
   p.table_pages = table_pages;
   p.n_pages = n_pages;
-  p.n_moves = n_seq > 0 && n_seq <= PAGED_MAX_SEQ ? n_seq * PAGE : 0;
+  p.n_moves = n_seq > 0 && n_seq <= PAGED_MAX_SEQ ? n_seq * PAGE : 1;      // (other numbers of rows are refused below)
   return rearrange(&p, workspace, workspace_bytes, false, stream);
 }
 

@@ -7,9 +7,9 @@
 
 #include "heatkv.h"
 
-static PyObject *s_data_ptr, *s_stride, *s_dtype, *s_shape, *s_numel, *s_nbytes, *s_is_contiguous, *s_get_device, *s_cuda_stream, *s_addr, *s_device,
+static PyObject *s_data_ptr, *s_stride, *s_dtype, *s_shape, *s_numel, *s_nbytes, *s_is_contiguous, *s_get_device, *s_cuda_stream, *s_addr, *s_addr4, *s_device,
     *s_torch_dtype;
-static PyObject *type_int32, *type_float32;
+static PyObject *type_int32, *type_float32, *type_uint8, *type_bool;
 static PyObject *hook_device, *hook_stream;      /* torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream */
 
 /* whole number that a method (or, attribute != 0, an attribute) gives; INT64_MIN where there is none */
@@ -84,14 +84,14 @@ static int stream_of(PyObject* stream, int64_t device, void** out) {
   PyErr_Clear();
   return 0;
 }
-/* a pool's or batch's structure, kept alive by the object that the caller holds */
-static const void* structure(PyObject* x, int64_t* device) {
-  const int64_t at = number(x, s_addr, 1);
+/* a pool's or batch's structure, kept alive by the object that the caller holds (a pool of 4 bits has its address under another name) */
+static const void* structure(PyObject* x, PyObject* name, int64_t* device) {
+  const int64_t at = number(x, name, 1);
   *device = number(x, s_device, 1);
   return at > 0 && *device >= 0 ? (const void*)(intptr_t)at : NULL;
 }
-static const heatkv_paged_pool* pool_of(PyObject* x, int64_t* device, PyObject** type) {
-  const heatkv_paged_pool* pool = structure(x, device);
+static const void* pool_of(PyObject* x, PyObject* name, int64_t* device, PyObject** type) {
+  const void* pool = structure(x, name, device);
   *type = pool ? PyObject_GetAttr(x, s_torch_dtype) : NULL;       /* (held by torch, too) */
   if (!*type) PyErr_Clear();
   Py_XDECREF(*type);
@@ -126,7 +126,7 @@ static PyObject* py_paged_store(PyObject* self, PyObject* const* a, Py_ssize_t n
   const heatkv_paged_pool* pool;
   void *stream, *slots;
   Rows k, v;
-  if (n_args != 5 || !(pool = pool_of(a[0], &device, &type)) || (n = number(a[3], s_numel, 0)) < 0 || n > INT_MAX ||
+  if (n_args != 5 || !(pool = pool_of(a[0], s_addr, &device, &type)) || (n = number(a[3], s_numel, 0)) < 0 || n > INT_MAX ||
       !rows(a[1], type, device, n, pool->n_kv_heads, pool->d, &k) || !rows(a[2], type, device, n, pool->n_kv_heads, pool->d, &v) ||
       k.tok != v.tok || k.head != v.head || !vector(a[3], n, device, &slots) || !stream_of(a[4], device, &stream))
     Py_RETURN_NONE;
@@ -139,7 +139,8 @@ static PyObject* py_paged_store(PyObject* self, PyObject* const* a, Py_ssize_t n
 
 /* what the calls over a batch have in common: (pool, batch, q, ..) and n_select lists of pages per token (sel None: none) */
 typedef struct {
-  const heatkv_paged_pool* pool;
+  const void* pool;                                 /* heatkv_paged_pool, or heatkv_paged4_pool */
+  int64_t n_kv_heads, d;
   const heatkv_paged_batch* batch;
   int64_t device;
   PyObject* type;
@@ -147,13 +148,23 @@ typedef struct {
   void *lists, *stream;
   int64_t n_select;
 } Call;
-static int call_of(PyObject* pool, PyObject* batch, PyObject* q, PyObject* sel, PyObject* stream, Call* c) {
+static int call_of(PyObject* pool, PyObject* name, PyObject* batch, PyObject* q, PyObject* sel, PyObject* stream, Call* c) {
   int64_t other, x[3];
-  if (!(c->pool = pool_of(pool, &c->device, &c->type)) || !(c->batch = structure(batch, &other)) || other != c->device ||
-      !rows(q, c->type, c->device, c->batch->n_tokens, 0, c->pool->d, &c->q) || c->q.heads > INT_MAX || !stream_of(stream, c->device, &c->stream))
+  if (!(c->pool = pool_of(pool, name, &c->device, &c->type))) return 0;
+  if (name == s_addr) {
+    const heatkv_paged_pool* p = c->pool;
+    c->n_kv_heads = p->n_kv_heads;
+    c->d = p->d;
+  } else {
+    const heatkv_paged4_pool* p = c->pool;
+    c->n_kv_heads = p->n_kv_heads;
+    c->d = p->d;
+  }
+  if (!(c->batch = structure(batch, s_addr, &other)) || other != c->device ||
+      !rows(q, c->type, c->device, c->batch->n_tokens, 0, c->d, &c->q) || c->q.heads > INT_MAX || !stream_of(stream, c->device, &c->stream))
     return 0;
   if (!sel) return 1;
-  if (!placed(sel, type_int32, c->device, &c->lists) || !extents(sel, s_shape, 0, 3, x) || x[0] != c->batch->n_tokens || x[1] != c->pool->n_kv_heads ||
+  if (!placed(sel, type_int32, c->device, &c->lists) || !extents(sel, s_shape, 0, 3, x) || x[0] != c->batch->n_tokens || x[1] != c->n_kv_heads ||
       x[2] > INT_MAX || !contiguous(sel))
     return 0;
   c->n_select = x[2];
@@ -168,7 +179,7 @@ typedef struct {
 static int results_of(const Call* c, PyObject* out, PyObject* lse, PyObject* workspace, Results* r) {
   int64_t x[2];
   r->lse = NULL;
-  if (!rows(out, c->type, c->device, c->batch->n_tokens, c->q.heads, c->pool->d, &r->out)) return 0;
+  if (!rows(out, c->type, c->device, c->batch->n_tokens, c->q.heads, c->d, &r->out)) return 0;
   if (lse != Py_None && (!placed(lse, type_float32, c->device, &r->lse) || !extents(lse, s_shape, 0, 2, x) || x[0] != c->batch->n_tokens ||
                          x[1] != c->q.heads || !contiguous(lse)))
     return 0;
@@ -178,24 +189,132 @@ static int results_of(const Call* c, PyObject* out, PyObject* lse, PyObject* wor
   return type && placed(workspace, type, c->device, &r->workspace) && (r->bytes = number(workspace, s_nbytes, 1)) >= 0 && contiguous(workspace);
 }
 
-static PyObject* py_paged_attention(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {      /* pool, batch, q, out, lse, ws, causal, scale, stream */
+/* pool, batch, q, out, lse, ws, causal, scale, stream */
+static PyObject* attention(PyObject* const* a, Py_ssize_t n_args, PyObject* name) {
   Call c;
   Results r;
-  if (n_args != 9 || !call_of(a[0], a[1], a[2], NULL, a[8], &c) || !results_of(&c, a[3], a[4], a[5], &r)) Py_RETURN_NONE;
+  if (n_args != 9 || !call_of(a[0], name, a[1], a[2], NULL, a[8], &c) || !results_of(&c, a[3], a[4], a[5], &r)) Py_RETURN_NONE;
   const int causal = PyObject_IsTrue(a[6]);
   const double scale = PyFloat_AsDouble(a[7]);
   if (PyErr_Occurred()) return NULL;
   const heatkv_token_strides st = {c.q.tok, c.q.head, r.out.tok, r.out.head};
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = heatkv_paged_attention(c.pool, c.batch, (int)c.q.heads, c.q.p, &st, causal, (float)scale, r.out.p, r.lse, r.workspace, (uint64_t)r.bytes, c.stream);
+  rc = name == s_addr ? heatkv_paged_attention(c.pool, c.batch, (int)c.q.heads, c.q.p, &st, causal, (float)scale, r.out.p, r.lse, r.workspace,
+                                               (uint64_t)r.bytes, c.stream)
+                      : heatkv_paged4_attention(c.pool, c.batch, (int)c.q.heads, c.q.p, &st, causal, (float)scale, r.out.p, r.lse, r.workspace,
+                                                (uint64_t)r.bytes, c.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+static PyObject* py_paged_attention(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return attention(a, n_args, s_addr); }
+static PyObject* py_paged4_attention(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return attention(a, n_args, s_addr4); }
+
+/* rows of K and V to their slots and back: (pool, k, v, slots, stream) */
+static PyObject* rows4(PyObject* const* a, Py_ssize_t n_args, int load) {
+  int64_t device, n;
+  PyObject* type;
+  const heatkv_paged4_pool* pool;
+  void *stream, *slots;
+  Rows k, v;
+  if (n_args != 5 || !(pool = pool_of(a[0], s_addr4, &device, &type)) || (n = number(a[3], s_numel, 0)) < 0 || n > INT_MAX ||
+      !rows(a[1], type, device, n, pool->n_kv_heads, pool->d, &k) || !rows(a[2], type, device, n, pool->n_kv_heads, pool->d, &v) ||
+      k.tok != v.tok || k.head != v.head || !vector(a[3], n, device, &slots) || !stream_of(a[4], device, &stream))
+    Py_RETURN_NONE;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = load ? heatkv_paged4_load(pool, slots, (int)n, k.p, v.p, k.tok, k.head, stream) : heatkv_paged4_store(pool, k.p, v.p, k.tok, k.head, slots, (int)n, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+static PyObject* py_paged4_store(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return rows4(a, n_args, 0); }
+static PyObject* py_paged4_load(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return rows4(a, n_args, 1); }
+
+/* (pool, from, to, stream) */
+static PyObject* move(PyObject* const* a, Py_ssize_t n_args, PyObject* name) {
+  int64_t device, n;
+  PyObject* type;
+  const void* pool;
+  void *stream, *from, *to;
+  if (n_args != 4 || !(pool = pool_of(a[0], name, &device, &type)) || (n = number(a[1], s_numel, 0)) < 0 || n > INT_MAX ||
+      !vector(a[1], n, device, &from) || !vector(a[2], n, device, &to) || !stream_of(a[3], device, &stream))
+    Py_RETURN_NONE;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = name == s_addr ? heatkv_paged_move(pool, from, to, (int)n, stream) : heatkv_paged4_move(pool, from, to, (int)n, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+static PyObject* py_paged_move(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return move(a, n_args, s_addr); }
+static PyObject* py_paged4_move(PyObject* self, PyObject* const* a, Py_ssize_t n_args) { return move(a, n_args, s_addr4); }
+
+/* what both calls that rearrange rows have: lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to,
+ * workspace, stream, from a[0] on; n_moves < 0: any number */
+typedef struct {
+  int64_t device, n, n_pages, n_moves, bytes, pages, stride, out_stride;
+  void *lengths, *table, *free, *state, *lengths_out, *table_out, *state_out, *from, *to, *workspace, *stream;
+} Rearranged;
+static int table_of(PyObject* t, int64_t n, int64_t device, void** p, int64_t* pages, int64_t* stride) {
+  int64_t shape[2], strides[2];
+  if (!placed(t, type_int32, device, p) || !extents(t, s_shape, 0, 2, shape) || !extents(t, s_stride, 1, 2, strides) || shape[0] != n ||
+      shape[1] > INT_MAX || strides[1] != 1)
+    return 0;
+  *pages = shape[1];
+  *stride = n > 1 ? strides[0] : shape[1];
+  return 1;
+}
+static int rearranged(PyObject* const* a, int by_row, Rearranged* r) {
+  int64_t pages;
+  r->device = number(a[0], s_get_device, 0);
+  r->n = number(a[0], s_numel, 0);
+  r->n_pages = number(a[2], s_numel, 0);
+  r->n_moves = by_row ? r->n * HEATKV_PAGE_TOKENS : number(a[7], s_numel, 0);
+  if (!stream_of(a[10], r->device, &r->stream) || r->n < 0 || r->n > INT_MAX / HEATKV_PAGE_TOKENS || r->n_pages < 0 || r->n_pages > INT_MAX ||
+      r->n_moves < 0 || r->n_moves > INT_MAX || !vector(a[0], r->n, r->device, &r->lengths) ||
+      !table_of(a[1], r->n, r->device, &r->table, &r->pages, &r->stride) || !vector(a[2], r->n_pages, r->device, &r->free) ||
+      !vector(a[3], 4, r->device, &r->state) || !vector(a[4], r->n, r->device, &r->lengths_out) ||
+      !table_of(a[5], r->n, r->device, &r->table_out, &pages, &r->out_stride) || pages != r->pages || !vector(a[6], 4, r->device, &r->state_out) ||
+      !vector(a[7], r->n_moves, r->device, &r->from) || !vector(a[8], r->n_moves, r->device, &r->to))
+    return 0;
+  PyObject* type = PyObject_GetAttr(a[9], s_dtype);
+  if (!type) PyErr_Clear();
+  Py_XDECREF(type);
+  return type && placed(a[9], type, r->device, &r->workspace) && (r->bytes = number(a[9], s_nbytes, 1)) >= 0 && contiguous(a[9]);
+}
+
+static PyObject* py_paged_fork(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {           /* parents, keep | None, .. */
+  Rearranged r;
+  void *parents, *keep = NULL;
+  if (n_args != 13 || !rearranged(a + 2, 1, &r) || !vector(a[0], r.n, r.device, &parents) || (a[1] != Py_None && !vector(a[1], r.n, r.device, &keep)))
+    Py_RETURN_NONE;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = heatkv_paged_fork(parents, keep, r.lengths, (int)r.n, r.table, r.stride, (int)r.pages, r.free, (int)r.n_pages, r.state, r.lengths_out, r.table_out,
+                         r.out_stride, r.state_out, r.from, r.to, r.workspace, (uint64_t)r.bytes, r.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+static PyObject* py_paged_compact(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {        /* stays, .. */
+  Rearranged r;
+  void* stays;
+  int64_t shape[2], strides[2];
+  if (n_args != 12 || !rearranged(a + 1, 0, &r)) Py_RETURN_NONE;
+  if ((!placed(a[0], type_bool, r.device, &stays) && !placed(a[0], type_uint8, r.device, &stays)) || !extents(a[0], s_shape, 0, 2, shape) ||
+      !extents(a[0], s_stride, 1, 2, strides) || shape[0] != r.n || shape[1] > INT_MAX || (strides[1] != 1 && shape[1] > 1))
+    Py_RETURN_NONE;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = heatkv_paged_compact(stays, r.n > 1 ? strides[0] : shape[1], (int)shape[1], r.lengths, (int)r.n, r.table, r.stride, (int)r.pages, r.free,
+                            (int)r.n_pages, r.state, r.lengths_out, r.table_out, r.out_stride, r.state_out, r.from, r.to, (int)r.n_moves, r.workspace,
+                            (uint64_t)r.bytes, r.stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
 
 static PyObject* py_paged_select(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {         /* pool, batch, q, sel, sink, local, stream */
   Call c;
-  if (n_args != 7 || !call_of(a[0], a[1], a[2], a[3], a[6], &c)) Py_RETURN_NONE;
+  if (n_args != 7 || !call_of(a[0], s_addr, a[1], a[2], a[3], a[6], &c)) Py_RETURN_NONE;
   const long sink = PyLong_AsLong(a[4]), local = PyLong_AsLong(a[5]);
   if (PyErr_Occurred()) return NULL;
   if (sink < INT_MIN || sink > INT_MAX || local < INT_MIN || local > INT_MAX) Py_RETURN_NONE;
@@ -210,7 +329,7 @@ static PyObject* py_paged_select(PyObject* self, PyObject* const* a, Py_ssize_t 
 static PyObject* py_paged_sparse_attention(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {  /* pool, batch, q, sel, out, lse, ws, scale, stream */
   Call c;
   Results r;
-  if (n_args != 9 || !call_of(a[0], a[1], a[2], a[3], a[8], &c) || !results_of(&c, a[4], a[5], a[6], &r)) Py_RETURN_NONE;
+  if (n_args != 9 || !call_of(a[0], s_addr, a[1], a[2], a[3], a[8], &c) || !results_of(&c, a[4], a[5], a[6], &r)) Py_RETURN_NONE;
   const double scale = PyFloat_AsDouble(a[7]);
   if (PyErr_Occurred()) return NULL;
   const heatkv_token_strides st = {c.q.tok, c.q.head, r.out.tok, r.out.head};
@@ -223,12 +342,14 @@ static PyObject* py_paged_sparse_attention(PyObject* self, PyObject* const* a, P
 }
 
 static PyObject* py_set_hooks(PyObject* self, PyObject* args) {
-  PyObject *device, *stream, *i, *f;
-  if (!PyArg_ParseTuple(args, "OOOO", &device, &stream, &i, &f)) return NULL;
+  PyObject *device, *stream, *i, *f, *u, *o;
+  if (!PyArg_ParseTuple(args, "OOOOOO", &device, &stream, &i, &f, &u, &o)) return NULL;
   hook_device = Py_NewRef(device);                              /* (once a process) */
   hook_stream = Py_NewRef(stream);
   type_int32 = Py_NewRef(i);
   type_float32 = Py_NewRef(f);
+  type_uint8 = Py_NewRef(u);
+  type_bool = Py_NewRef(o);
   Py_RETURN_NONE;
 }
 
@@ -241,7 +362,17 @@ static PyMethodDef methods[] = {
     {"select", (PyCFunction)(void (*)(void))py_paged_select, METH_FASTCALL, "(pool, batch, q, sel, sink, local, stream | None)"},
     {"sparse_attention", (PyCFunction)(void (*)(void))py_paged_sparse_attention, METH_FASTCALL,
      "(pool, batch, q, sel, out, lse | None, workspace, sm_scale, stream | None)"},
-    {"set_hooks", py_set_hooks, METH_VARARGS, "(current_device, raw_stream, torch.int32, torch.float32)"},
+    {"attention4", (PyCFunction)(void (*)(void))py_paged4_attention, METH_FASTCALL,
+     "(pool, batch, q, out, lse | None, workspace, causal, sm_scale, stream | None)"},
+    {"store4", (PyCFunction)(void (*)(void))py_paged4_store, METH_FASTCALL, "(pool, k_new, v_new, slot_map, stream | None)"},
+    {"load4", (PyCFunction)(void (*)(void))py_paged4_load, METH_FASTCALL, "(pool, k_out, v_out, slot_map, stream | None)"},
+    {"move", (PyCFunction)(void (*)(void))py_paged_move, METH_FASTCALL, "(pool, move_from, move_to, stream | None)"},
+    {"move4", (PyCFunction)(void (*)(void))py_paged4_move, METH_FASTCALL, "(pool, move_from, move_to, stream | None)"},
+    {"fork", (PyCFunction)(void (*)(void))py_paged_fork, METH_FASTCALL,
+     "(parents, keep_len | None, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace, stream | None)"},
+    {"compact", (PyCFunction)(void (*)(void))py_paged_compact, METH_FASTCALL,
+     "(stays, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace, stream | None)"},
+    {"set_hooks", py_set_hooks, METH_VARARGS, "(current_device, raw_stream, torch.int32, torch.float32, torch.uint8, torch.bool)"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -252,7 +383,7 @@ PyMODINIT_FUNC PyInit__paged(void) {
     const char* name;
   } names[] = {{&s_data_ptr, "data_ptr"}, {&s_stride, "stride"}, {&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_numel, "numel"}, {&s_nbytes, "nbytes"},
                {&s_is_contiguous, "is_contiguous"}, {&s_get_device, "get_device"}, {&s_cuda_stream, "cuda_stream"}, {&s_addr, "addr"},
-               {&s_device, "device"}, {&s_torch_dtype, "torch_dtype"}};
+               {&s_addr4, "addr4"}, {&s_device, "device"}, {&s_torch_dtype, "torch_dtype"}};
   for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
     if (!(*names[i].at = PyUnicode_InternFromString(names[i].name))) return NULL;
   return PyModule_Create(&module);

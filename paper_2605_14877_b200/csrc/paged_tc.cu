@@ -43,7 +43,7 @@ constexpr int KV_STAGES = 2;
 constexpr int REGS_LAUNCH = 168, REGS_SMALL = 72, REGS_SOFTMAX = 216;
 static_assert(128 * REGS_SMALL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register hand-over exceeds the CTA's allocation");
 // .. of the kernel over 4 bits, with four warps more
-constexpr int THREADS4 = 512, REGS4_LAUNCH = 128, REGS4_SMALL = 48, REGS4_SOFTMAX = 200, REGS4_CODES = 64;
+constexpr int THREADS4 = 512, REGS4_LAUNCH = 128, REGS4_SMALL = 56, REGS4_SOFTMAX = 200, REGS4_CODES = 56;
 static_assert(128 * (REGS4_SMALL + REGS4_CODES) + 256 * REGS4_SOFTMAX <= THREADS4 * REGS4_LAUNCH, "register hand-over exceeds the CTA's allocation");
 constexpr uint32_t HALF_COLS_BYTES = 128 * 128;        // one 64-column half of a 128-row tile
 constexpr uint32_t SLOT_BYTES = PAGE * 128;            // a page inside one column half
@@ -1003,26 +1003,25 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
       const int n_tiles = ring_word(ring, W_NT);
       for (int j = 0; j < n_tiles && ok; ++j, ++g) {
         const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
+        if (use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY) &&
+                          wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
 #pragma unroll 1
         for (int h = 0; h < 2 && ok; ++h, ++raw) {
           const uint32_t rs = raw % L::RAW_STAGES;
           const unsigned char* block = sgen + L::SM_OUT + rs * B::BYTES;
           ok = wait_all(bar(RAW_FULL + rs), (raw / L::RAW_STAGES) & 1, abort_flag, p.status, 1 + RAW_FULL);
-          if (ok && h == 0 && use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY);
           if (!ok) break;
           convert(block + B::K, block + B::KS, sgen + SM_K + st * TILE_BYTES + h * SLOT_BYTES);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (h == 1 && lane == 0) mbar_arrive(bar(K_FULL + st));
-          if (h == 0 && use > 0) ok = wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
-          if (!ok) break;
           convert(block + B::V, block + B::VS, sgen + SM_V + st * TILE_BYTES + h * SLOT_BYTES);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) {
-            if (h == 1) mbar_arrive(bar(V_FULL + st));
-            mbar_arrive(bar(RAW_EMPTY + rs));
-          }
+          if (lane == 0) mbar_arrive(bar(RAW_EMPTY + rs));
+        }
+        if (!ok) break;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(K_FULL + st));
+          mbar_arrive(bar(V_FULL + st));
         }
       }
       __syncwarp();

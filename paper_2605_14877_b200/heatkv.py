@@ -359,7 +359,7 @@ def _check(rc: int, where: str) -> None:
         raise HeatKVError(rc, where)
 
 
-_paged.set_hooks(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.int32, torch.float32)
+_paged.set_hooks(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.int32, torch.float32, torch.uint8, torch.bool)
 
 
 def _ids(seq_ids: Sequence[int]):
@@ -796,6 +796,9 @@ def _pool_kind(pool, kind):
 
 def heatkv_paged4_store(pool: PagedPool4, k_new, v_new, slot_map, stream=None) -> None:
     """K and V rows [n_tokens, n_kv_heads, d] (equal strides, d contiguous) to their slots, as 4-bit codes and scales."""
+    rc = _paged.store4(pool, k_new, v_new, slot_map, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged4_store")
     _pool_kind(pool, PagedPool4)
     n = slot_map.numel()
     slots = _vector(slot_map, n, "slot_map")
@@ -807,6 +810,9 @@ def heatkv_paged4_store(pool: PagedPool4, k_new, v_new, slot_map, stream=None) -
 
 def heatkv_paged4_load(pool: PagedPool4, slot_map, k_out, v_out, stream=None) -> None:
     """Rows of some slots back as 16-bit numbers, to k_out, v_out [n_tokens, n_kv_heads, d]; zeros where a slot is outside of the pool."""
+    rc = _paged.load4(pool, k_out, v_out, slot_map, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged4_load")
     _pool_kind(pool, PagedPool4)
     n = slot_map.numel()
     slots = _vector(slot_map, n, "slot_map")
@@ -827,6 +833,9 @@ def heatkv_paged4_workspace_bytes(pool: PagedPool4, batch: PagedBatch, n_heads: 
 def heatkv_paged4_attention(pool: PagedPool4, batch: PagedBatch, q, out, lse, workspace, causal: bool = True, sm_scale: float = 0.0,
                             stream=None) -> None:
     """heatkv_paged_attention over a cache in 4 bits."""
+    rc = _paged.attention4(pool, batch, q, out, lse, workspace, causal, sm_scale, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged4_attention")
     _pool_kind(pool, PagedPool4)
     st = _token_strides(pool, batch, q, out)
     rc = _lib.heatkv_paged4_attention(pool.addr4, batch.addr, q.size(1), q.data_ptr(), st, causal, sm_scale, out.data_ptr(), _lse(lse, q),
@@ -857,6 +866,9 @@ def heatkv_paged_fork(parents, keep_len, lengths, block_table, free_pages, state
                       stream=None) -> None:
     """Row i goes on as a copy of row parents[i] (-1: it is over), with its first keep_len[i] tokens at most (keep_len None: all).  move_from, move_to
     [64 * rows]: the moves for heatkv_paged_move."""
+    rc = _paged.fork(parents, keep_len, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_fork")
     old, new = _old_and_new(lengths, block_table, free_pages, state, lengths_out, table_out, state_out)
     n = lengths.numel()
     rc = _lib.heatkv_paged_fork(_vector(parents, n, "parents"), None if keep_len is None else _vector(keep_len, n, "keep_len"), *old, *new,
@@ -870,6 +882,9 @@ def heatkv_paged_compact(stays, lengths, block_table, free_pages, state, lengths
                          stream=None) -> None:
     """Tokens with stays[row, token] False (bool or uint8 [rows, width]) leave the cache, the others move together.  move_from, move_to (of one
     length, as many entries as may move): the moves for heatkv_paged_move."""
+    rc = _paged.compact(stays, lengths, block_table, free_pages, state, lengths_out, table_out, state_out, move_from, move_to, workspace, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_compact")
     old, new = _old_and_new(lengths, block_table, free_pages, state, lengths_out, table_out, state_out)
     n, n_moves = lengths.numel(), move_from.numel()
     if stays.dtype not in (torch.bool, torch.uint8) or stays.dim() != 2 or stays.size(0) != n or (stays.stride(1) != 1 and stays.size(1) > 1):
@@ -883,6 +898,9 @@ def heatkv_paged_compact(stays, lengths, block_table, free_pages, state, lengths
 
 def heatkv_paged_move(pool: PagedPool, move_from, move_to, stream=None) -> None:
     """K and V of all heads from slot move_from[i] to slot move_to[i] (either -1: nothing), and the summaries of pages whose last row is among those."""
+    rc = _paged.move(pool, move_from, move_to, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged_move")
     _pool_kind(pool, PagedPool)
     n = move_from.numel()
     rc = _lib.heatkv_paged_move(pool.addr, _vector(move_from, n, "move_from"), _vector(move_to, n, "move_to"), n,
@@ -892,6 +910,9 @@ def heatkv_paged_move(pool: PagedPool, move_from, move_to, stream=None) -> None:
 
 def heatkv_paged4_move(pool: PagedPool4, move_from, move_to, stream=None) -> None:
     """heatkv_paged_move in a cache in 4 bits."""
+    rc = _paged.move4(pool, move_from, move_to, stream)
+    if rc is not None:
+        return _check(rc, "heatkv_paged4_move")
     _pool_kind(pool, PagedPool4)
     n = move_from.numel()
     rc = _lib.heatkv_paged4_move(pool.addr4, _vector(move_from, n, "move_from"), _vector(move_to, n, "move_to"), n,

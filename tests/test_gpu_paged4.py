@@ -523,3 +523,102 @@ def test_move_in_4_bits(hk, d, Hkv):
     hk.heatkv_paged4_move(pool, _i32(source), _i32(target))
     for got, w in zip(P.unblock(blocks.cpu().numpy(), d), want):
         assert np.array_equal(got[0], w[0]) and np.array_equal(got[1], w[1])
+
+
+# ------------------------------------------------------------------------------------------------ all of it, as a server uses it
+
+@pytest.mark.parametrize("bits,dtype,d", [(4, "bf16", 128), (4, "fp16", 64), (16, "bf16", 64)])
+def test_cache_with_forks_and_compactions(hk, bits, dtype, d):
+    """A prompt answered three ways beside another request, rows cut back into pages that they share, tokens taken out, rows that end; two layers.
+    Every attention against the rows that a plain list has, every position, and in the end every page is free."""
+    from paper_2605_14877_b200.paged import PagedCache
+    layers, H, Hkv, rows, dt = 2, 6, 2, 4, DTYPES[dtype]
+    g, rng = torch.Generator("cuda").manual_seed(bits + d), np.random.default_rng(bits + d)
+    cache = PagedCache(layers, H, Hkv, d, n_pages=40, rows=rows, max_pages=12, dtype=dt, bits=bits)
+    held = [[[] for _ in range(rows)] for _ in range(layers)]      # (k, v) of every token, [heads, d] each
+    count = [0] * rows                                             # tokens that a row has had
+
+    def kept(x):
+        x = _np(x)
+        return P.values(*P.quantise(x)) if bits == 4 else x
+
+    def step(new):
+        s = cache.begin(new)
+        want = [count[i] + t for i, n in enumerate(new) for t in range(n)]
+        assert s.positions.tolist() == want
+        begin = np.concatenate([[0], np.cumsum(new)])
+        for layer in range(layers):
+            q, k, v = (torch.empty(sum(new), h, d, dtype=dt, device="cuda").normal_(generator=g) for h in (H, Hkv, Hkv))
+            out, lse = torch.full_like(q, 7.0), torch.full((sum(new), H), 7.0, device="cuda")
+            cache.attend(layer, s, q, k, v, out, lse)
+            k, v = kept(k), kept(v)
+            lens = []
+            for i, n in enumerate(new):
+                held[layer][i] += [(k[t], v[t]) for t in range(begin[i], begin[i + 1])]
+                lens.append((n, len(held[layer][i])))
+            # rows one behind another, as if in pages of their own
+            pages = [-(-n // PAGE) for _, n in lens]
+            table, at = np.full((rows, max(pages) + 1), -1), 0
+            kv = np.full((2, sum(pages) + 1, Hkv, PAGE, d), np.nan)
+            for i, p in enumerate(pages):
+                table[i, :p] = np.arange(at, at + p)
+                for t, pair in enumerate(held[layer][i]):
+                    kv[:, at + t // PAGE, :, t % PAGE] = pair
+                at += p
+            _check(out, lse, q, kv, lens, table, begin, Hkv, True, 1 / math.sqrt(d), dtype)
+        for i, n in enumerate(new):
+            count[i] += n
+
+    def fork(parents):
+        cache.fork(parents)
+        for layer in range(layers):
+            held[layer] = [[] if p is None else list(held[layer][p]) for p in parents]
+        count[:] = [0 if p is None else count[p] for p in parents]
+
+    def keep(lengths):
+        cache.keep(lengths)
+        for i, n in enumerate(lengths):
+            cut = len(held[0][i]) - n
+            if cut > 0:
+                count[i] = count[i] - cut if n else 0
+            for layer in range(layers):
+                del held[layer][i][n:]
+
+    step([200, 0, 0, 70])
+    fork([0, 0, 0, 3])
+    step([1, 2, 3, 1])
+    keep([1000, 150, 201, 64])                                     # row 1 into a page that it shares, row 2 to what was forked
+    step([5, 60, 1, 1])
+    stays = torch.from_numpy(rng.random((rows, 180)) < 0.6).cuda()
+    cache.compact(stays)
+    for layer in range(layers):
+        for i in range(rows):
+            held[layer][i] = [x for t, x in enumerate(held[layer][i]) if t >= 180 or stays[i, t]]
+    assert cache.lengths.tolist() == [len(x) for x in held[0]] and cache.state.tolist()[2] == 0
+    step([1, 1, 1, 1])
+    fork([1, None, 1, 2])                                          # row 0 is over, rows move
+    step([2, 0, 130, 1])
+    keep([1000, 0, 0, 30])
+    step([1, 40, 0, 1])
+    assert cache.lengths.tolist() == [len(x) for x in held[0]]
+    cache.check()
+    keep([0, 0, 0, 0])
+    assert cache.state.tolist()[1] == 40 and sorted(cache.free.tolist()) == list(range(40))
+
+
+def test_cache_that_runs_out_of_pages_for_forks(hk):
+    """Rows for which no page is left lose the tokens of the one that is not full, and say so; compaction then leaves a row as it is."""
+    from paper_2605_14877_b200.paged import PagedCache
+    cache = PagedCache(1, 2, 2, 64, n_pages=4, rows=3, max_pages=4, bits=4)
+    q = torch.zeros(130, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cache.attend(0, cache.begin([130, 0, 0]), q, q, q, torch.empty_like(q))
+    cache.fork([0, 0, 0])
+    assert cache.lengths.tolist() == [130, 130, 128] and cache.state.tolist()[1:3] == [0, 1]
+    stays = torch.ones(3, 130, dtype=torch.bool, device="cuda")
+    stays[:, 3] = False
+    cache.compact(stays)
+    assert cache.lengths.tolist() == [130, 130, 128] and cache.state.tolist()[2] == 3
+    cache.keep([0, 0, 128])
+    assert cache.lengths.tolist() == [0, 0, 128] and cache.state.tolist()[1] == 2
+    cache.compact(stays)
+    assert cache.lengths.tolist() == [0, 0, 127] and cache.state.tolist()[1:3] == [2, 0]

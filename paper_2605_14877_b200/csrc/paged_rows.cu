@@ -3,7 +3,9 @@
 //
 // Which pages are shared is nowhere kept: both calls mark the pages that the old table lists and those that the new one does, and what is only in
 // the first goes to the ring of free pages, in page order, so that the result does not depend on which CTA came first.  All of it is chains of a few
-// loads over tables of some thousand entries: what bounds it is the number of launches and of dependent loads.
+// loads over tables of some thousand entries: what bounds it is the number of launches and of dependent loads.  So pools of up to SMALL_PAGES
+// pages have their marks in one CTA's shared memory: a fork of few rows is one launch (32 rows of 1 to 40 pages 10.1 us in three launches with marks in
+// global memory), and a compaction two, one CTA of the second seeing to the marks while the others list the moves.
 #include <algorithm>
 
 #include "paged_rows.cuh"
@@ -13,7 +15,8 @@ namespace {
 
 constexpr int RT = 256;                        // threads of a CTA
 constexpr int DECIDE_THREADS = 1024;
-constexpr int PLACE_PAGES = 32;                // pages of a row whose moves a CTA lists
+constexpr int PLACE_THREADS = 512, PLACE_PAGES = 32;                // .. that lists the moves of so many pages of a row at a time
+constexpr int SMALL_PAGES = 16384, SMALL_ROWS = 1024, SMALL_ENTRIES = 32768;
 enum Mark : uint32_t { OLD = 1, WHOLE = 2, PART = 4 };   // listed by the old table; by the new one, all of the page or its first rows
 
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + PAGE - 1) / PAGE; }
@@ -32,30 +35,179 @@ __device__ __forceinline__ int ring_count(const RowsParams& p) { return min(max(
 template <int W>
 __device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t* sums, int64_t& all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t inc = v;
+  __shared__ int64_t total;
+  auto scan = [&](int64_t x) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += up;
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += up;
+    }
+    return x;
+  };
+  const int64_t inc = scan(v);
   __syncthreads();
   if (lane == 31) sums[warp] = inc;
   __syncthreads();
-  int64_t before = 0;
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const int64_t x = sums[w];
-    if (w < warp) before += x;
-    all += x;
+  if (warp == 0) {                               // (every thread adding up all warps' sums took longer than this and another barrier)
+    const int64_t x = lane < W ? sums[lane] : 0, s = scan(x);
+    if (lane < W) sums[lane] = s - x;
+    if (lane == 31) total = s;
   }
-  return before + inc - v;
+  __syncthreads();
+  all = total;
+  return sums[warp] + inc - v;
+}
+
+// Marks of up to SMALL_PAGES pages in shared memory, eight a word.
+// (rows of a family list the same pages: a look is cheaper than the next atomic on the same word)
+__device__ __forceinline__ void mark(uint32_t* flags, int page, uint32_t what) {
+  uint32_t* word = flags + (page >> 3);
+  what <<= (page & 7) * 4;
+  if ((*const_cast<volatile uint32_t*>(word) & what) != what) atomicOr(word, what);
+}
+__device__ __forceinline__ int flag_words(int n_pages) { return (n_pages + 7) / 8; }
+__device__ __forceinline__ bool goes_back(uint32_t mark) { return (mark & (OLD | WHOLE | PART)) == OLD; }
+// row.use(j, row.load(j)) for all rows, row = make(its number), and j below `pages`, by a CTA of T threads: a row by a warp, or by all of them where
+// rows are few.  Eight loads are on their way before the first is used.
+template <int T, typename Make>
+__device__ __forceinline__ void for_rows(int rows, int pages, Make make) {
+  constexpr int AHEAD = 8;
+  const bool few = rows < T / 64;
+  const int at = few ? threadIdx.x : threadIdx.x & 31, step = few ? T : 32;
+  for (int i = few ? 0 : threadIdx.x >> 5; i < rows; i += few ? 1 : T / 32) {
+    const auto row = make(i);
+    for (int base = at; base < pages; base += step * AHEAD) {
+      decltype(row.load(0)) x[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (base + u * step < pages) x[u] = row.load(base + u * step);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (base + u * step < pages) row.use(base + u * step, x[u]);
+    }
+  }
+}
+// Pages that go back to the ring's end, in page order, by a CTA of T threads; their number.
+template <int T>
+__device__ __forceinline__ int give_back_small(const RowsParams& p, const uint32_t* flags, int64_t* sums, int head, int free) {
+  int64_t before = 0, all;
+  const int words = flag_words(p.n_pages);
+  for (int base = 0; base < words; base += T) {
+    const int w = base + threadIdx.x;
+    const uint32_t x = w < words ? flags[w] : 0;
+    uint32_t back = 0;                           // (pages past the last have no marks)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) back |= (uint32_t)goes_back(x >> 4 * u) << u;
+    int64_t at = before + exclusive_sum<T / 32>(__popc(back), sums, all);
+    for (; back; back &= back - 1) p.free_pages[ring_place(p, head, free + at++)] = w * 8 + __ffs(back) - 1;
+    before += all;
+  }
+  return (int)before;
 }
 
 // ------------------------------------------------------------------------------------------------ fork
 // The row that a partly filled page stays with: one that goes on as itself before the others, then the lowest; larger is better, 0 is none.
 __device__ __forceinline__ uint32_t claim(int parent, int row) { return 2 * PAGED_MAX_SEQ - (parent == row ? row : PAGED_MAX_SEQ + row); }
 
+// What a row lists, and how much of it rows that go on from it have whole: its marks.
+struct ForkMarks {
+  const int32_t* table;
+  uint32_t* flags;
+  int n_pages, pages, whole;
+  __device__ __forceinline__ int load(int j) const { return j < pages ? table[j] : -1; }
+  __device__ __forceinline__ void use(int j, int page) const {
+    if ((uint32_t)page < (uint32_t)n_pages) mark(flags, page, j < whole ? OLD | WHOLE : OLD);
+  }
+};
+struct ForkCopy {
+  const int32_t* table;
+  int32_t* out;
+  int pages;
+  __device__ __forceinline__ int load(int j) const { return j < pages ? table[j] : -1; }
+  __device__ __forceinline__ void use(int j, int page) const { out[j] = page; }
+};
+// A fork of up to SMALL_ROWS rows and SMALL_ENTRIES entries of their table, by one CTA.
+__global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsParams p) {
+  extern __shared__ uint32_t sm[];
+  uint32_t* flags = sm;                                            // [flag_words]
+  uint32_t* claims = flags + flag_words(p.n_pages);                // [n_pages]
+  int32_t* had = reinterpret_cast<int32_t*>(claims + p.n_pages);   // [n_seq] tokens; then pages
+  int32_t* length = had + p.n_seq;                                 // [n_seq] of the row that goes on
+  int32_t* parent = length + p.n_seq;                              // [n_seq] -1: none
+  int32_t* wholes = parent + p.n_seq;                              // [n_seq] the most pages of the row that one which goes on from it has whole
+  int2* move = reinterpret_cast<int2*>(sm + (flag_words(p.n_pages) + p.n_pages + 4 * p.n_seq + 1) / 2 * 2);    // [n_seq] {page with the last tokens, page to copy it to}
+  __shared__ int64_t sums[DECIDE_THREADS / 32];
+  pdl_trigger();
+  for (int i = threadIdx.x; i < flag_words(p.n_pages) + p.n_pages; i += DECIDE_THREADS) sm[i] = 0;
+  pdl_wait();
+  const int head = ring_head(p), free = ring_count(p), i = threadIdx.x;
+  int of = -1, keep = INT32_MAX;
+  if (i < p.n_seq) {
+    had[i] = length_of(p, i);
+    of = p.parents[i];
+    if (p.keep_len) keep = max(p.keep_len[i], 0);
+    if (of >= p.n_seq || of < 0) of = -1;
+    parent[i] = of;
+    wholes[i] = 0;
+  }
+  __syncthreads();
+  int n = 0, last = -1;                                            // this thread's row: its tokens, and the page with the last ones if that is not full
+  if (i < p.n_seq && of >= 0) {
+    n = min(had[of], keep);
+    atomicMax(wholes + of, n / PAGE);
+    if (n % PAGE) last = p.table[of * p.table_stride + n / PAGE];
+    if (!valid(p, last)) last = -1;
+  }
+  if (i < p.n_seq) length[i] = n;
+  __syncthreads();
+  if (last >= 0) {
+    mark(flags, last, PART);
+    atomicMax(claims + last, claim(of, i));
+  }
+  for_rows<DECIDE_THREADS>(p.n_seq, p.table_pages, [&](int row) {
+    return ForkMarks{p.table + row * p.table_stride, flags, p.n_pages, pages_of(had[row]), wholes[row]};
+  });
+  for_rows<DECIDE_THREADS>(p.n_seq, p.table_pages, [&](int row) {
+    return ForkCopy{p.table + max(parent[row], 0) * p.table_stride, p.table_out + row * p.out_stride, pages_of(length[row])};
+  });
+  __syncthreads();
+  // who gets a page of its own for its last tokens
+  const bool wants = last >= 0 && ((flags[last >> 3] >> (last & 7) * 4 & WHOLE) || claims[last] != claim(of, i));
+  int64_t all;
+  const int64_t rank = exclusive_sum<DECIDE_THREADS / 32>(wants, sums, all);
+  if (i < p.n_seq) {
+    int fresh = -1;
+    if (wants) {
+      if (rank < free) fresh = ring_at(p, head, rank);
+      p.table_out[i * p.out_stride + n / PAGE] = fresh;
+      if (fresh < 0) length[i] = n = n / PAGE * PAGE;
+    }
+    move[i] = make_int2(last, fresh);
+    p.lengths_out[i] = n;
+  }
+  const int back = give_back_small<DECIDE_THREADS>(p, flags, sums, head, free), taken = (int)min(all, (int64_t)free);
+  __syncthreads();
+  for (int x = threadIdx.x; x < p.n_seq * PAGE; x += DECIDE_THREADS) {
+    const int row = x / PAGE, r = x % PAGE;
+    const int2 m = move[row];
+    const bool moves = m.y >= 0 && r < length[row] % PAGE;
+    p.move_from[x] = moves ? m.x * PAGE + r : -1;
+    p.move_to[x] = moves ? m.y * PAGE + r : -1;
+  }
+  if (threadIdx.x == 0) {
+    p.state_out[0] = ring_place(p, head, taken);
+    p.state_out[1] = free - taken + back;
+    p.state_out[2] = (int)(all - taken);
+    p.state_out[3] = back;
+  }
+}
+
+// The others, in launches of many CTAs with their marks in global memory.
+__global__ void __launch_bounds__(DECIDE_THREADS) zero_marks_kernel(const RowsParams p) {
+  pdl_trigger();
+  pdl_wait();
+  for (int64_t x = (int64_t)blockIdx.x * DECIDE_THREADS + threadIdx.x; x < p.n_pages; x += (int64_t)gridDim.x * DECIDE_THREADS) p.marks[x] = p.claims[x] = 0;
+}
 // CTA (x, i): row i's entries; marks of the old and the new lists.
 __global__ void __launch_bounds__(RT) fork_mark_kernel(const RowsParams p) {
   pdl_trigger();
@@ -134,9 +286,7 @@ __global__ void __launch_bounds__(DECIDE_THREADS) fork_decide_kernel(const RowsP
   }
 }
 
-// Pages that go back.
-__device__ __forceinline__ bool goes_back(uint32_t mark) { return (mark & (OLD | WHOLE | PART)) == OLD; }
-// .. of a chunk of the pool, where there is more than one: how many
+// Pages of a chunk of the pool, where there is more than one, that go back: how many.
 __global__ void __launch_bounds__(RT) chunk_kernel(const RowsParams p) {
   __shared__ int64_t sums[RT / 32];
   pdl_trigger();
@@ -147,8 +297,7 @@ __global__ void __launch_bounds__(RT) chunk_kernel(const RowsParams p) {
   exclusive_sum<RT / 32>(mine, sums, all);
   if (threadIdx.x == 0) p.chunk_sums[blockIdx.x] = (int)all;
 }
-// Pages that go back to the ring's end, chunk by chunk in page order, by CTAs of 1024 threads; marks made zero for the next call.  Gives the number of all of
-// them to CTA 0.
+// Pages that go back to the ring's end, chunk by chunk in page order, by CTAs of 1024 threads.  Gives the number of all of them to CTA 0.
 __device__ __forceinline__ int64_t give_back(const RowsParams& p, int64_t* sums) {
   int64_t before = 0, all, total = 0;
   const int c = blockIdx.x;
@@ -178,8 +327,7 @@ __device__ __forceinline__ int64_t give_back(const RowsParams& p, int64_t* sums)
     int64_t at = before + exclusive_sum<DECIDE_THREADS / 32>(n, sums, all);
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      if (back[u]) p.free_pages[(head + free + at++) % p.n_pages] = (int)(page0 + u);
-      if (page0 + u < end) p.marks[page0 + u] = p.claims[page0 + u] = 0;
+      if (back[u]) p.free_pages[ring_place(p, head, free + at++)] = (int)(page0 + u);
     }
     before += all;
   }
@@ -220,111 +368,162 @@ __device__ __forceinline__ uint64_t staying(const RowsParams& p, int i, int j, i
   return bits;
 }
 
-// A warp per page: how many of its tokens stay, and the old table's marks; per row, how many stay in all and the first page that something leaves
-// (pages before it are full, so that says how many move).
+// What the rows' tokens are counted in is there twice: a call counts in one and makes the other zero for the next.  Its number is what both kernels go
+// by: the first reads `was` and writes `is`, the second the other way round, so that no CTA reads a word that another is writing.
+__device__ __forceinline__ int2* row_stay(const RowsParams& p, int call) { return p.row_stay + (call & 1) * PAGED_MAX_SEQ; }
+
+// A warp per page: how many of its tokens stay; per row, how many stay in all and the first page that something leaves (pages before it are full,
+// so that says how many move).
 __global__ void __launch_bounds__(RT) compact_count_kernel(const RowsParams p) {
   pdl_trigger();
   pdl_wait();
-  const int i = blockIdx.y, length = length_of(p, i), pages = pages_of(length), lane = threadIdx.x & 31;
+  const int i = blockIdx.y, length = length_of(p, i), pages = pages_of(length), lane = threadIdx.x & 31, call = *p.was + 1;
+  int2* row = row_stay(p, call) + i;
   for (int j = blockIdx.x * (RT / 32) + (threadIdx.x >> 5); j < pages; j += gridDim.x * (RT / 32)) {
     const int stay = __popcll(staying(p, i, j, length, lane));
     if (lane == 0) {
       p.page_stay[(int64_t)i * p.table_pages + j] = stay;
-      const int page = p.table[i * p.table_stride + j];
-      if (valid(p, page)) atomicOr(p.marks + page, OLD);
-      atomicAdd(&p.row_stay[i].y, stay);
-      if (stay < min(PAGE, length - j * PAGE)) atomicMax(&p.row_stay[i].x, p.table_pages - j);
+      atomicAdd(&row->y, stay);
+      if (stay < min(PAGE, length - j * PAGE)) atomicMax(&row->x, p.table_pages - j);
     }
   }
+  if (blockIdx.x == 0 && i == 0 && threadIdx.x == 0) *p.is = call;
 }
 
-// The first page of row i that changes (-1: none) and the tokens that move.
-__device__ __forceinline__ int2 row_change(const RowsParams& p, int i) {
-  const int2 r = p.row_stay[i];
-  const int first = p.table_pages - r.x;
-  return r.x > 0 ? make_int2(first, r.y - first * PAGE) : make_int2(-1, 0);
-}
-
-// What the rows before row i take, and whether it is served: every CTA sums up for itself.
-struct RowPlan {
-  int first, moved;                            // first page that changes (-1: none, or refused), tokens that move
-  int64_t page_rank, move_rank;                // fresh pages and moves of the rows before
-};
-template <int T>
-__device__ __forceinline__ RowPlan plan_row(const RowsParams& p, int i, int64_t* sums, bool last, int64_t (&totals)[3]) {
-  // (rows before i; with `last`, all rows, and the totals: pages taken, rows refused, moves)
-  const int free = ring_count(p), n = last ? p.n_seq : i + 1, per = (n + T - 1) / T, x0 = min((int)threadIdx.x * per, n), x1 = min(x0 + per, n);
-  __shared__ RowPlan mine;
-  int64_t need = 0, moves = 0, all_need, all_moves;
+// The rows' plan, by a CTA of T threads that calls row(number, first page that changes (-1: none, or refused), tokens that move, fresh pages and moves of
+// the rows before) for rows 0 .. n - 1; what these take: {pages, rows refused, moves}.
+template <int T, typename Row>
+__device__ __forceinline__ void plan_rows(const RowsParams& p, int call, int n, int free, int64_t* sums, Row row, int64_t (&totals)[3]) {
+  const int2* stay = row_stay(p, call);
+  const int per = (n + T - 1) / T, x0 = min((int)threadIdx.x * per, n), x1 = min(x0 + per, n);
+  auto change = [&](int x) {
+    const int2 r = __ldcg(stay + x);
+    const int first = p.table_pages - r.x;
+    return r.x > 0 ? make_int2(first, r.y - first * PAGE) : make_int2(-1, 0);
+  };
+  int64_t need = 0, moves = 0, all;
   for (int x = x0; x < x1; ++x) {
-    const int2 r = row_change(p, x);
-    if (r.x >= 0) {
-      need += pages_of(r.y);
-      moves += r.y;
-    }
+    const int2 r = change(x);
+    need += pages_of(r.y);
+    moves += r.y;
   }
-  int64_t a = exclusive_sum<T / 32>(need, sums, all_need), b = exclusive_sum<T / 32>(moves, sums, all_moves);
+  int64_t a = exclusive_sum<T / 32>(need, sums, all), b = exclusive_sum<T / 32>(moves, sums, all);
   int64_t taken = 0, refused = 0, moved = 0;
   for (int x = x0; x < x1; ++x) {
-    const int2 r = row_change(p, x);
-    const int want = r.x >= 0 ? pages_of(r.y) : 0;
+    const int2 r = change(x);
+    const int want = pages_of(r.y);
     const bool served = r.x >= 0 && (want == 0 || (a + want <= free && b + r.y <= p.n_moves));
-    if (x == i) mine = {served ? r.x : -1, r.y, a, b};
+    row(x, served ? r.x : -1, r.y, a, b);
     if (want > 0) {
-      taken = served ? a + want : taken;
-      moved = served ? b + r.y : moved;
-      refused += !served;
+      if (served) {
+        taken = a + want;
+        moved = b + r.y;
+      } else {
+        ++refused;
+      }
       a += want;
       b += r.y;
     }
   }
+  // rows that are served are the first ones of those that want pages: the most that any thread saw
+  __shared__ unsigned long long most[2];
+  __shared__ unsigned int turned_down;
   __syncthreads();
-  if (last) {
-    __shared__ unsigned long long most[2];
-    if (threadIdx.x == 0) most[0] = most[1] = 0;
-    __syncthreads();
+  if (threadIdx.x == 0) most[0] = most[1] = turned_down = 0;
+  __syncthreads();
+  if (taken > 0) {
     atomicMax(&most[0], (unsigned long long)taken);
     atomicMax(&most[1], (unsigned long long)moved);
-    exclusive_sum<T / 32>(refused, sums, totals[1]);
-    __syncthreads();
-    totals[0] = (int64_t)most[0];
-    totals[2] = (int64_t)most[1];
   }
-  return mine;
+  if (refused > 0) atomicAdd(&turned_down, (unsigned)refused);
+  __syncthreads();
+  totals[0] = (int64_t)most[0];
+  totals[1] = turned_down;
+  totals[2] = (int64_t)most[1];
+}
+__device__ __forceinline__ void compact_state(const RowsParams& p, int head, int free, const int64_t (&totals)[3], int64_t back) {
+  p.state_out[0] = ring_place(p, head, totals[0]);
+  p.state_out[1] = (int)(free - totals[0] + back);
+  p.state_out[2] = (int)totals[1];
+  p.state_out[3] = (int)totals[2];
 }
 
-// CTA (x, i): row i's new entries, marks and moves.
-__global__ void __launch_bounds__(RT) compact_place_kernel(const RowsParams p) {
-  __shared__ int64_t sums[RT / 32];
+struct CompactRow {
+  const int32_t* table;
+  uint32_t* flags;
+  int n_pages, pages, first;
+  __device__ __forceinline__ int load(int j) const { return j < pages ? table[j] : -1; }
+  __device__ __forceinline__ void use(int j, int page) const {
+    if ((uint32_t)page < (uint32_t)n_pages) mark(flags, page, j < first ? OLD | WHOLE : OLD);
+  }
+};
+// CTA (x, i): row i's new entries and its moves.  SMALL: CTA (0, n_seq) sees to the pages that go back, else they are marked in global memory.
+template <bool SMALL>
+__global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const RowsParams p) {
+  extern __shared__ uint32_t flags[];                              // SMALL: [flag_words], then [n_seq] rows' first pages that change, and lengths
+  constexpr int T = PLACE_THREADS, W = T / 32;
+  __shared__ int64_t sums[W];
   pdl_trigger();
+  if (SMALL && (int)blockIdx.y == p.n_seq)
+    for (int x = threadIdx.x; x < flag_words(p.n_pages); x += T) flags[x] = 0;
   pdl_wait();
-  const int i = blockIdx.y, length = length_of(p, i), pages = pages_of(length), lane = threadIdx.x & 31, head = ring_head(p);
+  const int call = *p.is, head = ring_head(p), free = ring_count(p), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t totals[3];
-  const bool all_rows = blockIdx.x == 0 && i == 0;                 // this CTA says what all rows take, for the last kernel
-  const RowPlan r = plan_row<RT>(p, i, sums, all_rows, totals);
-  if (all_rows && threadIdx.x < 3) p.totals[threadIdx.x] = (int)totals[threadIdx.x];
-  const int32_t* stay = p.page_stay + (int64_t)i * p.table_pages;
-  const int first = r.first >= 0 ? r.first : pages, fresh = r.first >= 0 ? pages_of(r.moved) : 0;
-  for (int j = blockIdx.x * RT + threadIdx.x; j < p.table_pages; j += gridDim.x * RT) {
-    int page = -1;
-    if (j < first) {
-      page = p.table[i * p.table_stride + j];
-      if (valid(p, page)) atomicOr(p.marks + page, WHOLE);
-    } else if (j < first + fresh) {
-      page = ring_at(p, head, r.page_rank + (j - first));
+  if ((int)blockIdx.y == p.n_seq) {
+    if (blockIdx.x > 0) return;
+    int32_t* firsts = reinterpret_cast<int32_t*>(flags + (SMALL ? flag_words(p.n_pages) : 0));
+    plan_rows<T>(p, call, p.n_seq, free, sums, [&](int x, int first, int, int64_t, int64_t) { if (SMALL) firsts[x] = first; }, totals);
+    for (int x = threadIdx.x; x < PAGED_MAX_SEQ; x += T) row_stay(p, call + 1)[x] = make_int2(0, 0);
+    if (threadIdx.x == 0) *p.was = call;
+    if (SMALL) {
+      int32_t* lengths = firsts + p.n_seq;
+      for (int x = threadIdx.x; x < p.n_seq; x += T) lengths[x] = length_of(p, x);
+      __syncthreads();
+      for_rows<T>(p.n_seq, p.table_pages, [&](int x) {
+        return CompactRow{p.table + x * p.table_stride, flags, p.n_pages, pages_of(lengths[x]), firsts[x] >= 0 ? firsts[x] : INT32_MAX};
+      });
+      __syncthreads();
+      const int back = give_back_small<T>(p, flags, sums, head, free);
+      if (threadIdx.x == 0) compact_state(p, head, free, totals, back);
+    } else if (threadIdx.x < 3) {
+      p.totals[threadIdx.x] = (int)(threadIdx.x == 0 ? totals[0] : threadIdx.x == 1 ? totals[1] : totals[2]);
     }
+    return;
+  }
+  const int i = blockIdx.y, length = length_of(p, i), pages = pages_of(length);
+  __shared__ int first_page, moved;
+  __shared__ int64_t page_rank, move_rank;
+  const bool all_rows = blockIdx.x == 0 && i == 0;                 // (this CTA's moves past the last need the totals)
+  plan_rows<T>(p, call, all_rows ? p.n_seq : i + 1, free, sums, [&](int x, int first, int m, int64_t a, int64_t b) {
+    if (x != i) return;
+    first_page = first;
+    moved = m;
+    page_rank = a;
+    move_rank = b;
+  }, totals);
+  if (all_rows)
+    for (int64_t x = totals[2] + threadIdx.x; x < p.n_moves; x += T) p.move_from[x] = p.move_to[x] = -1;
+  const int32_t* stay = p.page_stay + (int64_t)i * p.table_pages;
+  const int first = first_page >= 0 ? first_page : pages, fresh = first_page >= 0 ? pages_of(moved) : 0;
+  for (int j = blockIdx.x * T + threadIdx.x; j < p.table_pages; j += gridDim.x * T) {
+    int page = -1;
+    if (j < max(first, SMALL ? 0 : pages)) {
+      page = p.table[i * p.table_stride + j];
+      if (!SMALL && valid(p, page)) atomicOr(p.marks + page, j < first ? OLD | WHOLE : OLD);
+    }
+    if (j >= first) page = j < first + fresh ? ring_at(p, head, page_rank + (j - first)) : -1;
     p.table_out[i * p.out_stride + j] = page;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.lengths_out[i] = r.first >= 0 ? first * PAGE + r.moved : length;
-  if (r.first < 0) return;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.lengths_out[i] = first_page >= 0 ? first * PAGE + moved : length;
+  if (first_page < 0) return;
   // a CTA's pages lie together: the tokens that move before them, and before each of them
   __shared__ int before_page[PLACE_PAGES];
   for (int c0 = first / PLACE_PAGES * PLACE_PAGES + blockIdx.x * PLACE_PAGES; c0 < pages; c0 += gridDim.x * PLACE_PAGES) {
     const int c1 = min(c0 + PLACE_PAGES, pages);
     int64_t mine = 0, upto;
 #pragma unroll 4
-    for (int j = first + threadIdx.x; j < c0; j += RT) mine += stay[j];
-    exclusive_sum<RT / 32>(mine, sums, upto);
+    for (int j = first + threadIdx.x; j < c0; j += T) mine += stay[j];
+    exclusive_sum<W>(mine, sums, upto);
     if (threadIdx.x < 32) {
       const int j = c0 + lane, n = j >= first && j < c1 ? stay[j] : 0;
       int inc = n;
@@ -336,7 +535,7 @@ __global__ void __launch_bounds__(RT) compact_place_kernel(const RowsParams p) {
       before_page[lane] = (int)upto + inc - n;
     }
     __syncthreads();
-    for (int j = max(first, c0) + (threadIdx.x >> 5); j < c1; j += RT / 32) {
+    for (int j = max(first, c0) + warp; j < c1; j += W) {
       const uint64_t bits = staying(p, i, j, length, lane);
       const int page = p.table[i * p.table_stride + j], before = before_page[j - c0];
 #pragma unroll
@@ -344,10 +543,10 @@ __global__ void __launch_bounds__(RT) compact_place_kernel(const RowsParams p) {
         const int at = u * 32 + lane;
         if (!(bits >> at & 1)) continue;
         const int rank = before + __popcll(bits & (((uint64_t)1 << at) - 1));
-        const int to = ring_at(p, head, r.page_rank + rank / PAGE);
+        const int to = ring_at(p, head, page_rank + rank / PAGE);
         const bool moves = valid(p, page) && valid(p, to);
-        p.move_from[r.move_rank + rank] = moves ? page * PAGE + at : -1;
-        p.move_to[r.move_rank + rank] = moves ? to * PAGE + rank % PAGE : -1;
+        p.move_from[move_rank + rank] = moves ? page * PAGE + at : -1;
+        p.move_to[move_rank + rank] = moves ? to * PAGE + rank % PAGE : -1;
       }
     }
     __syncthreads();
@@ -360,20 +559,7 @@ __global__ void __launch_bounds__(DECIDE_THREADS) compact_end_kernel(const RowsP
   pdl_wait();
   const int64_t back = give_back(p, sums);
   const int64_t totals[3] = {p.totals[0], p.totals[1], p.totals[2]};
-  for (int64_t x = totals[2] + (int64_t)blockIdx.x * DECIDE_THREADS + threadIdx.x; x < p.n_moves; x += (int64_t)gridDim.x * DECIDE_THREADS)
-    p.move_from[x] = p.move_to[x] = -1;
-  // zero again for the next call: what the rows' tokens were counted in
-  for (int i = blockIdx.x; i < p.n_seq; i += gridDim.x) {
-    const int pages = pages_of(length_of(p, i));
-    for (int j = threadIdx.x; j < pages; j += DECIDE_THREADS) p.page_stay[(int64_t)i * p.table_pages + j] = 0;
-    if (threadIdx.x == 0) p.row_stay[i] = make_int2(0, 0);
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    p.state_out[0] = (int)((ring_head(p) + totals[0]) % p.n_pages);
-    p.state_out[1] = (int)(ring_count(p) - totals[0] + back);
-    p.state_out[2] = (int)totals[1];
-    p.state_out[3] = (int)totals[2];
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) compact_state(p, ring_head(p), ring_count(p), totals, back);
 }
 
 // ------------------------------------------------------------------------------------------------ moves
@@ -460,31 +646,45 @@ __global__ void __launch_bounds__(MT) move4_kernel(const MoveParams p, int code_
 
 }  // namespace
 
-// First what any call has, of one size, so that calls of all sizes may share a workspace: what lies behind it is zero between calls.
+// (the words that must be zero before the first call come first, and are of one size, so that calls of all sizes may share a workspace)
 uint64_t rows_workspace_bytes(int n_seq, int table_pages, int n_pages) {
-  return ((uint64_t)4 * PAGED_MAX_SEQ + ROWS_CHUNKS + 64 + 2 * (uint64_t)n_pages + (uint64_t)n_seq * table_pages) * 4;
+  return ((uint64_t)6 * PAGED_MAX_SEQ + ROWS_CHUNKS + 64 + 2 * (uint64_t)n_pages + (uint64_t)n_seq * table_pages) * 4;
 }
 
 void place_rows_workspace(void* ws, RowsParams* p) {
   p->chunk = std::max(16384, (p->n_pages + ROWS_CHUNKS - 1) / ROWS_CHUNKS);
   p->chunks = (p->n_pages + p->chunk - 1) / p->chunk;
   p->row_stay = static_cast<int2*>(ws);
-  p->row_moves = p->row_stay + PAGED_MAX_SEQ;
+  p->row_moves = p->row_stay + 2 * PAGED_MAX_SEQ;
   p->chunk_sums = reinterpret_cast<int32_t*>(p->row_moves + PAGED_MAX_SEQ);
   p->totals = p->chunk_sums + ROWS_CHUNKS;
+  p->was = p->totals + 32;
+  p->is = p->totals + 33;
   p->marks = reinterpret_cast<uint32_t*>(p->totals + 64);
   p->claims = p->marks + p->n_pages;
   p->page_stay = reinterpret_cast<int32_t*>(p->claims + p->n_pages);
 }
 
 namespace {
+cudaError_t launch_zero_marks(const RowsParams& p, cudaStream_t stream) {
+  return launch_pdl(zero_marks_kernel, dim3(std::min(592, (p.n_pages + DECIDE_THREADS - 1) / DECIDE_THREADS)), dim3(DECIDE_THREADS), 0, stream, p);
+}
 cudaError_t launch_chunks(const RowsParams& p, cudaStream_t stream) {
   return p.chunks > 1 ? launch_pdl(chunk_kernel, dim3(p.chunks), dim3(RT), 0, stream, p) : cudaSuccess;
 }
 }  // namespace
 
 cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
-  cudaError_t rc = launch_pdl(fork_mark_kernel, dim3((unsigned)std::min(64, (p.table_pages + RT - 1) / RT), p.n_seq), dim3(RT), 0, stream, p);
+  cudaError_t rc;
+  if (p.n_pages <= SMALL_PAGES && p.n_seq <= SMALL_ROWS && (int64_t)p.n_seq * p.table_pages <= SMALL_ENTRIES) {
+    auto bytes = [](int n_pages, int n_seq) { return ((n_pages + 7) / 8 + n_pages + 6 * n_seq + 2) * 4; };
+    // (always the most that any call takes: the limit is the process's, and another thread may set it before this launch)
+    rc = cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, SMALL_ROWS));
+    return rc != cudaSuccess ? rc : launch_pdl(fork_small_kernel, dim3(1), dim3(DECIDE_THREADS), bytes(p.n_pages, p.n_seq), stream, p);
+  }
+  rc = launch_zero_marks(p, stream);
+  if (rc != cudaSuccess) return rc;
+  rc = launch_pdl(fork_mark_kernel, dim3((unsigned)std::min(64, (p.table_pages + RT - 1) / RT), p.n_seq), dim3(RT), 0, stream, p);
   if (rc != cudaSuccess) return rc;
   rc = launch_pdl(fork_decide_kernel, dim3(1), dim3(DECIDE_THREADS), 0, stream, p);
   if (rc == cudaSuccess) rc = launch_chunks(p, stream);
@@ -494,13 +694,16 @@ cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_paged_compact(const RowsParams& p, cudaStream_t stream) {
-  auto ctas = [&](int pages) { return dim3((unsigned)std::min(256, (p.table_pages + pages - 1) / pages), p.n_seq); };
-  cudaError_t rc = launch_pdl(compact_count_kernel, ctas(RT / 32), dim3(RT), 0, stream, p);
+  auto ctas = [&](int pages, int more) { return dim3((unsigned)std::min(256, (p.table_pages + pages - 1) / pages), p.n_seq + more); };
+  const bool small = p.n_pages <= SMALL_PAGES;
+  cudaError_t rc = small ? cudaSuccess : launch_zero_marks(p, stream);
+  if (rc == cudaSuccess) rc = launch_pdl(compact_count_kernel, ctas(RT / 32, 0), dim3(RT), 0, stream, p);
   if (rc != cudaSuccess) return rc;
-  rc = launch_pdl(compact_place_kernel, ctas(PLACE_PAGES), dim3(RT), 0, stream, p);
+  if (small) return launch_pdl(compact_place_kernel<true>, ctas(PLACE_PAGES, 1), dim3(PLACE_THREADS), ((p.n_pages + 7) / 8 + 2 * p.n_seq) * 4, stream, p);
+  rc = launch_pdl(compact_place_kernel<false>, ctas(PLACE_PAGES, 1), dim3(PLACE_THREADS), 0, stream, p);
   if (rc == cudaSuccess) rc = launch_chunks(p, stream);
   if (rc != cudaSuccess) return rc;
-  return launch_pdl(compact_end_kernel, dim3(std::max(p.chunks, std::min(p.n_seq, 148))), dim3(DECIDE_THREADS), 0, stream, p);
+  return launch_pdl(compact_end_kernel, dim3(p.chunks), dim3(DECIDE_THREADS), 0, stream, p);
 }
 
 cudaError_t launch_paged_move(const MoveParams& p, int bits, cudaStream_t stream) {

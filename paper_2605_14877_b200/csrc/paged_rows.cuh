@@ -17,10 +17,11 @@ struct RowsParams {
   int64_t table_stride, out_stride;
   int32_t *free_pages, *lengths_out, *table_out, *state_out, *move_from, *move_to;
   int32_t n_seq, table_pages, n_pages, n_moves;
-  // workspace; marks, claims, row_stay and page_stay are zero between calls
-  uint32_t *marks, *claims;                    // [n_pages]
+  // workspace; row_stay, `was` and `is` are zero before the first call
+  uint32_t *marks, *claims;                    // [n_pages] of large pools
   int2* row_moves;                             // [n_seq] fork: {page with the last tokens, length}, then {that page, fresh page}
-  int2* row_stay;                              // [n_seq] compact: {table_pages - first page that something leaves (0: none), tokens that stay}
+  int2* row_stay;                              // [2][4096] compact: {table_pages - first page that something leaves (0: none), tokens that stay}
+  int32_t *was, *is;                           // calls of compact so far, in turn
   int32_t *chunk_sums, *totals, *page_stay;    // page_stay [n_seq][table_pages]: tokens that stay
   int32_t chunk, chunks;
 };

@@ -39,6 +39,7 @@ struct Small4Params {
   Paged4Params q;
   float* ends;                                 // [CTAs][WARPS] rows of the unit that a warp's range begins inside of
   int32_t stages;
+  uint32_t inverse;                            // 2^32 / CTAs
 };
 
 // c += a x b for one 16 x 8 x 16 product of fp16
@@ -81,10 +82,16 @@ struct Requests {
 struct Runs {
   int64_t all, share;                          // a run's share in 2^-16
   int grid;
-  __device__ void deal(int64_t all_, int grid_) {
+  // (without a division of 64-bit numbers: a call with that much has as many runs as there are CTAs, whose reciprocal is `inverse` 2^-32)
+  __device__ void deal(int64_t all_, int ctas, uint32_t inverse) {
     all = all_;
-    grid = grid_;
-    share = (all << 16) / grid;
+    if (all < (1 << 15)) {
+      grid = max(min(ctas, ((int)all + SHARE - 1) / SHARE), 1);
+      share = ((uint32_t)all << 16) / (uint32_t)grid;
+    } else {
+      grid = ctas;
+      share = all * inverse >> 16;
+    }
   }
   __device__ int64_t raw(int c) const { return share * c >> 16; }
   // a border inside a unit of `pages` pages from `begin` on: not near its ends, not in a short one
@@ -158,6 +165,20 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_wait();
   if (threadIdx.x == 0) *abort_flag = *reinterpret_cast<volatile uint32_t*>(p.status) != 0;
+  // What the ranges will begin with comes to L2 while the lengths are on their way, each CTA's share of the lines, where all of it is a line a thread: the
+  // table, the query rows.
+  {
+    const int64_t line = (int64_t)blockIdx.x * THREADS + threadIdx.x, lines = (int64_t)gridDim.x * THREADS;
+    const int per_row = (p.table_pages + 31) / 32, row_lines = D / 64;
+    if ((int64_t)p.n_seq * per_row <= lines && line < (int64_t)p.n_seq * per_row) {
+      const int i = (int)line / per_row;
+      prefetch_l2(p.block_table + i * p.table_stride + ((int)line - i * per_row) * 32);
+    }
+    if ((int64_t)p.n_tokens * p.H * row_lines <= lines && line < (int64_t)p.n_tokens * p.H * row_lines) {
+      const int row = (int)line / row_lines, tok = row / p.H;
+      prefetch_l2(static_cast<const __half*>(p.q) + tok * p.q_tok + (row - tok * p.H) * p.q_head + ((int)line - row * row_lines) * 64);
+    }
+  }
   // ------------------------------------------------------------------ the run, and this warp's range of it
   Runs runs;
   {
@@ -211,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
       req.pre[p.n_seq] = at;
       req.units[p.n_seq] = at_units;
     }
-    runs.deal(all, (int)max(min((int64_t)gridDim.x, (all + SHARE - 1) / SHARE), (int64_t)1));
+    runs.deal(all, gridDim.x, sp.inverse);
     __syncthreads();
   }
   // rows of requests without keys
@@ -244,26 +265,23 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   const int n_run = (int)min(__shfl_sync(0xffffffffu, a_border, 1) - first_page, (int64_t)INT_MAX / 16);
   if (n_run <= 0) return;
   const int x0 = n_run * warp / WARPS, x1 = n_run * (warp + 1) / WARPS;
-  Unit<ROWS> unit;
-  int j0 = 0;                                                      // its page where the range begins
-  {
-    const int64_t y = first_page + min(x0, n_run - 1);
+  // the unit with page y of all, and the page's number in it
+  auto locate = [&](int64_t y, Unit<ROWS>& u) {
     int lo = 0, hi = p.n_seq - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (req.pages(mid) <= y) lo = mid; else hi = mid - 1;
     }
-    unit.seq = lo;
-    unit.tile = 0;
-    unit.set(req, p);
     const int64_t local = y - req.pages(lo);
-    const int u = divide(local, unit.pages);
-    j0 = (int)(local - (int64_t)u * unit.pages);
-    unit.head = (int)((uint32_t)u / (uint32_t)unit.tiles);
-    unit.tile = u - unit.head * unit.tiles;
-    unit.set(req, p);
-  }
-
+    const int pages = (req.keys[lo] + PAGE - 1) / PAGE, tiles = (req.count[lo] * p.G + ROWS - 1) / ROWS, number = divide(local, pages);
+    u.seq = lo;
+    u.head = (int)((uint32_t)number / (uint32_t)tiles);
+    u.tile = number - u.head * tiles;
+    u.set(req, p);
+    return (int)(local - (int64_t)number * pages);
+  };
+  Unit<ROWS> unit;
+  int j0 = locate(first_page + min(x0, n_run - 1), unit);          // its page where the range begins
   // ------------------------------------------------------------------ copies
   unsigned char* ring = smem + warp * stages * B::BYTES;
   Unit<ROWS> ahead = unit;                                         // the page to be sent for next: number ahead_j of this unit
@@ -587,6 +605,36 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
     // leaving early: every copy under way lands before the CTA exits
     for (int k = max(sent - stages, 0); k < sent; ++k) settle(full(k % stages), (k / stages) & 1);
   }
+  // Warp 0, while others are still at work: the units that the run's borders cut, by lane 0 the first, by lane 1 the last, and the CTAs that have
+  // parts of them.  (One unit that is both is lane 0's.)
+  int c0 = blockIdx.x, c1 = -1;
+  if (warp == 0) {
+    const int side = lane & 1;
+    Unit<ROWS> u;
+    const int j = locate(first_page + (side ? n_run - 1 : 0), u);
+    const bool cut = side ? j + 1 < u.pages : j > 0;
+    const int64_t begin = req.pre[u.seq] + ((int64_t)u.head * u.tiles + u.tile) * (u.pages + UNIT_END), end = begin + u.pages + UNIT_END;
+    // the last CTA whose run begins before `y`, a place of this unit (at its beginning: not behind it)
+    auto last_before = [&](int64_t y) {
+      auto before = [&](int c) {
+        const int64_t raw = runs.raw(c);
+        return raw < begin || (raw < end && Runs::snap(raw, begin, u.pages) < y);
+      };
+      int c = min(max((int)((float)y * 65536.f / (float)runs.share), 0), runs.grid - 1);
+      while (c + 1 < runs.grid && before(c + 1)) ++c;
+      while (c > 0 && !before(c)) --c;
+      return c;
+    };
+    const bool same = __shfl_sync(0xffffffffu, (int)(u.seq == __shfl_xor_sync(0xffffffffu, u.seq, 1) && u.head == __shfl_xor_sync(0xffffffffu, u.head, 1) &&
+                                                     u.tile == __shfl_xor_sync(0xffffffffu, u.tile, 1)), 0);
+    const bool began = __shfl_sync(0xffffffffu, (int)cut, 0), goes_on = __shfl_sync(0xffffffffu, (int)cut, 1);
+    if (side == 0 && began) {
+      c0 = last_before(begin + 1);
+      c1 = same && goes_on ? last_before(end) : (int)blockIdx.x;
+    }
+    if (side == 1 && goes_on && !(same && began)) c1 = last_before(end);
+    if (lane >= 2) c1 = -1;
+  }
   // ------------------------------------------------------------------ units that ranges' ends cut: added up by all warps, a row each
   __syncthreads();
   const int4 mine = lane < 2 * WARPS ? records[lane] : make_int4(-1, 0, 0, 0);
@@ -653,47 +701,26 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
   }
   // ------------------------------------------------------------------ units that the run's borders cut: added up by the CTA that leaves their last part
   const int first_lane = __ffs(met) - 1, last_lane = 31 - __clz(met);
-  const bool began = met && __shfl_sync(0xffffffffu, mine.w, first_lane) & 1, goes_on = met && __shfl_sync(0xffffffffu, mine.w, last_lane) & 2;
-  if (!began && !goes_on) return;
-  auto unit_of = [&](int of) {
-    unit.seq = __shfl_sync(0xffffffffu, mine.x, of);
-    unit.head = __shfl_sync(0xffffffffu, mine.y, of);
-    unit.tile = __shfl_sync(0xffffffffu, mine.z, of);
-    unit.set(req, p);
-  };
-  __threadfence();
+  const bool any_cut = met && ((__shfl_sync(0xffffffffu, mine.w, first_lane) & 1) || (__shfl_sync(0xffffffffu, mine.w, last_lane) & 2));
+  if (!any_cut) return;
   __syncthreads();
-  if (warp < 2 && (warp == 0 ? began : goes_on)) {                 // warp 0 sees to the first unit, warp 1 to the last; one that is both is the first
-    unit_of(warp == 0 ? first_lane : last_lane);
-    const int64_t begin = req.pre[unit.seq] + ((int64_t)unit.head * unit.tiles + unit.tile) * (unit.pages + UNIT_END), end = begin + unit.pages + UNIT_END;
-    // the last CTA whose run begins before `y`, a place of this unit (at its beginning: not behind it)
-    auto last_before = [&](int64_t y) {
-      auto before = [&](int c) {
-        const int64_t raw = runs.raw(c);
-        return raw < begin || (raw < end && Runs::snap(raw, begin, unit.pages) < y);
-      };
-      int c = min(max((int)((float)y * 65536.f / (float)runs.share), 0), runs.grid - 1);
-      while (c + 1 < runs.grid && before(c + 1)) ++c;
-      while (c > 0 && !before(c)) --c;
-      return c;
-    };
-    const bool both = warp == 0 && goes_on && __shfl_sync(0xffffffffu, (int)(mine.x == unit.seq && mine.y == unit.head && mine.z == unit.tile), last_lane);
-    const bool other = warp == 1 && began && __shfl_sync(0xffffffffu, (int)(mine.x == unit.seq && mine.y == unit.head && mine.z == unit.tile), first_lane);
-    const int c0 = warp == 0 ? last_before(begin + 1) : (int)blockIdx.x, c1 = warp == 1 || both ? last_before(end) : (int)blockIdx.x;
-    if (lane == 0 && !other) {
-      const uint32_t old = atomicAdd(p.counters + c0, 1u);
-      const bool last = old == (uint32_t)(c1 - c0);
-      if (last) *reinterpret_cast<volatile uint32_t*>(p.counters + c0) = 0;              // ready for the next launch
-      final_parts[warp] = last ? make_int2(c0, c1) : make_int2(0, -1);
-      __threadfence();
-    }
+  if (warp == 0 && c1 >= 0) {                                      // (lanes 0 and 1)
+    __threadfence();                                               // all warps' rows, behind the barrier
+    const bool last = atomicAdd(p.counters + c0, 1u) == (uint32_t)(c1 - c0);
+    if (last) *reinterpret_cast<volatile uint32_t*>(p.counters + c0) = 0;                // ready for the next launch
+    if (last) final_parts[lane] = make_int2(c0, c1);
+    __threadfence();
   }
   __syncthreads();
 #pragma unroll 1
   for (int u = 0; u < 2; ++u) {
     const int c0 = final_parts[u].x, c1 = final_parts[u].y;
     if (c1 < c0) continue;
-    unit_of(u == 0 ? first_lane : last_lane);
+    const int of = u == 0 ? first_lane : last_lane;
+    unit.seq = __shfl_sync(0xffffffffu, mine.x, of);
+    unit.head = __shfl_sync(0xffffffffu, mine.y, of);
+    unit.tile = __shfl_sync(0xffffffffu, mine.z, of);
+    unit.set(req, p);
     for (int row = warp; row < unit.rows; row += WARPS) {
       constexpr int N = D / 32, AHEAD = 8;
       auto part = [&](int c) { return p.partials + (2 * (int64_t)c + (c == c0)) * slot_floats(ROWS, D); };
@@ -754,6 +781,7 @@ cudaError_t launch(const Paged4Params& q, int n_sm, cudaStream_t stream) {
   Small4Params sp;
   sp.q = q;
   sp.ends = q.a.partials + slot_bytes(D, 8 * NT, 2 * n_sm) / 4;
+  sp.inverse = (uint32_t)((1ull << 32) / (unsigned)n_sm);
   // as many pages under way as shared memory holds (of a call of 3200 requests and more one a warp)
   sp.stages = std::max(1, std::min(MAX_STAGES, (room - fixed) / stage));
   auto kernel = paged4_small_kernel<D, NT, F16>;

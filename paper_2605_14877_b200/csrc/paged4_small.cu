@@ -11,10 +11,11 @@
 // The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that the cache is the operand with 16 rows and the queries the one with 8: a group of up to
 // eight heads costs half of what it would the other way round.  Which columns a step of a product takes is free as long as both operands take the
 // same, so a lane's part of K is what lies next to each other: 32 codes of one key (16 bytes) with their two scales, and of V 16 codes of one
-// key with their scale.  Codes become fp16 numbers in registers, exactly (Steps4): bf16 queries are scaled, row by row, to fp16's range by a power of
+// key with their scale.  Codes become fp16 numbers in registers, exactly (Steps4): queries are scaled, row by row, to fp16's range by a power of
 // two, and probabilities are fp16 for either type.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "paged4.cuh"
 #include "paged_wait.cuh"
@@ -24,20 +25,17 @@ namespace {
 
 using namespace tc;
 
-constexpr int WARPS = 8, THREADS = WARPS * 32;
+constexpr int MOST_WARPS = 12;
 constexpr int MAX_STAGES = 6;
 constexpr float MOVE = 8.f;                    // a reference moves when a maximum passes it by more than 2^MOVE (P fits fp16)
-#ifndef V_SHARE
-#define V_SHARE 4
-#endif
-constexpr int SHARE = V_SHARE;                      // pages of a run at least
+constexpr int SHARE = 4;                       // pages of a run at least
 constexpr int WHOLE = 8;                       // units of up to so many pages are never cut by a run's border
 constexpr int MIN_PART = 4;                    // pages of a part
 constexpr int UNIT_END = 1;                    // what a unit weighs beyond its pages: its rows in, its sums and rows out
 
 struct Small4Params {
   Paged4Params q;
-  float* ends;                                 // [CTAs][WARPS] rows of the unit that a warp's range begins inside of
+  float* ends;                                 // [CTAs][warps] rows of the unit that a warp's range begins inside of
   int32_t stages;
   uint32_t inverse;                            // 2^32 / CTAs
 };
@@ -135,13 +133,16 @@ struct Unit {
   }
 };
 
-template <int D, int NT, bool F16>
-__global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_constant__ Small4Params sp) {
+template <int D, int NT, bool F16, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __grid_constant__ Small4Params sp) {
   using B = Block4<D>;
-  constexpr int ROWS = 8 * NT;
+  constexpr int ROWS = 8 * NT, THREADS = WARPS * 32;
   constexpr int WORDS = D / 32;                                    // words of codes that a lane has of a key
   constexpr int MTILES = D / 16;                                   // 16-row tiles of O^T: two neighbouring columns of a lane each
   constexpr int KT = PAGE / 16;
+  // (with 16 rows the registers are better used otherwise: 32 requests, 16 heads a group, 24.7 us and 25.4)
+  constexpr bool UNEVEN = NT == 1;
+  using Steps = typename std::conditional<UNEVEN, Steps4Uneven, Steps4>::type;
   static_assert(ROWS * (D + 2) * 4 <= B::BYTES, "a warp's rows fit a stage");
   const Paged4Params& q4 = sp.q;
   const PagedParams& p = q4.a;
@@ -374,25 +375,30 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
         qf[nt][4 * i + 2] = q_rows[nt][i].z;
         qf[nt][4 * i + 3] = q_rows[nt][i].w;
       }
-      float down = 1.f;                                        // of row `row`: what it was divided by
-      if (!F16) {
+      // a row is divided by the power of two that makes its largest number 2^14 to 2^15, so that fp16 has room for it, and those that meet every second
+      // pair of a word of codes by 16
+      float down;                                                  // of row nt * 8 + gr: what it was divided by
+      {
+        float2 y[4 * WORDS];
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4 * WORDS; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qf[nt][i] << 16)), fabsf(__uint_as_float(qf[nt][i] & 0xffff0000u))));
+        for (int i = 0; i < 4 * WORDS; ++i) {
+          y[i] = F16 ? __half22float2(as_half2(qf[nt][i])) : make_float2(__uint_as_float(qf[nt][i] << 16), __uint_as_float(qf[nt][i] & 0xffff0000u));
+          top = fmaxf(top, fmaxf(fabsf(y[i].x), fabsf(y[i].y)));
+        }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^14 times the power of two in `top`; rows of infinities, of zeros or below 2^-86 are left as near as fp16 comes to them
+        // (rows of infinities, of zeros or below 2^-86 are left as near as fp16 comes to them)
         const int e = (int)(__float_as_uint(top) >> 23);
         const int power = top == 0.f || e == 255 ? 0 : min(14 + 127 - e, 100);
         const float up = __uint_as_float((uint32_t)(127 + power) << 23);
         down = __uint_as_float((uint32_t)(127 - power) << 23);
 #pragma unroll
-        for (int i = 0; i < 4 * WORDS; ++i)
-          qf[nt][i] = pack_half(__uint_as_float(qf[nt][i] << 16) * up, __uint_as_float(qf[nt][i] & 0xffff0000u) * up);
+        for (int i = 0; i < 4 * WORDS; ++i) qf[nt][i] = pack_half(y[i].x * (UNEVEN && (i & 1) ? up / 16.f : up), y[i].y * (UNEVEN && (i & 1) ? up / 16.f : up));
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        row_scale[nt][e] = F16 ? p.scale_log2 : p.scale_log2 * __shfl_sync(0xffffffffu, down, (2 * qd + e) * 4);
+        row_scale[nt][e] = p.scale_log2 * __shfl_sync(0xffffffffu, down, (2 * qd + e) * 4);
         const int mine = nt * 8 + 2 * qd + e;
         lim[nt][e] = p.causal && mine < unit.rows ? min(unit.pos0 + (unit.row0 + mine) / p.G + 1, unit.kv) : unit.kv;
         m_ref[nt][e] = NO_MAX;
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
       for (int g = 0; g < WORDS / 2; ++g) {                      // sixteen columns with one scale
 #pragma unroll
         for (int mt = 0; mt < KT; ++mt) {
-          const Steps4 a(__byte_perm(kb[mt][0], 0, g ? 0x4141 : 0x4040)), b(__byte_perm(kb[mt][1], 0, g ? 0x4141 : 0x4040));
+          const Steps a(__byte_perm(kb[mt][0], 0, g ? 0x4141 : 0x4040)), b(__byte_perm(kb[mt][1], 0, g ? 0x4141 : 0x4040));
 #pragma unroll
           for (int i = 2 * g; i < 2 * g + 2; ++i) {
             uint32_t ka[4], kc[4];
@@ -527,7 +533,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
           for (int u = 0; u < 4; ++u)
             if (mt * 16 + (u >> 1) * 8 + (u & 1 ? v1 : v0) >= there) bytes[u] = 0;
         }
-        const Steps4 a(bytes[0] | bytes[1] << 16), b(bytes[2] | bytes[3] << 16);
+        const Steps a(bytes[0] | bytes[1] << 16), b(bytes[2] | bytes[3] << 16);
 #pragma unroll
         for (int i = 0; i < WORDS / 2; ++i) {
           uint32_t a_even[4], a_odd[4], b_even[4], b_odd[4];
@@ -549,6 +555,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
       }
     }
     // ---------------------------------------------------------------- the rows of the unit, or of the part of it
+#pragma unroll
+    for (int j = 1; j < (UNEVEN ? MTILES : 0); j += 2)             // (every second pair was 16 times as large)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][nt][i] *= 1.f / 16.f;
     const bool begins = j0 == 0, ends = j0 + len == unit.pages;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -774,7 +786,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged4_small_kernel(const __grid_c
 
 uint64_t slot_bytes(int d, int rows, int slots) { return ((uint64_t)slots * slot_floats(rows, d) * 4 + 255) / 256 * 256; }
 
-template <int D, int NT, bool F16>
+template <int D, int NT, bool F16, int WARPS>
 cudaError_t launch(const Paged4Params& q, int n_sm, cudaStream_t stream) {
   constexpr int stage = WARPS * Block4<D>::BYTES, room = 226 * 1024 - 1024;
   const int fixed = Requests::bytes(q.a.n_seq);
@@ -784,25 +796,29 @@ cudaError_t launch(const Paged4Params& q, int n_sm, cudaStream_t stream) {
   sp.inverse = (uint32_t)((1ull << 32) / (unsigned)n_sm);
   // as many pages under way as shared memory holds (of a call of 3200 requests and more one a warp)
   sp.stages = std::max(1, std::min(MAX_STAGES, (room - fixed) / stage));
-  auto kernel = paged4_small_kernel<D, NT, F16>;
+  auto kernel = paged4_small_kernel<D, NT, F16, WARPS>;
   // (the kernel's limit is the process's: always the most that any call takes, as another thread may set it between this line and the launch)
   cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room);
   if (rc != cudaSuccess) return rc;
-  return launch_pdl(kernel, dim3(n_sm), dim3(THREADS), fixed + sp.stages * stage, stream, sp);
+  return launch_pdl(kernel, dim3(n_sm), dim3(WARPS * 32), fixed + sp.stages * stage, stream, sp);
 }
-template <int D>
+template <int D, bool F16>
 cudaError_t launch_typed(const Paged4Params& q, int rows, int n_sm, cudaStream_t stream) {
-  if (q.fp16) return rows <= 8 ? launch<D, 1, true>(q, n_sm, stream) : launch<D, 2, true>(q, n_sm, stream);
-  return rows <= 8 ? launch<D, 1, false>(q, n_sm, stream) : launch<D, 2, false>(q, n_sm, stream);
+  if (rows > 8) return launch<D, 2, F16, 8>(q, n_sm, stream);
+  // Twelve warps with two pages each under way where there is much to do, eight with three where the beginning and the end of a call weigh more (128-wide
+  // heads; 64 requests of 12 000 tokens, 8 kv heads, 166 us and 178, 256 of 50 to 1500 36.3 and 41.1, one of 131 000 41.3 and 42.3; 64 of 500 20.3 and 19.0).
+  const bool much = D == 128 && q.a.n_seq <= 340 && (int64_t)q.a.n_seq * q.a.Hkv * q.a.table_pages >= 16000;
+  return much ? launch<D, 1, F16, D == 128 ? 12 : 8>(q, n_sm, stream) : launch<D, 1, F16, 8>(q, n_sm, stream);
 }
 
 }  // namespace
 
-uint64_t paged4_small_partial_bytes(int d, int n_sm) { return slot_bytes(d, 16, 2 * n_sm) + slot_bytes(d, 16, WARPS * n_sm); }
+uint64_t paged4_small_partial_bytes(int d, int n_sm) { return slot_bytes(d, 16, 2 * n_sm) + slot_bytes(d, 16, MOST_WARPS * n_sm); }
 
 cudaError_t launch_paged4_small(const Paged4Params& p, int d, const PagedDevice& dev, cudaStream_t stream) {
   const int rows = (int64_t)std::max(1, p.a.max_new) * p.a.G <= 8 ? 8 : 16;
-  return d == 128 ? launch_typed<128>(p, rows, dev.n_sm, stream) : launch_typed<64>(p, rows, dev.n_sm, stream);
+  if (p.fp16) return d == 128 ? launch_typed<128, true>(p, rows, dev.n_sm, stream) : launch_typed<64, true>(p, rows, dev.n_sm, stream);
+  return d == 128 ? launch_typed<128, false>(p, rows, dev.n_sm, stream) : launch_typed<64, false>(p, rows, dev.n_sm, stream);
 }
 
 }  // namespace heatkv

@@ -201,6 +201,26 @@ def test_attention(hk, name, H, Hkv, d, dtype, causal):
     _attend(hk, pool, b, q, lens, table, q_begin, kv, Hkv, causal, dtype=dtype)
 
 
+@pytest.mark.parametrize("n,d", [(341, 128), (400, 64), (3300, 64), (4096, 128)])
+def test_attention_of_many_requests(hk, n, d):
+    """So many that their lengths take the place of pages under way."""
+    lens = [(1 + i % 2 * (i % 3 == 0), (i * 37) % 150) for i in range(n)]
+    rng, g = np.random.default_rng(n), torch.Generator("cuda").manual_seed(n)
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, 1, d, torch.bfloat16)
+    q = torch.empty(b.n_tokens, 2, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    _attend(hk, pool, b, q, lens, table, q_begin, kv, 1)
+
+
+@pytest.mark.parametrize("lens,Hkv", [([(1, 3000 + 500 * (i % 5)) for i in range(40)], 8), ([(1, 9000), (1, 64 * 100), (1, 7)], 2)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_of_much(hk, lens, Hkv, dtype):
+    """Units cut by many borders."""
+    rng, g = np.random.default_rng(Hkv), torch.Generator("cuda").manual_seed(Hkv)
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, Hkv, 128, DTYPES[dtype])
+    q = torch.empty(b.n_tokens, 3 * Hkv, 128, dtype=DTYPES[dtype], device="cuda").normal_(generator=g)
+    _attend(hk, pool, b, q, lens, table, q_begin, kv, Hkv, dtype=dtype)
+
+
 @pytest.mark.parametrize("G", [1, 3, 8, 9, 16, 17, 32, 33, 64, 128])
 def test_attention_any_group(hk, G):
     """Query heads per kv head, from one to 128."""

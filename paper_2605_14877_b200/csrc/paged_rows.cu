@@ -22,10 +22,12 @@ enum Mark : uint32_t { OLD = 1, WHOLE = 2, PART = 4 };   // listed by the old ta
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + PAGE - 1) / PAGE; }
 __device__ __forceinline__ int length_of(const RowsParams& p, int i) { return min(max(p.lengths[i], 0), p.table_pages * PAGE); }
 __device__ __forceinline__ bool valid(const RowsParams& p, int page) { return page >= 0 && page < p.n_pages; }
-// the ring's entry `i` places behind the oldest, i below twice the pages
+// the ring's entry `i` places behind the oldest, i up to twice the pages (a table that lists pages which a full ring has, too)
 __device__ __forceinline__ uint32_t ring_place(const RowsParams& p, int head, int64_t i) {
-  const uint32_t at = (uint32_t)head + (uint32_t)i;
-  return at < (uint32_t)p.n_pages ? at : at - (uint32_t)p.n_pages;
+  uint32_t at = (uint32_t)head + (uint32_t)i;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) at -= at < (uint32_t)p.n_pages ? 0u : (uint32_t)p.n_pages;
+  return at;
 }
 __device__ __forceinline__ int ring_at(const RowsParams& p, int head, int64_t i) { return p.free_pages[ring_place(p, head, i)]; }
 __device__ __forceinline__ int ring_head(const RowsParams& p) { return (p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages; }

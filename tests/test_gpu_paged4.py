@@ -334,6 +334,85 @@ def test_attention_captured_and_replayed(hk, name):
         _check(out, None, q, kv, shorter, table, q_begin, Hkv, True, 1 / math.sqrt(d), "bf16")
 
 
+@pytest.mark.parametrize("max_new", [1, 400])
+def test_attention_on_a_workspace_whose_status_is_set(hk, max_new):
+    """As after a wait that ran out: calls end at once whatever the workspace holds; zeroed, it serves again."""
+    lens, H, Hkv = [(1, 3000), (3, 700), (1, 64 * 40)], 8, 2
+    rng, g = np.random.default_rng(12), torch.Generator("cuda").manual_seed(12)
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, Hkv, 128, torch.bfloat16)
+    b.max_new = max_new
+    q = torch.empty(b.n_tokens, H, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    ws = _workspace(hk, pool, b, H)
+    words, head = ws.view(torch.int32), 64 + 8192          # status and counters; behind them what kernels hand to one another
+    for _ in range(3):
+        words[head:] = torch.randint(-2**31, 2**31 - 1, (len(words) - head,), generator=g, device="cuda").int()
+        words[0] = 1
+        hk.heatkv_paged4_attention(pool, b, q, torch.zeros_like(q), None, ws)
+        assert hk.heatkv_paged_status(ws) == -7
+    words.zero_()
+    out = torch.zeros_like(q)
+    hk.heatkv_paged4_attention(pool, b, q, out, None, ws)
+    assert hk.heatkv_paged_status(ws) == 0
+    _check(out, None, q, kv, lens, table, q_begin, Hkv, True, 1 / math.sqrt(128), "bf16")
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_pages_behind_two_gigabytes(hk, new):
+    """A pool whose last pages lie past 2^31 bytes: stored to, moved, attended to, read back."""
+    n_pages, kv, H, d = 250000, 300, 2, 128
+    blocks = torch.zeros(n_pages, 1, PAGE * (d + d // 8), dtype=torch.uint8, device="cuda")
+    pool = hk.PagedPool4.make(blocks, d, torch.bfloat16)
+    g = torch.Generator("cuda").manual_seed(new)
+    k, v, q = (torch.empty(n, h, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for n, h in ((kv, 1), (kv, 1), (new, H)))
+    first, last = np.arange(kv) + 5 * PAGE, np.arange(kv) + (n_pages - 5) * PAGE
+    hk.heatkv_paged4_store(pool, k, v, _i32(first))
+    hk.heatkv_paged4_move(pool, _i32(first), _i32(last))
+    back = torch.zeros_like(k), torch.zeros_like(v)
+    hk.heatkv_paged4_load(pool, _i32(last), *back)
+    want = [P.values(*P.quantise(_np(x))) for x in (k, v)]
+    for x, w in zip(back, want):
+        assert np.array_equal(_np(x), w)
+    table = np.arange(n_pages - 5, n_pages)[None]
+    b = hk.PagedBatch.make(_i32([0, new]), _i32([kv]), _i32(table), new, new)
+    full = np.full((2, 5, 1, PAGE, d), np.nan)
+    for x, w in zip(full, want):
+        for t in range(kv):
+            x[t // PAGE, :, t % PAGE] = w[t]
+    _attend(hk, pool, b, q, [(new, kv)], np.arange(5)[None], np.array([0, new]), full, 1)
+
+
+def test_calls_from_two_threads(hk):
+    """Each with a pool, a workspace and a stream of its own, calls of several kinds at once: the bits of one after another."""
+    import threading
+    lens = [[(1, 900), (1, 5000)], [(40, 300), (1, 700), (65, 65)]]
+    jobs = []
+    for n, l in enumerate(lens):
+        rng, g = np.random.default_rng(n), torch.Generator("cuda").manual_seed(n)
+        pool, b, _, q_begin, _ = _filled(hk, g, rng, l, 4, 128, torch.bfloat16)
+        q = torch.empty(b.n_tokens, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        ws, want = _workspace(hk, pool, b, 16), torch.zeros_like(q)
+        hk.heatkv_paged4_attention(pool, b, q, want, None, ws)
+        jobs.append((pool, b, q, ws, want))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(pool, b, q, ws, want):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(50):
+                out = torch.zeros_like(q)
+                hk.heatkv_paged4_attention(pool, b, q, out, None, ws)
+                if not torch.equal(out, want):
+                    wrong.append(b.n_tokens)
+
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 # ------------------------------------------------------------------------------------------------ rows between steps
 
 def _rows_state(hk, lengths, width, free, seed, shared=()):
@@ -482,6 +561,51 @@ def test_rows_share_a_workspace(hk):
             mask = torch.from_numpy(stays).cuda()
             got = _rearranged(hk, lambda *a: hk.heatkv_paged_compact(mask, *a), lengths, table, ring, head, free, sum(lengths) + 1, ws)
             _same(got, want, ring, head, free, done)
+
+
+@pytest.mark.parametrize("n_pages", [16384, 16385, 70000])
+def test_rows_of_large_pools(hk, n_pages):
+    """Pools at the end of what shared memory has marks for, behind it, and of several chunks; forks and compactions in turn on one workspace."""
+    ws = torch.zeros(hk.heatkv_paged_rows_workspace_bytes(9, 4000, n_pages), dtype=torch.uint8, device="cuda")
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        lengths = [int(x) for x in rng.integers(0, 64 * 3000, 5)] + [0, 1, 64, 0]
+        free = n_pages - 3 - sum(-(-x // PAGE) for x in lengths)
+        n_free = min(free, 9000)
+        table, fifo, ring, head, total = _rows_state(hk, lengths, 3200, free, seed)
+        assert total == n_pages
+        fifo = fifo[:n_free]
+        if seed % 2 == 0:
+            parents = [int(x) for x in rng.integers(-1, 9, 9)]
+            want = P.fork(parents, [10**7] * 9, lengths, table, fifo)
+            got = _rearranged(hk, lambda *a: hk.heatkv_paged_fork(_i32(parents), None, *a), lengths, table, ring, head, n_free, 9 * PAGE, ws)
+            _same(got, want, ring, head, n_free, len(want[6]))
+        else:
+            stays = rng.random((9, 64 * 3000)) < 0.7
+            *want, done = P.compact(stays, lengths, table, fifo, sum(lengths))
+            mask = torch.from_numpy(stays).cuda()
+            got = _rearranged(hk, lambda *a: hk.heatkv_paged_compact(mask, *a), lengths, table, ring, head, n_free, sum(lengths), ws)
+            _same(got, want, ring, head, n_free, done)
+
+
+@pytest.mark.parametrize("n_pages", [50, 20000])
+def test_rings_and_tables_that_contradict_each_other(hk, n_pages):
+    """A full ring whose pages the table lists all the same: nothing outside of the buffers is written, for whatever the result is worth."""
+    guard = 4096
+    free = torch.full((n_pages + 2 * guard,), -5, dtype=torch.int32, device="cuda")
+    ring = free[guard: guard + n_pages]
+    ring.copy_(torch.arange(n_pages))
+    table, lengths = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None], _i32([n_pages * PAGE])
+    ws = torch.zeros(hk.heatkv_paged_rows_workspace_bytes(1, n_pages, n_pages), dtype=torch.uint8, device="cuda")
+    moves = [torch.zeros(n_pages * PAGE, dtype=torch.int32, device="cuda") for _ in range(2)]
+    stays = torch.zeros(1, n_pages * PAGE, dtype=torch.bool, device="cuda")
+    for call, args in ((hk.heatkv_paged_fork, (_i32([-1]), None)), (hk.heatkv_paged_compact, (stays,))):
+        for state in ([n_pages - 1, n_pages], [-1, 2**31 - 1], [2**31 - 1, -7]):
+            out, state_out = torch.zeros_like(table), _i32([0] * 4)
+            call(*args, lengths, table, ring, _i32([*state, 0, 0]), _i32([0]), out, state_out, *(m[:PAGE] if args[-1] is None else m for m in moves), ws)
+            torch.cuda.synchronize()
+            assert (free[:guard] == -5).all() and (free[guard + n_pages:] == -5).all()
+            assert (ring >= 0).all() and (ring < n_pages).all() and (out == -1).all()
 
 
 # ------------------------------------------------------------------------------------------------ moves

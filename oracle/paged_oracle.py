@@ -83,7 +83,7 @@ def _e4m3():
 
 def quantise(x, exp=0):
     """Rows [.., d] -> (codes from -7 to 7, scale bytes [.., d / 16])."""
-    x = np.asarray(x, dtype=np.float64).reshape(*x.shape[:-1], -1, 16) * 2.0 ** -exp
+    x = np.asarray(x, dtype=np.float64).reshape(*x.shape[:-1], x.shape[-1] // 16, 16) * 2.0 ** -exp
     want = np.minimum(np.abs(x).max(-1).astype(np.float32) * np.float32(1 / 7), np.float32(448)).astype(np.float64)
     numbers = _e4m3()
     above = np.minimum(np.searchsorted(numbers, want), 126)
@@ -92,7 +92,7 @@ def quantise(x, exp=0):
     byte = np.where(up < down, above, np.where(up > down, below, np.where(above % 2 == 0, above, below)))
     scale = numbers[byte][..., None]
     code = np.where(scale > 0, np.clip(np.rint(x / np.where(scale > 0, scale, 1.0)), -7, 7), 0)
-    return code.reshape(*x.shape[:-2], -1).astype(np.int64), byte.astype(np.int64)
+    return code.reshape(*x.shape[:-2], 16 * x.shape[-2]).astype(np.int64), byte.astype(np.int64)
 
 
 def values(code, byte, exp=0):

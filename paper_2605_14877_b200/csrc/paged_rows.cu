@@ -33,11 +33,11 @@ __device__ __forceinline__ int ring_at(const RowsParams& p, int head, int64_t i)
 __device__ __forceinline__ int ring_head(const RowsParams& p) { return (p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages; }
 __device__ __forceinline__ int ring_count(const RowsParams& p) { return min(max(p.state_in[1], 0), p.n_pages); }
 
-// Exclusive sum over a CTA of W warps; `all` gets the sum.
-template <int W>
-__device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t* sums, int64_t& all) {
+// Exclusive sums over a CTA of W warps, of K numbers of each thread; `all` gets the sums.  `sums` has K * W entries.
+template <int W, int K>
+__device__ __forceinline__ void exclusive_sums(int64_t (&v)[K], int64_t* sums, int64_t (&all)[K]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  __shared__ int64_t total;
+  __shared__ int64_t total[K];
   auto scan = [&](int64_t x) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -46,18 +46,32 @@ __device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t* sums, int64
     }
     return x;
   };
-  const int64_t inc = scan(v);
+  int64_t inc[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) inc[k] = scan(v[k]);
   __syncthreads();
-  if (lane == 31) sums[warp] = inc;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (lane == 31) sums[k * W + warp] = inc[k];
   __syncthreads();
-  if (warp == 0) {                               // (every thread adding up all warps' sums took longer than this and another barrier)
-    const int64_t x = lane < W ? sums[lane] : 0, s = scan(x);
-    if (lane < W) sums[lane] = s - x;
-    if (lane == 31) total = s;
+  if (warp < K) {                                // (every thread adding up all warps' sums took longer than this and another barrier)
+    const int64_t x = lane < W ? sums[warp * W + lane] : 0, s = scan(x);
+    if (lane < W) sums[warp * W + lane] = s - x;
+    if (lane == 31) total[warp] = s;
   }
   __syncthreads();
-  all = total;
-  return sums[warp] + inc - v;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    all[k] = total[k];
+    v[k] = sums[k * W + warp] + inc[k] - v[k];
+  }
+}
+template <int W>
+__device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t* sums, int64_t& all) {
+  int64_t x[1] = {v}, total[1];
+  exclusive_sums<W>(x, sums, total);
+  all = total[0];
+  return x[0];
 }
 
 // Marks of up to SMALL_PAGES pages in shared memory, eight a word.
@@ -124,22 +138,35 @@ struct ForkMarks {
 struct ForkCopy {
   const int32_t* table;
   int32_t* out;
-  int pages;
+  int pages, last;                               // last: the entry of a page that is not full, which is not written here
   __device__ __forceinline__ int load(int j) const { return j < pages ? table[j] : -1; }
-  __device__ __forceinline__ void use(int j, int page) const { out[j] = page; }
+  __device__ __forceinline__ void use(int j, int page) const {
+    if (j != last) out[j] = page;
+  }
 };
-// A fork of up to SMALL_ROWS rows and SMALL_ENTRIES entries of their table, by one CTA.
+// A fork of up to SMALL_ROWS rows and SMALL_ENTRIES entries of their table: CTA 0 decides, the others copy full pages' entries, so many rows each.
+__host__ __device__ constexpr int copied_rows(int n_seq) { return n_seq < DECIDE_THREADS / 64 ? 1 : DECIDE_THREADS / 32; }
 __global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsParams p) {
   extern __shared__ uint32_t sm[];
   uint32_t* flags = sm;                                            // [flag_words]
   uint32_t* claims = flags + flag_words(p.n_pages);                // [n_pages]
   int32_t* had = reinterpret_cast<int32_t*>(claims + p.n_pages);   // [n_seq] tokens; then pages
   int32_t* length = had + p.n_seq;                                 // [n_seq] of the row that goes on
-  int32_t* parent = length + p.n_seq;                              // [n_seq] -1: none
-  int32_t* wholes = parent + p.n_seq;                              // [n_seq] the most pages of the row that one which goes on from it has whole
-  int2* move = reinterpret_cast<int2*>(sm + (flag_words(p.n_pages) + p.n_pages + 4 * p.n_seq + 1) / 2 * 2);    // [n_seq] {page with the last tokens, page to copy it to}
+  int32_t* wholes = length + p.n_seq;                              // [n_seq] the most pages of the row that one which goes on from it has whole
+  int2* move = reinterpret_cast<int2*>(sm + (flag_words(p.n_pages) + p.n_pages + 3 * p.n_seq + 1) / 2 * 2);    // [n_seq] {page with the last tokens, page to copy it to}
   __shared__ int64_t sums[DECIDE_THREADS / 32];
   pdl_trigger();
+  if (blockIdx.x > 0) {
+    pdl_wait();
+    const int rows = copied_rows(p.n_seq), first = (blockIdx.x - 1) * rows;
+    for_rows<DECIDE_THREADS>(min(rows, p.n_seq - first), p.table_pages, [&](int row) {
+      const int i = first + row, of = p.parents[i];
+      const bool on = of >= 0 && of < p.n_seq;
+      const int n = on ? min(length_of(p, of), p.keep_len ? max(p.keep_len[i], 0) : INT32_MAX) : 0;
+      return ForkCopy{p.table + (on ? of : 0) * p.table_stride, p.table_out + i * p.out_stride, pages_of(n), n % PAGE ? n / PAGE : -1};
+    });
+    return;
+  }
   for (int i = threadIdx.x; i < flag_words(p.n_pages) + p.n_pages; i += DECIDE_THREADS) sm[i] = 0;
   pdl_wait();
   const int head = ring_head(p), free = ring_count(p), i = threadIdx.x;
@@ -149,16 +176,15 @@ __global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsPa
     of = p.parents[i];
     if (p.keep_len) keep = max(p.keep_len[i], 0);
     if (of >= p.n_seq || of < 0) of = -1;
-    parent[i] = of;
     wholes[i] = 0;
   }
   __syncthreads();
-  int n = 0, last = -1;                                            // this thread's row: its tokens, and the page with the last ones if that is not full
+  int n = 0, last = -1, listed = -1;                               // this thread's row: its tokens, and the page with the last ones if that is not full
   if (i < p.n_seq && of >= 0) {
     n = min(had[of], keep);
     atomicMax(wholes + of, n / PAGE);
-    if (n % PAGE) last = p.table[of * p.table_stride + n / PAGE];
-    if (!valid(p, last)) last = -1;
+    if (n % PAGE) listed = p.table[of * p.table_stride + n / PAGE];
+    if (valid(p, listed)) last = listed;
   }
   if (i < p.n_seq) length[i] = n;
   __syncthreads();
@@ -169,9 +195,6 @@ __global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsPa
   for_rows<DECIDE_THREADS>(p.n_seq, p.table_pages, [&](int row) {
     return ForkMarks{p.table + row * p.table_stride, flags, p.n_pages, pages_of(had[row]), wholes[row]};
   });
-  for_rows<DECIDE_THREADS>(p.n_seq, p.table_pages, [&](int row) {
-    return ForkCopy{p.table + max(parent[row], 0) * p.table_stride, p.table_out + row * p.out_stride, pages_of(length[row])};
-  });
   __syncthreads();
   // who gets a page of its own for its last tokens
   const bool wants = last >= 0 && ((flags[last >> 3] >> (last & 7) * 4 & WHOLE) || claims[last] != claim(of, i));
@@ -179,11 +202,9 @@ __global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsPa
   const int64_t rank = exclusive_sum<DECIDE_THREADS / 32>(wants, sums, all);
   if (i < p.n_seq) {
     int fresh = -1;
-    if (wants) {
-      if (rank < free) fresh = ring_at(p, head, rank);
-      p.table_out[i * p.out_stride + n / PAGE] = fresh;
-      if (fresh < 0) length[i] = n = n / PAGE * PAGE;
-    }
+    if (wants && rank < free) fresh = ring_at(p, head, rank);
+    if (n % PAGE) p.table_out[i * p.out_stride + n / PAGE] = wants ? fresh : listed;
+    if (wants && fresh < 0) length[i] = n = n / PAGE * PAGE;
     move[i] = make_int2(last, fresh);
     p.lengths_out[i] = n;
   }
@@ -393,9 +414,9 @@ __global__ void __launch_bounds__(RT) compact_count_kernel(const RowsParams p) {
 }
 
 // The rows' plan, by a CTA of T threads that calls row(number, first page that changes (-1: none, or refused), tokens that move, fresh pages and moves of
-// the rows before) for rows 0 .. n - 1; what these take: {pages, rows refused, moves}.
+// the rows before) for rows 0 .. n - 1, and is together again behind it.  totals, if it is not null: what the rows take, {pages, rows refused, moves}.
 template <int T, typename Row>
-__device__ __forceinline__ void plan_rows(const RowsParams& p, int call, int n, int free, int64_t* sums, Row row, int64_t (&totals)[3]) {
+__device__ __forceinline__ void plan_rows(const RowsParams& p, int call, int n, int free, int64_t* sums, Row row, int64_t* totals) {
   const int2* stay = row_stay(p, call);
   const int per = (n + T - 1) / T, x0 = min((int)threadIdx.x * per, n), x1 = min(x0 + per, n);
   auto change = [&](int x) {
@@ -403,36 +424,36 @@ __device__ __forceinline__ void plan_rows(const RowsParams& p, int call, int n, 
     const int first = p.table_pages - r.x;
     return r.x > 0 ? make_int2(first, r.y - first * PAGE) : make_int2(-1, 0);
   };
-  int64_t need = 0, moves = 0, all;
+  int64_t before[2] = {0, 0}, all[2];            // pages and moves
   for (int x = x0; x < x1; ++x) {
     const int2 r = change(x);
-    need += pages_of(r.y);
-    moves += r.y;
+    before[0] += pages_of(r.y);
+    before[1] += r.y;
   }
-  int64_t a = exclusive_sum<T / 32>(need, sums, all), b = exclusive_sum<T / 32>(moves, sums, all);
+  exclusive_sums<T / 32>(before, sums, all);
+  __shared__ unsigned long long most[2];
+  __shared__ unsigned int turned_down;
+  if (threadIdx.x == 0) most[0] = most[1] = turned_down = 0;
   int64_t taken = 0, refused = 0, moved = 0;
   for (int x = x0; x < x1; ++x) {
     const int2 r = change(x);
     const int want = pages_of(r.y);
-    const bool served = r.x >= 0 && (want == 0 || (a + want <= free && b + r.y <= p.n_moves));
-    row(x, served ? r.x : -1, r.y, a, b);
+    const bool served = r.x >= 0 && (want == 0 || (before[0] + want <= free && before[1] + r.y <= p.n_moves));
+    row(x, served ? r.x : -1, r.y, before[0], before[1]);
     if (want > 0) {
+      before[0] += want;
+      before[1] += r.y;
       if (served) {
-        taken = a + want;
-        moved = b + r.y;
+        taken = before[0];
+        moved = before[1];
       } else {
         ++refused;
       }
-      a += want;
-      b += r.y;
     }
   }
+  __syncthreads();
+  if (!totals) return;
   // rows that are served are the first ones of those that want pages: the most that any thread saw
-  __shared__ unsigned long long most[2];
-  __shared__ unsigned int turned_down;
-  __syncthreads();
-  if (threadIdx.x == 0) most[0] = most[1] = turned_down = 0;
-  __syncthreads();
   if (taken > 0) {
     atomicMax(&most[0], (unsigned long long)taken);
     atomicMax(&most[1], (unsigned long long)moved);
@@ -460,11 +481,12 @@ struct CompactRow {
   }
 };
 // CTA (x, i): row i's new entries and its moves.  SMALL: CTA (0, n_seq) sees to the pages that go back, else they are marked in global memory.
+// What does not hang on the other rows is loaded before their sums.
 template <bool SMALL>
 __global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const RowsParams p) {
   extern __shared__ uint32_t flags[];                              // SMALL: [flag_words], then [n_seq] rows' first pages that change, and lengths
-  constexpr int T = PLACE_THREADS, W = T / 32;
-  __shared__ int64_t sums[W];
+  constexpr int T = PLACE_THREADS, W = T / 32, PER = PLACE_PAGES / W;
+  __shared__ int64_t sums[2 * W];
   pdl_trigger();
   if (SMALL && (int)blockIdx.y == p.n_seq)
     for (int x = threadIdx.x; x < flag_words(p.n_pages); x += T) flags[x] = 0;
@@ -474,13 +496,13 @@ __global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const Rows
   if ((int)blockIdx.y == p.n_seq) {
     if (blockIdx.x > 0) return;
     int32_t* firsts = reinterpret_cast<int32_t*>(flags + (SMALL ? flag_words(p.n_pages) : 0));
+    int32_t* lengths = firsts + p.n_seq;
+    if (SMALL)
+      for (int x = threadIdx.x; x < p.n_seq; x += T) lengths[x] = length_of(p, x);
     plan_rows<T>(p, call, p.n_seq, free, sums, [&](int x, int first, int, int64_t, int64_t) { if (SMALL) firsts[x] = first; }, totals);
     for (int x = threadIdx.x; x < PAGED_MAX_SEQ; x += T) row_stay(p, call + 1)[x] = make_int2(0, 0);
     if (threadIdx.x == 0) *p.was = call;
     if (SMALL) {
-      int32_t* lengths = firsts + p.n_seq;
-      for (int x = threadIdx.x; x < p.n_seq; x += T) lengths[x] = length_of(p, x);
-      __syncthreads();
       for_rows<T>(p.n_seq, p.table_pages, [&](int x) {
         return CompactRow{p.table + x * p.table_stride, flags, p.n_pages, pages_of(lengths[x]), firsts[x] >= 0 ? firsts[x] : INT32_MAX};
       });
@@ -493,6 +515,27 @@ __global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const Rows
     return;
   }
   const int i = blockIdx.y, length = length_of(p, i), pages = pages_of(length);
+  const int32_t* stay = p.page_stay + (int64_t)i * p.table_pages;
+  // PLACE_PAGES pages at a time: this thread's part of the tokens that stay in pages before them, lane's page's; its warp's pages' tokens and entries
+  int64_t mine;
+  int n, entry[PER];
+  uint64_t bits[PER];
+  auto fetch = [&](int c0) {
+    mine = n = 0;
+    if (c0 >= pages) return;
+#pragma unroll 4
+    for (int j = threadIdx.x; j < c0; j += T) mine += stay[j];
+    if (c0 + lane < pages) n = stay[c0 + lane];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int j = c0 + warp + u * W;
+      if (j >= pages) break;
+      entry[u] = p.table[i * p.table_stride + j];
+      bits[u] = staying(p, i, j, length, lane);
+    }
+  };
+  int c0 = blockIdx.x * PLACE_PAGES;
+  fetch(c0);
   __shared__ int first_page, moved;
   __shared__ int64_t page_rank, move_rank;
   const bool all_rows = blockIdx.x == 0 && i == 0;                 // (this CTA's moves past the last need the totals)
@@ -502,10 +545,9 @@ __global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const Rows
     moved = m;
     page_rank = a;
     move_rank = b;
-  }, totals);
+  }, all_rows ? totals : nullptr);
   if (all_rows)
     for (int64_t x = totals[2] + threadIdx.x; x < p.n_moves; x += T) p.move_from[x] = p.move_to[x] = -1;
-  const int32_t* stay = p.page_stay + (int64_t)i * p.table_pages;
   const int first = first_page >= 0 ? first_page : pages, fresh = first_page >= 0 ? pages_of(moved) : 0;
   for (int j = blockIdx.x * T + threadIdx.x; j < p.table_pages; j += gridDim.x * T) {
     int page = -1;
@@ -518,33 +560,32 @@ __global__ void __launch_bounds__(PLACE_THREADS) compact_place_kernel(const Rows
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) p.lengths_out[i] = first_page >= 0 ? first * PAGE + moved : length;
   if (first_page < 0) return;
-  // a CTA's pages lie together: the tokens that move before them, and before each of them
+  // the tokens that move before each of a CTA's pages; all of the pages before the first that changes are full
   __shared__ int before_page[PLACE_PAGES];
-  for (int c0 = first / PLACE_PAGES * PLACE_PAGES + blockIdx.x * PLACE_PAGES; c0 < pages; c0 += gridDim.x * PLACE_PAGES) {
-    const int c1 = min(c0 + PLACE_PAGES, pages);
-    int64_t mine = 0, upto;
-#pragma unroll 4
-    for (int j = first + threadIdx.x; j < c0; j += T) mine += stay[j];
+  for (; c0 < pages; c0 += gridDim.x * PLACE_PAGES, fetch(c0)) {
+    if (c0 + PLACE_PAGES <= first) continue;
+    int64_t upto;
     exclusive_sum<W>(mine, sums, upto);
     if (threadIdx.x < 32) {
-      const int j = c0 + lane, n = j >= first && j < c1 ? stay[j] : 0;
       int inc = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int up = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += up;
       }
-      before_page[lane] = (int)upto + inc - n;
+      before_page[lane] = (int)upto + inc - n - first * PAGE;
     }
     __syncthreads();
-    for (int j = max(first, c0) + warp; j < c1; j += W) {
-      const uint64_t bits = staying(p, i, j, length, lane);
-      const int page = p.table[i * p.table_stride + j], before = before_page[j - c0];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int at = u * 32 + lane;
-        if (!(bits >> at & 1)) continue;
-        const int rank = before + __popcll(bits & (((uint64_t)1 << at) - 1));
+    for (int u = 0; u < PER; ++u) {
+      const int j = c0 + warp + u * W;
+      if (j < first || j >= pages) continue;
+      const int page = entry[u], before = before_page[j - c0];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int at = half * 32 + lane;
+        if (!(bits[u] >> at & 1)) continue;
+        const int rank = before + __popcll(bits[u] & (((uint64_t)1 << at) - 1));
         const int to = ring_at(p, head, page_rank + rank / PAGE);
         const bool moves = valid(p, page) && valid(p, to);
         p.move_from[move_rank + rank] = moves ? page * PAGE + at : -1;
@@ -679,10 +720,10 @@ cudaError_t launch_chunks(const RowsParams& p, cudaStream_t stream) {
 cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
   cudaError_t rc;
   if (p.n_pages <= SMALL_PAGES && p.n_seq <= SMALL_ROWS && (int64_t)p.n_seq * p.table_pages <= SMALL_ENTRIES) {
-    auto bytes = [](int n_pages, int n_seq) { return ((n_pages + 7) / 8 + n_pages + 6 * n_seq + 2) * 4; };
+    auto bytes = [](int n_pages, int n_seq) { return ((n_pages + 7) / 8 + n_pages + 5 * n_seq + 2) * 4; };
     // (always the most that any call takes: the limit is the process's, and another thread may set it before this launch)
     rc = cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, SMALL_ROWS));
-    return rc != cudaSuccess ? rc : launch_pdl(fork_small_kernel, dim3(1), dim3(DECIDE_THREADS), bytes(p.n_pages, p.n_seq), stream, p);
+    return rc != cudaSuccess ? rc : launch_pdl(fork_small_kernel, dim3(1 + (p.n_seq + copied_rows(p.n_seq) - 1) / copied_rows(p.n_seq)), dim3(DECIDE_THREADS), bytes(p.n_pages, p.n_seq), stream, p);
   }
   rc = launch_zero_marks(p, stream);
   if (rc != cudaSuccess) return rc;

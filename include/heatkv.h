@@ -556,7 +556,8 @@ int heatkv_paged4_load(const heatkv_paged4_pool* pool /*HOST*/, const int32_t* s
                        int64_t tok_stride, int64_t head_stride, void* stream);
 
 /* heatkv_paged_workspace_bytes and heatkv_paged_attention for a cache in 4 bits: the same arguments and results; what the pool holds
- * past kv_len and in pages that no table lists may be any bytes.  heatkv_paged_status looks at this workspace, too. */
+ * past kv_len and in pages that no table lists may be any bytes.  sm_scale times 2^k_exp must lie between 1e-27 and 1e22.
+ * heatkv_paged_status looks at this workspace, too. */
 int heatkv_paged4_workspace_bytes(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, uint64_t* bytes);
 int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_batch* batch, int n_heads, const void* q,
                             const heatkv_token_strides* st, int causal, float sm_scale, void* out, float* lse, void* workspace,

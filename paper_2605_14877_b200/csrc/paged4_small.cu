@@ -398,7 +398,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        row_scale[nt][e] = p.scale_log2 * __shfl_sync(0xffffffffu, down, (2 * qd + e) * 4);
+        // (a normal number: 0 times a masked logit, or infinity times 0, would be none; logits below are 2^-90 then, or less)
+        row_scale[nt][e] = fminf(fmaxf(p.scale_log2 * __shfl_sync(0xffffffffu, down, (2 * qd + e) * 4), 0x1p-126f), 0x1p127f);
         const int mine = nt * 8 + 2 * qd + e;
         lim[nt][e] = p.causal && mine < unit.rows ? min(unit.pos0 + (unit.row0 + mine) / p.G + 1, unit.kv) : unit.kv;
         m_ref[nt][e] = NO_MAX;

@@ -334,12 +334,13 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
   Paged4Params p;
   int rc = attention_params(pool, batch, n_heads, q, st, sm_scale, out, lse, &p.a);
   if (rc != HEATKV_OK) return rc;
+  p.a.scale_log2 *= ldexpf(VALUES4_UNIT, pool->k_exp);
+  if (!(p.a.scale_log2 >= 1e-25f && p.a.scale_log2 <= 1e25f)) return HEATKV_ERR_INVALID_ARG;       // (0 times a masked logit, infinity times 0)
   PagedDevice dev;
   if (!paged_device(&dev)) return done(cudaErrorInitializationError);
   rc = place_workspace(workspace4_bytes(dev, pool->d, p.a.G, p.a.Hkv, p.a.n_tokens, p.a.n_seq), workspace, bytes, &p.a);
   if (rc != HEATKV_OK) return rc;
   p.a.causal = causal != 0;
-  p.a.scale_log2 *= ldexpf(VALUES4_UNIT, pool->k_exp);
   p.v_unit = ldexpf(VALUES4_UNIT, pool->v_exp);
   p.blocks = static_cast<const unsigned char*>(pool->blocks);
   p.page_stride = pool->page_stride;

@@ -356,6 +356,17 @@ def test_attention_on_a_workspace_whose_status_is_set(hk, max_new):
     _check(out, None, q, kv, lens, table, q_begin, Hkv, True, 1 / math.sqrt(128), "bf16")
 
 
+@pytest.mark.parametrize("new", [1, 5, 70])
+@pytest.mark.parametrize("k_exp,of_q", [(-64, 2.0**-110), (-64, 2.0**68), (64, 2.0**-64)])
+def test_attention_at_the_ends_of_the_exponents(hk, k_exp, of_q, new):
+    """Keys and values of 2^-64 and 2^64, query rows that make their logits nothing, or large, or ordinary."""
+    lens, H, Hkv = [(new, 300), (new, 64), (1, 1)], 8, 2
+    rng, g = np.random.default_rng(new), torch.Generator("cuda").manual_seed(new)
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, Hkv, 128, torch.bfloat16, (k_exp, k_exp), size=2.0**k_exp)
+    q = torch.empty(b.n_tokens, H, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g).mul_(of_q)
+    _attend(hk, pool, b, q, lens, table, q_begin, kv, Hkv)
+
+
 @pytest.mark.parametrize("new", [1, 70])
 def test_pages_behind_two_gigabytes(hk, new):
     """A pool whose last pages lie past 2^31 bytes: stored to, moved, attended to, read back."""

@@ -66,6 +66,11 @@ def test_arguments_of_rows():
     assert move(a=None) == move(b=None) == move(n=0) == INVALID
 
 
+def test_scales_of_logits_that_32_bits_do_not_hold():
+    for k_exp, scale in ((-64, 1e-20), (64, 1e10), (0, 1e-30), (0, 1e25)):
+        assert _attention(_pool(k_exp=k_exp), scale=scale) == INVALID
+
+
 def test_arguments_of_fork_and_compact():
     size = C.c_uint64()
     assert H._lib.heatkv_paged_rows_workspace_bytes(3, 5, 10, C.byref(size)) == 0 and size.value % 4 == 0

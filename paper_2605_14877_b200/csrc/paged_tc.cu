@@ -1003,26 +1003,27 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
       const int n_tiles = ring_word(ring, W_NT);
       for (int j = 0; j < n_tiles && ok; ++j, ++g) {
         const uint32_t st = g % KV_STAGES, use = g / KV_STAGES;
-        if (use > 0) ok = wait_all(bar(K_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + K_EMPTY) &&
-                          wait_all(bar(V_EMPTY + st), (use - 1) & 1, abort_flag, p.status, 1 + V_EMPTY);
+        // K of both pages first: the next logits need it while V's place is still taken
 #pragma unroll 1
-        for (int h = 0; h < 2 && ok; ++h, ++raw) {
-          const uint32_t rs = raw % L::RAW_STAGES;
-          const unsigned char* block = sgen + L::SM_OUT + rs * B::BYTES;
-          ok = wait_all(bar(RAW_FULL + rs), (raw / L::RAW_STAGES) & 1, abort_flag, p.status, 1 + RAW_FULL);
+        for (int v = 0; v < 2 && ok; ++v) {
+          const uint32_t empty = v ? V_EMPTY : K_EMPTY;
+          if (use > 0) ok = wait_all(bar(empty + st), (use - 1) & 1, abort_flag, p.status, 1 + empty);
+#pragma unroll 1
+          for (int h = 0; h < 2 && ok; ++h) {
+            const uint32_t rs = (raw + h) % L::RAW_STAGES;
+            const unsigned char* block = sgen + L::SM_OUT + rs * B::BYTES;
+            if (v == 0) ok = wait_all(bar(RAW_FULL + rs), ((raw + h) / L::RAW_STAGES) & 1, abort_flag, p.status, 1 + RAW_FULL);
+            if (!ok) break;
+            convert(block + (v ? B::V : B::K), block + (v ? B::VS : B::KS), sgen + (v ? SM_V : SM_K) + st * TILE_BYTES + h * SLOT_BYTES);
+            __syncwarp();
+            if (v == 1 && lane == 0) mbar_arrive(bar(RAW_EMPTY + rs));
+          }
           if (!ok) break;
-          convert(block + B::K, block + B::KS, sgen + SM_K + st * TILE_BYTES + h * SLOT_BYTES);
-          convert(block + B::V, block + B::VS, sgen + SM_V + st * TILE_BYTES + h * SLOT_BYTES);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(RAW_EMPTY + rs));
+          if (lane == 0) mbar_arrive(bar((v ? V_FULL : K_FULL) + st));
         }
-        if (!ok) break;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar(K_FULL + st));
-          mbar_arrive(bar(V_FULL + st));
-        }
+        raw += 2;
       }
       __syncwarp();
       if (ok && lane == 0) mbar_arrive(bar(ITEM_EMPTY + slot));

@@ -38,7 +38,7 @@ using namespace tc;
 
 constexpr int BM = 128, BN = 128;
 constexpr int THREADS = 384;
-constexpr int KV_STAGES = 2;
+constexpr int MOST_KV_STAGES = 4;
 // Register hand-over between warpgroups, inside what the launch allocates (checked against the compiled kernel before it runs).
 constexpr int REGS_LAUNCH = 168, REGS_SMALL = 72, REGS_SOFTMAX = 216;
 static_assert(128 * REGS_SMALL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register hand-over exceeds the CTA's allocation");
@@ -53,10 +53,19 @@ constexpr uint32_t STAGE_BYTES = 2048;                 // per softmax warp: 32 r
 constexpr int LIST_ENTRIES = 2048, LIST_WORDS = 2048;
 constexpr uint32_t LIST_BYTES = LIST_ENTRIES * 2 + LIST_WORDS * 4;
 
+enum Bar : uint32_t {
+  Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 8, V_FULL = 12, V_EMPTY = 16, S_FULL = 20, P_FULL = 22, PV_DONE = 26, ITEM_FULL = 28, ITEM_EMPTY = 30,
+  DRAIN = 32, N_BARS,
+  RAW_FULL = 52, RAW_EMPTY = 58                        // CODES: where SPARSE has its tiles' pages
+};
+constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 288, BAR_INFO = BAR_RING + 128, BAR_BYTES = BAR_INFO + 160;
+static_assert(K_EMPTY - K_FULL == MOST_KV_STAGES && BAR_ABORT + 4 <= BAR_RING, "barriers of up to four key tiles");
+static_assert(RAW_FULL * 8 == BAR_INFO && RAW_EMPTY - RAW_FULL >= 6 && (RAW_EMPTY + 6) * 8 <= BAR_BYTES, "barriers of up to six blocks");
 template <int D, bool CODES = false>
 struct Layout {
   static constexpr int NCH = D / 64;
   static constexpr uint32_t TILE_BYTES = NCH * HALF_COLS_BYTES;
+  static constexpr int KV_STAGES = CODES && D == 64 ? 4 : 2;            // key tiles
   static constexpr uint32_t SM_Q = 0;
   static constexpr uint32_t SM_K = SM_Q + 2 * TILE_BYTES;
   static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;
@@ -64,19 +73,12 @@ struct Layout {
   // CODES: blocks of the cache instead of rows on their way out
   static constexpr uint32_t RAW_STAGES = D == 128 ? 3 : 6;
   static constexpr uint32_t SM_BAR = SM_OUT + (CODES ? RAW_STAGES * block4_bytes(D) : 8 * STAGE_BYTES);
-  static constexpr uint32_t SM_LIST = SM_BAR + 512;
-  static constexpr uint32_t SM_ALLOC = SM_BAR + 512 + 1024;             // (and the lists where pages are selected)
+  static constexpr uint32_t SM_LIST = SM_BAR + BAR_BYTES;
+  static constexpr uint32_t SM_ALLOC = SM_BAR + BAR_BYTES + 1024;             // (and the lists where pages are selected)
   static_assert(SM_ALLOC + (CODES ? 0 : LIST_BYTES + LIST_ENTRIES * 2) <= 227 * 1024, "shared memory of one CTA");
   // one part of a cut item: O of both tiles (groups of four columns outermost), then references and sums
   static constexpr int SLOT_FLOATS = 2 * BM * D + 2 * 2 * BM;
 };
-enum Bar : uint32_t {
-  Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = 6, V_FULL = 8, V_EMPTY = 10, S_FULL = 12, P_FULL = 14, PV_DONE = 18, ITEM_FULL = 20, ITEM_EMPTY = 22,
-  DRAIN = 24, N_BARS,
-  RAW_FULL = 48, RAW_EMPTY = 54                        // CODES: where SPARSE has its tiles' pages
-};
-constexpr uint32_t BAR_TMEM_PTR = N_BARS * 8, BAR_ABORT = BAR_TMEM_PTR + 4, BAR_RING = 256, BAR_INFO = 384;
-static_assert(RAW_FULL * 8 == BAR_INFO && RAW_EMPTY - RAW_FULL >= 6 && (RAW_EMPTY + 6) * 8 <= 512, "barriers of up to six blocks");
 constexpr int INFO_RING = 4;                           // key tiles whose pages and bits are kept: the copy warp is at most two ahead of the softmax
 enum InfoWord : int { I_PLACE = 0, I_BITS = 2, INFO_WORDS = 8 };   // two places; bits of tile A for both, of tile B for both
 enum ItemWord : int { W_KIND = 0, W_SEQ, W_HEAD, W_TOK0, W_TOKENS, W_POS0, W_KV, W_J0, W_NT, W_TILES, W_C0, W_C1, W_SEEK };
@@ -544,7 +546,7 @@ template <int D, bool F16, bool SPARSE, bool CODES>
 __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ TcMaps maps) {
   using L = Layout<D, CODES>;
   using B = Block4<D>;
-  constexpr int NCH = L::NCH;
+  constexpr int NCH = L::NCH, KV_STAGES = L::KV_STAGES;
   constexpr uint32_t TILE_BYTES = L::TILE_BYTES, SM_Q = L::SM_Q, SM_K = L::SM_K, SM_V = L::SM_V, SM_OUT = L::SM_OUT, SM_BAR = L::SM_BAR;
   // How far (log2) a maximum may rise above the reference of its row's exponentials: bf16 and the 32-bit sums have room for 2^32,
   // fp16 probabilities for 2^15.

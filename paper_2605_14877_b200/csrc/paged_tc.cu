@@ -70,9 +70,11 @@ struct Layout {
   static constexpr uint32_t SM_K = SM_Q + 2 * TILE_BYTES;
   static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;
   static constexpr uint32_t SM_OUT = SM_V + KV_STAGES * TILE_BYTES;
-  // CODES: blocks of the cache instead of rows on their way out
+  // CODES: blocks of the cache; of 128-wide heads instead of rows on their way out
+  static constexpr bool STAGED = !(CODES && D == 128);
   static constexpr uint32_t RAW_STAGES = D == 128 ? 3 : 6;
-  static constexpr uint32_t SM_BAR = SM_OUT + (CODES ? RAW_STAGES * block4_bytes(D) : 8 * STAGE_BYTES);
+  static constexpr uint32_t SM_RAW = SM_OUT + (STAGED ? 8 * STAGE_BYTES : 0);
+  static constexpr uint32_t SM_BAR = SM_RAW + (CODES ? RAW_STAGES * block4_bytes(D) : 0);
   static constexpr uint32_t SM_LIST = SM_BAR + BAR_BYTES;
   static constexpr uint32_t SM_ALLOC = SM_BAR + BAR_BYTES + 1024;             // (and the lists where pages are selected)
   static_assert(SM_ALLOC + (CODES ? 0 : LIST_BYTES + LIST_ENTRIES * 2) <= 227 * 1024, "shared memory of one CTA");
@@ -661,7 +663,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
               const uint32_t rs = raw % L::RAW_STAGES, round = raw / L::RAW_STAGES;
               if (round > 0) ok = wait_all(bar(RAW_EMPTY + rs), (round - 1) & 1, abort_flag, p.status, 1 + RAW_EMPTY);
               if (!ok) break;
-              unsigned char* dst = sgen + L::SM_OUT + rs * B::BYTES;
+              unsigned char* dst = sgen + L::SM_RAW + rs * B::BYTES;
               const int pg = h ? pg1 : pg0;
               if (pg >= 0) {
                 if (leader) {
@@ -1013,7 +1015,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
 #pragma unroll 1
           for (int h = 0; h < 2 && ok; ++h) {
             const uint32_t rs = (raw + h) % L::RAW_STAGES;
-            const unsigned char* block = sgen + L::SM_OUT + rs * B::BYTES;
+            const unsigned char* block = sgen + L::SM_RAW + rs * B::BYTES;
             if (v == 0) ok = wait_all(bar(RAW_FULL + rs), ((raw + h) / L::RAW_STAGES) & 1, abort_flag, p.status, 1 + RAW_FULL);
             if (!ok) break;
             convert(block + (v ? B::V : B::K), block + (v ? B::VS : B::KS), sgen + (v ? SM_V : SM_K) + st * TILE_BYTES + h * SLOT_BYTES);
@@ -1170,7 +1172,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
           const int64_t o_at = (int64_t)tok * p.o_tok + (int64_t)hd * p.o_head;
           // 32 columns of the warp's rows, through shared memory so that four lanes write 64 bytes of a row
           auto store_rows = [&](const float (&acc)[32], float inv, int c) {
-            if constexpr (CODES) {                                           // (the blocks have the place: a lane writes 64 bytes of its row)
+            if constexpr (!L::STAGED) {                                         // (the blocks have the place: a lane writes 64 bytes of its row)
 #pragma unroll
               for (int i = 0; i < 32; i += 8)
                 if (valid)

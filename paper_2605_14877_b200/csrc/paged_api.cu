@@ -346,12 +346,12 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
   p.page_stride = pool->page_stride;
   p.head_stride = pool->head_stride;
   p.fp16 = pool->dtype == HEATKV_DTYPE_FP16;
-  // Up to two tiles of 16 rows: the warp-level kernel (8 kv heads of 4 heads; 32 requests of 10 000 tokens, 16 rows 117 us and 254 on the tensor-memory
-  // kernel, 32 rows 219 and 254, 48 rows 318 and 255).  More where there is little to do in all, a tile of `table_pages` pages weighing eight more: one
-  // request of 10 000, 96 rows (7920) 37 and 63, of 300 11.9 and 16.8; 8 requests of 2500, 64 rows (12 288) 44.8 and 39.6; 32 of 300, 64 rows (14 336) 37.4
-  // and 33.9.  Three tiles up to four times as much, as a batch's requests are mostly shorter than its table is wide: 24 of 40 to 8000 tokens, 42 rows
-  // (38 900) 20.8 and 35.9; 8 of 10 000, 48 rows (31 700) 91 and 83.
-  const int64_t tiles = ((int64_t)p.a.max_new * p.a.G + 15) / 16, units = (int64_t)p.a.n_seq * p.a.Hkv, little = tiles == 3 ? 40000 : 10000;
+  // Up to two tiles of 16 rows: the warp-level kernel (8 kv heads of 4 heads; 32 requests of 10 000 tokens, 16 rows 114 us and 242 on the tensor-memory
+  // kernel, 32 rows 213 and 242, 48 rows 310 and 242).  More where there is little to do in all, a tile of `table_pages` pages weighing eight more: one
+  // request of 10 000, 96 rows (7920) 37 and 62, of 300 11.9 and 16.1; two of 10 000, 64 rows (10 560) 42 and 55; 8 of 2500, 64 rows (12 288) 45 and 38; 32 of
+  // 300, 64 rows (14 336) 38 and 32.  Three tiles up to four times as much, as a batch's requests are mostly shorter than its table is wide: 24 of 40 to 8000
+  // tokens, 42 rows (38 900) 21 and 37; 8 that are all of 10 000, 48 rows (31 700) 90 and 80.
+  const int64_t tiles = ((int64_t)p.a.max_new * p.a.G + 15) / 16, units = (int64_t)p.a.n_seq * p.a.Hkv, little = tiles == 3 ? 40000 : 12000;
   const bool few = tiles <= 2 || (units <= little && tiles <= little && units * tiles * ((int64_t)p.a.table_pages + 8) <= little);
   return done((few ? launch_paged4_small : launch_paged4_tc)(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
 }

@@ -572,7 +572,8 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
  * heatkv_paged_release must not be used while rows share pages (it would give them back for all): heatkv_paged_fork does its work, too.
  *   lengths DEVICE [n_seq] tokens of every row; block_table, table_out DEVICE [n_seq][table_pages], rows table_stride and out_stride apart
  *   free_pages DEVICE [n_pages] in and out, state, state_out DEVICE int32[4] as in heatkv_paged_tables
- *   workspace DEVICE, heatkv_paged_rows_workspace_bytes, 16-byte aligned, zero before its first use; for calls that do not overlap */
+ *   workspace DEVICE, heatkv_paged_rows_workspace_bytes, 16-byte aligned, zero before its first use; forks and compactions of any sizes that it is
+ *   large enough for may take turns on it, none may overlap */
 int heatkv_paged_rows_workspace_bytes(int n_seq, int table_pages, int n_pages, uint64_t* bytes);
 
 /* Row i goes on as a copy of row parents[i] (its own number: as it is; none of 0 .. n_seq - 1: it is over) with its first keep_len[i] tokens at most

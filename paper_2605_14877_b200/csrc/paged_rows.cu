@@ -4,8 +4,10 @@
 // Which pages are shared is nowhere kept: both calls mark the pages that the old table lists and those that the new one does, and what is only in
 // the first goes to the ring of free pages, in page order, so that the result does not depend on which CTA came first.  All of it is chains of a few
 // loads over tables of some thousand entries: what bounds it is the number of launches and of dependent loads.  So pools of up to SMALL_PAGES
-// pages have their marks in one CTA's shared memory: a fork of few rows is one launch (32 rows of 1 to 40 pages 10.1 us in three launches with marks in
-// global memory), and a compaction two, one CTA of the second seeing to the marks while the others list the moves.
+// pages have their marks in one CTA's shared memory: a fork of few rows is one launch, where that CTA decides while others copy the entries that no
+// decision changes (32 rows of 1 to 40 pages 4.9 us, in three launches with marks in global memory 10.1; 97 rows of 141 pages 7.4, by one CTA alone 10.3),
+// and a compaction two, one CTA of the second seeing to the marks while the others list the moves (100 000 tokens of one row 9.0 us, 40 rows of 50 to 9000
+// 8.4; the first with marks in global memory 16.8).
 #include <algorithm>
 
 #include "paged_rows.cuh"
@@ -608,8 +610,10 @@ __global__ void __launch_bounds__(DECIDE_THREADS) compact_end_kernel(const RowsP
 // ------------------------------------------------------------------------------------------------ moves
 constexpr int MT = 256, MOVE_UNROLL = 4;
 
-// Words of K and V of all heads of an entry, MOVE_UNROLL of them per thread, whose loads are all on their way at once.  What bounds it is reading
-// and writing.
+// Words of K and V of all heads of an entry, MOVE_UNROLL of them per thread, whose loads are all on their way at once (two or eight, or hints that the
+// words are used once, are no better).  What bounds it is reading and writing: 30 000 tokens of 8 heads of 128 in 16 bits, 247 MB, take 41 us (6.0 TB/s).
+// In 4 bits a row is 64 bytes of codes and 8 of scales: of rows that lie apart DRAM brings their neighbours, too (33 000 tokens, two in five of their pages':
+// 76 MB read for 38, 21.5 us).
 // A cache of 16 bits: 16 bytes of K and of V.
 struct Words16 {
   using Word = int4;

@@ -18,8 +18,10 @@
 // token per lane and tile) and hands the tokens' bits to the softmax warps beside each tile.
 // (A tile has at most 32 tokens there, one a bit of a word, so that groups of one or two heads fill a quarter or half of its 128 rows.)
 // Over a cache in 4 bits (CODES) warp 0 sends for whole blocks (codes and scales of K and V of a page and head), which four more warps, 12-15, turn into
-// the tiles of 16-bit numbers that TMA brings otherwise, exactly (paged4.cuh); rows go out without a detour through shared memory, whose place the
-// blocks take.
+// the tiles of 16-bit numbers that TMA brings otherwise, exactly (paged4.cuh): K of a key tile first, as the next logits wait for it while V's place is
+// still taken (K and V together: 408 us instead of 340 for the first shape below).  Of 128-wide heads rows go out without a detour through shared
+// memory, whose place the blocks take.  A quarter of the bytes, no fewer products: 340 us on the first shape, 1190 TFLOP/s, as over 16 bits; 64-wide
+// heads 300 us (675), one in ten slower than over 16 bits, as the codes' instructions stand in the way of the softmax's.
 // What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 to 470 us,
 // 1160 to 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax warps'
 // waits for tensor memory (half the products per exponential: 32 heads of the first shape 666 us, 815 TFLOP/s; no unit is busy more than 57 %).
@@ -65,7 +67,8 @@ template <int D, bool CODES = false>
 struct Layout {
   static constexpr int NCH = D / 64;
   static constexpr uint32_t TILE_BYTES = NCH * HALF_COLS_BYTES;
-  static constexpr int KV_STAGES = CODES && D == 64 ? 4 : 2;            // key tiles
+  // key tiles; where there is room the warps that turn codes into numbers may be four ahead (three chunks, 40 heads of 64: 152 us with two, 150)
+  static constexpr int KV_STAGES = CODES && D == 64 ? 4 : 2;
   static constexpr uint32_t SM_Q = 0;
   static constexpr uint32_t SM_K = SM_Q + 2 * TILE_BYTES;
   static constexpr uint32_t SM_V = SM_K + KV_STAGES * TILE_BYTES;

@@ -148,12 +148,13 @@ class PagedCache:
 
     def compact(self, stays: torch.Tensor) -> None:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their
-        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left.  Tokens move into free
-        pages: rows for which those do not suffice stay as they are (`state[2]` counts them)."""
+        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left (so `keep` is to cut such a
+        row behind its last token that left).  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]` counts
+        them)."""
         if stays.dtype is not torch.bool or stays.dim() != 2 or stays.shape[0] != self.rows:
             raise ValueError(f"stays: expected bool [{self.rows}, tokens], got {stays.dtype} {tuple(stays.shape)}")
         before = self.lengths
-        self._rearrange(hk.heatkv_paged_compact, (stays,), max(sum(self.at_most), 1))
+        self._rearrange(hk.heatkv_paged_compact, (stays,), min(max(sum(self.at_most), 1), self.free.numel() * hk.PAGE_TOKENS))
         gone = before - self.lengths
         self.gone = gone if self.gone is None else self.gone + gone
         self._forget()

@@ -424,6 +424,37 @@ def test_calls_from_two_threads(hk):
     assert not wrong
 
 
+def test_graphs_that_share_a_workspace(hk):
+    """Captured calls of both kernels over 4 bits and of both over 16, on one workspace, replayed in any order: the bits of calls by themselves."""
+    calls, size = [], 0
+    for n, l in enumerate(([(1, 900), (1, 9000), (2, 70)], [(300, 1000), (1, 700), (65, 65)])):
+        rng, g = np.random.default_rng(n), torch.Generator("cuda").manual_seed(n)
+        pool, b, table, _, _ = _filled(hk, g, rng, l, 2, 128, torch.bfloat16)
+        pages = [torch.empty(pool.n_pages, 2, PAGE, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in "kv"]
+        pool16 = hk.PagedPool.make(*pages)
+        q = torch.empty(b.n_tokens, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        for p, bytes_of, attend in ((pool, hk.heatkv_paged4_workspace_bytes, hk.heatkv_paged4_attention),
+                                    (pool16, hk.heatkv_paged_workspace_bytes, hk.heatkv_paged_attention)):
+            need = bytes_of(p, b, 16)
+            want, out = torch.zeros_like(q), torch.zeros_like(q)
+            attend(p, b, q, want, None, torch.zeros(need, dtype=torch.uint8, device="cuda"))
+            calls.append((attend, p, b, q, out, want, pages))
+            size = max(size, need)
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for attend, p, b, q, out, _, _ in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            attend(p, b, q, out, None, ws)
+        graphs.append(graph)
+    for i in (0, 1, 2, 3, 3, 1, 0, 2, 0, 0, 3, 2, 1):
+        out, want = calls[i][4:6]
+        out.zero_()
+        graphs[i].replay()
+        assert torch.equal(out, want), i
+    assert hk.heatkv_paged_status(ws) == 0
+
+
 # ------------------------------------------------------------------------------------------------ rows between steps
 
 def _rows_state(hk, lengths, width, free, seed, shared=()):
@@ -617,6 +648,56 @@ def test_rings_and_tables_that_contradict_each_other(hk, n_pages):
             torch.cuda.synchronize()
             assert (free[:guard] == -5).all() and (free[guard + n_pages:] == -5).all()
             assert (ring >= 0).all() and (ring < n_pages).all() and (out == -1).all()
+
+
+@pytest.mark.parametrize("n_pages", [400, 20000])
+def test_rows_captured_and_replayed(hk, n_pages):
+    """A fork, its moves, a compaction and its moves as one graph, replayed over states of different lengths: what the calls give one by one."""
+    n, width, moved = 9, 20, 9 * 20 * PAGE
+    g = torch.Generator("cuda").manual_seed(n_pages)
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device="cuda")      # noqa: E731
+    blocks = _garbage(g, 400, 2, 64)
+    pool, ws = hk.PagedPool4.make(blocks, 64, torch.bfloat16), torch.zeros(hk.heatkv_paged_rows_workspace_bytes(n, width, n_pages), dtype=torch.uint8, device="cuda")
+    parents, stays, lengths, table, ring, state = i32(n), torch.zeros(n, 1000, dtype=torch.bool, device="cuda"), i32(n), i32(n, width), i32(n_pages), i32(4)
+    made = [(i32(n), i32(n, width), i32(4), i32(m), i32(m)) for m in (n * PAGE, moved)]
+
+    def step(ws):
+        (l1, t1, s1, *m1), (l2, t2, s2, *m2) = made
+        hk.heatkv_paged_fork(parents, None, lengths, table, ring, state, l1, t1, s1, *m1, ws)
+        hk.heatkv_paged4_move(pool, *m1)
+        hk.heatkv_paged_compact(stays, l1, t1, ring, s1, l2, t2, s2, *m2, ws)
+        hk.heatkv_paged4_move(pool, *m2)
+
+    graph = torch.cuda.CUDAGraph()
+    first = blocks.clone()
+    step(ws)
+    with torch.cuda.graph(graph):
+        step(ws)
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        lens = [int(x) for x in rng.integers(0, 900, n)]
+        held = sum(-(-x // PAGE) for x in lens)
+        pages, at = rng.permutation(400), 0
+        for i, x in enumerate(lens):
+            k = -(-x // PAGE)
+            table[i] = -1
+            table[i, :k] = _i32(pages[at: at + k])
+            at += k
+        ring[: 400 - held] = _i32(pages[held:])
+        free = ring.clone()
+        state.copy_(_i32([0, 400 - held, 0, 0]))
+        lengths.copy_(_i32(lens))
+        parents.copy_(_i32(rng.integers(-1, n, n)))
+        stays.copy_(torch.from_numpy(rng.random((n, 1000)) < 0.6))
+        got = []
+        for run in (lambda: step(torch.zeros_like(ws)), graph.replay):
+            ring.copy_(free)
+            blocks.copy_(first)
+            run()
+            got.append([x.clone() for x in (*made[0], *made[1], ring, blocks)])
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
+        assert got[0][2][2] == 0 and got[0][7][2] == 0               # nobody lost tokens or was left as it was
 
 
 # ------------------------------------------------------------------------------------------------ moves

@@ -104,6 +104,24 @@ struct Runs {
     return at < MIN_PART ? begin : pages - at < MIN_PART ? end : y;
   }
 };
+// The last of 0 .. n - 1 where f is not above y[k], by a whole warp, 32 places at a time (f ascends from f(0) <= y[k]; lane by lane, halving: decode of 64
+// requests 35.7 us instead of 35.2).
+template <int K, typename F>
+__device__ __forceinline__ void last_not_above(int n, F f, const int64_t (&y)[K], int (&at)[K]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 0; k < K; ++k) at[k] = 0;
+  for (int size = n; size > 1;) {
+    const int step = (size + 31) / 32, off = lane * step;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = at[k] + off;
+      const bool not_above = off < size && i < n && f(i) <= y[k];
+      at[k] += max(__popc(__ballot_sync(0xffffffffu, not_above)) - 1, 0) * step;
+    }
+    size = step;
+  }
+}
 __device__ __forceinline__ int divide(int64_t a, int b) { return a >> 31 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b); }
 
 // A unit, and the pages of it that some row sees.
@@ -253,41 +271,37 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
       for (int64_t j = threadIdx.x; j < n; j += THREADS) p.lse[b * p.H + j] = -INFINITY;
   }
   if ((int)blockIdx.x >= runs.grid || runs.all == 0) return;
-  // pages before the border of CTA c
-  auto border = [&](int c) {
+  // pages before the borders of this CTA and of the next, in lanes' turn
+  auto border = [&](int c, int at) {
     if (c == runs.grid) return req.pages(p.n_seq);
     const int64_t y = runs.raw(c);
-    int lo = 0, hi = p.n_seq - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (req.pre[mid] <= y) lo = mid; else hi = mid - 1;
-    }
-    const int pages = (req.keys[lo] + PAGE - 1) / PAGE, unit = divide(y - req.pre[lo], pages + UNIT_END);
-    const int64_t begin = req.pre[lo] + (int64_t)unit * (pages + UNIT_END);
-    const int64_t at = Runs::snap(y, begin, pages) - begin;
-    return req.pages(lo) + (int64_t)unit * pages + min(at, (int64_t)pages);
+    const int pages = (req.keys[at] + PAGE - 1) / PAGE, number = divide(y - req.pre[at], pages + UNIT_END);
+    const int64_t begin = req.pre[at] + (int64_t)number * (pages + UNIT_END);
+    return req.pages(at) + (int64_t)number * pages + min(Runs::snap(y, begin, pages) - begin, (int64_t)pages);
   };
-  const int64_t a_border = border(blockIdx.x + (lane & 1)), first_page = __shfl_sync(0xffffffffu, a_border, 0);        // (both at once)
+  const int64_t raw[2] = {runs.raw(blockIdx.x), runs.raw(blockIdx.x + 1)};
+  int in[2];
+  last_not_above(p.n_seq, [&](int i) { return req.pre[i]; }, raw, in);
+  const int64_t a_border = border(blockIdx.x + (lane & 1), lane & 1 ? in[1] : in[0]), first_page = __shfl_sync(0xffffffffu, a_border, 0);
   const int n_run = (int)min(__shfl_sync(0xffffffffu, a_border, 1) - first_page, (int64_t)INT_MAX / 16);
   if (n_run <= 0) return;
   const int x0 = n_run * warp / WARPS, x1 = n_run * (warp + 1) / WARPS;
-  // the unit with page y of all, and the page's number in it
-  auto locate = [&](int64_t y, Unit<ROWS>& u) {
-    int lo = 0, hi = p.n_seq - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (req.pages(mid) <= y) lo = mid; else hi = mid - 1;
-    }
-    const int64_t local = y - req.pages(lo);
-    const int pages = (req.keys[lo] + PAGE - 1) / PAGE, tiles = (req.count[lo] * p.G + ROWS - 1) / ROWS, number = divide(local, pages);
-    u.seq = lo;
+  // the unit with page y of all, one of request `seq`, and the page's number in it
+  auto locate = [&](int64_t y, int seq, Unit<ROWS>& u) {
+    const int64_t local = y - req.pages(seq);
+    const int pages = (req.keys[seq] + PAGE - 1) / PAGE, tiles = (req.count[seq] * p.G + ROWS - 1) / ROWS, number = divide(local, pages);
+    u.seq = seq;
     u.head = (int)((uint32_t)number / (uint32_t)tiles);
     u.tile = number - u.head * tiles;
     u.set(req, p);
     return (int)(local - (int64_t)number * pages);
   };
+  auto pages_before = [&](int i) { return req.pages(i); };
   Unit<ROWS> unit;
-  int j0 = locate(first_page + min(x0, n_run - 1), unit);          // its page where the range begins
+  const int64_t range[1] = {first_page + min(x0, n_run - 1)};
+  int range_seq[1];
+  last_not_above(p.n_seq, pages_before, range, range_seq);
+  int j0 = locate(range[0], range_seq[0], unit);                   // its page where the range begins
   // ------------------------------------------------------------------ copies
   unsigned char* ring = smem + warp * stages * B::BYTES;
   Unit<ROWS> ahead = unit;                                         // the page to be sent for next: number ahead_j of this unit
@@ -629,7 +643,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
   if (warp == 0) {
     const int side = lane & 1;
     Unit<ROWS> u;
-    const int j = locate(first_page + (side ? n_run - 1 : 0), u);
+    const int64_t ends[2] = {first_page, first_page + n_run - 1};
+    int seqs[2];
+    last_not_above(p.n_seq, pages_before, ends, seqs);
+    const int j = locate(side ? ends[1] : ends[0], side ? seqs[1] : seqs[0], u);
     const bool cut = side ? j + 1 < u.pages : j > 0;
     const int64_t begin = req.pre[u.seq] + ((int64_t)u.head * u.tiles + u.tile) * (u.pages + UNIT_END), end = begin + u.pages + UNIT_END;
     // the last CTA whose run begins before `y`, a place of this unit (at its beginning: not behind it)

@@ -15,8 +15,8 @@
 // two, and probabilities are fp16 for either type.
 //
 // What bounds it: long contexts the reading and, nearly as much, the instructions that make numbers of codes (64 requests of 12 000 tokens, 8 kv heads of four:
-// 885 MB in 167 us, 5.3 TB/s; a page takes an SM 370 to 440 cycles); ordinary ones the ends of the call: 64 requests of 300 to 12 000 are 35.7 us for
-// 101 MB, of which 4 pass before the first page (lengths, runs, table, pages: one load behind another) and 3.5 after the last (the SMs' differences,
+// 885 MB in 164 us, 5.4 TB/s; a page takes an SM 370 to 440 cycles); ordinary ones the ends of the call: 64 requests of 300 to 12 000 are 35.2 us for
+// 101 MB, of which 4.4 pass before the first page (lengths, runs, table, pages: one load behind another) and 4 to 5 after most warps' last (the SMs' differences,
 // parts added up, a fence and a counter).  One token over 200 keys is 7.7 us, the same chain.
 #include <algorithm>
 #include <climits>

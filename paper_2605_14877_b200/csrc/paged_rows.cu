@@ -725,8 +725,9 @@ cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
   cudaError_t rc;
   if (p.n_pages <= SMALL_PAGES && p.n_seq <= SMALL_ROWS && (int64_t)p.n_seq * p.table_pages <= SMALL_ENTRIES) {
     auto bytes = [](int n_pages, int n_seq) { return ((n_pages + 7) / 8 + n_pages + 5 * n_seq + 2) * 4; };
-    // (always the most that any call takes: the limit is the process's, and another thread may set it before this launch)
-    rc = cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, SMALL_ROWS));
+    // (always the most that any call takes: the limit is the process's, and another thread may set it before this launch; 47 KB need no limit raised)
+    rc = bytes(p.n_pages, p.n_seq) <= 47 * 1024 ? cudaSuccess
+                                                : cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, SMALL_ROWS));
     return rc != cudaSuccess ? rc : launch_pdl(fork_small_kernel, dim3(1 + (p.n_seq + copied_rows(p.n_seq) - 1) / copied_rows(p.n_seq)), dim3(DECIDE_THREADS), bytes(p.n_pages, p.n_seq), stream, p);
   }
   rc = launch_zero_marks(p, stream);

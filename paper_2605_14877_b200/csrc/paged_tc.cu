@@ -21,7 +21,7 @@
 // the tiles of 16-bit numbers that TMA brings otherwise, exactly (paged4.cuh): K of a key tile first, as the next logits wait for it while V's place is
 // still taken (K and V together: 408 us instead of 340 for the first shape below).  Of 128-wide heads rows go out without a detour through shared
 // memory, whose place the blocks take.  A quarter of the bytes, no fewer products: 340 us on the first shape, 1190 TFLOP/s, as over 16 bits; 64-wide
-// heads 300 us (675), one in ten slower than over 16 bits, as the codes' instructions stand in the way of the softmax's.
+// heads 294 us (690), one in ten slower than over 16 bits, as the codes' instructions stand in the way of the softmax's.
 // What bounds it: 128-wide heads the matrix unit and, back to back, power (2 sequences of 4096 new tokens over 8096 keys, 16 heads: 450 to 470 us,
 // 1160 to 1200 TFLOP/s; three causal prompts of 2100 to 4096 tokens, 32 heads, whose items are short: 213 us, 880); 64-wide heads the softmax warps'
 // waits for tensor memory (half the products per exponential: 32 heads of the first shape 666 us, 815 TFLOP/s; no unit is busy more than 57 %).
@@ -558,8 +558,10 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
   constexpr float THRESHOLD = F16 ? 8.f : RESCALE_THRESHOLD;
   // One pair of exponentials in four on the FMA units where the exponential unit is as busy as anything (64-wide heads: a chunk of 1500
   // tokens behind 20 000, 40 heads, 439 us without, 396 with one pair in four, 438 with one in two; 128-wide heads, bound by the products:
-  // no difference, and 6 % slower with one in two).
+  // no difference, and 6 % slower with one in two).  Beside the warps that turn codes into numbers one in eight (three chunks, 40 heads: 149.8 us with none
+  // or one in four, 147.1).
   constexpr bool POLY = D == 64;
+  constexpr int POLY_EVERY = CODES ? 8 : 4;
   const PagedParams& p = tp.a;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -1118,7 +1120,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
             for (int i = 0; i < 32; i += 2) {
               const uint64_t xx = fma2(pack2(__uint_as_float(rc[i]), __uint_as_float(rc[i + 1])), scale2, shift);
               float e0, e1;
-              if (POLY && (i >> 1 & 3) == 3) {
+              if (POLY && (i >> 1) % POLY_EVERY == POLY_EVERY - 1) {
                 exp2_pair(xx, e0, e1);
               } else {
                 float x0, x1;

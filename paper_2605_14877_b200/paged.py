@@ -140,11 +140,12 @@ class PagedCache:
         if len(parents) != self.rows or any(p is not None and not 0 <= p < self.rows for p in parents):
             raise ValueError(f"parents: expected {self.rows} rows or None, got {list(parents)}")
         of = torch.tensor([-1 if p is None else p for p in parents], dtype=torch.int32, device=self.device)
-        if self.gone is not None:
-            self.gone = torch.where(of >= 0, self.gone[of.clamp(min=0).long()], 0)
         self._rearrange(hk.heatkv_paged_fork, (of, None), self.rows * hk.PAGE_TOKENS)
+        if self.gone is not None:
+            self.gone = self.gone[of.clamp(min=0).long()]
         self.at_most = [0 if p is None else self.at_most[p] for p in parents]
         self.shared = True
+        self._forget()
 
     def compact(self, stays: torch.Tensor) -> None:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their

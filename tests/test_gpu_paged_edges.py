@@ -1,0 +1,43 @@
+"""Edges of the paged cache in 4 bits and of rows between steps that the other tests do not reach."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+
+@pytest.fixture(scope="module")
+def hk():
+    import paper_2605_14877_b200 as hk
+    return hk
+
+
+def _cache(**more):
+    from paper_2605_14877_b200.paged import PagedCache
+    return PagedCache(1, 2, 2, 64, **more)
+
+
+def _begin(cache, new):
+    """A step whose tokens are stored; the positions of its tokens, row by row."""
+    step, n = cache.begin(new), sum(new)
+    x = torch.zeros(n, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cache.attend(0, step, x, x, x, torch.empty_like(x))
+    at = np.concatenate([[0], np.cumsum(new)])
+    return [step.positions.tolist()[a:b] for a, b in zip(at, at[1:])]
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_a_row_that_lost_its_tokens_to_a_fork_begins_anew(hk, bits):
+    """No page is free: a copy of a row of less than a page has nothing, and whoever comes next in its place starts at position 0."""
+    cache = _cache(n_pages=4, rows=3, max_pages=4, bits=bits)
+    _begin(cache, [128, 0, 40])
+    stays = torch.ones(3, 40, dtype=torch.bool, device="cuda")
+    stays[2, 5:25] = False
+    cache.compact(stays)
+    _begin(cache, [64, 0, 0])
+    assert cache.lengths.tolist() == [192, 0, 20] and cache.state.tolist()[1] == 0
+    cache.fork([0, 2, 2])
+    assert cache.lengths.tolist() == [192, 0, 20] and cache.state.tolist()[2] == 1
+    cache.fork([None, 1, 2])
+    assert _begin(cache, [0, 5, 3]) == [[], [0, 1, 2, 3, 4], [40, 41, 42]]

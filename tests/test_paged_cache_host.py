@@ -1,0 +1,155 @@
+"""PagedCache's own part of the work, on the CPU: the library's calls are played by the plain oracle, and what lies in every slot is a token's number, so that a
+row's tokens, their order and the positions of those to come are compared with a plain list of them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as P
+from paper_2605_14877_b200 import heatkv as H
+from paper_2605_14877_b200.paged import PagedCache
+
+PAGE = 64
+
+
+class Server:
+    """A cache of one layer, the oracle behind its calls, and the lists: `held` has (number, position) of every token of a row, `next` the position of the one
+    to come."""
+
+    def __init__(self, monkeypatch, n_pages, rows, max_pages, bits=4):
+        self.slots, self.tokens, self.calls = np.full(n_pages * PAGE, -1), 0, []
+        for name in ("tables", "release", "fork", "compact"):
+            monkeypatch.setattr(H, f"heatkv_paged_{name}", getattr(self, f"_{name}"))
+        for name in ("paged", "paged4"):
+            monkeypatch.setattr(H, f"heatkv_{name}_workspace_bytes", lambda *a: 256)
+            monkeypatch.setattr(H, f"heatkv_{name}_move", self._move)
+        self.cache = PagedCache(1, 2, 1, 64, n_pages=n_pages, rows=rows, max_pages=max_pages, device="cpu", bits=bits)
+        self.held, self.next = [[] for _ in range(rows)], [0] * rows
+
+    # ---- the library's calls
+    @staticmethod
+    def _ring(free, state):
+        head, count = state.tolist()[:2]
+        return [int(free[(head + j) % len(free)]) for j in range(count)]
+
+    def _tables(self, new, past, free, state, state_out, table, q_begin, kv_len, slots, positions):
+        self.calls.append("tables")
+        fifo = self._ring(free, state)
+        made, begin, kv, slot, pos, taken, refused = P.tables(new.tolist(), past.tolist(), fifo, table.numpy(), len(slots))
+        for out, x in ((table, made), (q_begin, begin), (kv_len, kv), (slots, slot), (positions, pos)):
+            out.copy_(torch.from_numpy(np.asarray(x)))
+        state_out.copy_(torch.tensor([(int(state[0]) + taken) % len(free), len(fifo) - taken, refused, int(new.sum())]))
+
+    def _back(self, free, state, state_out, taken, back, third, fourth):
+        head, count = state.tolist()[:2]
+        for j, page in enumerate(back):
+            free[(head + count + j) % len(free)] = page
+        state_out.copy_(torch.tensor([(head + taken) % len(free), count - taken + len(back), third, fourth]))
+
+    def _release(self, kv_len, keep_len, table, free, state, state_out):
+        self.calls.append("release")
+        back = [int(page) for row, n, k in zip(table, kv_len.tolist(), keep_len.tolist()) for page in row[-(-min(n, k) // PAGE): -(-n // PAGE)]]
+        assert len(set(back)) == len(back) and not set(back) & set(self._ring(free, state))            # (no page for two rows)
+        self._back(free, state, state_out, 0, back, 0, len(back))
+
+    def _fork(self, parents, keep, lengths, table, free, state, lengths_out, table_out, state_out, source, target, workspace):
+        self.calls.append("fork")
+        new, made, a, b, taken, cut, back = P.fork(parents.tolist(), [10**9] * len(parents) if keep is None else keep.tolist(), lengths.tolist(), table.numpy(),
+                                                   self._ring(free, state))
+        for out, x in ((lengths_out, new), (table_out, made), (source, a), (target, b)):
+            out.copy_(torch.from_numpy(x))
+        self._back(free, state, state_out, taken, back, cut, len(back))
+
+    def _compact(self, stays, lengths, table, free, state, lengths_out, table_out, state_out, source, target, workspace):
+        self.calls.append("compact")
+        new, made, a, b, taken, refused, back, done = P.compact(stays.numpy(), lengths.tolist(), table.numpy(), self._ring(free, state), len(source))
+        for out, x in ((lengths_out, new), (table_out, made), (source, a), (target, b)):
+            out.copy_(torch.from_numpy(np.asarray(x)))
+        self._back(free, state, state_out, taken, back, refused, done)
+
+    def _move(self, pool, source, target):
+        self.calls.append("move")
+        pairs = [(a, b) for a, b in zip(source.tolist(), target.tolist()) if a >= 0 and b >= 0]
+        for b, x in [(b, self.slots[a]) for a, b in pairs]:
+            self.slots[b] = x
+
+    # ---- what a server does
+    def check(self):
+        lengths, table = self.cache.lengths.tolist(), self.cache.table
+        assert lengths == [len(x) for x in self.held]
+        assert all(a >= n for a, n in zip(self.cache.at_most, lengths))
+        for i, row in enumerate(self.held):
+            assert [int(self.slots[int(table[i][t // PAGE]) * PAGE + t % PAGE]) for t in range(len(row))] == [number for number, _ in row], i
+        listed = {int(table[i][j]) for i, n in enumerate(lengths) for j in range(-(-n // PAGE))}
+        ring = self._ring(self.cache.free, self.cache.state)
+        assert sorted(listed | set(ring)) == list(range(len(self.cache.free))) and len(listed) + len(ring) == len(self.cache.free)
+
+    def begin(self, new):
+        step = self.cache.begin(new)
+        slots, positions, at = step.slots.tolist(), step.positions.tolist(), 0
+        for i, n in enumerate(new):
+            if step.kv_len[i] > 0:
+                assert positions[at: at + n] == list(range(self.next[i], self.next[i] + n)), i
+                for slot in slots[at: at + n]:
+                    self.slots[slot] = self.tokens
+                    self.held[i].append((self.tokens, self.next[i]))
+                    self.tokens += 1
+                    self.next[i] += 1
+            at += n
+        self.check()
+
+    def cut(self, i, n):
+        """To the n tokens that the row has; the next one takes the place of the first that went."""
+        if n < len(self.held[i]):
+            self.next[i] = self.held[i][n][1] if n else 0
+            del self.held[i][n:]
+
+    def _lost(self, wanted):
+        """Rows have at most the tokens of a page that is not full fewer than they were to have, and say so."""
+        short = 0
+        for i, (n, want) in enumerate(zip(self.cache.lengths.tolist(), wanted)):
+            assert n in (want, want // PAGE * PAGE)
+            short += n != want
+            self.cut(i, n)
+        assert self.cache.state.tolist()[2] == short
+        self.check()
+        return short
+
+    def fork(self, parents):
+        self.cache.fork(parents)
+        self.held = [[] if p is None else list(self.held[p]) for p in parents]
+        self.next = [0 if p is None else self.next[p] for p in parents]
+        return self._lost([len(x) for x in self.held])
+
+    def keep(self, lengths):
+        self.cache.keep(lengths)
+        for i, n in enumerate(lengths):
+            self.cut(i, n)
+        return self._lost([len(x) for x in self.held])
+
+    def compact(self, stays):
+        stays = torch.as_tensor(stays, dtype=torch.bool)
+        before = [len(x) for x in self.held]
+        self.cache.compact(stays)
+        for i, n in enumerate(self.cache.lengths.tolist()):
+            kept = [x for t, x in enumerate(self.held[i]) if t >= stays.shape[1] or stays[i, t]]
+            if n == len(kept):
+                self.held[i] = kept
+                self.next[i] = self.next[i] if kept else 0
+            else:
+                assert n == before[i] and self.cache.state[2] > 0
+        self.check()
+
+
+def test_a_row_that_lost_its_tokens_to_a_fork_begins_anew(monkeypatch):
+    """No page is free: a copy of a row of less than a page has nothing, and whoever comes next in its place starts at position 0."""
+    s = Server(monkeypatch, n_pages=4, rows=3, max_pages=4)
+    s.begin([192, 0, 40])
+    stays = np.ones((3, 40), dtype=bool)
+    stays[2, 5:25] = False
+    s.keep([128, 0, 40])
+    s.compact(stays)
+    s.begin([64, 0, 0])
+    assert s.cache.lengths.tolist() == [192, 0, 20] and s.cache.state.tolist()[1] == 0
+    assert s.fork([0, 2, 2]) == 1 and s.cache.lengths.tolist() == [192, 0, 20]
+    s.fork([None, 1, 2])
+    s.begin([0, 5, 3])

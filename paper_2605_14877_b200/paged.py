@@ -118,12 +118,20 @@ class PagedCache:
             raise hk.HeatKVError(status, "PagedCache.check")
 
     def keep(self, lengths: Sequence[int]) -> None:
-        """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free; more than it has: it stays as it is)."""
+        """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free; more than it has: it stays as it is).  Where rows share
+        pages, a row that is cut to a place inside a page which another row has whole gets a copy of it, from a free page or one that this
+        call frees.  Where there is none it loses that page's tokens, too: `lengths` says what it has, and `state[2]` counts such rows."""
         if len(lengths) != self.rows or min(lengths) < 0:
             raise ValueError(f"lengths: expected {self.rows} numbers of tokens, none below 0, got {list(lengths)}")
         keep = torch.tensor(list(lengths), dtype=torch.int32, device=self.device)
         if self.shared:
-            self._rearrange(hk.heatkv_paged_fork, (torch.arange(self.rows, dtype=torch.int32, device=self.device), keep), self.rows * hk.PAGE_TOKENS)
+            own = torch.arange(self.rows, dtype=torch.int32, device=self.device)
+            if any(n < a and n % hk.PAGE_TOKENS for a, n in zip(self.at_most, lengths)):
+                # whole pages first: that takes none, moves nothing, and what it frees is there for the copies
+                most = self.table.shape[1]
+                whole = torch.tensor([min(-(-n // hk.PAGE_TOKENS), most) * hk.PAGE_TOKENS for n in lengths], dtype=torch.int32, device=self.device)
+                self._rearrange(hk.heatkv_paged_fork, (own, whole), self.rows * hk.PAGE_TOKENS, moves=False)
+            self._rearrange(hk.heatkv_paged_fork, (own, keep), self.rows * hk.PAGE_TOKENS)
             self.at_most = [min(a, n) for a, n in zip(self.at_most, lengths)]
             self._forget()
             return
@@ -160,8 +168,8 @@ class PagedCache:
         self.gone = gone if self.gone is None else self.gone + gone
         self._forget()
 
-    def _rearrange(self, call, what, n_moves: int) -> None:
-        """One of the two calls that write new lengths and a new table, and the moves of K and V that it asks for."""
+    def _rearrange(self, call, what, n_moves: int, moves: bool = True) -> None:
+        """One of the two calls that write new lengths and a new table, and the moves of K and V that it asks for (moves False: it asks for none)."""
         if self.rows_workspace is None:
             need = hk.heatkv_paged_rows_workspace_bytes(self.rows, self.table.shape[1], self.free.numel())
             self.rows_workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
@@ -175,7 +183,7 @@ class PagedCache:
         self.lengths, self.table = lengths, table
         self.state, self.other_state = self.other_state, self.state
         move = hk.heatkv_paged_move if self.bits == 16 else hk.heatkv_paged4_move
-        for pool in self.pools:
+        for pool in self.pools if moves else ():
             move(pool, source, target)
 
     def _forget(self) -> None:

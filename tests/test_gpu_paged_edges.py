@@ -41,3 +41,18 @@ def test_a_row_that_lost_its_tokens_to_a_fork_begins_anew(hk, bits):
     assert cache.lengths.tolist() == [192, 0, 20] and cache.state.tolist()[2] == 1
     cache.fork([None, 1, 2])
     assert _begin(cache, [0, 5, 3]) == [[], [0, 1, 2, 3, 4], [40, 41, 42]]
+
+
+def test_a_cut_into_a_shared_page_takes_a_page_that_the_same_call_frees(hk):
+    """Row 0 is cut to a place inside a page that row 1 has whole, no page is free before row 2 ends in the same call: its tokens, too, are there."""
+    cache = _cache(n_pages=3, rows=3, max_pages=4, bits=16)
+    k, v = (torch.arange(138, device="cuda").remainder(101)[:, None, None].expand(138, 2, 64).bfloat16().contiguous() for _ in "kv")
+    cache.attend(0, cache.begin([128, 0, 10]), k, k, v, torch.empty_like(k))
+    cache.fork([0, 0, 2])
+    cache.keep([100, 128, 0])
+    assert cache.lengths.tolist() == [100, 128, 0] and cache.state.tolist()[1:3] == [0, 0]
+    pages = cache.table[:, :2].long()
+    assert len({*pages[0].tolist(), int(pages[1, 1])}) == 3 and pages[0, 0] == pages[1, 0]
+    for i, n in ((0, 100), (1, 128)):
+        for x, new in zip(cache.pools[0].tensors, (k, v)):
+            assert torch.equal(x[pages[i]].transpose(1, 2).reshape(128, 2, 64)[:n], new[:n])

@@ -153,3 +153,34 @@ def test_a_row_that_lost_its_tokens_to_a_fork_begins_anew(monkeypatch):
     assert s.fork([0, 2, 2]) == 1 and s.cache.lengths.tolist() == [192, 0, 20]
     s.fork([None, 1, 2])
     s.begin([0, 5, 3])
+
+
+def test_a_cut_into_a_shared_page_takes_a_page_that_the_same_call_frees(monkeypatch):
+    """Row 0 is cut to a place inside a page that row 1 has whole, and no page is free before row 2 ends in the same call."""
+    s = Server(monkeypatch, n_pages=3, rows=3, max_pages=4)
+    s.begin([128, 0, 10])
+    s.fork([0, 0, 2])
+    assert s.cache.state.tolist()[1] == 0
+    assert s.keep([100, 128, 0]) == 0 and s.cache.lengths.tolist() == [100, 128, 0]
+    assert s.cache.state.tolist()[1] == 0
+    # nothing is freed: then the page's tokens are lost, and the call says so
+    s.fork([1, 1, None])
+    s.begin([0, 0, 1])
+    assert s.keep([100, 2**31 - 1, 1000]) == 1 and s.cache.lengths.tolist() == [64, 128, 1]
+    # one row's pages are enough for another's copy, whatever their order
+    s = Server(monkeypatch, n_pages=5, rows=3, max_pages=4)
+    s.begin([128, 0, 192])
+    s.fork([0, 0, 2])
+    assert s.cache.state.tolist()[1] == 0
+    assert s.keep([1000, 65, 150]) == 1                    # (the third row keeps its third page)
+    assert s.keep([30, 1000, 64]) == 0 and s.cache.lengths.tolist() == [30, 64, 64]
+
+
+def test_a_cut_of_whole_rows_is_one_call(monkeypatch):
+    """Only a place inside a page may want a page: rows that end, or that are not cut, take no second call."""
+    s = Server(monkeypatch, n_pages=9, rows=3, max_pages=4)
+    s.begin([128, 0, 10])
+    s.fork([0, 0, 2])
+    s.calls.clear()
+    s.keep([1000, 0, 1000])
+    assert s.calls.count("fork") == 1

@@ -56,7 +56,9 @@ class PagedCache:
         self.moves = new(2, 0)
         self.rows_workspace: Optional[torch.Tensor] = None
         self.shared = False                            # do rows list the same pages
-        self.gone: Optional[torch.Tensor] = None       # tokens of every row that `compact` took out
+        # tokens that `compact` took out of every row, and in front of each of its first `upto` places
+        self.gone: Optional[torch.Tensor] = None
+        self.left, self.upto = new(rows, 0), new(rows)
 
     def begin(self, new: Sequence[int]) -> Step:
         """Pages and slots of a step with new[i] new tokens in row i (0: none).  Pages are wanted in row order, and from the first row that the free
@@ -150,23 +152,41 @@ class PagedCache:
         of = torch.tensor([-1 if p is None else p for p in parents], dtype=torch.int32, device=self.device)
         self._rearrange(hk.heatkv_paged_fork, (of, None), self.rows * hk.PAGE_TOKENS)
         if self.gone is not None:
-            self.gone = self.gone[of.clamp(min=0).long()]
+            row = of.clamp(min=0).long()
+            self.gone, self.left, self.upto = self.gone[row], self.left[row], self.upto[row]
         self.at_most = [0 if p is None else self.at_most[p] for p in parents]
         self.shared = True
         self._forget()
 
     def compact(self, stays: torch.Tensor) -> None:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their
-        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left (so `keep` is to cut such a
-        row behind its last token that left).  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]` counts
-        them)."""
+        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left; a row that is cut later goes on at
+        the position of the first token that went.  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]`
+        counts them)."""
         if stays.dtype is not torch.bool or stays.dim() != 2 or stays.shape[0] != self.rows:
             raise ValueError(f"stays: expected bool [{self.rows}, tokens], got {stays.dtype} {tuple(stays.shape)}")
         before = self.lengths
         self._rearrange(hk.heatkv_paged_compact, (stays,), min(max(sum(self.at_most), 1), self.free.numel() * hk.PAGE_TOKENS))
-        gone = before - self.lengths
-        self.gone = gone if self.gone is None else self.gone + gone
+        self._count_out(stays, before)
         self._forget()
+
+    def _count_out(self, stays: torch.Tensor, before: torch.Tensor) -> None:
+        """What left in front of every place of the rows that a compaction changed (it leaves the lengths of the others as they were)."""
+        if self.gone is None:
+            self.gone = torch.zeros_like(before)
+        width, known = max(stays.shape[1], self.left.shape[1]), self.left.shape[1]
+        place = torch.arange(width, dtype=torch.int32, device=self.device)
+        leaves = (place < before[:, None]) & (self.lengths < before)[:, None]
+        leaves[:, : stays.shape[1]] &= ~stays
+        leaves[:, stays.shape[1]:] = False
+        in_front = leaves.cumsum(1, dtype=torch.int32)
+        left = self.gone[:, None] + in_front
+        left[:, :known] += torch.where(place[:known] < self.upto[:, None], self.left - self.gone[:, None], 0)
+        # (those that left are written behind the others, to a column that is dropped)
+        self.left = torch.zeros(self.rows, width + 1, dtype=torch.int32, device=self.device).scatter_(
+            1, torch.where(leaves, width, place - in_front).long(), left)[:, :width]
+        went = before - self.lengths
+        self.upto, self.gone = torch.minimum(self.lengths, width - went), self.gone + went
 
     def _rearrange(self, call, what, n_moves: int, moves: bool = True) -> None:
         """One of the two calls that write new lengths and a new table, and the moves of K and V that it asks for (moves False: it asks for none)."""
@@ -187,6 +207,11 @@ class PagedCache:
             move(pool, source, target)
 
     def _forget(self) -> None:
-        """A row that is over has nothing that left it."""
-        if self.gone is not None:
-            self.gone = torch.where(self.lengths > 0, self.gone, 0)
+        """Rows that were cut count on from the first token that went, and a row that is over has nothing that left it."""
+        if self.gone is None:
+            return
+        if self.left.shape[1] > 0:
+            at = self.lengths.clamp(max=self.left.shape[1] - 1).long()[:, None]
+            self.gone = torch.where(self.lengths < self.upto, self.left.gather(1, at)[:, 0], self.gone)
+            self.upto = torch.minimum(self.upto, self.lengths)
+        self.gone = torch.where(self.lengths > 0, self.gone, 0)

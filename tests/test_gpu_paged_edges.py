@@ -56,3 +56,23 @@ def test_a_cut_into_a_shared_page_takes_a_page_that_the_same_call_frees(hk):
     for i, n in ((0, 100), (1, 128)):
         for x, new in zip(cache.pools[0].tensors, (k, v)):
             assert torch.equal(x[pages[i]].transpose(1, 2).reshape(128, 2, 64)[:n], new[:n])
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_positions_of_a_row_that_is_cut_among_tokens_of_which_some_left(hk, bits):
+    """The next token takes the position of the first one that went, whether a call was asked for the cut or had no page for a copy."""
+    cache = _cache(n_pages=4, rows=2, max_pages=4, bits=bits)
+    _begin(cache, [150, 0])
+    stays = torch.ones(2, 150, dtype=torch.bool, device="cuda")
+    stays[0, 140:145] = False
+    cache.compact(stays)
+    _begin(cache, [0, 64])
+    cache.fork([0, 0])
+    assert cache.lengths.tolist() == [145, 128]
+    cache.fork([None, 1])
+    assert _begin(cache, [0, 2]) == [[], [128, 129]]
+    stays[1, 50:60] = False
+    cache.compact(stays)
+    assert cache.lengths.tolist() == [0, 120]
+    cache.keep([0, 52])
+    assert _begin(cache, [1, 1]) == [[0], [62]]

@@ -184,3 +184,44 @@ def test_a_cut_of_whole_rows_is_one_call(monkeypatch):
     s.calls.clear()
     s.keep([1000, 0, 1000])
     assert s.calls.count("fork") == 1
+
+
+def test_positions_of_a_row_that_is_cut_among_tokens_of_which_some_left(monkeypatch):
+    """The next token takes the position of the first one that went, whether a call was asked for the cut or had no page for a copy."""
+    s = Server(monkeypatch, n_pages=4, rows=2, max_pages=4)
+    s.begin([150, 0])
+    stays = np.ones((2, 150), dtype=bool)
+    stays[0, 140:145] = False
+    s.compact(stays)
+    s.begin([0, 64])
+    assert s.fork([0, 0]) == 1 and s.cache.lengths.tolist() == [145, 128]
+    s.fork([None, 1])
+    s.begin([0, 30])                                       # positions 128 ..: none of the lost page's tokens had left before them
+    s.begin([60, 0])
+    stays[:, 10:20] = stays[1, 100:130] = False
+    s.compact(stays)
+    s.keep([1000, 95])
+    s.begin([1, 1])
+    s.keep([14, 50])
+    s.begin([2, 2])
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_a_server_at_random(monkeypatch, seed):
+    """Steps, forks, cuts and compactions in any order, with and without enough pages: tokens, positions and pages as the lists have them."""
+    rng = np.random.default_rng(seed)
+    rows = int(rng.integers(1, 6))
+    s = Server(monkeypatch, n_pages=int(rng.integers(3, 25)), rows=rows, max_pages=int(rng.integers(2, 7)), bits=4 if seed % 2 else 16)
+    for _ in range(60):
+        length = lambda i: len(s.held[i])                                      # noqa: E731
+        kind = rng.choice(["begin", "begin", "begin", "fork", "keep", "compact"])
+        if kind == "begin":
+            new = [int(rng.choice([0, 1, 3, 40, 64, 100])) for _ in range(rows)]
+            if sum(new):
+                s.begin(new)
+        elif kind == "fork":
+            s.fork([None if rng.random() < 0.15 else int(rng.integers(rows)) if rng.random() < 0.5 else i for i in range(rows)])
+        elif kind == "keep":
+            s.keep([int(rng.choice([0, length(i), 10**6, rng.integers(length(i) + 1), rng.integers(length(i) + 1)])) for i in range(rows)])
+        else:
+            s.compact(rng.random((rows, int(rng.integers(1, 300)))) < rng.choice([0.1, 0.6, 0.97, 1.0]))

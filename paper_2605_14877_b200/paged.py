@@ -55,7 +55,7 @@ class PagedCache:
         self.other: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
         self.moves = new(2, 0)
         self.rows_workspace: Optional[torch.Tensor] = None
-        self.shared = False                            # do rows list the same pages
+        self.shared = False                            # may rows list the same pages
         # tokens that `compact` took out of every row, and in front of each of its first `upto` places
         self.gone: Optional[torch.Tensor] = None
         self.left, self.upto = new(rows, 0), new(rows)
@@ -135,6 +135,7 @@ class PagedCache:
                 self._rearrange(hk.heatkv_paged_fork, (own, whole), self.rows * hk.PAGE_TOKENS, moves=False)
             self._rearrange(hk.heatkv_paged_fork, (own, keep), self.rows * hk.PAGE_TOKENS)
             self.at_most = [min(a, n) for a, n in zip(self.at_most, lengths)]
+            self.shared = sum(n > 0 for n in self.at_most) > 1
             self._forget()
             return
         hk.heatkv_paged_release(self.lengths, keep, self.table, self.free, self.state, self.other_state)
@@ -155,7 +156,8 @@ class PagedCache:
             row = of.clamp(min=0).long()
             self.gone, self.left, self.upto = self.gone[row], self.left[row], self.upto[row]
         self.at_most = [0 if p is None else self.at_most[p] for p in parents]
-        self.shared = True
+        parents = [p for p, n in zip(parents, self.at_most) if n]
+        self.shared = (self.shared or len(set(parents)) < len(parents)) and len(parents) > 1
         self._forget()
 
     def compact(self, stays: torch.Tensor) -> None:

@@ -225,3 +225,29 @@ def test_a_server_at_random(monkeypatch, seed):
             s.keep([int(rng.choice([0, length(i), 10**6, rng.integers(length(i) + 1), rng.integers(length(i) + 1)])) for i in range(rows)])
         else:
             s.compact(rng.random((rows, int(rng.integers(1, 300)))) < rng.choice([0.1, 0.6, 0.97, 1.0]))
+
+
+def test_rows_that_share_no_page_are_cut_without_a_fork(monkeypatch):
+    """A cache knows when rows list no page together any more: rows that only move share none, nor does the last row that is left."""
+    s = Server(monkeypatch, n_pages=12, rows=3, max_pages=4)
+    s.begin([130, 70, 0])
+    s.fork([1, 0, None])
+    s.calls.clear()
+    s.keep([60, 100, 0])
+    assert s.calls == ["release"]
+    s.fork([0, 1, 0])
+    s.keep([10, 100, 1000])
+    assert "fork" in s.calls
+    s.keep([0, 0, 1000])
+    s.calls.clear()
+    s.keep([0, 0, 30])
+    assert s.calls == ["release"]
+    s.begin([5, 0, 200])
+    s.fork([0, None, 2])
+    s.keep([0, 0, 130])
+    assert s.calls == ["release", "tables", "fork", "move", "release"]
+    s.fork([2, 2, 2])                                      # (from now on they do, whoever ends)
+    s.keep([1000, 0, 1000])
+    s.calls.clear()
+    s.keep([100, 0, 1000])
+    assert "release" not in s.calls

@@ -587,6 +587,7 @@ int heatkv_paged_fork(const int32_t* parents, const int32_t* keep_len, const int
                       uint64_t workspace_bytes, void* stream);
 
 /* Token t of row i leaves the cache where stays[i][t] (DEVICE bytes, rows stays_stride apart, stays_width of each) is 0; tokens past the width stay.
+ * (stays may be NULL where the width is 0.)
  * Pages before the first token that leaves stay as they are; the tokens behind move together into fresh pages, in order.  Rows take their fresh
  * pages in row order; from the first row on for which the free ones, or the n_moves entries of move_from and move_to, do not suffice, every
  * row that needs some is left as it is.  The moves lie one after another, row by row, token by token; -1 past the last.

@@ -410,7 +410,7 @@ int heatkv_paged_compact(const uint8_t* stays, int64_t stays_stride, int stays_w
                          int64_t table_stride, int table_pages, int32_t* free_pages, int n_pages, const int32_t* state, int32_t* lengths_out,
                          int32_t* table_out, int64_t out_stride, int32_t* state_out, int32_t* move_from, int32_t* move_to, int n_moves,
                          void* workspace, uint64_t workspace_bytes, void* stream) {
-  if (!stays || stays_width < 0 || stays_stride < stays_width) return HEATKV_ERR_INVALID_ARG;
+  if ((!stays && stays_width > 0) || stays_width < 0 || stays_stride < stays_width) return HEATKV_ERR_INVALID_ARG;      // (a mask of no width has no address)
   RowsParams p = {};
   p.mask = stays;
   p.mask_stride = stays_stride;

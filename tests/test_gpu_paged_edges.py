@@ -76,3 +76,16 @@ def test_positions_of_a_row_that_is_cut_among_tokens_of_which_some_left(hk, bits
     assert cache.lengths.tolist() == [0, 120]
     cache.keep([0, 52])
     assert _begin(cache, [1, 1]) == [[0], [62]]
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_a_mask_of_no_width(hk, bits):
+    """Tokens past a mask's width stay: all of them, of a mask that has none."""
+    cache = _cache(n_pages=8, rows=2, max_pages=4, bits=bits)
+    _begin(cache, [150, 3])
+    table = cache.table[:, :3].clone()
+    for stays in (torch.ones(2, 0, dtype=torch.bool, device="cuda"), torch.zeros(2, 9, dtype=torch.bool, device="cuda")[:, :0]):
+        cache.compact(stays)
+        assert cache.lengths.tolist() == [150, 3] and cache.state.tolist()[1:] == [4, 0, 0]
+        assert torch.equal(cache.table[0, :3], table[0]) and cache.table[1, 0] == table[1, 0]
+    assert _begin(cache, [1, 1]) == [[150], [3]]

@@ -251,3 +251,16 @@ def test_rows_that_share_no_page_are_cut_without_a_fork(monkeypatch):
     s.calls.clear()
     s.keep([100, 0, 1000])
     assert "release" not in s.calls
+
+
+def test_a_mask_of_no_width(monkeypatch):
+    s = Server(monkeypatch, n_pages=8, rows=2, max_pages=4)
+    s.begin([150, 3])
+    s.compact(np.ones((2, 0)))
+    s.begin([1, 1])
+    stays = np.ones((2, 100))
+    stays[:, 1:60:2] = 0
+    s.compact(stays)
+    s.compact(np.ones((2, 0)))
+    s.keep([5, 1000])
+    s.begin([1, 1])

@@ -122,12 +122,13 @@ class PagedCache:
     def keep(self, lengths: Sequence[int]) -> None:
         """Cuts row i back to lengths[i] tokens (0: the request is over, its row and pages are free; more than it has: it stays as it is).  Where rows share
         pages, a row that is cut to a place inside a page which another row has whole gets a copy of it, from a free page or one that this
-        call frees.  Where there is none it loses that page's tokens, too: `lengths` says what it has, and `state[2]` counts such rows."""
+        call frees.  Where there is none it loses that page's tokens, too, and goes on at the position of the first of them: `lengths` says what it has, and
+        `state[2]` counts such rows."""
         if len(lengths) != self.rows or min(lengths) < 0:
             raise ValueError(f"lengths: expected {self.rows} numbers of tokens, none below 0, got {list(lengths)}")
         keep = torch.tensor(list(lengths), dtype=torch.int32, device=self.device)
         if self.shared:
-            own = torch.arange(self.rows, dtype=torch.int32, device=self.device)
+            own, asked = torch.arange(self.rows, dtype=torch.int32, device=self.device), torch.minimum(self.lengths, keep)
             if any(n < a and n % hk.PAGE_TOKENS for a, n in zip(self.at_most, lengths)):
                 # whole pages first: that takes none, moves nothing, and what it frees is there for the copies
                 most = self.table.shape[1]
@@ -136,7 +137,7 @@ class PagedCache:
             self._rearrange(hk.heatkv_paged_fork, (own, keep), self.rows * hk.PAGE_TOKENS)
             self.at_most = [min(a, n) for a, n in zip(self.at_most, lengths)]
             self.shared = sum(n > 0 for n in self.at_most) > 1
-            self._forget()
+            self._forget(asked)
             return
         hk.heatkv_paged_release(self.lengths, keep, self.table, self.free, self.state, self.other_state)
         self.state, self.other_state = self.other_state, self.state
@@ -146,25 +147,26 @@ class PagedCache:
 
     def fork(self, parents: Sequence[Optional[int]]) -> None:
         """Row i goes on as a copy of row parents[i] (its own number: as it is; None: it is over).  Full pages are shared; of a page that is not full every
-        row but one gets a copy, from a free page each.  Where those end, rows lose that page's tokens: `lengths` says what they have, and
-        `state[2]` counts them."""
+        row but one gets a copy, from a free page each.  Where those end, rows lose that page's tokens and go on at the position of the first of them: `lengths`
+        says what they have, and `state[2]` counts them."""
         if len(parents) != self.rows or any(p is not None and not 0 <= p < self.rows for p in parents):
             raise ValueError(f"parents: expected {self.rows} rows or None, got {list(parents)}")
         of = torch.tensor([-1 if p is None else p for p in parents], dtype=torch.int32, device=self.device)
+        before = self.lengths
         self._rearrange(hk.heatkv_paged_fork, (of, None), self.rows * hk.PAGE_TOKENS)
-        if self.gone is not None:
-            row = of.clamp(min=0).long()
-            self.gone, self.left, self.upto = self.gone[row], self.left[row], self.upto[row]
         self.at_most = [0 if p is None else self.at_most[p] for p in parents]
         parents = [p for p, n in zip(parents, self.at_most) if n]
         self.shared = (self.shared or len(set(parents)) < len(parents)) and len(parents) > 1
-        self._forget()
+        if self.gone is not None:
+            row = of.clamp(min=0).long()
+            self.gone, self.left, self.upto = self.gone[row], self.left[row], self.upto[row]
+            self._forget(torch.where(of >= 0, before[row], 0))
 
     def compact(self, stays: torch.Tensor) -> None:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their
-        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left; a row that is cut later goes on at
-        the position of the first token that went.  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]`
-        counts them)."""
+        order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left (so `keep` is to cut such a
+        row behind its last token that left).  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]` counts
+        them)."""
         if stays.dtype is not torch.bool or stays.dim() != 2 or stays.shape[0] != self.rows:
             raise ValueError(f"stays: expected bool [{self.rows}, tokens], got {stays.dtype} {tuple(stays.shape)}")
         before = self.lengths
@@ -208,12 +210,14 @@ class PagedCache:
         for pool in self.pools if moves else ():
             move(pool, source, target)
 
-    def _forget(self) -> None:
-        """Rows that were cut count on from the first token that went, and a row that is over has nothing that left it."""
+    def _forget(self, asked: Optional[torch.Tensor] = None) -> None:
+        """A row that is over has nothing that left it; one that was cut deeper than `asked` goes on at the position of the first token that it was not to lose."""
         if self.gone is None:
             return
         if self.left.shape[1] > 0:
-            at = self.lengths.clamp(max=self.left.shape[1] - 1).long()[:, None]
-            self.gone = torch.where(self.lengths < self.upto, self.left.gather(1, at)[:, 0], self.gone)
+            if asked is not None:
+                in_front = lambda n: torch.where(n < self.upto, self.left.gather(1, n.clamp(max=self.left.shape[1] - 1).long()[:, None])[:, 0],      # noqa: E731
+                                                 self.gone)
+                self.gone = self.gone - in_front(asked) + in_front(self.lengths)
             self.upto = torch.minimum(self.upto, self.lengths)
         self.gone = torch.where(self.lengths > 0, self.gone, 0)

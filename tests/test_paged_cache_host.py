@@ -97,19 +97,21 @@ class Server:
             at += n
         self.check()
 
-    def cut(self, i, n):
-        """To the n tokens that the row has; the next one takes the place of the first that went."""
-        if n < len(self.held[i]):
-            self.next[i] = self.held[i][n][1] if n else 0
-            del self.held[i][n:]
+    @staticmethod
+    def _in_front(row, to_come, n):
+        """How many tokens left in front of place n of a row."""
+        return row[n][1] - n if n < len(row) else to_come - len(row)
 
-    def _lost(self, wanted):
-        """Rows have at most the tokens of a page that is not full fewer than they were to have, and say so."""
+    def _cut(self, wanted):
+        """Rows cut to the numbers of tokens that were wanted, which go on as many positions behind those as before, or to that number's whole pages: then
+        they go on at the first token that they were not to lose.  How many those are."""
         short = 0
         for i, (n, want) in enumerate(zip(self.cache.lengths.tolist(), wanted)):
+            row, to_come = self.held[i], self.next[i]
             assert n in (want, want // PAGE * PAGE)
             short += n != want
-            self.cut(i, n)
+            left = to_come - len(row) - self._in_front(row, to_come, want) + self._in_front(row, to_come, n)
+            self.held[i], self.next[i] = row[:n], n + left if n else 0
         assert self.cache.state.tolist()[2] == short
         self.check()
         return short
@@ -118,13 +120,11 @@ class Server:
         self.cache.fork(parents)
         self.held = [[] if p is None else list(self.held[p]) for p in parents]
         self.next = [0 if p is None else self.next[p] for p in parents]
-        return self._lost([len(x) for x in self.held])
+        return self._cut([len(x) for x in self.held])
 
     def keep(self, lengths):
         self.cache.keep(lengths)
-        for i, n in enumerate(lengths):
-            self.cut(i, n)
-        return self._lost([len(x) for x in self.held])
+        return self._cut([min(len(x), n) for x, n in zip(self.held, lengths)])
 
     def compact(self, stays):
         stays = torch.as_tensor(stays, dtype=torch.bool)
@@ -186,24 +186,30 @@ def test_a_cut_of_whole_rows_is_one_call(monkeypatch):
     assert s.calls.count("fork") == 1
 
 
-def test_positions_of_a_row_that_is_cut_among_tokens_of_which_some_left(monkeypatch):
-    """The next token takes the position of the first one that went, whether a call was asked for the cut or had no page for a copy."""
+def test_positions_of_a_row_that_lost_tokens_among_which_some_had_left(monkeypatch):
+    """A call that has no page for a copy cuts a row where nobody asked it to: the next token takes the position of the first one that was lost."""
     s = Server(monkeypatch, n_pages=4, rows=2, max_pages=4)
     s.begin([150, 0])
     stays = np.ones((2, 150), dtype=bool)
     stays[0, 140:145] = False
     s.compact(stays)
     s.begin([0, 64])
-    assert s.fork([0, 0]) == 1 and s.cache.lengths.tolist() == [145, 128]
+    assert s.fork([0, 0]) == 1 and s.cache.lengths.tolist() == [145, 128] and s.next == [150, 128]
     s.fork([None, 1])
-    s.begin([0, 30])                                       # positions 128 ..: none of the lost page's tokens had left before them
+    s.begin([0, 30])
     s.begin([60, 0])
-    stays[:, 10:20] = stays[1, 100:130] = False
+    # the same by a cut, in front of which others had left
+    s = Server(monkeypatch, n_pages=5, rows=3, max_pages=4)
+    s.begin([150, 0, 0])
+    stays = np.ones((3, 150), dtype=bool)
+    stays[0, 70:77] = stays[0, 141] = False
     s.compact(stays)
-    s.keep([1000, 95])
-    s.begin([1, 1])
-    s.keep([14, 50])
-    s.begin([2, 2])
+    s.begin([50, 0, 0])
+    s.fork([0, 0, 2])
+    s.begin([0, 0, 64])
+    assert s.cache.lengths.tolist() == [192, 192, 64] and s.cache.state.tolist()[1] == 1 and s.next == [200, 200, 64]
+    s.begin([0, 0, 1])
+    assert s.keep([180, 1000, 1000]) == 1 and s.cache.lengths.tolist() == [128, 192, 65] and s.next == [135, 200, 65]
 
 
 @pytest.mark.parametrize("seed", range(30))

@@ -32,7 +32,10 @@ using namespace tc;
 
 constexpr int MOST_WARPS = 12;
 constexpr int MAX_STAGES = 6;
-constexpr float MOVE = 8.f;                    // a reference moves when a maximum passes it by more than 2^MOVE (P fits fp16)
+// A row's reference is set 2^BELOW under its maximum and moves when a maximum passes it by more than 2^MOVE: probabilities fit fp16, and the smallest that do
+// not round to nothing there are 2^-(25 + BELOW) of the largest.  (With references at the maximum a key 2^25.5 under it counted in the sum and not in the
+// output: 260 000 such keys beside a heavy one are half a percent of it, and were missing.)
+constexpr float BELOW = 7.f, MOVE = 15.f;
 constexpr int SHARE = 4;                       // pages of a run at least
 constexpr int WHOLE = 8;                       // units of up to so many pages are never cut by a run's border
 constexpr int MIN_PART = 4;                    // pages of a part
@@ -508,7 +511,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-            const float m_new = fmaxf(m_ref[nt][e], t), f = exp2f(m_ref[nt][e] - m_new);
+            const float m_new = fmaxf(m_ref[nt][e], t - BELOW), f = exp2f(m_ref[nt][e] - m_new);
             m_ref[nt][e] = m_new;
             l_sum[nt][e] *= f;
 #pragma unroll
@@ -518,8 +521,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
             }
           }
       }
-      // probabilities: their sums take them as 32-bit numbers, the product with V rounded to fp16, as the matrix unit wants its operands
+      // probabilities: their sums take them as 32-bit numbers (a page's for themselves first: a long row's is off by an eighth of the roundings), the product
+      // with V rounded to fp16, as the matrix unit wants its operands
       uint32_t pf[KT][NT][2];
+      float of_page[NT][2];
 #pragma unroll
       for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
@@ -528,10 +533,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) paged4_small_kernel(const __gri
           for (int u = 0; u < 2; ++u) {
             const float e0 = ex2_approx(fmaf(s[mt][nt][2 * u], row_scale[nt][0], -m_ref[nt][0]));
             const float e1 = ex2_approx(fmaf(s[mt][nt][2 * u + 1], row_scale[nt][1], -m_ref[nt][1]));
-            l_sum[nt][0] += e0;
-            l_sum[nt][1] += e1;
+            of_page[nt][0] = mt + u == 0 ? e0 : of_page[nt][0] + e0;
+            of_page[nt][1] = mt + u == 0 ? e1 : of_page[nt][1] + e1;
             pf[mt][nt][u] = transpose8(pack_half(e0, e1));
           }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) l_sum[nt][e] += of_page[nt][e];
       const int there = unit.kv - first;                         // keys of the page that exist
 #pragma unroll
       for (int mt = 0; mt < KT; ++mt) {

@@ -554,8 +554,9 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
   constexpr int NCH = L::NCH, KV_STAGES = L::KV_STAGES;
   constexpr uint32_t TILE_BYTES = L::TILE_BYTES, SM_Q = L::SM_Q, SM_K = L::SM_K, SM_V = L::SM_V, SM_OUT = L::SM_OUT, SM_BAR = L::SM_BAR;
   // How far (log2) a maximum may rise above the reference of its row's exponentials: bf16 and the 32-bit sums have room for 2^32,
-  // fp16 probabilities for 2^15.
-  constexpr float THRESHOLD = F16 ? 8.f : RESCALE_THRESHOLD;
+  // fp16 probabilities for 2^15.  Over 4 bits fp16's references lie 2^7 under the maximum, so that the smallest probabilities which do not round to nothing are
+  // 2^-32 of the largest (very many light keys beside a heavy one: paged4_small.cu).
+  constexpr float BELOW = CODES && F16 ? 7.f : 0.f, THRESHOLD = F16 ? 8.f + BELOW : RESCALE_THRESHOLD;
   // One pair of exponentials in four on the FMA units where the exponential unit is as busy as anything (64-wide heads: a chunk of 1500
   // tokens behind 20 000, 40 heads, 439 us without, 396 with one pair in four, 438 with one in two; 128-wide heads, bound by the products:
   // no difference, and 6 % slower with one in two).  Beside the warps that turn codes into numbers one in eight (three chunks, 40 heads: 149.8 us with none
@@ -1139,7 +1140,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
           const bool grow = valid && m_new > m_ref + THRESHOLD;
           if (j > 0 && __any_sync(0xffffffffu, grow)) {
             // O is complete up to tile j - 1: the commit behind S_FULL covers every product issued before it
-            const float f = grow ? exp2f(m_ref - m_new) : 1.f;
+            const float f = grow ? exp2f(m_ref - (m_new - BELOW)) : 1.f;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
               uint32_t r[32];
@@ -1152,7 +1153,7 @@ __global__ void __launch_bounds__(CODES ? THREADS4 : THREADS, 1) paged_tc_kernel
             tmem_wait_st();
             l_sum *= f;
           }
-          if (grow) m_ref = m_new;
+          if (grow) m_ref = m_new - BELOW;
           const uint64_t shift2 = pack2(-m_ref, -m_ref);
           exp_chunk(r0, sel0 ? shift2 : none2, 0);
           exp_chunk(r1, sel0 ? shift2 : none2, 1);

@@ -97,3 +97,42 @@ def test_a_mask_of_no_width(hk, bits):
         assert cache.lengths.tolist() == [150, 3] and cache.state.tolist()[1:] == [4, 0, 0]
         assert torch.equal(cache.table[0, :3], table[0]) and cache.table[1, 0] == table[1, 0]
     assert _begin(cache, [1, 1]) == [[150], [3]]
+
+
+# ------------------------------------------------------------------------------------------------ kernels
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,n_seq,G", [(1, 250, 2), (1, 160, 12), (70, 19, 2)])
+def test_one_heavy_key_and_very_many_light_ones(hk, new, n_seq, G, d, dtype):
+    """A key that holds most of the weight and 262 143 whose weights are 2^-25.5 of its: together half a percent of the output.  (All of a request's pages but the
+    first are the same one, and there are so many requests that most are no two warps' or CTAs' work.)
+
+    Weights are rounded to 16 bits, in fp16 to half of 2^-24 at least where they are subnormal.  They are held against a reference that the heaviest key
+    is 2^7 above, or more, so that is 2^-32 of the whole for each of them; beyond that the roundings of weights and output, u each, and the 32-bit
+    logits and exponentials as elsewhere, which move a weight by 2 ((d + 8) 2^-24 |q k| scale + 2^-18).  Sums of 32 bits, each rounded to 2^-24 of what is
+    there already: a page's 64 weights and its products with values are added up first, at the coarsest, so there are a page's eight additions
+    a thread and 4 096 to the sum, and of products four (of sixteen keys) a page, whose additions are off by 2^-23."""
+    pages, Hkv, u = 4096, 8, 2.0**-8 if dtype == "bf16" else 2.0**-11
+    blocks = torch.zeros(2, Hkv, hk.PagedPool4.block_bytes(d), dtype=torch.uint8, device="cuda")
+    pool = hk.PagedPool4.make(blocks, d, DTYPES[dtype])
+    k, v = torch.zeros(2 * PAGE, Hkv, d, dtype=DTYPES[dtype], device="cuda"), torch.ones(2 * PAGE, Hkv, d, dtype=DTYPES[dtype], device="cuda")
+    k[0, :, 0], v[0] = 7.0, 0.0
+    hk.heatkv_paged4_store(pool, k, v, _i32(range(2 * PAGE)))
+    table = torch.ones(n_seq, pages, dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    b = hk.PagedBatch.make(_i32(np.arange(n_seq + 1) * new), _i32([pages * PAGE] * n_seq), table, n_seq * new, new)
+    q = torch.zeros(n_seq * new, Hkv * G, d, dtype=DTYPES[dtype], device="cuda")
+    q[:, :, 0] = 1.0
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = torch.zeros(hk.heatkv_paged4_workspace_bytes(pool, b, Hkv * G), dtype=torch.uint8, device="cuda")
+    scale = float(np.float32(25.5 * math.log(2) / 7))
+    hk.heatkv_paged4_attention(pool, b, q, out, lse, ws, causal=False, sm_scale=scale)
+    assert hk.heatkv_paged_status(ws) == 0
+    light, value = (pages * PAGE - 1) * math.exp(-7 * scale), float(P.values(*P.quantise(np.ones((1, 16))))[0, 0])
+    want, off = value * light / (1 + light), (d + 8) * 2.0**-24 * 7 * scale + 2.0**-18
+    sums, products = (pages + 128) * 2.0**-24, 4 * pages * 2.0**-23
+    tol = (2 * u + 2 * off + sums + products) * want + pages * PAGE * 2.0**-32 * value
+    worst = (float((out.double() - want).abs().max()), float((lse.double() - (7 * scale + math.log1p(light))).abs().max()))
+    assert worst[0] <= tol < want / 40, (worst, tol, want)
+    assert worst[1] <= off + sums + 2.0**-22 * 20, (worst, off + sums)

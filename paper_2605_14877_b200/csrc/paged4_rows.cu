@@ -20,7 +20,7 @@ __device__ __forceinline__ float2 widen2(uint32_t w, bool fp16) {
 __host__ __device__ inline float power_of_two(int e) { return ldexpf(1.f, e); }
 
 // Eight columns as 4-byte words of pairs -> their codes + 8.  A code is the nearest whole number to x / s, ties to even: x r with r = 1 / s in 32 bits is off by
-// less than 2^-19, a quotient of an 11-bit and a 4-bit number that is no tie is 2^-11 away from the nearest one, so the step of 2^-16 to which
+// less than 2^-20, a quotient of an 11-bit and a 4-bit number that is no tie is 2^-12 away from the nearest one, so the step of 2^-16 to which
 // adding 192 rounds x r makes ties ties again and moves nothing across one; 192 is even.  Adding 1.5 * 2^23 then rounds to a whole number, whose low bits
 // are 192 + code: its lowest four, one of them turned round, are the field.  CLAMP: quotients may exceed 7 (where the scale is the largest there is,
 // or so small that it has fewer bits).

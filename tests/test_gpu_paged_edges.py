@@ -136,3 +136,28 @@ def test_one_heavy_key_and_very_many_light_ones(hk, new, n_seq, G, d, dtype):
     worst = (float((out.double() - want).abs().max()), float((lse.double() - (7 * scale + math.log1p(light))).abs().max()))
     assert worst[0] <= tol < want / 40, (worst, tol, want)
     assert worst[1] <= off + sums + 2.0**-22 * 20, (worst, off + sums)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("exp", [0, -5, 9])
+def test_codes_of_ties_and_of_their_neighbours(hk, dtype, exp):
+    """For every scale of four bits and every pair of codes: the number in the middle of them, and the two 16-bit numbers on either side of it."""
+    kind = {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    groups = []
+    for power in (-4, -1, 0, 2) if dtype == "fp16" else (-6, -4, 0, 5):
+        for m in range(8, 16):
+            s = m * 2.0 ** (power - 3 + exp)
+            ties = torch.tensor([(c + 0.5) * s for c in range(7)], dtype=torch.float64).to(kind)
+            assert torch.equal(ties.double(), torch.tensor([(c + 0.5) * s for c in range(7)], dtype=torch.float64))
+            near = torch.stack([(ties.view(torch.int16) + by).view(kind) for by in (-2, -1, 0, 1, 2)], 1).flatten()[:34]    # (6.5 s and two steps: below 7 s)
+            for x in (near, -near):
+                x = torch.cat([x, torch.zeros(-len(x) % 15, dtype=kind)]).view(-1, 15)
+                groups.append(torch.cat([torch.full((len(x), 1), 7 * s, dtype=torch.float64).to(kind), x], 1))
+    x = torch.cat(groups)
+    x = torch.cat([x, torch.zeros(-len(x) % 4, 16, dtype=kind)]).view(-1, 1, 64).cuda()
+    n_pages = -(-len(x) // PAGE)
+    blocks = torch.zeros(n_pages, 1, hk.PagedPool4.block_bytes(64), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged4_store(hk.PagedPool4.make(blocks, 64, kind, exp, exp), x, x.flip(2).contiguous(), _i32(range(len(x))))
+    for got, rows in zip(P.unblock(blocks.cpu().numpy(), 64), (x, x.flip(2))):
+        for g, want in zip(got, P.quantise(_np(rows), exp)):
+            assert np.array_equal(g[:, 0].reshape(-1, g.shape[-1])[: len(x)], want[:, 0])

@@ -1,5 +1,7 @@
 // Entry points of the paged cache: checks of arguments and kernel choice.
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "paged_rows.cuh"
 #include "paged_wait.cuh"
@@ -346,13 +348,18 @@ int heatkv_paged4_attention(const heatkv_paged4_pool* pool, const heatkv_paged_b
   p.page_stride = pool->page_stride;
   p.head_stride = pool->head_stride;
   p.fp16 = pool->dtype == HEATKV_DTYPE_FP16;
-  // Up to two tiles of 16 rows: the warp-level kernel (8 kv heads of 4 heads; 32 requests of 10 000 tokens, 16 rows 114 us and 242 on the tensor-memory
-  // kernel, 32 rows 213 and 242, 48 rows 310 and 242).  More where there is little to do in all, a tile of `table_pages` pages weighing eight more: one
-  // request of 10 000, 96 rows (7920) 37 and 62, of 300 11.9 and 16.1; two of 10 000, 64 rows (10 560) 42 and 55; 8 of 2500, 64 rows (12 288) 45 and 38; 32 of
-  // 300, 64 rows (14 336) 38 and 32.  Three tiles up to four times as much, as a batch's requests are mostly shorter than its table is wide: 24 of 40 to 8000
-  // tokens, 42 rows (38 900) 21 and 37; 8 that are all of 10 000, 48 rows (31 700) 90 and 80.
-  const int64_t tiles = ((int64_t)p.a.max_new * p.a.G + 15) / 16, units = (int64_t)p.a.n_seq * p.a.Hkv, little = tiles == 3 ? 40000 : 12000;
-  const bool few = tiles <= 2 || (units <= little && tiles <= little && units * tiles * ((int64_t)p.a.table_pages + 8) <= little);
+  // The warp-level kernel takes a tile of 16 rows over a page in somewhat less than half of the time in which the tensor-memory kernel takes 128 rows over it (8 kv
+  // heads of 4 heads, 32 requests of 10 000 tokens: 16 rows 114 us and 242, 32 rows 213 and 242, 48 rows 310 and 242), so up to two tiles a request are its own, and
+  // beyond those it pays as long as what it does more, the tiles past two times the table's pages, is little beside the ends of the other's call and items (a tile
+  // weighs twelve pages more).  Requests with all their tiles are as many as the step's tokens make (a prompt among single tokens is one); lengths are
+  // not known here, a table is as wide as its longest.  2700 random shapes of 3 to 150 tiles, its time over the other's, by weight: where all requests are as long
+  // as the table is wide 0.76 at 2000 to 4000, 0.91 at 7000 to 10 000, 1.08 at 10 000 to 14 000, 1.4 at 20 000 to 40 000; where lengths are spread, where a chunk
+  // comes with single tokens, and of whole prompts 0.7 to 0.8 at 7000 to 10 000, 0.8 at 10 000 to 14 000, 0.8 to 1.0 at 14 000 to 20 000, 1.0 to 1.25 at 20 000
+  // to 40 000.  (A longest request that the step's tokens do not hold says nothing of how many are as long.)
+  const double tiles = (double)(((int64_t)p.a.max_new * p.a.G + 15) / 16);
+  const double all_tiles = p.a.n_tokens < p.a.max_new ? INFINITY : (double)p.a.n_tokens * p.a.G / 16 + p.a.n_seq * 0.5;
+  const double full = std::min((double)p.a.n_seq, all_tiles / tiles);
+  const bool few = full * p.a.Hkv * (tiles - 2) * ((double)p.a.table_pages + 12) <= 10000;
   return done((few ? launch_paged4_small : launch_paged4_tc)(p, pool->d, dev, static_cast<cudaStream_t>(stream)));
 }
 

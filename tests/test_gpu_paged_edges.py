@@ -161,3 +161,17 @@ def test_codes_of_ties_and_of_their_neighbours(hk, dtype, exp):
     for got, rows in zip(P.unblock(blocks.cpu().numpy(), 64), (x, x.flip(2))):
         for g, want in zip(got, P.quantise(_np(rows), exp)):
             assert np.array_equal(g[:, 0].reshape(-1, g.shape[-1])[: len(x)], want[:, 0])
+
+
+@pytest.mark.parametrize("lens,H,Hkv", [
+    ([(12, 10000)] * 8, 32, 8), ([(12, 10000)] * 7, 32, 8),                               # three tiles, either side of what the warp-level kernel takes
+    ([(6, 5000)] + [(1, 40 + 61 * i) for i in range(23)], 28, 4), ([(6, 5000)] * 40, 28, 4),
+    ([(200, 700)] + [(1, 30 + 7 * i) for i in range(60)], 8, 8), ([(900, 2000)] + [(1, 30 + 7 * i) for i in range(60)], 8, 8),
+    ([(33, 33)], 1, 1), ([(33, 33), (0, 64), (1, 0)], 2, 2), ([(2, 900)] * 3, 96, 2)])
+def test_attention_on_either_side_of_the_kernels_border(hk, lens, H, Hkv):
+    """Drafts, chunks among single tokens and small prompts, where the choice of kernel changes."""
+    from test_gpu_paged4 import _attend, _filled
+    rng, g = np.random.default_rng(len(lens)), torch.Generator("cuda").manual_seed(H)
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, Hkv, 64, torch.float16)
+    q = torch.empty(b.n_tokens, H, 64, dtype=torch.float16, device="cuda").normal_(generator=g)
+    _attend(hk, pool, b, q, lens, table, q_begin, kv, Hkv, dtype="fp16")

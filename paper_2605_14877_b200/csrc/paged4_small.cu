@@ -838,8 +838,9 @@ template <int D, bool F16>
 cudaError_t launch_typed(const Paged4Params& q, int rows, int n_sm, cudaStream_t stream) {
   if (rows > 8) return launch<D, 2, F16, 8>(q, n_sm, stream);
   // Twelve warps with two pages each under way where there is much to do, eight with three where the beginning and the end of a call weigh more (128-wide
-  // heads; 64 requests of 12 000 tokens, 8 kv heads, 166 us and 178, 256 of 50 to 1500 36.3 and 41.1, one of 131 000 41.3 and 42.3; 64 of 500 20.3 and 19.0).
-  const bool much = D == 128 && q.a.n_seq <= 340 && (int64_t)q.a.n_seq * q.a.Hkv * q.a.table_pages >= 16000;
+  // heads).  Time of twelve over eight, one to 256 requests of 2 and 8 kv heads, by pages of the table and kv head: 1.00 to 1.12 at 4000, 1.01 at 8000, 1.00 at 9000 and
+  // 10 000, 0.98 to 1.00 at 11 000 to 14 000, 0.97 to 0.99 at 16 000, 0.95 at 32 000 (requests of spread lengths 0.85 to 1.01 there).
+  const bool much = D == 128 && q.a.n_seq <= 340 && (int64_t)q.a.n_seq * q.a.Hkv * q.a.table_pages >= 10000;
   return much ? launch<D, 1, F16, D == 128 ? 12 : 8>(q, n_sm, stream) : launch<D, 1, F16, 8>(q, n_sm, stream);
 }
 

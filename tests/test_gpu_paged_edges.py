@@ -175,3 +175,14 @@ def test_attention_on_either_side_of_the_kernels_border(hk, lens, H, Hkv):
     pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, Hkv, 64, torch.float16)
     q = torch.empty(b.n_tokens, H, 64, dtype=torch.float16, device="cuda").normal_(generator=g)
     _attend(hk, pool, b, q, lens, table, q_begin, kv, Hkv, dtype="fp16")
+
+
+@pytest.mark.parametrize("lens", [[(1, 64 * 1248)], [(1, 64 * 1249)], [(1, 64 * 40 + 1)] + [(1, 100 + 67 * i) for i in range(28)],
+                                  [(1, 64 * 40 + 1)] + [(1, 100 + 67 * i) for i in range(29)]])
+def test_attention_on_either_side_of_the_borders_of_warps(hk, lens):
+    """One row tile, eight kv heads of 128 columns, where the number of warps changes."""
+    from test_gpu_paged4 import _attend, _filled
+    rng, g = np.random.default_rng(len(lens)), torch.Generator("cuda").manual_seed(len(lens))
+    pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, 8, 128, torch.bfloat16)
+    q = torch.empty(b.n_tokens, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    _attend(hk, pool, b, q, lens, table, q_begin, kv, 8)

@@ -3,8 +3,8 @@
 //
 // Which pages are shared is nowhere kept: both calls mark the pages that the old table lists and those that the new one does, and what is only in
 // the first goes to the ring of free pages, in page order, so that the result does not depend on which CTA came first.  All of it is chains of a few
-// loads over tables of some thousand entries: what bounds it is the number of launches and of dependent loads.  So pools of up to SMALL_PAGES
-// pages have their marks in one CTA's shared memory: a fork of few rows is one launch, where that CTA decides while others copy the entries that no
+// loads over tables of some thousand entries: what bounds it is the number of launches and of dependent loads.  So small pools and tables (one_cta) have their
+// marks in one CTA's shared memory: a fork is one launch, where that CTA decides while others copy the entries that no
 // decision changes (32 rows of 1 to 40 pages 4.9 us, in three launches with marks in global memory 10.1; 97 rows of 141 pages 7.4, by one CTA alone 10.3),
 // and a compaction two, one CTA of the second seeing to the marks while the others list the moves (100 000 tokens of one row 9.0 us, 40 rows of 50 to 9000
 // 8.4; the first with marks in global memory 16.8).
@@ -18,7 +18,16 @@ namespace {
 constexpr int RT = 256;                        // threads of a CTA
 constexpr int DECIDE_THREADS = 1024;
 constexpr int PLACE_THREADS = 512, PLACE_PAGES = 32;                // .. that lists the moves of so many pages of a row at a time
-constexpr int SMALL_PAGES = 16384, SMALL_ROWS = 1024, SMALL_ENTRIES = 32768;
+// What one CTA sees to, with the pages' marks in its shared memory.  Its time grows with the rows (64 moves each, by that CTA alone) and the entries, that of the
+// launches of many CTAs with the pages: a fork takes 0.5 to 0.9 of theirs with 4 to 96 rows, over 4000 pages 1.0 with 128, 1.15 with 160, 1.5 with 256, over 16 384
+// pages 0.7, 0.85 and 1.1, and with 16 000 to 32 768 entries 0.8 to 1.0, with more 1.1 to 2.5; compactions the same of rows, and 0.7 to 0.9 below 8000 entries,
+// 0.95 to 1.1 at 8000 to 16 000, 1.05 to 1.2 at 16 000 to 32 768.
+constexpr int SMALL_PAGES = 16384, FORK_ENTRIES = 32768, COMPACT_ENTRIES = 12000;
+__host__ __device__ constexpr int small_rows(int n_pages) { return 112 + n_pages / 192; }
+inline bool one_cta(const RowsParams& p, int entries) {
+  return p.n_pages <= SMALL_PAGES && p.n_seq <= small_rows(p.n_pages) && (int64_t)p.n_seq * p.table_pages <= entries;
+}
+static_assert(small_rows(SMALL_PAGES) <= DECIDE_THREADS, "a thread a row");
 enum Mark : uint32_t { OLD = 1, WHOLE = 2, PART = 4 };   // listed by the old table; by the new one, all of the page or its first rows
 
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + PAGE - 1) / PAGE; }
@@ -146,7 +155,7 @@ struct ForkCopy {
     if (j != last) out[j] = page;
   }
 };
-// A fork of up to SMALL_ROWS rows and SMALL_ENTRIES entries of their table: CTA 0 decides, the others copy full pages' entries, so many rows each.
+// A fork of few rows (one_cta): CTA 0 decides, the others copy full pages' entries, so many rows each.
 __host__ __device__ constexpr int copied_rows(int n_seq) { return n_seq < DECIDE_THREADS / 64 ? 1 : DECIDE_THREADS / 32; }
 __global__ void __launch_bounds__(DECIDE_THREADS) fork_small_kernel(const RowsParams p) {
   extern __shared__ uint32_t sm[];
@@ -262,9 +271,6 @@ __global__ void __launch_bounds__(RT) fork_mark_kernel(const RowsParams p) {
     p.row_moves[i] = make_int2(valid(p, last) ? last : -1, length);          // the page with its last tokens, if that is not full
   }
 }
-
-// Pages of chunk c that go back.
-__device__ __forceinline__ bool goes_back(const RowsParams& p, int page) { return (p.marks[page] & (OLD | WHOLE | PART)) == OLD; }
 
 // Who gets a page of its own for its last tokens: a CTA with all rows, up to four a thread.
 __global__ void __launch_bounds__(DECIDE_THREADS) fork_decide_kernel(const RowsParams p) {
@@ -617,7 +623,6 @@ constexpr int MT = 256, MOVE_UNROLL = 4;
 // A cache of 16 bits: 16 bytes of K and of V.
 struct Words16 {
   using Word = int4;
-  static constexpr int PARTS = 2;
   __device__ static int words(const MoveParams& p) { return p.Hkv * (p.d / 8); }
   __device__ static int64_t at(const MoveParams& p, uint32_t slot, int w, int) {
     const int ch = p.d / 8, h = w / ch, c = w - h * ch;
@@ -629,7 +634,6 @@ struct Words16 {
 template <int D>
 struct Codes4 {
   using Word = typename std::conditional<D == 128, int4, int2>::type;
-  static constexpr int PARTS = 2;
   __device__ static int words(const MoveParams& p) { return p.Hkv * 4; }
   __device__ static int64_t at(const MoveParams& p, uint32_t slot, int w, int part) {
     using B = Block4<D>;
@@ -641,7 +645,6 @@ struct Codes4 {
 template <int D>
 struct Scales4 {
   using Word = typename std::conditional<D == 128, int2, int>::type;
-  static constexpr int PARTS = 2;
   __device__ static int words(const MoveParams& p) { return p.Hkv; }
   __device__ static int64_t at(const MoveParams& p, uint32_t slot, int w, int part) {
     using B = Block4<D>;
@@ -723,11 +726,11 @@ cudaError_t launch_chunks(const RowsParams& p, cudaStream_t stream) {
 
 cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
   cudaError_t rc;
-  if (p.n_pages <= SMALL_PAGES && p.n_seq <= SMALL_ROWS && (int64_t)p.n_seq * p.table_pages <= SMALL_ENTRIES) {
+  if (one_cta(p, FORK_ENTRIES)) {
     auto bytes = [](int n_pages, int n_seq) { return ((n_pages + 7) / 8 + n_pages + 5 * n_seq + 2) * 4; };
     // (always the most that any call takes: the limit is the process's, and another thread may set it before this launch; 47 KB need no limit raised)
     rc = bytes(p.n_pages, p.n_seq) <= 47 * 1024 ? cudaSuccess
-                                                : cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, SMALL_ROWS));
+                                                : cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(SMALL_PAGES, small_rows(SMALL_PAGES)));
     return rc != cudaSuccess ? rc : launch_pdl(fork_small_kernel, dim3(1 + (p.n_seq + copied_rows(p.n_seq) - 1) / copied_rows(p.n_seq)), dim3(DECIDE_THREADS), bytes(p.n_pages, p.n_seq), stream, p);
   }
   rc = launch_zero_marks(p, stream);
@@ -743,7 +746,7 @@ cudaError_t launch_paged_fork(const RowsParams& p, cudaStream_t stream) {
 
 cudaError_t launch_paged_compact(const RowsParams& p, cudaStream_t stream) {
   auto ctas = [&](int pages, int more) { return dim3((unsigned)std::min(256, (p.table_pages + pages - 1) / pages), p.n_seq + more); };
-  const bool small = p.n_pages <= SMALL_PAGES;
+  const bool small = one_cta(p, COMPACT_ENTRIES);
   cudaError_t rc = small ? cudaSuccess : launch_zero_marks(p, stream);
   if (rc == cudaSuccess) rc = launch_pdl(compact_count_kernel, ctas(RT / 32, 0), dim3(RT), 0, stream, p);
   if (rc != cudaSuccess) return rc;

@@ -186,3 +186,29 @@ def test_attention_on_either_side_of_the_borders_of_warps(hk, lens):
     pool, b, table, q_begin, kv = _filled(hk, g, rng, lens, 8, 128, torch.bfloat16)
     q = torch.empty(b.n_tokens, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
     _attend(hk, pool, b, q, lens, table, q_begin, kv, 8)
+
+
+@pytest.mark.parametrize("n,width,pages", [(112, 9, 0), (114, 9, 0), (132, 9, 4000), (133, 9, 4000), (197, 9, 16384), (198, 9, 16384), (16, 750, 4000), (16, 751, 4000),
+                                           (64, 512, 4000), (64, 513, 4000)])
+def test_rows_on_either_side_of_what_one_cta_sees_to(hk, n, width, pages):
+    """Forks and compactions where other launches take over: as many rows and entries as one CTA takes, and more (pages 0: as many as there have to be)."""
+    from test_gpu_paged4 import _rearranged, _rows_state, _same
+    ws = None
+    for seed in range(3):
+        rng = np.random.default_rng(seed)
+        lengths = [int(x) for x in rng.integers(0, 200, n)]
+        held = sum(-(-x // PAGE) for x in lengths)
+        table, fifo, ring, head, n_pages = _rows_state(hk, lengths, width, max(pages - held - 3, 90), seed)
+        assert n_pages == pages or pages == 0
+        if ws is None:
+            ws = torch.zeros(hk.heatkv_paged_rows_workspace_bytes(n, width, 16384), dtype=torch.uint8, device="cuda")
+        fifo = fifo[:90]
+        parents, keep = [int(x) for x in rng.integers(-1, n, n)], [int(x) for x in rng.integers(0, 250, n)]
+        want = P.fork(parents, keep, lengths, table, fifo)
+        got = _rearranged(hk, lambda *a: hk.heatkv_paged_fork(_i32(parents), _i32(keep), *a), lengths, table, ring.copy(), head, 90, n * PAGE, ws)
+        _same(got, want, ring.copy(), head, 90, len(want[6]))
+        stays = rng.random((n, 200)) < 0.8
+        *want, done = P.compact(stays, lengths, table, fifo, sum(lengths))
+        mask = torch.from_numpy(stays).cuda()
+        got = _rearranged(hk, lambda *a: hk.heatkv_paged_compact(mask, *a), lengths, table, ring.copy(), head, 90, sum(lengths), ws)
+        _same(got, want, ring.copy(), head, 90, done)

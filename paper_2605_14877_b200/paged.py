@@ -49,7 +49,7 @@ class PagedCache:
         self.state = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=self.device)
         self.other_state = new(4)
         self.lengths = new(rows)                       # tokens of every row
-        self.at_most = [0] * rows                      # ... as far as the host knows: more where rows sat a step out
+        self.at_most = [0] * rows                      # ... as far as the host knows: more where rows sat a step out, or tokens left
         self.workspace: Optional[torch.Tensor] = None
         # what `fork` and `compact` need, from their first use on: the other table and lengths, moves, a workspace
         self.other: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
@@ -166,7 +166,8 @@ class PagedCache:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their
         order and the positions that they were encoded with, and `begin` goes on counting positions as if nothing had left (so `keep` is to cut such a
         row behind its last token that left).  Tokens move into free pages: rows for which those do not suffice stay as they are (`state[2]` counts
-        them)."""
+        them).  The host does not learn how many tokens are left, which steps and further compactions are sized by: `keep` with a number that no row exceeds
+        tells it."""
         if stays.dtype is not torch.bool or stays.dim() != 2 or stays.shape[0] != self.rows:
             raise ValueError(f"stays: expected bool [{self.rows}, tokens], got {stays.dtype} {tuple(stays.shape)}")
         before = self.lengths

@@ -58,7 +58,7 @@ class PagedCache:
         self.shared = False                            # may rows list the same pages
         # tokens that `compact` took out of every row, and in front of each of its first `upto` places
         self.gone: Optional[torch.Tensor] = None
-        self.left, self.upto = new(rows, 0), new(rows)
+        self.left, self.upto, self.places = new(rows, 0, dt=torch.int64), new(rows), new(0, dt=torch.int64)
 
     def begin(self, new: Sequence[int]) -> Step:
         """Pages and slots of a step with new[i] new tokens in row i (0: none).  Pages are wanted in row order, and from the first row that the free
@@ -128,7 +128,8 @@ class PagedCache:
             raise ValueError(f"lengths: expected {self.rows} numbers of tokens, none below 0, got {list(lengths)}")
         keep = torch.tensor(list(lengths), dtype=torch.int32, device=self.device)
         if self.shared:
-            own, asked = torch.arange(self.rows, dtype=torch.int32, device=self.device), torch.minimum(self.lengths, keep)
+            own = torch.arange(self.rows, dtype=torch.int32, device=self.device)
+            asked = torch.minimum(self.lengths, keep) if self._may_run_out() else None
             if any(n < a and n % hk.PAGE_TOKENS for a, n in zip(self.at_most, lengths)):
                 # whole pages first: that takes none, moves nothing, and what it frees is there for the copies
                 most = self.table.shape[1]
@@ -152,7 +153,7 @@ class PagedCache:
         if len(parents) != self.rows or any(p is not None and not 0 <= p < self.rows for p in parents):
             raise ValueError(f"parents: expected {self.rows} rows or None, got {list(parents)}")
         of = torch.tensor([-1 if p is None else p for p in parents], dtype=torch.int32, device=self.device)
-        before = self.lengths
+        before, short = self.lengths, self._may_run_out()
         self._rearrange(hk.heatkv_paged_fork, (of, None), self.rows * hk.PAGE_TOKENS)
         self.at_most = [0 if p is None else self.at_most[p] for p in parents]
         parents = [p for p, n in zip(parents, self.at_most) if n]
@@ -160,7 +161,7 @@ class PagedCache:
         if self.gone is not None:
             row = of.clamp(min=0).long()
             self.gone, self.left, self.upto = self.gone[row], self.left[row], self.upto[row]
-            self._forget(torch.where(of >= 0, before[row], 0))
+            self._forget(torch.where(of >= 0, before[row], 0) if short else None)
 
     def compact(self, stays: torch.Tensor) -> None:
         """Token t of row i leaves the cache where stays[i, t] (bool, on the device) is False; tokens past its width stay.  The others keep their
@@ -177,19 +178,23 @@ class PagedCache:
 
     def _count_out(self, stays: torch.Tensor, before: torch.Tensor) -> None:
         """What left in front of every place of the rows that a compaction changed (it leaves the lengths of the others as they were)."""
+        changed = self.lengths < before
         if self.gone is None:
             self.gone = torch.zeros_like(before)
-        width, known = max(stays.shape[1], self.left.shape[1]), self.left.shape[1]
-        place = torch.arange(width, dtype=torch.int32, device=self.device)
-        leaves = (place < before[:, None]) & (self.lengths < before)[:, None]
-        leaves[:, : stays.shape[1]] &= ~stays
-        leaves[:, stays.shape[1]:] = False
-        in_front = leaves.cumsum(1, dtype=torch.int32)
-        left = self.gone[:, None] + in_front
-        left[:, :known] += torch.where(place[:known] < self.upto[:, None], self.left - self.gone[:, None], 0)
+        if stays.shape[1] < self.left.shape[1]:        # (what the mask does not reach stays)
+            stays = torch.nn.functional.pad(stays, (0, self.left.shape[1] - stays.shape[1]), value=True)
+        width = stays.shape[1]
+        if self.places.numel() < width:
+            self.places = torch.arange(width, device=self.device)
+        place = self.places[:width]
+        leaves = (place < torch.where(changed, before, 0)[:, None]) > stays
+        in_front = leaves.cumsum(1)
+        left = in_front + self.gone[:, None]
+        known = self.left.shape[1]
+        if known > 0:
+            left[:, :known] = torch.where(place[:known] < self.upto[:, None], self.left + in_front[:, :known], left[:, :known])
         # (those that left are written behind the others, to a column that is dropped)
-        self.left = torch.zeros(self.rows, width + 1, dtype=torch.int32, device=self.device).scatter_(
-            1, torch.where(leaves, width, place - in_front).long(), left)[:, :width]
+        self.left = left.new_empty(self.rows, width + 1).scatter_(1, (place - in_front).masked_fill_(leaves, width), left)[:, :width]
         went = before - self.lengths
         self.upto, self.gone = torch.minimum(self.lengths, width - went), self.gone + went
 
@@ -210,6 +215,10 @@ class PagedCache:
         move = hk.heatkv_paged_move if self.bits == 16 else hk.heatkv_paged4_move
         for pool in self.pools if moves else ():
             move(pool, source, target)
+
+    def _may_run_out(self) -> bool:
+        """May a call that gives every row a page find too few, for rows of which tokens left?"""
+        return self.gone is not None and self.free.numel() < self.rows + sum(min(-(-n // hk.PAGE_TOKENS), self.table.shape[1]) for n in self.at_most)
 
     def _forget(self, asked: Optional[torch.Tensor] = None) -> None:
         """A row that is over has nothing that left it; one that was cut deeper than `asked` goes on at the position of the first token that it was not to lose."""
